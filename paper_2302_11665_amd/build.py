@@ -28,6 +28,7 @@ SIM_MULTI_SRC = os.path.join(CSRC, "sim_multi.hip")
 SIM_ALG2_SRC = os.path.join(CSRC, "sim_alg2.hip")
 SIM_BATCH_SRC = os.path.join(CSRC, "sim_batch.hip")
 SIM_SPEC_SRC = os.path.join(CSRC, "sim_spec.hip")
+OPS_SRCS = tuple(os.path.join(CSRC, f"ops_{n}.hip") for n in ("linear", "cache", "attend"))  # a served model's step
 LANE_WIDTHS = (1, 2, 4, 8, 16, 32, 64)  # one launcher translation unit per width
 SIM_LIB = os.path.join(BUILD, "libalpaserve_sim.so")
 PROBE_SRC = os.path.join(CSRC, "peak_probe.hip")
@@ -75,6 +76,8 @@ def build_sim(extra_flags=(), jobs=None) -> str:
              (SIM_BATCH_SRC, os.path.join(obj_dir, "sim_batch.o"), []),
              (SIM_SPEC_SRC, os.path.join(obj_dir, "sim_spec.o"), []),
              (SIM_MULTI_SRC, os.path.join(obj_dir, "sim_multi.o"), [])]
+    for src in OPS_SRCS:
+        units.append((src, os.path.join(obj_dir, os.path.basename(src).replace(".hip", ".o")), []))
     for w in LANE_WIDTHS:
         units.append((SIM_LAUNCH_SRC, os.path.join(obj_dir, f"sim_launch_w{w}.o"), [f"-DAS_W={w}"]))
 

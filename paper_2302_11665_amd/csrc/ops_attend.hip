@@ -1,0 +1,588 @@
+// Attention of a step's queries over a cache held in 4 bits, and the attention
+// weight that every cached token gets (alpaserve_ops.h).
+//
+// A group's value is code * d + m, so with codes c
+//   q.k     = sum over groups of  d (sum q c) + m (sum q)
+//   sum p v = sum over tokens of  (p d) c + p m
+// and the codes enter v_mfma_f32_16x16x32 as 16 + c, which a shift, a mask and
+// an or make of 4 bits (bf16 holds 16..31 in steps of 1/8, fp16 in steps of
+// 1/64); the 16 is taken out in fp32: the first product starts from -16 sum q,
+// the second is corrected by 16 (p d).  Queries are exact in the first product;
+// p d enters the second as two bf16 numbers.
+//
+// The products are K q^T and V^T p^T: the queries that share a key/value head
+// are the 16 columns.  A lane of the first product's result then holds, for one
+// query, the slots 4 g + 0..3 (g = lane / 16) of each 16, which are the slots
+// that the same lane has to supply to the second: p never leaves its lane, and a
+// word of V holds the channel's codes for just those 8 slots.  A query's running
+// maximum is the same in its four lanes, its sum is kept per lane.
+#include "ops_common.hpp"
+
+using as_host::fail;
+
+namespace as_ops {
+
+constexpr int kWaves = 4;
+constexpr float kFloor = -1e30f;  // running maximum before any slot was seen
+
+struct AttArgs {
+  CacheArgs c;
+  const uint16_t* q;
+  int64_t q_seq, q_token;
+  const int32_t* length;
+  void* out;
+  float* part_o;   // [n_seqs * n_heads][splits][rows][dim], not normalised
+  float* part_ml;  // [n_seqs * n_heads][splits][rows][2]: maximum (log2 units), sum
+  float* row_ml;   // [n_seqs * n_heads][rows][2] for the weights: maximum, 1 / sum
+  const float* acc_in;
+  float* acc_out;
+  float c_log2;      // scale * log2(e)
+  uint32_t page_mul; // ceil(2^32 / (page / 32)), 0 for pages of 32
+  int32_t n_queries, per, rows, splits, row_groups;
+};
+
+// ---------------------------------------------------------------- 4-bit codes
+
+// 16 + c of a word's eight codes, as bf16 or fp16 pairs.
+template <int TYPE>
+__device__ __forceinline__ v4u expand(uint32_t w) {
+  v4u r;
+  if (TYPE == AS_BF16) {
+    r[0] = ((w << 3) & 0x00780078u) | 0x41804180u;
+    r[1] = ((w >> 1) & 0x00780078u) | 0x41804180u;
+    r[2] = ((w >> 5) & 0x00780078u) | 0x41804180u;
+    r[3] = ((w >> 9) & 0x00780078u) | 0x41804180u;
+  } else {
+    r[0] = ((w << 6) & 0x03c003c0u) | 0x4c004c00u;
+    r[1] = ((w << 2) & 0x03c003c0u) | 0x4c004c00u;
+    r[2] = ((w >> 2) & 0x03c003c0u) | 0x4c004c00u;
+    r[3] = ((w >> 6) & 0x03c003c0u) | 0x4c004c00u;
+  }
+  return r;
+}
+
+template <int TYPE>
+__device__ __forceinline__ v4f mfma(v4u a, v4u b, v4f c) {
+  if (TYPE == AS_BF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0,
+                                                   0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+
+// The halves of a (scale, minimum) word.
+__device__ __forceinline__ float par_d(uint32_t w) { return (float)__builtin_bit_cast(v2h, w)[0]; }
+__device__ __forceinline__ float par_m(uint32_t w) { return (float)__builtin_bit_cast(v2h, w)[1]; }
+
+// What a lane holds of 32 slots of one head.
+template <int DIM, int GROUP>
+struct Keys {
+  uint32_t k[2][DIM / 32];
+  v4u par[DIM / GROUP][2];
+};
+template <int DIM, int GROUP>
+struct Values {
+  uint32_t v[DIM / 16];
+  v4u par[DIM / GROUP][2];
+};
+
+// Row (page and head) of a block of 32 slots of a sequence, or -1; at: its
+// first slot's place on the page.
+__device__ __forceinline__ int64_t block_row(const AttArgs& p, int b, int h, int blk, int& at) {
+  const int pb = p.page_mul ? (int)__umulhi((uint32_t)blk, p.page_mul) : blk;
+  at = blk * 32 - pb * p.c.page;
+  return cache_row(p.c, b, h, pb);
+}
+
+template <int DIM, int GROUP>
+__device__ __forceinline__ void load_keys(const AttArgs& p, int64_t row, int at, int lane, Keys<DIM, GROUP>& x) {
+  const uint32_t* k = p.c.k + (row * p.c.page + at) * (DIM / 8) + (lane & 15) * (DIM / 8) + (lane >> 4) * (DIM / 32);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    if (DIM == 128) {
+      const v4u w = *reinterpret_cast<const v4u*>(k + t * 16 * (DIM / 8));
+#pragma unroll
+      for (int i = 0; i < DIM / 32; ++i) x.k[t][i] = w[i];
+    } else {
+      const v2u w = *reinterpret_cast<const v2u*>(k + t * 16 * (DIM / 8));
+#pragma unroll
+      for (int i = 0; i < DIM / 32; ++i) x.k[t][i] = w[i];
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < DIM / GROUP; ++g)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      x.par[g][t] = *reinterpret_cast<const v4u*>(p.c.k_par + (row * (DIM / GROUP) + g) * p.c.page + at + 16 * t +
+                                                  (lane >> 4) * 4);
+}
+
+template <int DIM, int GROUP>
+__device__ __forceinline__ void load_values(const AttArgs& p, int64_t row, int at, int lane, Values<DIM, GROUP>& x) {
+  const uint32_t* v = p.c.v + (row * p.c.page + at) * (DIM / 8) + lane * (DIM / 16);
+#pragma unroll
+  for (int j = 0; j < DIM / 64; ++j) {
+    const v4u w = *reinterpret_cast<const v4u*>(v + 4 * j);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.v[4 * j + i] = w[i];
+  }
+#pragma unroll
+  for (int g = 0; g < DIM / GROUP; ++g)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      x.par[g][t] = *reinterpret_cast<const v4u*>(p.c.v_par + (row * (DIM / GROUP) + g) * p.c.page + at + 16 * t +
+                                                  (lane >> 4) * 4);
+}
+
+// Sixteen queries as the second operand of K q^T: lane's channels 32 i + 8 g +
+// 0..7 of query row lane % 16; the sums over each group's channels.
+template <int TYPE, int DIM, int GROUP>
+struct Queries {
+  v4u q[DIM / 32];
+  float sum[DIM / GROUP];
+  int limit;  // slots that the query sees
+};
+
+template <int TYPE, int DIM, int GROUP>
+__device__ __forceinline__ void load_queries(const AttArgs& p, int b, int h, int row, int n, int lane,
+                                             Queries<TYPE, DIM, GROUP>& x) {
+  const int t = row / p.per;
+  const uint16_t* q = p.q + b * p.q_seq + t * p.q_token + (int64_t)(h * p.per + row - t * p.per) * DIM + (lane >> 4) * 8;
+  // rows beyond the last are zero and see what the last sees; they are not stored
+  x.limit = n - p.n_queries + (row < p.rows ? t : p.n_queries - 1) + 1;
+#pragma unroll
+  for (int g = 0; g < DIM / GROUP; ++g) {
+    float s = 0.0f;
+#pragma unroll
+    for (int i = g * (GROUP / 32); i < (g + 1) * (GROUP / 32); ++i) {
+      x.q[i] = row < p.rows ? *reinterpret_cast<const v4u*>(q + 32 * i) : v4u{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s += to_f32<TYPE>(x.q[i][j] & 0xffffu) + to_f32<TYPE>(x.q[i][j] >> 16);
+    }
+    x.sum[g] = sum_over_rows(s);
+  }
+}
+
+// q.k of the lane's query and 2 x 4 slots.
+template <int TYPE, int DIM, int GROUP>
+__device__ __forceinline__ void scores(const v4u (&kf)[DIM / 32], const v4u (&par)[DIM / GROUP],
+                                       const Queries<TYPE, DIM, GROUP>& q, float (&s)[4]) {
+#pragma unroll
+  for (int g = 0; g < DIM / GROUP; ++g) {
+    const float c = -16.0f * q.sum[g];
+    v4f a = {c, c, c, c};
+#pragma unroll
+    for (int i = g * (GROUP / 32); i < (g + 1) * (GROUP / 32); ++i) a = mfma<TYPE>(kf[i], q.q[i], a);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float m = par_m(par[g][r]) * q.sum[g];
+      s[r] = fmaf(par_d(par[g][r]), a[r], g == 0 ? m : s[r] + m);
+    }
+  }
+}
+
+// The part of a sequence that a workgroup takes.
+struct Part {
+  int b, h, split, row0, n;
+  int first, end;  // blocks of 32 slots
+};
+
+__device__ __forceinline__ int clamped_length(const AttArgs& p, int b) {
+  const int64_t cap = (int64_t)p.c.max_pages * p.c.page;
+  return (int)max((int64_t)0, min((int64_t)p.length[b], cap));
+}
+
+// ---------------------------------------------------------------- attention
+
+// One workgroup per (sequence, head, split of its slots, 16 NT query rows); its
+// four wavefronts take 32 slots in turn and join their results in LDS.
+template <int TYPE, int DIM, int GROUP, int NT>
+__global__ __launch_bounds__(64 * kWaves) void attend(AttArgs p) {
+  constexpr int NG = DIM / GROUP;
+  __shared__ float ml[kWaves][16][2];
+  __shared__ float part[kWaves][16][DIM + 4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Neighbouring workgroup numbers go to different XCDs: the row groups of one
+  // part, which read the same slots, are a multiple of 8 apart.
+  const int unit = (int)(blockIdx.x / (8 * p.row_groups)) * 8 + (int)(blockIdx.x & 7);
+  const int rg = (int)(blockIdx.x / 8) % p.row_groups;
+  const int bh = unit / p.splits, split = unit % p.splits;
+  if (bh >= p.c.n_seqs * p.c.n_heads) return;
+  const int b = bh / p.c.n_heads, h = bh % p.c.n_heads;
+  const int n = clamped_length(p, b);
+  const int row0 = rg * 16 * NT;
+  const int blocks = (n + 31) / 32, per_split = (blocks + p.splits - 1) / p.splits;
+  // slots that the group's last and first rows see
+  const int last = min(n, n - p.n_queries + min(row0 + 16 * NT - 1, p.rows - 1) / p.per + 1);
+  const int least = n - p.n_queries + row0 / p.per + 1;
+  const int end = min((split + 1) * per_split, max(0, (last + 31) / 32));
+
+  Queries<TYPE, DIM, GROUP> q[NT];
+  v4f o[NT][DIM / 16];
+  float shift[NT][NG], mref[NT], sum[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    load_queries<TYPE, DIM, GROUP>(p, b, h, row0 + 16 * t + (lane & 15), n, lane, q[t]);
+    mref[t] = kFloor;
+    sum[t] = 0.0f;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) shift[t][g] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < DIM / 16; ++i) o[t][i] = v4f{0, 0, 0, 0};
+  }
+
+  for (int blk = split * per_split + wave; blk < end; blk += kWaves) {
+    int at;
+    const int64_t row = block_row(p, b, h, blk, at);
+    if (row < 0) continue;
+    Keys<DIM, GROUP> kx;
+    Values<DIM, GROUP> vx;
+    load_keys<DIM, GROUP>(p, row, at, lane, kx);
+    load_values<DIM, GROUP>(p, row, at, lane, vx);
+    const bool ragged = blk * 32 + 32 > least;
+    float s[NT][8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      v4u kf[DIM / 32], par[NG];
+#pragma unroll
+      for (int i = 0; i < DIM / 32; ++i) kf[i] = expand<TYPE>(kx.k[t][i]);
+#pragma unroll
+      for (int g = 0; g < NG; ++g) par[g] = kx.par[g][t];
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        float x[4];
+        scores<TYPE, DIM, GROUP>(kf, par, q[u], x);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[u][4 * t + r] = x[r] * p.c_log2;
+      }
+    }
+    const int slot0 = blk * 32 + (lane >> 4) * 4;
+    if (ragged) {
+#pragma unroll
+      for (int u = 0; u < NT; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) s[u][e] = -kInf;
+    }
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      float top = fmaxf(fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])),
+                        fmaxf(fmaxf(s[u][4], s[u][5]), fmaxf(s[u][6], s[u][7])));
+      // The reference follows the maximum only where it is passed by a factor
+      // of 2^8: sums and products stay far from fp32's range, and the sums so
+      // far are hardly ever scaled.
+      if (__any(top > mref[u] + 8.0f)) {
+        const float m = fmaxf(mref[u], max_over_rows(top));
+        const float f = __builtin_amdgcn_exp2f(mref[u] - m);
+        mref[u] = m;
+        sum[u] *= f;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) shift[u][g] *= f;
+#pragma unroll
+        for (int i = 0; i < DIM / 16; ++i) o[u][i] *= f;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        s[u][e] = __builtin_amdgcn_exp2f(s[u][e] - mref[u]);
+        sum[u] += s[u][e];
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      v4u hi[NT], lo[NT];
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float pd[2];
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const int e = 2 * j + z;
+            const uint32_t w = vx.par[g][e >> 2][e & 3];
+            float x = s[u][e] * par_d(w), y = s[u][e] * par_m(w);
+            // a slot that is not seen may hold anything, infinities and NaN too
+            if (ragged && slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) x = y = 0.0f;
+            pd[z] = x;
+            shift[u][g] += fmaf(-16.0f, x, y);
+          }
+          hi[u][j] = pack_bf16(pd[0], pd[1]);
+          lo[u][j] = pack_bf16(pd[0] - __uint_as_float(hi[u][j] << 16),
+                               pd[1] - __uint_as_float(hi[u][j] & 0xffff0000u));
+        }
+      }
+#pragma unroll
+      for (int i = g * (GROUP / 16); i < (g + 1) * (GROUP / 16); ++i) {
+        const v4u vf = expand<AS_BF16>(vx.v[i]);
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+          o[u][i] = mfma<AS_BF16>(vf, hi[u], o[u][i]);
+          o[u][i] = mfma<AS_BF16>(vf, lo[u], o[u][i]);
+        }
+      }
+    }
+  }
+
+  // Join the wavefronts, 16 rows at a time.
+#pragma unroll
+  for (int u = 0; u < NT; ++u) {
+    const float total = sum_over_rows(sum[u]);
+    if (lane < 16) {
+      ml[wave][lane][0] = mref[u];
+      ml[wave][lane][1] = total;
+    }
+    __syncthreads();
+    float m = kFloor;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[w][lane & 15][0]);
+    const float f = __builtin_amdgcn_exp2f(mref[u] - m);
+#pragma unroll
+    for (int i = 0; i < DIM / 16; ++i) {
+      const float add = sum_over_rows(shift[u][i * 16 / GROUP]);
+      v4f x = (o[u][i] + add) * f;
+      *reinterpret_cast<v4f*>(&part[wave][lane & 15][16 * i + (lane >> 4) * 4]) = x;
+    }
+    __syncthreads();
+    for (int j = threadIdx.x; j < 16 * DIM / 4; j += 64 * kWaves) {
+      const int r = j / (DIM / 4), d = j % (DIM / 4) * 4;
+      const int row = row0 + 16 * u + r;
+      if (row >= p.rows) continue;
+      v4f x = {0, 0, 0, 0};
+      float top = kFloor, l = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        x += *reinterpret_cast<const v4f*>(&part[w][r][d]);
+        top = fmaxf(top, ml[w][r][0]);
+      }
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) l += ml[w][r][1] * __builtin_amdgcn_exp2f(ml[w][r][0] - top);
+      const int64_t at = ((int64_t)bh * p.splits + split) * p.rows + row;
+      if (p.splits > 1) *reinterpret_cast<v4f*>(p.part_o + at * DIM + d) = x;
+      if (p.part_ml && d == 0) {
+        p.part_ml[at * 2] = top;
+        p.part_ml[at * 2 + 1] = l;
+      }
+      if (p.splits == 1) {
+        const int t = row / p.per;
+        uint16_t* out = reinterpret_cast<uint16_t*>(p.out) +
+                        (((int64_t)b * p.n_queries + t) * p.c.n_heads * p.per + h * p.per + row - t * p.per) * DIM + d;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = from_f32<TYPE>(l == 0.0f ? 0.0f : x[e] / l);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the splits: one workgroup per row, a thread per channel.
+template <int TYPE, int DIM>
+__global__ __launch_bounds__(DIM) void join(AttArgs p) {
+  const int row = blockIdx.x % p.rows, bh = blockIdx.x / p.rows, d = threadIdx.x;
+  const int64_t base = (int64_t)bh * p.splits * p.rows + row;
+  float m = kFloor;
+  for (int s = 0; s < p.splits; ++s) m = fmaxf(m, p.part_ml[(base + (int64_t)s * p.rows) * 2]);
+  float l = 0.0f, x = 0.0f;
+  for (int s = 0; s < p.splits; ++s) {
+    const int64_t at = base + (int64_t)s * p.rows;
+    const float f = __builtin_amdgcn_exp2f(p.part_ml[at * 2] - m);
+    l = fmaf(p.part_ml[at * 2 + 1], f, l);
+    if (p.splits > 1) x = fmaf(p.part_o[at * DIM + d], f, x);
+  }
+  const int b = bh / p.c.n_heads, h = bh % p.c.n_heads, t = row / p.per;
+  if (p.splits > 1)
+    reinterpret_cast<uint16_t*>(p.out)[(((int64_t)b * p.n_queries + t) * p.c.n_heads * p.per + h * p.per + row -
+                                        t * p.per) * DIM + d] = from_f32<TYPE>(l == 0.0f ? 0.0f : x / l);
+  if (p.row_ml && d == 0) {
+    p.row_ml[((int64_t)bh * p.rows + row) * 2] = m;
+    p.row_ml[((int64_t)bh * p.rows + row) * 2 + 1] = l == 0.0f ? 0.0f : 1.0f / l;
+  }
+}
+
+// The tokens' weights, from the keys once more now that every query's maximum
+// and sum are known: one wavefront per 32 slots, all queries of the head.
+template <int TYPE, int DIM, int GROUP>
+__global__ __launch_bounds__(64 * kWaves) void weigh(AttArgs p) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int bh = blockIdx.y, b = bh / p.c.n_heads, h = bh % p.c.n_heads;
+  const int n = clamped_length(p, b);
+  const int blk = blockIdx.x * kWaves + wave;
+  if (blk * 32 >= n) return;
+  int at;
+  const int64_t row = block_row(p, b, h, blk, at);
+  if (row < 0) return;
+  Keys<DIM, GROUP> kx;
+  load_keys<DIM, GROUP>(p, row, at, lane, kx);
+  v4u kf[2][DIM / 32], par[2][DIM / GROUP];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+#pragma unroll
+    for (int i = 0; i < DIM / 32; ++i) kf[t][i] = expand<TYPE>(kx.k[t][i]);
+#pragma unroll
+    for (int g = 0; g < DIM / GROUP; ++g) par[t][g] = kx.par[g][t];
+  }
+  float w[8] = {};
+  const int slot0 = blk * 32 + (lane >> 4) * 4;
+  for (int r0 = 0; r0 < p.rows; r0 += 16) {
+    const int r = r0 + (lane & 15);
+    Queries<TYPE, DIM, GROUP> q;
+    load_queries<TYPE, DIM, GROUP>(p, b, h, r, n, lane, q);
+    if (r >= p.rows) q.limit = 0;
+    const float* ml = p.row_ml + ((int64_t)bh * p.rows + min(r, p.rows - 1)) * 2;
+    const float m = ml[0], inv = ml[1];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      float x[4];
+      scores<TYPE, DIM, GROUP>(kf[t], par[t], q, x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (slot0 + 16 * t + e < q.limit) w[4 * t + e] += __builtin_amdgcn_exp2f(x[e] * p.c_log2 - m) * inv;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) w[e] += __shfl_xor(w[e], o);
+  }
+  // lane e of each row of 16 stores slot e
+  float x = w[0];
+#pragma unroll
+  for (int e = 1; e < 8; ++e) x = (lane & 15) == e ? w[e] : x;
+  const int e = lane & 15, s = 16 * (e >> 2) + (lane >> 4) * 4 + (e & 3);
+  if (e < 8 && blk * 32 + s < n) {
+    const int64_t i = row * p.c.page + at + s;
+    p.acc_out[i] = (p.acc_in ? p.acc_in[i] : 0.0f) + x;
+  }
+}
+
+// Splits of a sequence's slots: enough workgroups to fill the compute units
+// several times over, none with fewer than 256 slots.
+int choose_splits(const as_cache_t* c, int row_groups) {
+  const int64_t units = (int64_t)c->n_seqs * c->n_heads * row_groups;
+  const int64_t slots = (int64_t)c->max_pages * c->page;
+  int64_t s = (1024 + units - 1) / units;
+  const int64_t most = (slots + 255) / 256;
+  if (s > most) s = most;
+  if (s > 512) s = 512;
+  return s < 1 ? 1 : (int)s;
+}
+
+int row_tiles(int rows) { return rows > 16 ? 2 : 1; }
+
+struct Plan {
+  int per, rows, tiles, row_groups, splits;
+  int64_t o_bytes, ml_bytes, row_bytes;
+};
+
+Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) {
+  Plan pl;
+  pl.per = n_q_heads / c->n_heads;
+  pl.rows = pl.per * n_queries;
+  pl.tiles = row_tiles(pl.rows);
+  pl.row_groups = (pl.rows + 16 * pl.tiles - 1) / (16 * pl.tiles);
+  pl.splits = choose_splits(c, pl.row_groups);
+  const int64_t rows = (int64_t)c->n_seqs * c->n_heads * pl.rows;
+  pl.o_bytes = pl.splits > 1 ? round_up(rows * pl.splits * c->dim * 4, 256) : 0;
+  pl.ml_bytes = pl.splits > 1 || weights ? round_up(rows * pl.splits * 8, 256) : 0;
+  pl.row_bytes = weights ? round_up(rows * 8, 256) : 0;
+  return pl;
+}
+
+int check_queries(const as_cache_t* c, int32_t n_queries, int32_t n_q_heads) {
+  if (n_queries < 0 || n_q_heads < 1 || n_q_heads % c->n_heads)
+    return fail(AS_E_INVALID_ARG, "attention_kv4: %d queries of %d heads over %d key/value heads", n_queries,
+                n_q_heads, c->n_heads);
+  if (n_queries > 65536 || n_q_heads > 65536)
+    return fail(AS_E_LIMITS, "attention_kv4: %d queries of %d heads (at most 65536 each)", n_queries, n_q_heads);
+  if ((int64_t)c->n_seqs * c->n_heads > 65535)
+    return fail(AS_E_LIMITS, "attention_kv4: %d sequences of %d heads (at most 65535 in all)", c->n_seqs, c->n_heads);
+  if ((int64_t)c->n_seqs * n_queries * n_q_heads > (1 << 26))
+    return fail(AS_E_LIMITS, "attention_kv4: %d sequences, %d queries, %d heads (at most 2^26 rows in all)", c->n_seqs,
+                n_queries, n_q_heads);
+  return AS_OK;
+}
+
+template <int TYPE, int DIM, int GROUP>
+int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
+  const int64_t units = round_up((int64_t)p.c.n_seqs * p.c.n_heads * pl.splits, 8) * pl.row_groups;
+  const dim3 g((unsigned)units), t(64 * kWaves);
+  if (pl.tiles == 1)
+    hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 1>), g, t, 0, s, p);
+  else
+    hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 2>), g, t, 0, s, p);
+  if (pl.splits > 1 || p.acc_out)
+    hipLaunchKernelGGL((join<TYPE, DIM>), dim3((unsigned)((int64_t)p.c.n_seqs * p.c.n_heads * p.rows)), dim3(DIM), 0,
+                       s, p);
+  if (p.acc_out) {
+    const int64_t blocks = (int64_t)p.c.max_pages * p.c.page / 32;
+    hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP>),
+                       dim3((unsigned)((blocks + kWaves - 1) / kWaves), (unsigned)(p.c.n_seqs * p.c.n_heads)), t, 0,
+                       s, p);
+  }
+  return launched("attention_kv4");
+}
+
+template <int TYPE>
+int launch_by_shape(const AttArgs& p, const Plan& pl, hipStream_t s) {
+  if (p.c.dim == 64)
+    return p.c.group == 32 ? launch_attention<TYPE, 64, 32>(p, pl, s) : launch_attention<TYPE, 64, 64>(p, pl, s);
+  if (p.c.group == 32) return launch_attention<TYPE, 128, 32>(p, pl, s);
+  if (p.c.group == 64) return launch_attention<TYPE, 128, 64>(p, pl, s);
+  return launch_attention<TYPE, 128, 128>(p, pl, s);
+}
+
+}  // namespace as_ops
+
+using namespace as_ops;
+
+extern "C" {
+
+int64_t as_attention_kv4_workspace(const as_cache_t* cache, int32_t n_queries, int32_t n_q_heads, int32_t weights) {
+  if (check_cache(cache, "attention_kv4", false, false) != AS_OK ||
+      check_queries(cache, n_queries, n_q_heads) != AS_OK || cache->n_seqs == 0 || n_queries == 0)
+    return 0;
+  const Plan pl = make_plan(cache, n_queries, n_q_heads, weights != 0);
+  return pl.o_bytes + pl.ml_bytes + pl.row_bytes;
+}
+
+int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32_t n_queries, int32_t n_q_heads,
+                     int64_t q_seq, int64_t q_token, const int32_t* length, float scale, void* out,
+                     const float* acc_in, float* acc_out, void* workspace, int64_t workspace_bytes, void* stream) {
+  int rc = check_cache(cache, "attention_kv4", false, false);
+  if (rc != AS_OK) return rc;
+  rc = check_queries(cache, n_queries, n_q_heads);
+  if (rc != AS_OK) return rc;
+  if (type != AS_BF16 && type != AS_F16) return fail(AS_E_INVALID_ARG, "attention_kv4: type %d", type);
+  if (!(scale > 0.0f) || scale > 3.0e38f) return fail(AS_E_INVALID_ARG, "attention_kv4: scale %g", (double)scale);
+  if (cache->n_seqs == 0 || n_queries == 0) return as_host::ok();
+  if (!q || !length || !out) return fail(AS_E_INVALID_ARG, "attention_kv4: null pointer");
+  if (!aligned(q, 16) || q_seq % 8 || q_token % 8)
+    return fail(AS_E_INVALID_ARG, "attention_kv4: queries have to be aligned to 16 bytes, strides a multiple of 8");
+  const Plan pl = make_plan(cache, n_queries, n_q_heads, acc_out != nullptr);
+  const int64_t need = pl.o_bytes + pl.ml_bytes + pl.row_bytes;
+  if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 256))))
+    return fail(AS_E_INVALID_ARG, "attention_kv4: workspace of %lld bytes, %lld needed (aligned to 256)",
+                (long long)workspace_bytes, (long long)need);
+  AttArgs p{};
+  p.c = cache_args(cache);
+  p.q = reinterpret_cast<const uint16_t*>(q);
+  p.q_seq = q_seq;
+  p.q_token = q_token;
+  p.length = length;
+  p.out = out;
+  char* ws = reinterpret_cast<char*>(workspace);
+  p.part_o = pl.o_bytes ? reinterpret_cast<float*>(ws) : nullptr;
+  p.part_ml = pl.ml_bytes ? reinterpret_cast<float*>(ws + pl.o_bytes) : nullptr;
+  p.row_ml = pl.row_bytes ? reinterpret_cast<float*>(ws + pl.o_bytes + pl.ml_bytes) : nullptr;
+  p.acc_in = acc_in;
+  p.acc_out = acc_out;
+  p.c_log2 = scale * 1.4426950408889634f;
+  const int pb = cache->page / 32;
+  p.page_mul = pb > 1 ? (uint32_t)((((uint64_t)1 << 32) + pb - 1) / pb) : 0;
+  p.n_queries = n_queries;
+  p.per = pl.per;
+  p.rows = pl.rows;
+  p.splits = pl.splits;
+  p.row_groups = pl.row_groups;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  return type == AS_BF16 ? launch_by_shape<AS_BF16>(p, pl, s) : launch_by_shape<AS_F16>(p, pl, s);
+}
+
+}  // extern "C"

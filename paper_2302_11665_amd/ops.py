@@ -1,0 +1,316 @@
+"""Thin ctypes binding of the operators of a served model's step (see
+include/alpaserve_ops.h): linear layers with 8-bit weights, a paged cache of 4
+bits with attention over it, and the cache's eviction by accumulated weight.
+
+Argument marshalling only, as in `sim`: arrays are torch CUDA tensors, outputs
+and scratch memory are torch allocations, calls run on torch's current stream of
+the tensors' device, and errors raise `sim.SimError`.  None of the operators has
+a gradient.
+"""
+from __future__ import annotations
+
+import ctypes
+import dataclasses
+
+import torch
+
+from . import sim
+
+AS_BF16, AS_F16, AS_F32 = 0, 1, 2
+AS_I8_MAX_INPUTS = 131072
+_TYPES = {torch.bfloat16: AS_BF16, torch.float16: AS_F16, torch.float32: AS_F32}
+
+_P, _I32, _I64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+
+
+class as_cache_t(ctypes.Structure):
+    _fields_ = [("n_pages", _I32), ("n_heads", _I32), ("dim", _I32), ("group", _I32), ("page", _I32),
+                ("n_seqs", _I32), ("max_pages", _I32), ("reserved", _I32), ("k", _P), ("v", _P),
+                ("k_par", _P), ("v_par", _P), ("pos", _P), ("acc", _P), ("page_table", _P)]
+
+
+_lib = None
+
+
+def lib():
+    global _lib
+    if _lib is None:
+        L = sim.lib()
+        C = ctypes.POINTER(as_cache_t)
+        for name, res, args in (
+                ("as_i8_bytes", _I64, [_I64, _I64]),
+                ("as_quantize_i8", ctypes.c_int, [_P, _I32, _I64, _I64, _I64, _P, _P, _P]),
+                ("as_linear_i8_workspace", _I64, [_I64, _I64, _I64]),
+                ("as_linear_i8", ctypes.c_int, [_P, _I32, _I64, _I64, _I64, _P, _P, _P, _I64, _P, _I32, _I64, _P,
+                                                _I64, _P]),
+                ("as_cache_append", ctypes.c_int, [C, _P, _P, _I32, _I32, _I64, _I64, _I64, _I64, _P, _P, _P, _P,
+                                                   _P]),
+                ("as_attention_kv4_workspace", _I64, [C, _I32, _I32, _I32]),
+                ("as_attention_kv4", ctypes.c_int, [C, _P, _I32, _I32, _I32, _I64, _I64, _P, ctypes.c_float, _P, _P,
+                                                    _P, _P, _I64, _P]),
+                ("as_cache_evict_workspace", _I64, [C, _I32]),
+                ("as_cache_evict", ctypes.c_int, [C, C, _P, _P, _I32, _I32, _P, _P, _I64, _P])):
+            f = getattr(L, name)
+            f.restype, f.argtypes = res, args
+        _lib = L
+    return _lib
+
+
+def _bad(msg):
+    raise sim.SimError(sim.AS_E_INVALID_ARG, msg)
+
+
+def _need(x, name, dtypes, dim=None, device=None, contiguous=True):
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        _bad(f"{name}: a CUDA tensor is needed")
+    if x.dtype not in dtypes:
+        _bad(f"{name}: type {x.dtype}")
+    if dim is not None and x.dim() != dim:
+        _bad(f"{name}: {x.dim()} dimensions, {dim} needed")
+    if device is not None and x.device != device:
+        _bad(f"{name}: on {x.device}, not {device}")
+    if contiguous and not x.is_contiguous():
+        _bad(f"{name}: not contiguous")
+    return x
+
+
+class _On:
+    """The current stream of a tensor's device, that device current meanwhile."""
+
+    def __init__(self, x):
+        self.index = x.device.index
+        self.other = None
+
+    def __enter__(self):
+        if torch.cuda.current_device() != self.index:
+            self.other = torch.cuda.device(self.index)
+            self.other.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *e):
+        if self.other is not None:
+            self.other.__exit__(*e)
+
+
+def _workspace(n, device):
+    """Scratch memory of one call (torch's allocator keeps it stream-ordered), and its address."""
+    if n == 0:
+        return None, None
+    w = torch.empty(n, dtype=torch.uint8, device=device)
+    return w, w.data_ptr()
+
+
+_16 = (torch.bfloat16, torch.float16)
+_FLOATS = (torch.bfloat16, torch.float16, torch.float32)
+
+
+# ------------------------------------------------------------------- 8 bits
+
+@dataclasses.dataclass
+class PackedWeight:
+    """A linear layer's weights of 8 bits: codes in the tiles that
+    `as_quantize_i8` writes (int8, as_i8_bytes(n_out, n_in) of them), one fp32
+    scale per output."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+    n_out: int
+    n_in: int
+
+    @property
+    def nbytes(self) -> int:
+        return self.codes.numel() + self.scale.numel() * 4
+
+
+def pack_weight(w) -> PackedWeight:
+    """Quantise weights [n_out, n_in] (bf16, fp16 or fp32) per output, once."""
+    _need(w, "weight", _FLOATS, 2, contiguous=False)
+    if w.stride(1) != 1:
+        w = w.contiguous()
+    n, k = w.shape
+    codes = torch.empty(lib().as_i8_bytes(n, k), dtype=torch.int8, device=w.device)
+    scale = torch.empty(n, dtype=torch.float32, device=w.device)
+    with _On(w) as s:
+        sim._check(lib().as_quantize_i8(w.data_ptr(), _TYPES[w.dtype], n, k, max(k, w.stride(0)), codes.data_ptr(),
+                                        scale.data_ptr(), s))
+    return PackedWeight(codes, scale, n, k)
+
+
+def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
+    """x [..., n_in] (bf16 or fp16) quantised per token, times the packed
+    weights: [..., n_out] of `dtype` (default: x's; fp32 allowed).  `out`, if
+    given, is [tokens, n_out] with contiguous rows."""
+    _need(x, "x", _16, contiguous=False)
+    dev = x.device
+    lead = x.shape[:-1]
+    if x.dim() < 1 or x.shape[-1] != w.n_in:
+        _bad(f"linear_i8: x has {tuple(x.shape)}, the weights take {w.n_in} inputs")
+    x2 = x if x.dim() == 2 else x.reshape(-1, w.n_in)
+    if x2.stride(1) != 1 and w.n_in > 1:
+        x2 = x2.contiguous()
+    t = x2.shape[0]
+    _need(w.codes, "weight codes", (torch.int8, torch.uint8), device=dev)
+    _need(w.scale, "weight scale", (torch.float32,), device=dev)
+    if w.codes.numel() != lib().as_i8_bytes(w.n_out, w.n_in) or w.scale.numel() != w.n_out:
+        _bad(f"linear_i8: {w.codes.numel()} codes and {w.scale.numel()} scales for {w.n_out} x {w.n_in} weights")
+    if bias is not None and _need(bias, "bias", (torch.float32,), device=dev).numel() != w.n_out:
+        _bad(f"linear_i8: {bias.numel()} biases for {w.n_out} outputs")
+    if out is None:
+        y = torch.empty((t, w.n_out), dtype=dtype or x.dtype, device=dev)
+    else:
+        y = _need(out, "out", _FLOATS, 2, dev, contiguous=False)
+        if tuple(y.shape) != (t, w.n_out) or (w.n_out > 1 and y.stride(1) != 1) or (dtype and y.dtype != dtype):
+            _bad(f"linear_i8: out has {tuple(y.shape)} with strides {y.stride()}, {y.dtype}")
+    if y.dtype not in _TYPES:
+        _bad(f"linear_i8: type {y.dtype}")
+    n = lib().as_linear_i8_workspace(t, w.n_in, w.n_out)
+    _keep, ws = _workspace(n, dev)
+    with _On(x) as s:
+        sim._check(lib().as_linear_i8(x2.data_ptr(), _TYPES[x.dtype], t, w.n_in, max(w.n_in, x2.stride(0)),
+                                      w.codes.data_ptr(), w.scale.data_ptr(),
+                                      None if bias is None else bias.data_ptr(), w.n_out, y.data_ptr(),
+                                      _TYPES[y.dtype], max(w.n_out, y.stride(0)), ws, n, s))
+    return y if out is not None or x.dim() == 2 else y.view(*lead, w.n_out)
+
+
+# -------------------------------------------------------------------- cache
+
+@dataclasses.dataclass
+class Cache:
+    """A paged cache of 4 bits; the arrays are those of as_cache_t:
+    k int32 [pages, heads, page, 4, dim/32], v int32 [pages, heads, page/32, 4,
+    16, dim/16], k_par and v_par float16 [pages, heads, dim/group, page, 2], pos
+    int32 and acc float32 [pages, heads, page] (either may be None where no
+    weights are kept), page_table int32 [seqs, max_pages]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_par: torch.Tensor
+    v_par: torch.Tensor
+    pos: torch.Tensor
+    acc: torch.Tensor
+    page_table: torch.Tensor
+
+    def __post_init__(self):
+        dev = self.k.device
+        i32 = (torch.int32,)
+        _need(self.k, "cache.k", i32, 5)
+        _need(self.v, "cache.v", i32, 6, dev)
+        pages, heads, page, four, words = self.k.shape
+        dim = words * 32
+        _need(self.k_par, "cache.k_par", (torch.float16,), 5, dev)
+        _need(self.v_par, "cache.v_par", (torch.float16,), 5, dev)
+        groups = self.k_par.shape[2]
+        want = (pages, heads, groups, page, 2)
+        if four != 4 or groups < 1 or tuple(self.k_par.shape) != want or tuple(self.v_par.shape) != want or tuple(
+                self.v.shape) != (pages, heads, page // 32, 4, 16, dim // 16) or page % 32 or dim % groups:
+            _bad(f"cache: arrays of {tuple(self.k.shape)}, {tuple(self.v.shape)}, {tuple(self.k_par.shape)} and "
+                 f"{tuple(self.v_par.shape)} do not belong together")
+        for name, x, kind in (("pos", self.pos, torch.int32), ("acc", self.acc, torch.float32)):
+            if x is not None and tuple(_need(x, "cache." + name, (kind,), 3, dev).shape) != (pages, heads, page):
+                _bad(f"cache.{name}: {tuple(x.shape)}")
+        _need(self.page_table, "cache.page_table", i32, 2, dev)
+        ptr = lambda x: None if x is None else x.data_ptr()  # noqa: E731
+        self._c = as_cache_t(pages, heads, dim, dim // groups, page, self.page_table.shape[0],
+                             self.page_table.shape[1], 0, self.k.data_ptr(), self.v.data_ptr(),
+                             self.k_par.data_ptr(), self.v_par.data_ptr(), ptr(self.pos), ptr(self.acc),
+                             self.page_table.data_ptr())
+
+    @staticmethod
+    def empty(n_pages, n_heads, dim, page_table, group=64, page=64, device="cuda") -> "Cache":
+        """A cache of zeros."""
+        z = lambda shape, dtype: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
+        par = (n_pages, n_heads, dim // group, page, 2)
+        return Cache(k=z((n_pages, n_heads, page, 4, dim // 32), torch.int32),
+                     v=z((n_pages, n_heads, page // 32, 4, 16, dim // 16), torch.int32),
+                     k_par=z(par, torch.float16), v_par=z(par, torch.float16),
+                     pos=z((n_pages, n_heads, page), torch.int32), acc=z((n_pages, n_heads, page), torch.float32),
+                     page_table=page_table)
+
+    @property
+    def bytes_per_slot(self) -> int:
+        """Bytes of one slot of all heads: codes, scales, position and weight."""
+        c = self._c
+        return c.n_heads * (c.dim + 8 * (c.dim // c.group) + (self.pos is not None) * 4 + (self.acc is not None) * 4)
+
+
+def _counts(x, name, cache):
+    if _need(x, name, (torch.int32,), 1, cache.k.device).shape[0] != cache._c.n_seqs:
+        _bad(f"{name}: {x.shape[0]} entries for {cache._c.n_seqs} sequences")
+    return x.data_ptr()
+
+
+def _tokens(x, name, cache, heads):
+    """x [seqs, tokens, heads, dim] with its last two dimensions contiguous."""
+    _need(x, name, _16, 4, cache.k.device, contiguous=False)
+    if x.shape[0] != cache._c.n_seqs or x.shape[3] != cache._c.dim or (heads and x.shape[2] != heads):
+        _bad(f"{name}: {tuple(x.shape)}")
+    dim = x.shape[3]
+    if x.stride(3) != 1 or (x.shape[2] > 1 and x.stride(2) != dim):
+        x = x.contiguous()
+    return x
+
+
+def cache_append(cache: Cache, k, v, start, first_pos=None, held=False):
+    """Put k, v [seqs, tokens, heads, dim] into slots start[b].. of every
+    sequence (start: int32 [seqs]); positions count from first_pos[b] (default:
+    start).  With `held`, returns the values that the cache holds for them now
+    (two fp32 tensors of k's shape)."""
+    heads = cache._c.n_heads
+    k, v = _tokens(k, "k", cache, heads), _tokens(v, "v", cache, heads)
+    if k.shape != v.shape or k.dtype != v.dtype:
+        _bad(f"cache_append: k has {tuple(k.shape)} {k.dtype}, v {tuple(v.shape)} {v.dtype}")
+    at = _counts(start, "start", cache)
+    pos = None if first_pos is None else _counts(first_pos, "first_pos", cache)
+    hk = torch.empty(k.shape, dtype=torch.float32, device=k.device) if held else None
+    hv = torch.empty(k.shape, dtype=torch.float32, device=k.device) if held else None
+    with _On(k) as s:
+        sim._check(lib().as_cache_append(cache._c, k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], k.shape[1],
+                                         k.stride(0), k.stride(1), v.stride(0), v.stride(1), at, pos,
+                                         hk.data_ptr() if held else None, hv.data_ptr() if held else None, s))
+    return (hk, hv) if held else None
+
+
+def attention_kv4(q, cache: Cache, length, scale=None, acc_in=None, acc_out=None):
+    """Attention of q [seqs, queries, q_heads, dim] (bf16 or fp16) over the
+    first length[b] slots of every sequence, the queries being the last of them:
+    query i sees slots below length - queries + i + 1.  `scale` defaults to
+    dim ** -0.5.  With acc_out (fp32, laid out as cache.acc), acc_out = acc_in +
+    the attention weight that every slot got from the queries of its head."""
+    q = _tokens(q, "q", cache, 0)
+    if q.data_ptr() % 16 or q.stride(0) % 8 or q.stride(1) % 8:
+        q = q.contiguous()
+        if q.data_ptr() % 16:
+            q = q.clone(memory_format=torch.contiguous_format)
+    n = _counts(length, "length", cache)
+    c = cache._c
+    rows = (c.n_pages, c.n_heads, c.page)
+    for name, x in (("acc_in", acc_in), ("acc_out", acc_out)):
+        if x is not None and tuple(_need(x, name, (torch.float32,), 3, q.device).shape) != rows:
+            _bad(f"{name}: {tuple(x.shape)}")
+    if acc_in is not None and acc_out is None:
+        _bad("attention_kv4: acc_in without acc_out")
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    heads = q.shape[2]
+    need = lib().as_attention_kv4_workspace(c, q.shape[1], heads, 0 if acc_out is None else 1)
+    _keep, ws = _workspace(need, q.device)
+    with _On(q) as s:
+        sim._check(lib().as_attention_kv4(c, q.data_ptr(), _TYPES[q.dtype], q.shape[1], heads, q.stride(0),
+                                          q.stride(1), n, c.dim ** -0.5 if scale is None else scale, out.data_ptr(),
+                                          None if acc_in is None else acc_in.data_ptr(),
+                                          None if acc_out is None else acc_out.data_ptr(), ws, need, s))
+    return out
+
+
+def cache_evict(src: Cache, dst: Cache, length, total, keep, recent):
+    """Copy to `dst` what a budget of `keep` tokens keeps of every sequence and
+    head of `src`: the `recent` newest positions (total[b] tokens were there in
+    all) and, of the others, those of the largest accumulated weight, in slot
+    order.  Returns the new lengths, int32 [seqs]."""
+    n, t = _counts(length, "length", src), _counts(total, "total", src)
+    if src.k.device != dst.k.device:
+        _bad("cache_evict: caches on different devices")
+    new = torch.empty(length.shape[0], dtype=torch.int32, device=length.device)
+    need = lib().as_cache_evict_workspace(src._c, keep)
+    _keep, ws = _workspace(need, length.device)
+    with _On(length) as s:
+        sim._check(lib().as_cache_evict(src._c, dst._c, n, t, keep, recent, new.data_ptr(), ws, need, s))
+    return new

@@ -1,0 +1,129 @@
+"""C-ABI checks of the operators of a served model's step that need no GPU:
+exports, struct layout, and refusals before anything touches the device."""
+import ctypes
+import os
+import re
+
+import pytest
+
+from paper_2302_11665_amd import build, sim
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(build.SIM_LIB):
+        pytest.skip("HIP library not built")
+    from paper_2302_11665_amd import ops
+    return ops.lib()
+
+
+def cache(**over):
+    from paper_2302_11665_amd import ops
+    f = dict(n_pages=8, n_heads=2, dim=64, group=64, page=32, n_seqs=2, max_pages=4, reserved=0, k=0x1000, v=0x2000,
+             k_par=0x3000, v_par=0x4000, pos=0x5000, acc=0x6000, page_table=0x7000)
+    f.update(over)
+    return ops.as_cache_t(**f)
+
+
+def test_exports_every_declared_function(L):
+    with open(os.path.join(ROOT, "include", "alpaserve_ops.h")) as f:
+        src = re.sub(r"/\*.*?\*/", "", f.read(), flags=re.S)
+    names = set(re.findall(r"\b(as_[a-z_0-9]+)\s*\(", src))
+    assert {"as_linear_i8", "as_attention_kv4", "as_cache_append", "as_cache_evict"} <= names
+    for n in names:
+        assert hasattr(L, n), n
+
+
+def test_struct_layout():
+    from paper_2302_11665_amd import ops
+    assert ctypes.sizeof(ops.as_cache_t) == 8 * 4 + 7 * 8
+    assert ops.as_cache_t.k.offset == 32 and ops.as_cache_t.page_table.offset == 80
+
+
+def test_linear_refusals(L):
+    def call(x=0x100, xt=0, t=4, k=64, xs=64, w=0x1000, ws=0x2000, n=32, y=0x3000, yt=0, ys=32, work=0x4000, wb=1 << 20):
+        return L.as_linear_i8(x, xt, t, k, xs, w, ws, None, n, y, yt, ys, work, wb, None)
+
+    for kw in (dict(x=None), dict(w=None), dict(ws=None), dict(y=None), dict(xt=2), dict(xt=9), dict(yt=3),
+               dict(yt=-1), dict(t=-1), dict(k=0), dict(n=0), dict(xs=63), dict(ys=31), dict(w=0x1001),
+               dict(wb=0), dict(work=None), dict(work=0x4010)):
+        assert call(**kw) == sim.AS_E_INVALID_ARG, kw
+        assert "linear_i8" in sim.as_last_error()
+    assert call(k=131073, xs=131073) == sim.AS_E_LIMITS
+    assert call(t=1 << 21) == sim.AS_E_LIMITS
+    assert call(n=1 << 25, ys=1 << 25) == sim.AS_E_LIMITS
+    assert call(t=0, x=None, y=None, work=None, wb=0) == sim.AS_OK
+    assert sim.as_last_error() == ""
+
+
+def test_quantize_refusals(L):
+    def call(x=0x100, t=0, r=4, c=64, s=64, codes=0x1000, scale=0x2000):
+        return L.as_quantize_i8(x, t, r, c, s, codes, scale, None)
+
+    for kw in (dict(x=None), dict(codes=None), dict(scale=None), dict(t=5), dict(r=-1), dict(c=0), dict(s=63),
+               dict(codes=0x1008)):
+        assert call(**kw) == sim.AS_E_INVALID_ARG, kw
+    assert call(c=131073, s=131073) == sim.AS_E_LIMITS
+    assert call(r=0, x=None) == sim.AS_OK
+    assert L.as_i8_bytes(17, 129) == 32 * 256 and L.as_i8_bytes(0, 5) == 0 and L.as_i8_bytes(1, 131073) == 0
+
+
+BAD_CACHES = [dict(dim=96), dict(group=16), dict(group=128), dict(page=48), dict(page=0), dict(page=8192),
+              dict(n_heads=0), dict(n_heads=2000), dict(max_pages=1 << 26)]
+WRONG_CACHES = [dict(n_pages=-1), dict(n_seqs=-1), dict(max_pages=-1), dict(reserved=1), dict(k=None), dict(v=None),
+                dict(k_par=None), dict(v_par=None), dict(page_table=None), dict(k=0x1004), dict(v_par=0x4002)]
+
+
+def test_cache_refusals(L):
+    calls = [lambda c: L.as_attention_kv4(c, 0x100, 0, 1, 4, 256, 256, 0x200, 0.1, 0x300, None, None, 0x400, 1 << 20,
+                                          None),
+             lambda c: L.as_cache_append(c, 0x100, 0x200, 0, 1, 128, 128, 128, 128, 0x300, None, None, None, None),
+             lambda c: L.as_cache_evict(c, cache(), 0x100, 0x200, 8, 2, 0x300, 0x400, 1 << 20, None),
+             lambda c: L.as_cache_evict(cache(), c, 0x100, 0x200, 8, 2, 0x300, 0x400, 1 << 20, None)]
+    for f in calls:
+        for kw in BAD_CACHES:
+            assert f(cache(**kw)) == sim.AS_E_LIMITS, kw
+        for kw in WRONG_CACHES:
+            assert f(cache(**kw)) == sim.AS_E_INVALID_ARG, kw
+        assert f(None) == sim.AS_E_INVALID_ARG
+    for f in calls[2:]:
+        assert f(cache(pos=None)) == sim.AS_E_INVALID_ARG
+        assert f(cache(acc=None)) == sim.AS_E_INVALID_ARG
+
+
+def test_attention_refusals(L):
+    def call(c=None, q=0x100, t=0, nq=1, hq=4, qs=256, qt=256, n=0x200, scale=0.1, out=0x300, work=0x400, wb=1 << 20):
+        return L.as_attention_kv4(c or cache(), q, t, nq, hq, qs, qt, n, scale, out, None, None, work, wb, None)
+
+    for kw in (dict(q=None), dict(n=None), dict(out=None), dict(t=2), dict(nq=-1), dict(hq=3), dict(hq=0),
+               dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(q=0x108),
+               dict(qs=255), dict(qt=4)):
+        assert call(**kw) == sim.AS_E_INVALID_ARG, kw
+        assert "attention_kv4" in sim.as_last_error()
+    assert call(hq=131072) == sim.AS_E_LIMITS and call(nq=70000) == sim.AS_E_LIMITS
+    long = cache(max_pages=4096, n_pages=8192)
+    need = L.as_attention_kv4_workspace(long, 1, 4, 1)
+    assert need > 0 and call(c=long, wb=L.as_attention_kv4_workspace(long, 1, 4, 0) - 1) == sim.AS_E_INVALID_ARG
+    assert call(nq=0, q=None) == sim.AS_OK and call(c=cache(n_seqs=0), q=None) == sim.AS_OK
+    assert L.as_attention_kv4_workspace(None, 1, 4, 1) == 0
+
+
+def test_append_and_evict_refusals(L):
+    def app(k=0x100, v=0x200, t=0, n=1, start=0x300):
+        return L.as_cache_append(cache(), k, v, t, n, 128, 128, 128, 128, start, None, None, None, None)
+
+    for kw in (dict(k=None), dict(v=None), dict(start=None), dict(t=2), dict(n=-1)):
+        assert app(**kw) == sim.AS_E_INVALID_ARG, kw
+    assert app(n=1 << 25) == sim.AS_E_LIMITS
+    assert app(n=0, k=None) == sim.AS_OK
+
+    def ev(dst=None, n=0x100, total=0x200, keep=8, recent=2, out=0x300, work=0x400, wb=1 << 20):
+        return L.as_cache_evict(cache(), dst or cache(), n, total, keep, recent, out, work, wb, None)
+
+    for kw in (dict(n=None), dict(total=None), dict(out=None), dict(work=None), dict(wb=0), dict(work=0x410),
+               dict(keep=0), dict(keep=129), dict(recent=-1), dict(recent=9), dict(dst=cache(dim=128)),
+               dict(dst=cache(group=32)), dict(dst=cache(n_heads=1)), dict(dst=cache(n_seqs=1))):
+        assert ev(**kw) == sim.AS_E_INVALID_ARG, kw
+    assert L.as_cache_evict(cache(n_seqs=0), cache(n_seqs=0), None, None, 8, 2, None, None, 0, None) == sim.AS_OK
