@@ -74,22 +74,16 @@ def _need(x, name, dtypes, dim=None, device=None, contiguous=True):
     return x
 
 
-class _On:
-    """The current stream of a tensor's device, that device current meanwhile."""
-
-    def __init__(self, x):
-        self.index = x.device.index
-        self.other = None
-
-    def __enter__(self):
-        if torch.cuda.current_device() != self.index:
-            self.other = torch.cuda.device(self.index)
-            self.other.__enter__()
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *e):
-        if self.other is not None:
-            self.other.__exit__(*e)
+def _call(fn, device, *args):
+    """fn(*args, stream) on the current stream of the tensors' device, that device current meanwhile."""
+    index = device.index
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if rc != sim.AS_OK:
+        sim._check(rc)
 
 
 def _workspace(n, device):
@@ -129,9 +123,8 @@ def pack_weight(w) -> PackedWeight:
     n, k = w.shape
     codes = torch.empty(lib().as_i8_bytes(n, k), dtype=torch.int8, device=w.device)
     scale = torch.empty(n, dtype=torch.float32, device=w.device)
-    with _On(w) as s:
-        sim._check(lib().as_quantize_i8(w.data_ptr(), _TYPES[w.dtype], n, k, max(k, w.stride(0)), codes.data_ptr(),
-                                        scale.data_ptr(), s))
+    _call(lib().as_quantize_i8, w.device, w.data_ptr(), _TYPES[w.dtype], n, k, max(k, w.stride(0)),
+          codes.data_ptr(), scale.data_ptr())
     return PackedWeight(codes, scale, n, k)
 
 
@@ -139,9 +132,9 @@ def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
     """x [..., n_in] (bf16 or fp16) quantised per token, times the packed
     weights: [..., n_out] of `dtype` (default: x's; fp32 allowed).  `out`, if
     given, is [tokens, n_out] with contiguous rows."""
+    L = lib()
     _need(x, "x", _16, contiguous=False)
     dev = x.device
-    lead = x.shape[:-1]
     if x.dim() < 1 or x.shape[-1] != w.n_in:
         _bad(f"linear_i8: x has {tuple(x.shape)}, the weights take {w.n_in} inputs")
     x2 = x if x.dim() == 2 else x.reshape(-1, w.n_in)
@@ -150,7 +143,7 @@ def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
     t = x2.shape[0]
     _need(w.codes, "weight codes", (torch.int8, torch.uint8), device=dev)
     _need(w.scale, "weight scale", (torch.float32,), device=dev)
-    if w.codes.numel() != lib().as_i8_bytes(w.n_out, w.n_in) or w.scale.numel() != w.n_out:
+    if w.codes.numel() != L.as_i8_bytes(w.n_out, w.n_in) or w.scale.numel() != w.n_out:
         _bad(f"linear_i8: {w.codes.numel()} codes and {w.scale.numel()} scales for {w.n_out} x {w.n_in} weights")
     if bias is not None and _need(bias, "bias", (torch.float32,), device=dev).numel() != w.n_out:
         _bad(f"linear_i8: {bias.numel()} biases for {w.n_out} outputs")
@@ -162,14 +155,12 @@ def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
             _bad(f"linear_i8: out has {tuple(y.shape)} with strides {y.stride()}, {y.dtype}")
     if y.dtype not in _TYPES:
         _bad(f"linear_i8: type {y.dtype}")
-    n = lib().as_linear_i8_workspace(t, w.n_in, w.n_out)
+    n = L.as_linear_i8_workspace(t, w.n_in, w.n_out)
     _keep, ws = _workspace(n, dev)
-    with _On(x) as s:
-        sim._check(lib().as_linear_i8(x2.data_ptr(), _TYPES[x.dtype], t, w.n_in, max(w.n_in, x2.stride(0)),
-                                      w.codes.data_ptr(), w.scale.data_ptr(),
-                                      None if bias is None else bias.data_ptr(), w.n_out, y.data_ptr(),
-                                      _TYPES[y.dtype], max(w.n_out, y.stride(0)), ws, n, s))
-    return y if out is not None or x.dim() == 2 else y.view(*lead, w.n_out)
+    _call(L.as_linear_i8, dev, x2.data_ptr(), _TYPES[x.dtype], t, w.n_in, max(w.n_in, x2.stride(0)),
+          w.codes.data_ptr(), w.scale.data_ptr(), None if bias is None else bias.data_ptr(), w.n_out, y.data_ptr(),
+          _TYPES[y.dtype], max(w.n_out, y.stride(0)), ws, n)
+    return y if out is not None or x.dim() == 2 else y.view(*x.shape[:-1], w.n_out)
 
 
 # -------------------------------------------------------------------- cache
@@ -262,10 +253,9 @@ def cache_append(cache: Cache, k, v, start, first_pos=None, held=False):
     pos = None if first_pos is None else _counts(first_pos, "first_pos", cache)
     hk = torch.empty(k.shape, dtype=torch.float32, device=k.device) if held else None
     hv = torch.empty(k.shape, dtype=torch.float32, device=k.device) if held else None
-    with _On(k) as s:
-        sim._check(lib().as_cache_append(cache._c, k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], k.shape[1],
-                                         k.stride(0), k.stride(1), v.stride(0), v.stride(1), at, pos,
-                                         hk.data_ptr() if held else None, hv.data_ptr() if held else None, s))
+    _call(lib().as_cache_append, k.device, cache._c, k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], k.shape[1],
+          k.stride(0), k.stride(1), v.stride(0), v.stride(1), at, pos, hk.data_ptr() if held else None,
+          hv.data_ptr() if held else None)
     return (hk, hv) if held else None
 
 
@@ -290,13 +280,12 @@ def attention_kv4(q, cache: Cache, length, scale=None, acc_in=None, acc_out=None
         _bad("attention_kv4: acc_in without acc_out")
     out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     heads = q.shape[2]
-    need = lib().as_attention_kv4_workspace(c, q.shape[1], heads, 0 if acc_out is None else 1)
+    L = lib()
+    need = L.as_attention_kv4_workspace(c, q.shape[1], heads, 0 if acc_out is None else 1)
     _keep, ws = _workspace(need, q.device)
-    with _On(q) as s:
-        sim._check(lib().as_attention_kv4(c, q.data_ptr(), _TYPES[q.dtype], q.shape[1], heads, q.stride(0),
-                                          q.stride(1), n, c.dim ** -0.5 if scale is None else scale, out.data_ptr(),
-                                          None if acc_in is None else acc_in.data_ptr(),
-                                          None if acc_out is None else acc_out.data_ptr(), ws, need, s))
+    _call(L.as_attention_kv4, q.device, c, q.data_ptr(), _TYPES[q.dtype], q.shape[1], heads, q.stride(0), q.stride(1),
+          n, c.dim ** -0.5 if scale is None else scale, out.data_ptr(), None if acc_in is None else acc_in.data_ptr(),
+          None if acc_out is None else acc_out.data_ptr(), ws, need)
     return out
 
 
@@ -309,8 +298,8 @@ def cache_evict(src: Cache, dst: Cache, length, total, keep, recent):
     if src.k.device != dst.k.device:
         _bad("cache_evict: caches on different devices")
     new = torch.empty(length.shape[0], dtype=torch.int32, device=length.device)
-    need = lib().as_cache_evict_workspace(src._c, keep)
+    L = lib()
+    need = L.as_cache_evict_workspace(src._c, keep)
     _keep, ws = _workspace(need, length.device)
-    with _On(length) as s:
-        sim._check(lib().as_cache_evict(src._c, dst._c, n, t, keep, recent, new.data_ptr(), ws, need, s))
+    _call(L.as_cache_evict, length.device, src._c, dst._c, n, t, keep, recent, new.data_ptr(), ws, need)
     return new
