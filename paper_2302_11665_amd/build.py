@@ -44,6 +44,9 @@ HIP_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-fPIC", "-shared", "-Wall", "-Wno-unused-function", "-Wno-unused-command-line-argument",
 ]
+# The operators' matrix instructions keep their sums in ordinary registers: the
+# softmax's scaling of them would otherwise copy each one both ways.
+OPS_FLAGS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 
 
 def _run(cmd):
@@ -77,7 +80,7 @@ def build_sim(extra_flags=(), jobs=None) -> str:
              (SIM_SPEC_SRC, os.path.join(obj_dir, "sim_spec.o"), []),
              (SIM_MULTI_SRC, os.path.join(obj_dir, "sim_multi.o"), [])]
     for src in OPS_SRCS:
-        units.append((src, os.path.join(obj_dir, os.path.basename(src).replace(".hip", ".o")), []))
+        units.append((src, os.path.join(obj_dir, os.path.basename(src).replace(".hip", ".o")), OPS_FLAGS))
     for w in LANE_WIDTHS:
         units.append((SIM_LAUNCH_SRC, os.path.join(obj_dir, f"sim_launch_w{w}.o"), [f"-DAS_W={w}"]))
 

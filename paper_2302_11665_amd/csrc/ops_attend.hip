@@ -39,6 +39,8 @@ struct AttArgs {
   float c_log2;      // scale * log2(e)
   uint32_t page_mul; // ceil(2^32 / (page / 32)), 0 for pages of 32
   int32_t n_queries, per, rows, splits, row_groups;
+  int32_t chunk, row_span;  // blocks of 32 slots and query rows of a workgroup of attend
+  int32_t weigh_chunk;      // blocks of a workgroup of weigh
 };
 
 // ---------------------------------------------------------------- 4-bit codes
@@ -46,19 +48,17 @@ struct AttArgs {
 // 16 + c of a word's eight codes, as bf16 or fp16 pairs.
 template <int TYPE>
 __device__ __forceinline__ v4u expand(uint32_t w) {
-  v4u r;
-  if (TYPE == AS_BF16) {
-    r[0] = ((w << 3) & 0x00780078u) | 0x41804180u;
-    r[1] = ((w >> 1) & 0x00780078u) | 0x41804180u;
-    r[2] = ((w >> 5) & 0x00780078u) | 0x41804180u;
-    r[3] = ((w >> 9) & 0x00780078u) | 0x41804180u;
-  } else {
-    r[0] = ((w << 6) & 0x03c003c0u) | 0x4c004c00u;
-    r[1] = ((w << 2) & 0x03c003c0u) | 0x4c004c00u;
-    r[2] = ((w >> 2) & 0x03c003c0u) | 0x4c004c00u;
-    r[3] = ((w >> 6) & 0x03c003c0u) | 0x4c004c00u;
-  }
-  return r;
+  // Kept out of the compiler's sight: with its value unknown, mask and or
+  // become one instruction.
+  uint32_t sixteen = TYPE == AS_BF16 ? 0x41804180u : 0x4c004c00u;
+  uint32_t mask = TYPE == AS_BF16 ? 0x00780078u : 0x03c003c0u;
+  asm("" : "+v"(sixteen));
+  asm("" : "+s"(mask));
+  if (TYPE == AS_BF16)
+    return v4u{((w << 3) & mask) | sixteen, ((w >> 1) & mask) | sixteen, ((w >> 5) & mask) | sixteen,
+               ((w >> 9) & mask) | sixteen};
+  return v4u{((w << 6) & mask) | sixteen, ((w << 2) & mask) | sixteen, ((w >> 2) & mask) | sixteen,
+             ((w >> 6) & mask) | sixteen};
 }
 
 template <int TYPE>
@@ -180,12 +180,6 @@ __device__ __forceinline__ void scores(const v4u (&kf)[DIM / 32], const v4u (&pa
   }
 }
 
-// The part of a sequence that a workgroup takes.
-struct Part {
-  int b, h, split, row0, n;
-  int first, end;  // blocks of 32 slots
-};
-
 __device__ __forceinline__ int clamped_length(const AttArgs& p, int b) {
   const int64_t cap = (int64_t)p.c.max_pages * p.c.page;
   return (int)max((int64_t)0, min((int64_t)p.length[b], cap));
@@ -193,8 +187,114 @@ __device__ __forceinline__ int clamped_length(const AttArgs& p, int b) {
 
 // ---------------------------------------------------------------- attention
 
-// One workgroup per (sequence, head, split of its slots, 16 NT query rows); its
-// four wavefronts take 32 slots in turn and join their results in LDS.
+// Sums over the slots that a wavefront has seen, for 16 NT queries.
+template <int DIM, int GROUP, int NT>
+struct Sums {
+  v4f o[NT][DIM / 16];
+  float shift[NT][DIM / GROUP];  // sum of p m - 16 p d over the lane's slots
+  float mref[NT], sum[NT];       // reference of the exponents (log2 units), sum of p over the lane's slots
+};
+
+// 32 slots more.
+template <int TYPE, int DIM, int GROUP, int NT>
+__device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int least, int lane,
+                                             const Queries<TYPE, DIM, GROUP> (&q)[NT], const Keys<DIM, GROUP>& kx,
+                                             const Values<DIM, GROUP>& vx, Sums<DIM, GROUP, NT>& a) {
+  constexpr int NG = DIM / GROUP;
+  const bool ragged = blk * 32 + 32 > least;
+  float s[NT][8];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    v4u kf[DIM / 32], par[NG];
+#pragma unroll
+    for (int i = 0; i < DIM / 32; ++i) kf[i] = expand<TYPE>(kx.k[t][i]);
+#pragma unroll
+    for (int g = 0; g < NG; ++g) par[g] = kx.par[g][t];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      float x[4];
+      scores<TYPE, DIM, GROUP>(kf, par, q[u], x);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[u][4 * t + r] = x[r];
+    }
+  }
+  const int slot0 = blk * 32 + (lane >> 4) * 4;
+  if (ragged) {
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) s[u][e] = -kInf;
+  }
+#pragma unroll
+  for (int u = 0; u < NT; ++u) {
+    const float top = p.c_log2 * fmaxf(fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])),
+                                       fmaxf(fmaxf(s[u][4], s[u][5]), fmaxf(s[u][6], s[u][7])));
+    // The reference follows the maximum only where it is passed by a factor
+    // of 2^8: sums and products stay far from fp32's range, and the sums so
+    // far are hardly ever scaled.
+    if (__any(top > a.mref[u] + 8.0f)) {
+      const float m = fmaxf(a.mref[u], max_over_rows(top));
+      const float f = __builtin_amdgcn_exp2f(a.mref[u] - m);
+      a.mref[u] = m;
+      a.sum[u] *= f;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) a.shift[u][g] *= f;
+#pragma unroll
+      for (int i = 0; i < DIM / 16; ++i) a.o[u][i] *= f;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s[u][e] = __builtin_amdgcn_exp2f(fmaf(s[u][e], p.c_log2, -a.mref[u]));
+      a.sum[u] += s[u][e];
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    v4u hi[NT], lo[NT];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float pd[2];
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const int e = 2 * j + z;
+          const uint32_t w = vx.par[g][e >> 2][e & 3];
+          float d = par_d(w), m = par_m(w);
+          // a slot that is not seen may hold anything, infinities and NaN too
+          if (ragged && slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) d = m = 0.0f;
+          pd[z] = s[u][e] * d;
+          a.shift[u][g] = fmaf(s[u][e], m, a.shift[u][g]);
+          a.shift[u][g] = fmaf(-16.0f, pd[z], a.shift[u][g]);
+        }
+        hi[u][j] = pack_bf16(pd[0], pd[1]);
+        lo[u][j] = pack_bf16(pd[0] - __uint_as_float(hi[u][j] << 16), pd[1] - __uint_as_float(hi[u][j] & 0xffff0000u));
+      }
+    }
+#pragma unroll
+    for (int i = g * (GROUP / 16); i < (g + 1) * (GROUP / 16); ++i) {
+      const v4u vf = expand<AS_BF16>(vx.v[i]);
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        a.o[u][i] = mfma<AS_BF16>(vf, hi[u], a.o[u][i]);
+        a.o[u][i] = mfma<AS_BF16>(vf, lo[u], a.o[u][i]);
+      }
+    }
+  }
+}
+
+// Blocks of 32 slots that the query rows row0.. (`count` of them) see, and the
+// slots that the first of them sees.
+__device__ __forceinline__ int seen_blocks(const AttArgs& p, int n, int row0, int count, int& least) {
+  const int last = min(n, n - p.n_queries + min(row0 + count - 1, p.rows - 1) / p.per + 1);
+  least = n - p.n_queries + row0 / p.per + 1;
+  return max(0, (last + 31) / 32);
+}
+
+// One workgroup per (sequence, head, run of p.chunk blocks of 32 slots, 16 NT
+// query rows); its four wavefronts take the blocks in turn, the next one's words
+// on their way while one is worked on, and join their results in LDS.
 template <int TYPE, int DIM, int GROUP, int NT>
 __global__ __launch_bounds__(64 * kWaves) void attend(AttArgs p) {
   constexpr int NG = DIM / GROUP;
@@ -210,136 +310,71 @@ __global__ __launch_bounds__(64 * kWaves) void attend(AttArgs p) {
   const int b = bh / p.c.n_heads, h = bh % p.c.n_heads;
   const int n = clamped_length(p, b);
   const int row0 = rg * 16 * NT;
-  const int blocks = (n + 31) / 32, per_split = (blocks + p.splits - 1) / p.splits;
-  // slots that the group's last and first rows see
-  const int last = min(n, n - p.n_queries + min(row0 + 16 * NT - 1, p.rows - 1) / p.per + 1);
-  const int least = n - p.n_queries + row0 / p.per + 1;
-  const int end = min((split + 1) * per_split, max(0, (last + 31) / 32));
+  int least;
+  const int seen = seen_blocks(p, n, row0, 16 * NT, least);
+  const int end = min((split + 1) * p.chunk, seen);
+  int blk = split * p.chunk + wave;
+  if (p.splits > 1 && split * p.chunk >= seen) return;
 
+  Keys<DIM, GROUP> kx[2];
+  Values<DIM, GROUP> vx[2];
+  int64_t row[2];
+  int at[2];
+  row[0] = row[1] = -1;
+  if (blk < end) row[0] = block_row(p, b, h, blk, at[0]);
+  if (blk + kWaves < end) row[1] = block_row(p, b, h, blk + kWaves, at[1]);
+  if (row[0] >= 0) {
+    load_keys<DIM, GROUP>(p, row[0], at[0], lane, kx[0]);
+    load_values<DIM, GROUP>(p, row[0], at[0], lane, vx[0]);
+  }
   Queries<TYPE, DIM, GROUP> q[NT];
-  v4f o[NT][DIM / 16];
-  float shift[NT][NG], mref[NT], sum[NT];
+  Sums<DIM, GROUP, NT> a;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     load_queries<TYPE, DIM, GROUP>(p, b, h, row0 + 16 * t + (lane & 15), n, lane, q[t]);
-    mref[t] = kFloor;
-    sum[t] = 0.0f;
+    a.mref[t] = kFloor;
+    a.sum[t] = 0.0f;
 #pragma unroll
-    for (int g = 0; g < NG; ++g) shift[t][g] = 0.0f;
+    for (int g = 0; g < NG; ++g) a.shift[t][g] = 0.0f;
 #pragma unroll
-    for (int i = 0; i < DIM / 16; ++i) o[t][i] = v4f{0, 0, 0, 0};
+    for (int i = 0; i < DIM / 16; ++i) a.o[t][i] = v4f{0, 0, 0, 0};
   }
 
-  for (int blk = split * per_split + wave; blk < end; blk += kWaves) {
-    int at;
-    const int64_t row = block_row(p, b, h, blk, at);
-    if (row < 0) continue;
-    Keys<DIM, GROUP> kx;
-    Values<DIM, GROUP> vx;
-    load_keys<DIM, GROUP>(p, row, at, lane, kx);
-    load_values<DIM, GROUP>(p, row, at, lane, vx);
-    const bool ragged = blk * 32 + 32 > least;
-    float s[NT][8];
+  // Two blocks a turn, so that the words in flight need no moves.
+  while (blk < end) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      v4u kf[DIM / 32], par[NG];
-#pragma unroll
-      for (int i = 0; i < DIM / 32; ++i) kf[i] = expand<TYPE>(kx.k[t][i]);
-#pragma unroll
-      for (int g = 0; g < NG; ++g) par[g] = kx.par[g][t];
-#pragma unroll
-      for (int u = 0; u < NT; ++u) {
-        float x[4];
-        scores<TYPE, DIM, GROUP>(kf, par, q[u], x);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[u][4 * t + r] = x[r] * p.c_log2;
+    for (int z = 0; z < 2; ++z) {
+      if (row[z ^ 1] >= 0) {
+        load_keys<DIM, GROUP>(p, row[z ^ 1], at[z ^ 1], lane, kx[z ^ 1]);
+        load_values<DIM, GROUP>(p, row[z ^ 1], at[z ^ 1], lane, vx[z ^ 1]);
       }
-    }
-    const int slot0 = blk * 32 + (lane >> 4) * 4;
-    if (ragged) {
-#pragma unroll
-      for (int u = 0; u < NT; ++u)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) s[u][e] = -kInf;
-    }
-#pragma unroll
-    for (int u = 0; u < NT; ++u) {
-      float top = fmaxf(fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])),
-                        fmaxf(fmaxf(s[u][4], s[u][5]), fmaxf(s[u][6], s[u][7])));
-      // The reference follows the maximum only where it is passed by a factor
-      // of 2^8: sums and products stay far from fp32's range, and the sums so
-      // far are hardly ever scaled.
-      if (__any(top > mref[u] + 8.0f)) {
-        const float m = fmaxf(mref[u], max_over_rows(top));
-        const float f = __builtin_amdgcn_exp2f(mref[u] - m);
-        mref[u] = m;
-        sum[u] *= f;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) shift[u][g] *= f;
-#pragma unroll
-        for (int i = 0; i < DIM / 16; ++i) o[u][i] *= f;
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        s[u][e] = __builtin_amdgcn_exp2f(s[u][e] - mref[u]);
-        sum[u] += s[u][e];
-      }
-    }
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      v4u hi[NT], lo[NT];
-#pragma unroll
-      for (int u = 0; u < NT; ++u) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float pd[2];
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const int e = 2 * j + z;
-            const uint32_t w = vx.par[g][e >> 2][e & 3];
-            float x = s[u][e] * par_d(w), y = s[u][e] * par_m(w);
-            // a slot that is not seen may hold anything, infinities and NaN too
-            if (ragged && slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) x = y = 0.0f;
-            pd[z] = x;
-            shift[u][g] += fmaf(-16.0f, x, y);
-          }
-          hi[u][j] = pack_bf16(pd[0], pd[1]);
-          lo[u][j] = pack_bf16(pd[0] - __uint_as_float(hi[u][j] << 16),
-                               pd[1] - __uint_as_float(hi[u][j] & 0xffff0000u));
-        }
-      }
-#pragma unroll
-      for (int i = g * (GROUP / 16); i < (g + 1) * (GROUP / 16); ++i) {
-        const v4u vf = expand<AS_BF16>(vx.v[i]);
-#pragma unroll
-        for (int u = 0; u < NT; ++u) {
-          o[u][i] = mfma<AS_BF16>(vf, hi[u], o[u][i]);
-          o[u][i] = mfma<AS_BF16>(vf, lo[u], o[u][i]);
-        }
-      }
+      const bool here = row[z] >= 0;
+      row[z] = -1;
+      if (blk + 2 * kWaves < end) row[z] = block_row(p, b, h, blk + 2 * kWaves, at[z]);
+      if (here) attend_block<TYPE, DIM, GROUP, NT>(p, blk, least, lane, q, kx[z], vx[z], a);
+      blk += kWaves;
     }
   }
 
   // Join the wavefronts, 16 rows at a time.
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
-    const float total = sum_over_rows(sum[u]);
+    const float total = sum_over_rows(a.sum[u]);
     if (lane < 16) {
-      ml[wave][lane][0] = mref[u];
+      ml[wave][lane][0] = a.mref[u];
       ml[wave][lane][1] = total;
     }
     __syncthreads();
     float m = kFloor;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[w][lane & 15][0]);
-    const float f = __builtin_amdgcn_exp2f(mref[u] - m);
+    const float f = __builtin_amdgcn_exp2f(a.mref[u] - m);
+    float add[NG];
 #pragma unroll
-    for (int i = 0; i < DIM / 16; ++i) {
-      const float add = sum_over_rows(shift[u][i * 16 / GROUP]);
-      v4f x = (o[u][i] + add) * f;
-      *reinterpret_cast<v4f*>(&part[wave][lane & 15][16 * i + (lane >> 4) * 4]) = x;
-    }
+    for (int g = 0; g < NG; ++g) add[g] = sum_over_rows(a.shift[u][g]);
+#pragma unroll
+    for (int i = 0; i < DIM / 16; ++i)
+      *reinterpret_cast<v4f*>(&part[wave][lane & 15][16 * i + (lane >> 4) * 4]) = (a.o[u][i] + add[i * 16 / GROUP]) * f;
     __syncthreads();
     for (int j = threadIdx.x; j < 16 * DIM / 4; j += 64 * kWaves) {
       const int r = j / (DIM / 4), d = j % (DIM / 4) * 4;
@@ -372,113 +407,179 @@ __global__ __launch_bounds__(64 * kWaves) void attend(AttArgs p) {
   }
 }
 
-// Joins the splits: one workgroup per row, a thread per channel.
+// Joins the splits, one workgroup per row: every split's factor first, then
+// their sums, four channels to a thread and several splits side by side.
+constexpr int kMaxSplits = 1024;
+
 template <int TYPE, int DIM>
-__global__ __launch_bounds__(DIM) void join(AttArgs p) {
-  const int row = blockIdx.x % p.rows, bh = blockIdx.x / p.rows, d = threadIdx.x;
+__global__ __launch_bounds__(256) void join(AttArgs p) {
+  constexpr int kSide = 256 / (DIM / 4);
+  __shared__ float factor[kMaxSplits];
+  __shared__ float red[2][4];
+  __shared__ v4f sums[kSide][DIM / 4];
+  const int row = blockIdx.x % p.rows, bh = blockIdx.x / p.rows;
+  const int b = bh / p.c.n_heads, h = bh % p.c.n_heads, tid = threadIdx.x;
+  const int rows_wg = p.row_span;
+  int least;
+  const int seen = seen_blocks(p, clamped_length(p, b), row / rows_wg * rows_wg, rows_wg, least);
+  const int live = p.splits > 1 ? (seen + p.chunk - 1) / p.chunk : 1;
   const int64_t base = (int64_t)bh * p.splits * p.rows + row;
   float m = kFloor;
-  for (int s = 0; s < p.splits; ++s) m = fmaxf(m, p.part_ml[(base + (int64_t)s * p.rows) * 2]);
-  float l = 0.0f, x = 0.0f;
-  for (int s = 0; s < p.splits; ++s) {
-    const int64_t at = base + (int64_t)s * p.rows;
-    const float f = __builtin_amdgcn_exp2f(p.part_ml[at * 2] - m);
-    l = fmaf(p.part_ml[at * 2 + 1], f, l);
-    if (p.splits > 1) x = fmaf(p.part_o[at * DIM + d], f, x);
+  for (int s = tid; s < live; s += 256) m = fmaxf(m, p.part_ml[(base + (int64_t)s * p.rows) * 2]);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if ((tid & 63) == 0) red[0][tid >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  float l = 0.0f;
+  for (int s = tid; s < live; s += 256) {
+    const float* ml = p.part_ml + (base + (int64_t)s * p.rows) * 2;
+    const float f = __builtin_amdgcn_exp2f(ml[0] - m);
+    factor[s] = f;
+    l += f * ml[1];
   }
-  const int b = bh / p.c.n_heads, h = bh % p.c.n_heads, t = row / p.per;
-  if (p.splits > 1)
-    reinterpret_cast<uint16_t*>(p.out)[(((int64_t)b * p.n_queries + t) * p.c.n_heads * p.per + h * p.per + row -
-                                        t * p.per) * DIM + d] = from_f32<TYPE>(l == 0.0f ? 0.0f : x / l);
-  if (p.row_ml && d == 0) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
+  if ((tid & 63) == 0) red[1][tid >> 6] = l;
+  __syncthreads();
+  l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+  if (p.row_ml && tid == 0) {
     p.row_ml[((int64_t)bh * p.rows + row) * 2] = m;
     p.row_ml[((int64_t)bh * p.rows + row) * 2 + 1] = l == 0.0f ? 0.0f : 1.0f / l;
   }
+  if (p.splits == 1) return;
+  const int d = tid % (DIM / 4), side = tid / (DIM / 4);
+  v4f x = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int s = side; s < live; s += kSide)
+    x += *reinterpret_cast<const v4f*>(p.part_o + (base + (int64_t)s * p.rows) * DIM + 4 * d) * factor[s];
+  sums[side][d] = x;
+  __syncthreads();
+  if (side) return;
+#pragma unroll
+  for (int s = 1; s < kSide; ++s) x += sums[s][d];
+  const int t = row / p.per;
+  uint16_t* out = reinterpret_cast<uint16_t*>(p.out) +
+                  (((int64_t)b * p.n_queries + t) * p.c.n_heads * p.per + h * p.per + row - t * p.per) * DIM + 4 * d;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[e] = from_f32<TYPE>(l == 0.0f ? 0.0f : x[e] / l);
+}
+
+// The sum of x over the 16 lanes of a row, in every one of them.
+__device__ __forceinline__ float sum_in_row(float x) {
+  x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x128, 0xf, 0xf, false));  // row_ror:8
+  x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x124, 0xf, 0xf, false));
+  x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x122, 0xf, 0xf, false));
+  x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x121, 0xf, 0xf, false));
+  return x;
 }
 
 // The tokens' weights, from the keys once more now that every query's maximum
-// and sum are known: one wavefront per 32 slots, all queries of the head.
+// and sum are known: one workgroup per run of blocks, whose wavefronts take them
+// in turn, all queries of the head.  With at most 16 rows the queries stay in
+// registers.
 template <int TYPE, int DIM, int GROUP>
 __global__ __launch_bounds__(64 * kWaves) void weigh(AttArgs p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int bh = blockIdx.y, b = bh / p.c.n_heads, h = bh % p.c.n_heads;
   const int n = clamped_length(p, b);
-  const int blk = blockIdx.x * kWaves + wave;
-  if (blk * 32 >= n) return;
-  int at;
-  const int64_t row = block_row(p, b, h, blk, at);
-  if (row < 0) return;
-  Keys<DIM, GROUP> kx;
-  load_keys<DIM, GROUP>(p, row, at, lane, kx);
-  v4u kf[2][DIM / 32], par[2][DIM / GROUP];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-#pragma unroll
-    for (int i = 0; i < DIM / 32; ++i) kf[t][i] = expand<TYPE>(kx.k[t][i]);
-#pragma unroll
-    for (int g = 0; g < DIM / GROUP; ++g) par[t][g] = kx.par[g][t];
-  }
-  float w[8] = {};
-  const int slot0 = blk * 32 + (lane >> 4) * 4;
-  for (int r0 = 0; r0 < p.rows; r0 += 16) {
+  const int end = min((int)(blockIdx.x + 1) * p.weigh_chunk, (n + 31) / 32);
+  int blk = (int)blockIdx.x * p.weigh_chunk + wave;
+  if (blk >= end) return;
+  Queries<TYPE, DIM, GROUP> q;
+  float m = 0.0f, inv = 0.0f;
+  auto queries = [&](int r0) {
     const int r = r0 + (lane & 15);
-    Queries<TYPE, DIM, GROUP> q;
     load_queries<TYPE, DIM, GROUP>(p, b, h, r, n, lane, q);
     if (r >= p.rows) q.limit = 0;
     const float* ml = p.row_ml + ((int64_t)bh * p.rows + min(r, p.rows - 1)) * 2;
-    const float m = ml[0], inv = ml[1];
+    m = ml[0], inv = ml[1];
+  };
+  queries(0);
+  Keys<DIM, GROUP> kx[2];
+  int64_t row[2];
+  int at[2];
+  row[0] = block_row(p, b, h, blk, at[0]);
+  row[1] = -1;
+  if (blk + kWaves < end) row[1] = block_row(p, b, h, blk + kWaves, at[1]);
+  if (row[0] >= 0) load_keys<DIM, GROUP>(p, row[0], at[0], lane, kx[0]);
+  while (blk < end) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      float x[4];
-      scores<TYPE, DIM, GROUP>(kf[t], par[t], q, x);
+    for (int z = 0; z < 2; ++z) {
+      if (row[z ^ 1] >= 0) load_keys<DIM, GROUP>(p, row[z ^ 1], at[z ^ 1], lane, kx[z ^ 1]);
+      const int64_t here = row[z];
+      const int place = at[z];
+      row[z] = -1;
+      if (blk + 2 * kWaves < end) row[z] = block_row(p, b, h, blk + 2 * kWaves, at[z]);
+      if (here >= 0) {
+        v4u kf[2][DIM / 32], par[2][DIM / GROUP];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (slot0 + 16 * t + e < q.limit) w[4 * t + e] += __builtin_amdgcn_exp2f(x[e] * p.c_log2 - m) * inv;
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+          for (int i = 0; i < DIM / 32; ++i) kf[t][i] = expand<TYPE>(kx[z].k[t][i]);
+#pragma unroll
+          for (int g = 0; g < DIM / GROUP; ++g) par[t][g] = kx[z].par[g][t];
+        }
+        float w[8] = {};
+        const int slot0 = blk * 32 + (lane >> 4) * 4;
+        for (int r0 = 0; r0 < p.rows; r0 += 16) {
+          if (p.rows > 16) queries(r0);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            float x[4];
+            scores<TYPE, DIM, GROUP>(kf[t], par[t], q, x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (slot0 + 16 * t + e < q.limit) w[4 * t + e] += __builtin_amdgcn_exp2f(fmaf(x[e], p.c_log2, -m)) * inv;
+          }
+        }
+        // lane e of each row of 16 stores slot e
+        float x = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float y = sum_in_row(w[e]);
+          x = (lane & 15) == e ? y : x;
+        }
+        const int e = lane & 15, s = 16 * (e >> 2) + (lane >> 4) * 4 + (e & 3);
+        if (e < 8 && blk * 32 + s < n) {
+          const int64_t i = here * p.c.page + place + s;
+          p.acc_out[i] = (p.acc_in ? p.acc_in[i] : 0.0f) + x;
+        }
+      }
+      blk += kWaves;
     }
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) w[e] += __shfl_xor(w[e], o);
-  }
-  // lane e of each row of 16 stores slot e
-  float x = w[0];
-#pragma unroll
-  for (int e = 1; e < 8; ++e) x = (lane & 15) == e ? w[e] : x;
-  const int e = lane & 15, s = 16 * (e >> 2) + (lane >> 4) * 4 + (e & 3);
-  if (e < 8 && blk * 32 + s < n) {
-    const int64_t i = row * p.c.page + at + s;
-    p.acc_out[i] = (p.acc_in ? p.acc_in[i] : 0.0f) + x;
-  }
 }
-
-// Splits of a sequence's slots: enough workgroups to fill the compute units
-// several times over, none with fewer than 256 slots.
-int choose_splits(const as_cache_t* c, int row_groups) {
-  const int64_t units = (int64_t)c->n_seqs * c->n_heads * row_groups;
-  const int64_t slots = (int64_t)c->max_pages * c->page;
-  int64_t s = (1024 + units - 1) / units;
-  const int64_t most = (slots + 255) / 256;
-  if (s > most) s = most;
-  if (s > 512) s = 512;
-  return s < 1 ? 1 : (int)s;
-}
-
-int row_tiles(int rows) { return rows > 16 ? 2 : 1; }
 
 struct Plan {
-  int per, rows, tiles, row_groups, splits;
+  int per, rows, tiles, row_groups, splits, chunk, weigh_chunk, weigh_groups;
   int64_t o_bytes, ml_bytes, row_bytes;
 };
+
+// Blocks of 32 slots to a workgroup of four wavefronts: at least two for each
+// wavefront, and more where that still leaves about 2048 workgroups.  Runs of one
+// length balance ragged sequences: those beyond a sequence's end return at once.
+int choose_chunk(int64_t blocks, int64_t units, int64_t target) {
+  int64_t c = blocks * units / target;
+  c = c < 8 ? 8 : round_up(c, 8);
+  const int64_t least = (blocks + kMaxSplits - 1) / kMaxSplits;
+  return (int)(c > least ? c : round_up(least, 8));
+}
 
 Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) {
   Plan pl;
   pl.per = n_q_heads / c->n_heads;
   pl.rows = pl.per * n_queries;
-  pl.tiles = row_tiles(pl.rows);
+  pl.tiles = pl.rows > 16 ? 2 : 1;
   pl.row_groups = (pl.rows + 16 * pl.tiles - 1) / (16 * pl.tiles);
-  pl.splits = choose_splits(c, pl.row_groups);
-  const int64_t rows = (int64_t)c->n_seqs * c->n_heads * pl.rows;
+  const int64_t heads = (int64_t)c->n_seqs * c->n_heads;
+  int64_t blocks = (int64_t)c->max_pages * c->page / 32;
+  if (blocks < 1) blocks = 1;
+  pl.chunk = choose_chunk(blocks, heads * pl.row_groups, 2048);
+  pl.splits = (int)((blocks + pl.chunk - 1) / pl.chunk);
+  pl.weigh_chunk = choose_chunk(blocks, heads, 2048);
+  pl.weigh_groups = (int)((blocks + pl.weigh_chunk - 1) / pl.weigh_chunk);
+  const int64_t rows = heads * pl.rows;
   pl.o_bytes = pl.splits > 1 ? round_up(rows * pl.splits * c->dim * 4, 256) : 0;
   pl.ml_bytes = pl.splits > 1 || weights ? round_up(rows * pl.splits * 8, 256) : 0;
   pl.row_bytes = weights ? round_up(rows * 8, 256) : 0;
@@ -508,14 +609,11 @@ int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
   else
     hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 2>), g, t, 0, s, p);
   if (pl.splits > 1 || p.acc_out)
-    hipLaunchKernelGGL((join<TYPE, DIM>), dim3((unsigned)((int64_t)p.c.n_seqs * p.c.n_heads * p.rows)), dim3(DIM), 0,
+    hipLaunchKernelGGL((join<TYPE, DIM>), dim3((unsigned)((int64_t)p.c.n_seqs * p.c.n_heads * p.rows)), dim3(256), 0,
                        s, p);
-  if (p.acc_out) {
-    const int64_t blocks = (int64_t)p.c.max_pages * p.c.page / 32;
+  if (p.acc_out)
     hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP>),
-                       dim3((unsigned)((blocks + kWaves - 1) / kWaves), (unsigned)(p.c.n_seqs * p.c.n_heads)), t, 0,
-                       s, p);
-  }
+                       dim3((unsigned)pl.weigh_groups, (unsigned)(p.c.n_seqs * p.c.n_heads)), t, 0, s, p);
   return launched("attention_kv4");
 }
 
@@ -581,6 +679,9 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
   p.rows = pl.rows;
   p.splits = pl.splits;
   p.row_groups = pl.row_groups;
+  p.chunk = pl.chunk;
+  p.row_span = 16 * pl.tiles;
+  p.weigh_chunk = pl.weigh_chunk;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return type == AS_BF16 ? launch_by_shape<AS_BF16>(p, pl, s) : launch_by_shape<AS_F16>(p, pl, s);
 }
