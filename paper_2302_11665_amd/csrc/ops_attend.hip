@@ -16,6 +16,8 @@
 // that the same lane has to supply to the second: p never leaves its lane, and a
 // word of V holds the channel's codes for just those 8 slots.  A query's running
 // maximum is the same in its four lanes, its sum is kept per lane.
+#include <type_traits>
+
 #include "ops_common.hpp"
 
 using as_host::fail;
@@ -45,21 +47,25 @@ struct AttArgs {
 
 // ---------------------------------------------------------------- 4-bit codes
 
-// 16 + c of a word's eight codes, as bf16 or fp16 pairs.
+// 16 + c of a word's eight codes, as bf16 or fp16 pairs.  The two constants are
+// made once, out of the compiler's sight: with their values unknown, mask and
+// or become one instruction.
 template <int TYPE>
-__device__ __forceinline__ v4u expand(uint32_t w) {
-  // Kept out of the compiler's sight: with its value unknown, mask and or
-  // become one instruction.
+struct Expand {
   uint32_t sixteen = TYPE == AS_BF16 ? 0x41804180u : 0x4c004c00u;
   uint32_t mask = TYPE == AS_BF16 ? 0x00780078u : 0x03c003c0u;
-  asm("" : "+v"(sixteen));
-  asm("" : "+s"(mask));
-  if (TYPE == AS_BF16)
-    return v4u{((w << 3) & mask) | sixteen, ((w >> 1) & mask) | sixteen, ((w >> 5) & mask) | sixteen,
-               ((w >> 9) & mask) | sixteen};
-  return v4u{((w << 6) & mask) | sixteen, ((w << 2) & mask) | sixteen, ((w >> 2) & mask) | sixteen,
-             ((w >> 6) & mask) | sixteen};
-}
+  __device__ __forceinline__ Expand() {
+    asm("" : "+v"(sixteen));
+    asm("" : "+s"(mask));
+  }
+  __device__ __forceinline__ v4u operator()(uint32_t w) const {
+    if (TYPE == AS_BF16)
+      return v4u{((w << 3) & mask) | sixteen, ((w >> 1) & mask) | sixteen, ((w >> 5) & mask) | sixteen,
+                 ((w >> 9) & mask) | sixteen};
+    return v4u{((w << 6) & mask) | sixteen, ((w << 2) & mask) | sixteen, ((w >> 2) & mask) | sixteen,
+               ((w >> 6) & mask) | sixteen};
+  }
+};
 
 template <int TYPE>
 __device__ __forceinline__ v4f mfma(v4u a, v4u b, v4f c) {
@@ -69,21 +75,14 @@ __device__ __forceinline__ v4f mfma(v4u a, v4u b, v4f c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
 }
 
-// The halves of a (scale, minimum) word.
-__device__ __forceinline__ float par_d(uint32_t w) { return (float)__builtin_bit_cast(v2h, w)[0]; }
-__device__ __forceinline__ float par_m(uint32_t w) { return (float)__builtin_bit_cast(v2h, w)[1]; }
-
-// What a lane holds of 32 slots of one head.
-template <int DIM, int GROUP>
-struct Keys {
-  uint32_t k[2][DIM / 32];
-  v4u par[DIM / GROUP][2];
-};
-template <int DIM, int GROUP>
-struct Values {
-  uint32_t v[DIM / 16];
-  v4u par[DIM / GROUP][2];
-};
+// fma(x, y, z) in fp32 with y the scale (low half) or the minimum (high half)
+// of a word; the conversion is part of the instruction.
+__device__ __forceinline__ float fma_d(float x, uint32_t w, float z) {
+  return fmaf(x, (float)__builtin_bit_cast(v2h, w)[0], z);
+}
+__device__ __forceinline__ float fma_m(float x, uint32_t w, float z) {
+  return fmaf(x, (float)__builtin_bit_cast(v2h, w)[1], z);
+}
 
 // Row (page and head) of a block of 32 slots of a sequence, or -1; at: its
 // first slot's place on the page.
@@ -93,44 +92,100 @@ __device__ __forceinline__ int64_t block_row(const AttArgs& p, int b, int h, int
   return cache_row(p.c, b, h, pb);
 }
 
-template <int DIM, int GROUP>
-__device__ __forceinline__ void load_keys(const AttArgs& p, int64_t row, int at, int lane, Keys<DIM, GROUP>& x) {
-  const uint32_t* k = p.c.k + (row * p.c.page + at) * (DIM / 8) + (lane & 15) * (DIM / 8) + (lane >> 4) * (DIM / 32);
+// A wavefront's ring in LDS: each stage takes 32 slots of a head, which come
+// straight from memory.  A lane's words lie 64 bytes from its neighbour's in
+// K, and the scales are the same for 16 lanes: as loads into registers these
+// cost the vector cache several times the cycles of a contiguous KiB, so the
+// lanes take them out of LDS instead.  The 16-byte pieces of K's slots are
+// turned by the slot's number, which spreads a read of one piece of many slots
+// over the banks.
+template <int DIM, int GROUP, bool WITH_V>
+struct Stage {
+  static constexpr int kNG = DIM / GROUP;
+  static constexpr int kWords = 32 * DIM / 2;                    // bytes of 32 slots' codes
+  static constexpr int kParAt = WITH_V ? 2 * kWords : kWords;
+  static constexpr int kBytes = kParAt + (WITH_V ? 2 : 1) * kNG * 128;
+  static constexpr int kLoads = kParAt / 1024 + (WITH_V ? 2 : 1);
+
+  // Load 16 bytes a lane from a place that all lanes share plus the lane's own offset.
+  __device__ static __forceinline__ void load16(const void* base, uint32_t offset, uint8_t* dst) {
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void*)(reinterpret_cast<const uint8_t*>(base) + offset),
+        (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+  }
+
+  // Start the loads of a block; row < 0 (no such page) loads the pool's first
+  // one, which is not used.
+  __device__ static __forceinline__ void bring(const AttArgs& p, int64_t row, int at, uint32_t lane, uint8_t* lds) {
+    if (row < 0) row = 0, at = 0;
+    const int64_t words = (row * p.c.page + at) * (DIM / 8), pars = row * kNG * p.c.page + at;
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    if (DIM == 128) {
-      const v4u w = *reinterpret_cast<const v4u*>(k + t * 16 * (DIM / 8));
+    for (int j = 0; j < kWords / 1024; ++j) {
+      const uint32_t piece = 64 * j + lane;
+      load16(p.c.k + words, (DIM == 128 ? piece ^ (piece >> 3 & 3) : piece) * 16, lds + j * 1024);
+    }
+    if (WITH_V) {
 #pragma unroll
-      for (int i = 0; i < DIM / 32; ++i) x.k[t][i] = w[i];
-    } else {
-      const v2u w = *reinterpret_cast<const v2u*>(k + t * 16 * (DIM / 8));
-#pragma unroll
-      for (int i = 0; i < DIM / 32; ++i) x.k[t][i] = w[i];
+      for (int j = 0; j < kWords / 1024; ++j)
+        load16(p.c.v + words, j * 1024 + lane * 16, lds + kWords + j * 1024);
+    }
+    if (lane < kNG * 8) {
+      const uint32_t offset = (lane >> 3) * (uint32_t)p.c.page * 4 + (lane & 7) * 16;
+      load16(p.c.k_par + pars, offset, lds + kParAt);
+      if (WITH_V) load16(p.c.v_par + pars, offset, lds + kParAt + kNG * 128);
     }
   }
-#pragma unroll
-  for (int g = 0; g < DIM / GROUP; ++g)
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-      x.par[g][t] = *reinterpret_cast<const v4u*>(p.c.k_par + (row * (DIM / GROUP) + g) * p.c.page + at + 16 * t +
-                                                  (lane >> 4) * 4);
-}
 
-template <int DIM, int GROUP>
-__device__ __forceinline__ void load_values(const AttArgs& p, int64_t row, int at, int lane, Values<DIM, GROUP>& x) {
-  const uint32_t* v = p.c.v + (row * p.c.page + at) * (DIM / 8) + lane * (DIM / 16);
+  // A lane's words of K of slot 16 t + lane % 16, and the scales of group n of
+  // slots 16 t + 4 (lane / 16) + 0..3.
+  __device__ static __forceinline__ void keys(const uint8_t* lds, int lane, int t, uint32_t (&k)[DIM / 32]) {
+    const int s = 16 * t + (lane & 15), g = lane >> 4;
+    if (DIM == 128) {
+      const v4u w = *reinterpret_cast<const v4u*>(lds + s * 64 + (g ^ (s >> 1 & 3)) * 16);
 #pragma unroll
-  for (int j = 0; j < DIM / 64; ++j) {
-    const v4u w = *reinterpret_cast<const v4u*>(v + 4 * j);
+      for (int i = 0; i < DIM / 32; ++i) k[i] = w[i];
+    } else {
+      const v2u w = *reinterpret_cast<const v2u*>(lds + s * 32 + g * 8);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x.v[4 * j + i] = w[i];
+      for (int i = 0; i < DIM / 32; ++i) k[i] = w[i];
+    }
   }
+  __device__ static __forceinline__ v4u key_scales(const uint8_t* lds, int lane, int t, int n) {
+    return *reinterpret_cast<const v4u*>(lds + kParAt + n * 128 + t * 64 + (lane >> 4) * 16);
+  }
+  // A lane's words of V: channels 16 i + lane % 16 for the i of group n.
+  __device__ static __forceinline__ void values(const uint8_t* lds, int lane, int n, uint32_t (&v)[GROUP / 16]) {
+    const uint8_t* at = lds + kWords + lane * (DIM / 4) + n * (GROUP / 4);
+    if (GROUP == 32) {
+      const v2u w = *reinterpret_cast<const v2u*>(at);
+      v[0] = w[0], v[1] = w[1];
+    } else {
 #pragma unroll
-  for (int g = 0; g < DIM / GROUP; ++g)
+      for (int j = 0; j < GROUP / 64; ++j) {
+        const v4u w = *reinterpret_cast<const v4u*>(at + 16 * j);
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-      x.par[g][t] = *reinterpret_cast<const v4u*>(p.c.v_par + (row * (DIM / GROUP) + g) * p.c.page + at + 16 * t +
-                                                  (lane >> 4) * 4);
+        for (int i = 0; i < 4; ++i) v[4 * j + i] = w[i];
+      }
+    }
+  }
+  __device__ static __forceinline__ v4u value_scales(const uint8_t* lds, int lane, int t, int n) {
+    return key_scales(lds, lane, t, kNG + n);
+  }
+};
+
+// Wait until at most N of the wavefront's loads are on their way; what is read
+// from LDS afterwards is read afterwards.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "six bits");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
+  asm volatile("" ::: "memory");
+}
+// Wait for the wavefront's LDS reads: their place may be written again.
+__device__ __forceinline__ void wait_reads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0), nothing else
+  asm volatile("" ::: "memory");
 }
 
 // Sixteen queries as the second operand of K q^T: lane's channels 32 i + 8 g +
@@ -174,8 +229,8 @@ __device__ __forceinline__ void scores(const v4u (&kf)[DIM / 32], const v4u (&pa
     for (int i = g * (GROUP / 32); i < (g + 1) * (GROUP / 32); ++i) a = mfma<TYPE>(kf[i], q.q[i], a);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const float m = par_m(par[g][r]) * q.sum[g];
-      s[r] = fmaf(par_d(par[g][r]), a[r], g == 0 ? m : s[r] + m);
+      s[r] = fma_m(q.sum[g], par[g][r], g == 0 ? 0.0f : s[r]);
+      s[r] = fma_d(a[r], par[g][r], s[r]);
     }
   }
 }
@@ -187,6 +242,11 @@ __device__ __forceinline__ int clamped_length(const AttArgs& p, int b) {
 
 // ---------------------------------------------------------------- attention
 
+// The compiler's scheduler stays on its side of this: a block's steps one after
+// the other need half the registers that they take when mixed, and the other
+// wavefronts of the SIMD fill the gaps.
+__device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
+
 // Sums over the slots that a wavefront has seen, for 16 NT queries.
 template <int DIM, int GROUP, int NT>
 struct Sums {
@@ -195,21 +255,24 @@ struct Sums {
   float mref[NT], sum[NT];       // reference of the exponents (log2 units), sum of p over the lane's slots
 };
 
-// 32 slots more.
-template <int TYPE, int DIM, int GROUP, int NT>
-__device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int least, int lane,
-                                             const Queries<TYPE, DIM, GROUP> (&q)[NT], const Keys<DIM, GROUP>& kx,
-                                             const Values<DIM, GROUP>& vx, Sums<DIM, GROUP, NT>& a) {
+// 32 slots more; RAGGED: some are not seen by some query.
+template <int TYPE, int DIM, int GROUP, int NT, bool RAGGED>
+__device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int lane,
+                                             const Queries<TYPE, DIM, GROUP> (&q)[NT], const uint8_t* lds,
+                                             const Expand<TYPE>& key_codes, const Expand<AS_BF16>& value_codes,
+                                             Sums<DIM, GROUP, NT>& a) {
   constexpr int NG = DIM / GROUP;
-  const bool ragged = blk * 32 + 32 > least;
+  typedef Stage<DIM, GROUP, true> S;
   float s[NT][8];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
+    uint32_t k[DIM / 32];
+    S::keys(lds, lane, t, k);
     v4u kf[DIM / 32], par[NG];
 #pragma unroll
-    for (int i = 0; i < DIM / 32; ++i) kf[i] = expand<TYPE>(kx.k[t][i]);
+    for (int g = 0; g < NG; ++g) par[g] = S::key_scales(lds, lane, t, g);
 #pragma unroll
-    for (int g = 0; g < NG; ++g) par[g] = kx.par[g][t];
+    for (int i = 0; i < DIM / 32; ++i) kf[i] = key_codes(k[i]);
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
       float x[4];
@@ -217,9 +280,10 @@ __device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int leas
 #pragma unroll
       for (int r = 0; r < 4; ++r) s[u][4 * t + r] = x[r];
     }
+    phase();
   }
   const int slot0 = blk * 32 + (lane >> 4) * 4;
-  if (ragged) {
+  if (RAGGED) {
 #pragma unroll
     for (int u = 0; u < NT; ++u)
 #pragma unroll
@@ -251,7 +315,12 @@ __device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int leas
   }
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    v4u hi[NT], lo[NT];
+    phase();
+    v4u par[2], hi[NT], lo[NT];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) par[t] = S::value_scales(lds, lane, t, g);
+    uint32_t v[GROUP / 16];
+    S::values(lds, lane, g, v);
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
 #pragma unroll
@@ -260,12 +329,11 @@ __device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int leas
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
           const int e = 2 * j + z;
-          const uint32_t w = vx.par[g][e >> 2][e & 3];
-          float d = par_d(w), m = par_m(w);
+          uint32_t w = par[e >> 2][e & 3];
           // a slot that is not seen may hold anything, infinities and NaN too
-          if (ragged && slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) d = m = 0.0f;
-          pd[z] = s[u][e] * d;
-          a.shift[u][g] = fmaf(s[u][e], m, a.shift[u][g]);
+          if (RAGGED && slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) w = 0;
+          pd[z] = fma_d(s[u][e], w, 0.0f);
+          a.shift[u][g] = fma_m(s[u][e], w, a.shift[u][g]);
           a.shift[u][g] = fmaf(-16.0f, pd[z], a.shift[u][g]);
         }
         hi[u][j] = pack_bf16(pd[0], pd[1]);
@@ -273,12 +341,14 @@ __device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int leas
       }
     }
 #pragma unroll
-    for (int i = g * (GROUP / 16); i < (g + 1) * (GROUP / 16); ++i) {
-      const v4u vf = expand<AS_BF16>(vx.v[i]);
+    for (int i = 0; i < GROUP / 16; ++i) {
+      if (i % 4 == 0) phase();
+      const v4u vf = value_codes(v[i]);
 #pragma unroll
       for (int u = 0; u < NT; ++u) {
-        a.o[u][i] = mfma<AS_BF16>(vf, hi[u], a.o[u][i]);
-        a.o[u][i] = mfma<AS_BF16>(vf, lo[u], a.o[u][i]);
+        v4f& o = a.o[u][g * (GROUP / 16) + i];
+        o = mfma<AS_BF16>(vf, hi[u], o);
+        o = mfma<AS_BF16>(vf, lo[u], o);
       }
     }
   }
@@ -293,13 +363,23 @@ __device__ __forceinline__ int seen_blocks(const AttArgs& p, int n, int row0, in
 }
 
 // One workgroup per (sequence, head, run of p.chunk blocks of 32 slots, 16 NT
-// query rows); its four wavefronts take the blocks in turn, the next one's words
-// on their way while one is worked on, and join their results in LDS.
+// query rows); its four wavefronts take the blocks in turn, each with a ring of
+// its own in LDS so that none waits for another, and join their results at the
+// end.
+constexpr int kStages = 2;
+template <int DIM, int GROUP>
+constexpr int attend_lds() {
+  constexpr int ring = kStages * Stage<DIM, GROUP, true>::kBytes, part = 16 * (DIM + 4) * 4;
+  return kWaves * (ring > part ? ring : part);
+}
+
 template <int TYPE, int DIM, int GROUP, int NT>
-__global__ __launch_bounds__(64 * kWaves) void attend(AttArgs p) {
+__global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : 2) - (DIM == 4 * GROUP)) void attend(AttArgs p) {
   constexpr int NG = DIM / GROUP;
+  typedef Stage<DIM, GROUP, true> S;
+  constexpr int kRing = kStages * S::kBytes;
   __shared__ float ml[kWaves][16][2];
-  __shared__ float part[kWaves][16][DIM + 4];
+  extern __shared__ __align__(16) uint8_t lds[];  // the rings, then the parts to be joined
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Neighbouring workgroup numbers go to different XCDs: the row groups of one
   // part, which read the same slots, are a multiple of 8 apart.
@@ -313,20 +393,9 @@ __global__ __launch_bounds__(64 * kWaves) void attend(AttArgs p) {
   int least;
   const int seen = seen_blocks(p, n, row0, 16 * NT, least);
   const int end = min((split + 1) * p.chunk, seen);
-  int blk = split * p.chunk + wave;
   if (p.splits > 1 && split * p.chunk >= seen) return;
 
-  Keys<DIM, GROUP> kx[2];
-  Values<DIM, GROUP> vx[2];
-  int64_t row[2];
-  int at[2];
-  row[0] = row[1] = -1;
-  if (blk < end) row[0] = block_row(p, b, h, blk, at[0]);
-  if (blk + kWaves < end) row[1] = block_row(p, b, h, blk + kWaves, at[1]);
-  if (row[0] >= 0) {
-    load_keys<DIM, GROUP>(p, row[0], at[0], lane, kx[0]);
-    load_values<DIM, GROUP>(p, row[0], at[0], lane, vx[0]);
-  }
+  uint8_t* ring = lds + wave * kRing;
   Queries<TYPE, DIM, GROUP> q[NT];
   Sums<DIM, GROUP, NT> a;
 #pragma unroll
@@ -340,26 +409,50 @@ __global__ __launch_bounds__(64 * kWaves) void attend(AttArgs p) {
     for (int i = 0; i < DIM / 16; ++i) a.o[t][i] = v4f{0, 0, 0, 0};
   }
 
-  // Two blocks a turn, so that the words in flight need no moves.
-  while (blk < end) {
+  const Expand<TYPE> key_codes;
+  const Expand<AS_BF16> value_codes;
+  int blk = split * p.chunk + wave;
+  uint32_t valid = 0;  // bit j: the block j turns on has a page
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      if (row[z ^ 1] >= 0) {
-        load_keys<DIM, GROUP>(p, row[z ^ 1], at[z ^ 1], lane, kx[z ^ 1]);
-        load_values<DIM, GROUP>(p, row[z ^ 1], at[z ^ 1], lane, vx[z ^ 1]);
-      }
-      const bool here = row[z] >= 0;
-      row[z] = -1;
-      if (blk + 2 * kWaves < end) row[z] = block_row(p, b, h, blk + 2 * kWaves, at[z]);
-      if (here) attend_block<TYPE, DIM, GROUP, NT>(p, blk, least, lane, q, kx[z], vx[z], a);
-      blk += kWaves;
-    }
+  for (int j = 0; j < kStages; ++j) {
+    if (blk + j * kWaves >= end) break;
+    int at;
+    const int64_t row = block_row(p, b, h, blk + j * kWaves, at);
+    valid |= (uint32_t)(row >= 0) << j;
+    if (p.c.n_pages > 0) S::bring(p, row, at, lane, ring + j * S::kBytes);
   }
+  int slot = 0;
+  // Blocks up to `to`, all of one kind.
+  auto blocks = [&](int to, auto ragged) {
+    for (; blk < to; blk += kWaves) {
+      int at = 0;
+      int64_t row = -1;
+      const bool more = blk + kStages * kWaves < end;
+      if (more) row = block_row(p, b, h, blk + kStages * kWaves, at);
+      if (blk + (kStages - 1) * kWaves < end)
+        wait_loads<(kStages - 1) * S::kLoads>();
+      else
+        wait_loads<0>();
+      uint8_t* here = ring + slot * S::kBytes;
+      if (valid & 1)
+        attend_block<TYPE, DIM, GROUP, NT, decltype(ragged)::value>(p, blk, lane, q, here, key_codes, value_codes, a);
+      valid = valid >> 1 | (uint32_t)(row >= 0) << (kStages - 1);
+      if (more) {
+        wait_reads();
+        if (p.c.n_pages > 0) S::bring(p, row, at, lane, here);
+      }
+      slot = slot + 1 == kStages ? 0 : slot + 1;
+    }
+  };
+  blocks(min(end, least >> 5), std::false_type());  // all 32 slots seen by all queries
+  blocks(end, std::true_type());
 
   // Join the wavefronts, 16 rows at a time.
+  float* part = reinterpret_cast<float*>(lds);  // [kWaves][16][DIM + 4]
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
     const float total = sum_over_rows(a.sum[u]);
+    __syncthreads();  // the rings, and the rows before, are done with
     if (lane < 16) {
       ml[wave][lane][0] = a.mref[u];
       ml[wave][lane][1] = total;
@@ -374,7 +467,8 @@ __global__ __launch_bounds__(64 * kWaves) void attend(AttArgs p) {
     for (int g = 0; g < NG; ++g) add[g] = sum_over_rows(a.shift[u][g]);
 #pragma unroll
     for (int i = 0; i < DIM / 16; ++i)
-      *reinterpret_cast<v4f*>(&part[wave][lane & 15][16 * i + (lane >> 4) * 4]) = (a.o[u][i] + add[i * 16 / GROUP]) * f;
+      *reinterpret_cast<v4f*>(part + (wave * 16 + (lane & 15)) * (DIM + 4) + 16 * i + (lane >> 4) * 4) =
+          (a.o[u][i] + add[i * 16 / GROUP]) * f;
     __syncthreads();
     for (int j = threadIdx.x; j < 16 * DIM / 4; j += 64 * kWaves) {
       const int r = j / (DIM / 4), d = j % (DIM / 4) * 4;
@@ -384,7 +478,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend(AttArgs p) {
       float top = kFloor, l = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        x += *reinterpret_cast<const v4f*>(&part[w][r][d]);
+        x += *reinterpret_cast<const v4f*>(part + (w * 16 + r) * (DIM + 4) + d);
         top = fmaxf(top, ml[w][r][0]);
       }
 #pragma unroll
@@ -403,7 +497,6 @@ __global__ __launch_bounds__(64 * kWaves) void attend(AttArgs p) {
         for (int e = 0; e < 4; ++e) out[e] = from_f32<TYPE>(l == 0.0f ? 0.0f : x[e] / l);
       }
     }
-    __syncthreads();
   }
 }
 
@@ -478,14 +571,17 @@ __device__ __forceinline__ float sum_in_row(float x) {
 // and sum are known: one workgroup per run of blocks, whose wavefronts take them
 // in turn, all queries of the head.  With at most 16 rows the queries stay in
 // registers.
+constexpr int kWeighStages = 2;
+
 template <int TYPE, int DIM, int GROUP>
-__global__ __launch_bounds__(64 * kWaves) void weigh(AttArgs p) {
+__global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 2 : 3) void weigh(AttArgs p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int bh = blockIdx.y, b = bh / p.c.n_heads, h = bh % p.c.n_heads;
   const int n = clamped_length(p, b);
   const int end = min((int)(blockIdx.x + 1) * p.weigh_chunk, (n + 31) / 32);
   int blk = (int)blockIdx.x * p.weigh_chunk + wave;
   if (blk >= end) return;
+  const Expand<TYPE> key_codes;
   Queries<TYPE, DIM, GROUP> q;
   float m = 0.0f, inv = 0.0f;
   auto queries = [&](int r0) {
@@ -496,30 +592,49 @@ __global__ __launch_bounds__(64 * kWaves) void weigh(AttArgs p) {
     m = ml[0], inv = ml[1];
   };
   queries(0);
-  Keys<DIM, GROUP> kx[2];
-  int64_t row[2];
-  int at[2];
-  row[0] = block_row(p, b, h, blk, at[0]);
-  row[1] = -1;
-  if (blk + kWaves < end) row[1] = block_row(p, b, h, blk + kWaves, at[1]);
-  if (row[0] >= 0) load_keys<DIM, GROUP>(p, row[0], at[0], lane, kx[0]);
+  typedef Stage<DIM, GROUP, false> S;
+  extern __shared__ __align__(16) uint8_t lds[];
+  uint8_t* ring = lds + wave * kWeighStages * S::kBytes;
+  int64_t rows[kWeighStages];
+  int places[kWeighStages];
+#pragma unroll
+  for (int j = 0; j < kWeighStages; ++j) {
+    rows[j] = -1;
+    if (blk + j * kWaves >= end) continue;
+    rows[j] = block_row(p, b, h, blk + j * kWaves, places[j]);
+    if (p.c.n_pages > 0) S::bring(p, rows[j], places[j], lane, ring + j * S::kBytes);
+  }
   while (blk < end) {
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      if (row[z ^ 1] >= 0) load_keys<DIM, GROUP>(p, row[z ^ 1], at[z ^ 1], lane, kx[z ^ 1]);
-      const int64_t here = row[z];
-      const int place = at[z];
-      row[z] = -1;
-      if (blk + 2 * kWaves < end) row[z] = block_row(p, b, h, blk + 2 * kWaves, at[z]);
+    for (int z = 0; z < kWeighStages; ++z) {
+      if (blk >= end) break;
+      const int64_t here = rows[z];
+      const int place = places[z];
+      const bool more = blk + kWeighStages * kWaves < end;
+      if (more) rows[z] = block_row(p, b, h, blk + kWeighStages * kWaves, places[z]);
+      // (older loads and stores of weights only make this wait longer)
+      if (blk + (kWeighStages - 1) * kWaves < end)
+        wait_loads<(kWeighStages - 1) * S::kLoads>();
+      else
+        wait_loads<0>();
+      uint32_t k[2][DIM / 32];
+      v4u par[2][DIM / GROUP];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        S::keys(ring + z * S::kBytes, lane, t, k[t]);
+#pragma unroll
+        for (int g = 0; g < DIM / GROUP; ++g) par[t][g] = S::key_scales(ring + z * S::kBytes, lane, t, g);
+      }
+      if (more) {
+        wait_reads();
+        if (p.c.n_pages > 0) S::bring(p, rows[z], places[z], lane, ring + z * S::kBytes);
+      }
       if (here >= 0) {
-        v4u kf[2][DIM / 32], par[2][DIM / GROUP];
+        v4u kf[2][DIM / 32];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int i = 0; i < DIM / 32; ++i) kf[t][i] = expand<TYPE>(kx[z].k[t][i]);
-#pragma unroll
-          for (int g = 0; g < DIM / GROUP; ++g) par[t][g] = kx[z].par[g][t];
-        }
+          for (int i = 0; i < DIM / 32; ++i) kf[t][i] = key_codes(k[t][i]);
         float w[8] = {};
         const int slot0 = blk * 32 + (lane >> 4) * 4;
         for (int r0 = 0; r0 < p.rows; r0 += 16) {
@@ -604,16 +719,19 @@ template <int TYPE, int DIM, int GROUP>
 int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
   const int64_t units = round_up((int64_t)p.c.n_seqs * p.c.n_heads * pl.splits, 8) * pl.row_groups;
   const dim3 g((unsigned)units), t(64 * kWaves);
+  const size_t lds = attend_lds<DIM, GROUP>();
   if (pl.tiles == 1)
-    hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 1>), g, t, 0, s, p);
+    hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 1>), g, t, lds, s, p);
   else
-    hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 2>), g, t, 0, s, p);
+    hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 2>), g, t, lds, s, p);
   if (pl.splits > 1 || p.acc_out)
     hipLaunchKernelGGL((join<TYPE, DIM>), dim3((unsigned)((int64_t)p.c.n_seqs * p.c.n_heads * p.rows)), dim3(256), 0,
                        s, p);
+  typedef Stage<DIM, GROUP, false> KeyStage;
   if (p.acc_out)
     hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP>),
-                       dim3((unsigned)pl.weigh_groups, (unsigned)(p.c.n_seqs * p.c.n_heads)), t, 0, s, p);
+                       dim3((unsigned)pl.weigh_groups, (unsigned)(p.c.n_seqs * p.c.n_heads)), t,
+                       (size_t)kWaves * kWeighStages * KeyStage::kBytes, s, p);
   return launched("attention_kv4");
 }
 
