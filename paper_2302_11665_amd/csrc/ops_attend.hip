@@ -39,7 +39,7 @@ struct AttArgs {
   const float* acc_in;
   float* acc_out;
   float c_log2;      // scale * log2(e)
-  uint32_t page_mul; // ceil(2^32 / (page / 32)), 0 for pages of 32
+  uint32_t page_mul; // page_magic of the cache's pages
   int32_t n_queries, per, rows, splits, row_groups;
   int32_t chunk, row_span;  // blocks of 32 slots and query rows of a workgroup of attend
   int32_t weigh_chunk;      // blocks of a workgroup of weigh
@@ -87,7 +87,7 @@ __device__ __forceinline__ float fma_m(float x, uint32_t w, float z) {
 // Row (page and head) of a block of 32 slots of a sequence, or -1; at: its
 // first slot's place on the page.
 __device__ __forceinline__ int64_t block_row(const AttArgs& p, int b, int h, int blk, int& at) {
-  const int pb = p.page_mul ? (int)__umulhi((uint32_t)blk, p.page_mul) : blk;
+  const int pb = page_index(blk, p.page_mul);
   at = blk * 32 - pb * p.c.page;
   return cache_row(p.c, b, h, pb);
 }
@@ -571,7 +571,7 @@ __device__ __forceinline__ float sum_in_row(float x) {
 // and sum are known: one workgroup per run of blocks, whose wavefronts take them
 // in turn, all queries of the head.  With at most 16 rows the queries stay in
 // registers.
-constexpr int kWeighStages = 2;
+constexpr int kWeighStages = 3;
 
 template <int TYPE, int DIM, int GROUP>
 __global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 2 : 3) void weigh(AttArgs p) {
@@ -594,15 +594,26 @@ __global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 2 : 3) void weigh(A
   queries(0);
   typedef Stage<DIM, GROUP, false> S;
   extern __shared__ __align__(16) uint8_t lds[];
-  uint8_t* ring = lds + wave * kWeighStages * S::kBytes;
+  constexpr int kStage = S::kBytes + 128;
+  uint8_t* ring = lds + wave * kWeighStages * kStage;
   int64_t rows[kWeighStages];
   int places[kWeighStages];
+  // a block's keys, and the weights that its slots had (anything without them)
+  auto bring = [&](int z) {
+    uint8_t* to = ring + z * kStage;
+    S::bring(p, rows[z], places[z], lane, to);
+    const int64_t i = max(rows[z], (int64_t)0) * p.c.page + (rows[z] < 0 ? 0 : places[z]);
+    const float* was = p.acc_in ? p.acc_in + i : reinterpret_cast<const float*>(p.c.k);
+    if (lane < 32)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(was + lane),
+                                       (__attribute__((address_space(3))) void*)(to + S::kBytes), 4, 0, 0);
+  };
 #pragma unroll
   for (int j = 0; j < kWeighStages; ++j) {
     rows[j] = -1;
     if (blk + j * kWaves >= end) continue;
     rows[j] = block_row(p, b, h, blk + j * kWaves, places[j]);
-    if (p.c.n_pages > 0) S::bring(p, rows[j], places[j], lane, ring + j * S::kBytes);
+    if (p.c.n_pages > 0) bring(j);
   }
   while (blk < end) {
 #pragma unroll
@@ -612,22 +623,24 @@ __global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 2 : 3) void weigh(A
       const int place = places[z];
       const bool more = blk + kWeighStages * kWaves < end;
       if (more) rows[z] = block_row(p, b, h, blk + kWeighStages * kWaves, places[z]);
-      // (older loads and stores of weights only make this wait longer)
+      // (a store of weights after those loads only makes this wait longer)
       if (blk + (kWeighStages - 1) * kWaves < end)
-        wait_loads<(kWeighStages - 1) * S::kLoads>();
+        wait_loads<(kWeighStages - 1) * (S::kLoads + 1)>();
       else
         wait_loads<0>();
       uint32_t k[2][DIM / 32];
       v4u par[2][DIM / GROUP];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        S::keys(ring + z * S::kBytes, lane, t, k[t]);
+        S::keys(ring + z * kStage, lane, t, k[t]);
 #pragma unroll
-        for (int g = 0; g < DIM / GROUP; ++g) par[t][g] = S::key_scales(ring + z * S::kBytes, lane, t, g);
+        for (int g = 0; g < DIM / GROUP; ++g) par[t][g] = S::key_scales(ring + z * kStage, lane, t, g);
       }
+      const int e8 = lane & 15, s8 = 16 * (e8 >> 2) + (lane >> 4) * 4 + (e8 & 3);  // the slot that lanes e8 < 8 store
+      const float was = e8 < 8 ? *reinterpret_cast<const float*>(ring + z * kStage + S::kBytes + s8 * 4) : 0.0f;
       if (more) {
         wait_reads();
-        if (p.c.n_pages > 0) S::bring(p, rows[z], places[z], lane, ring + z * S::kBytes);
+        if (p.c.n_pages > 0) bring(z);
       }
       if (here >= 0) {
         v4u kf[2][DIM / 32];
@@ -648,18 +661,14 @@ __global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 2 : 3) void weigh(A
               if (slot0 + 16 * t + e < q.limit) w[4 * t + e] += __builtin_amdgcn_exp2f(fmaf(x[e], p.c_log2, -m)) * inv;
           }
         }
-        // lane e of each row of 16 stores slot e
+        // lane e of each row of 16 stores its slot e
         float x = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float y = sum_in_row(w[e]);
           x = (lane & 15) == e ? y : x;
         }
-        const int e = lane & 15, s = 16 * (e >> 2) + (lane >> 4) * 4 + (e & 3);
-        if (e < 8 && blk * 32 + s < n) {
-          const int64_t i = here * p.c.page + place + s;
-          p.acc_out[i] = (p.acc_in ? p.acc_in[i] : 0.0f) + x;
-        }
+        if (e8 < 8 && blk * 32 + s8 < n) p.acc_out[here * p.c.page + place + s8] = (p.acc_in ? was : 0.0f) + x;
       }
       blk += kWaves;
     }
@@ -731,7 +740,7 @@ int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
   if (p.acc_out)
     hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP>),
                        dim3((unsigned)pl.weigh_groups, (unsigned)(p.c.n_seqs * p.c.n_heads)), t,
-                       (size_t)kWaves * kWeighStages * KeyStage::kBytes, s, p);
+                       (size_t)kWaves * kWeighStages * (KeyStage::kBytes + 128), s, p);
   return launched("attention_kv4");
 }
 
@@ -790,8 +799,7 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
   p.acc_in = acc_in;
   p.acc_out = acc_out;
   p.c_log2 = scale * 1.4426950408889634f;
-  const int pb = cache->page / 32;
-  p.page_mul = pb > 1 ? (uint32_t)((((uint64_t)1 << 32) + pb - 1) / pb) : 0;
+  p.page_mul = page_magic(cache->page);
   p.n_queries = n_queries;
   p.per = pl.per;
   p.rows = pl.rows;

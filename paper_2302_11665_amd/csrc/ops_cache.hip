@@ -174,21 +174,17 @@ struct EvictArgs {
   int32_t* out_length;
   int32_t* kept;  // [n_seqs * n_heads][keep] slots of src
   int32_t keep, recent;
+  uint32_t src_mul, dst_mul;  // page_magic of the caches' pages
+  bool vec;                   // src.pos and src.acc aligned to 16 bytes
 };
-
-constexpr int kSelThreads = 1024;
 
 // Order of a token among those to keep: the newest positions first, then by
 // weight; NaN last, and -0 as 0.
-__device__ __forceinline__ uint32_t order_key(const EvictArgs& p, int b, int h, int slot, int total) {
-  const int64_t row = cache_row(p.src, b, h, slot / p.src.page);
-  if (row < 0) return 0;
-  const int64_t at = row * p.src.page + slot % p.src.page;
-  if (p.src.pos[at] >= total - p.recent) return 0xffffffffu;
-  const float a = p.src.acc[at];
-  if (a != a) return 0;
-  const uint32_t u = __float_as_uint(a + 0.0f);
-  return (u >> 31) ? ~u : u | 0x80000000u;
+__device__ __forceinline__ uint32_t order_key(int pos, float acc, int newest) {
+  const uint32_t u = __float_as_uint(acc + 0.0f);
+  uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);  // all bits of a negative number, else the sign
+  k = acc != acc ? 0u : k;
+  return pos >= newest ? 0xffffffffu : k;
 }
 
 __device__ __forceinline__ int evict_length(const EvictArgs& p, int b) {
@@ -196,137 +192,281 @@ __device__ __forceinline__ int evict_length(const EvictArgs& p, int b) {
   return (int)max((int64_t)0, min((int64_t)p.length[b], cap));
 }
 
-// Which slots stay, one workgroup per (sequence, head): the keep-th largest key
-// by four rounds of 8 bits (a histogram of the keys that agree with the digits
-// found so far), then one pass in slot order that writes the slots above it and
-// as many equal ones as there is room for, lowest first.
-__global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs p) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t found[2];  // digits found, keys still to take among the equal ones
-  __shared__ uint32_t sums[kSelThreads / 64][2];
-  const int b = blockIdx.x / p.src.n_heads, h = blockIdx.x % p.src.n_heads;
-  const int n = evict_length(p, b);
-  if (h == 0 && threadIdx.x == 0) p.out_length[b] = min(n, p.keep);
-  int32_t* kept = p.kept + (int64_t)blockIdx.x * p.keep;
-  if (n <= p.keep) {
-    for (int s = threadIdx.x; s < n; s += kSelThreads) kept[s] = s;
-    return;
-  }
-  const int total = p.total[b];
-  uint32_t prefix = 0, want = (uint32_t)p.keep;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (threadIdx.x < 256) hist[threadIdx.x] = 0;
-    __syncthreads();
-    for (int s = threadIdx.x; s < n; s += kSelThreads) {
-      const uint32_t key = order_key(p, b, h, s, total);
-      if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(key >> shift) & 255u], 1u);
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      uint32_t above = 0;
-      int d = 255;
-      while (d > 0 && above + hist[d] < want) above += hist[d--];
-      found[0] = prefix | (uint32_t)d << shift;
-      found[1] = want - above;
-    }
-    __syncthreads();
-    prefix = found[0];
-    want = found[1];
-  }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t base = 0, ties = 0;  // slots written, equal keys met
-  for (int s0 = 0; s0 < n; s0 += kSelThreads) {
-    const int s = s0 + threadIdx.x;
-    const uint32_t key = s < n ? order_key(p, b, h, s, total) : 0;
-    const bool above = s < n && key > prefix, equal = s < n && key == prefix;
-    const uint64_t ma = __ballot(above), me = __ballot(equal);
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    __syncthreads();
-    if (lane == 0) {
-      sums[wave][0] = (uint32_t)__popcll(ma);
-      sums[wave][1] = (uint32_t)__popcll(me);
-    }
-    __syncthreads();
-    uint32_t a0 = 0, e0 = 0, a1 = 0, e1 = 0;
-#pragma unroll
-    for (int w = 0; w < kSelThreads / 64; ++w) {
-      if (w < wave) a0 += sums[w][0], e0 += sums[w][1];
-      a1 += sums[w][0], e1 += sums[w][1];
-    }
-    const uint32_t met = ties + e0 + (uint32_t)__popcll(me & below);  // equal keys before this slot
-    const uint32_t at = base + a0 + (uint32_t)__popcll(ma & below) + min(met, want) - min(ties, want);
-    if (above || (equal && met < want)) kept[at] = s;
-    base += a1 + min(ties + e1, want) - min(ties, want);
-    ties += e1;
-  }
+// Which slots stay, one workgroup per (sequence, head).  The keys are read once
+// and stay in registers, four neighbouring slots to a thread (sequences longer
+// than the registers are read again in every step).  The keep-th largest key is
+// found by three rounds of 11, 11 and 10 bits: a histogram in LDS of the keys
+// that agree with the digits found so far, and a sum over its bins from the
+// top.  11 bits hold an fp32 number's sign, exponent and two more bits: weights
+// that spread over powers of two spread over the bins, so few lanes add to the
+// same one.  Then every slot above the key, and as many equal ones as there is
+// room for, lowest slot first, is written at its place, which the counts of the
+// wavefronts before it give.
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+
+// Sum over the lanes up to and with this one: four steps within rows of 16
+// lanes, then the rows' last lanes to the rows after them.
+__device__ __forceinline__ uint32_t scan_lanes(uint32_t x) {
+#define AS_ADD_DPP(ctrl, rows) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false)
+  AS_ADD_DPP(0x111, 0xf);  // row_shr:1
+  AS_ADD_DPP(0x112, 0xf);
+  AS_ADD_DPP(0x114, 0xf);
+  AS_ADD_DPP(0x118, 0xf);
+  AS_ADD_DPP(0x142, 0xa);  // row_bcast:15
+  AS_ADD_DPP(0x143, 0xc);  // row_bcast:31
+#undef AS_ADD_DPP
+  return x;
 }
 
-// Words of one row (page and head) of a token, by cache_row's index.
-__device__ __forceinline__ int64_t token_row(const CacheArgs& c, int b, int h, int slot, int& in_page) {
-  in_page = slot % c.page;
-  return cache_row(c, b, h, slot / c.page);
+// Exclusive sum over the workgroup of one number a thread; total: of all.
+__device__ __forceinline__ uint32_t scan_threads(uint32_t x, uint32_t* waves, uint32_t& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t sum = scan_lanes(x);
+  __syncthreads();
+  if (lane == 63) waves[wave] = sum;
+  __syncthreads();
+  uint32_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kSelWaves; ++w) {
+    if (w < wave) before += waves[w];
+    total += waves[w];
+  }
+  return before + sum - x;
+}
+
+template <int QUADS>
+__global__ __launch_bounds__(kSelThreads) void evict_select(EvictArgs p) {
+  constexpr int kSeg = QUADS * 4 * kSelThreads;  // slots that the registers hold
+  __shared__ uint32_t hist[2048];
+  __shared__ uint32_t waves[kSelWaves];
+  __shared__ uint32_t found[2];  // digit, keys still to take among those that have it
+  __shared__ uint32_t sums[2][QUADS * kSelWaves];
+  const int b = blockIdx.x / p.src.n_heads, h = blockIdx.x % p.src.n_heads;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = evict_length(p, b);
+  if (h == 0 && tid == 0) p.out_length[b] = min(n, p.keep);
+  int32_t* kept = p.kept + (int64_t)blockIdx.x * p.keep;
+  if (n <= p.keep) {
+    for (int s = tid; s < n; s += kSelThreads) kept[s] = s;
+    return;
+  }
+  const int newest = p.total[b] - p.recent;
+  const int segs = (n + kSeg - 1) / kSeg;
+  uint32_t key[QUADS][4];
+  // Slots seg * kSeg + (j * threads + tid) * 4 + e.  Those beyond n get the
+  // lowest key, 0; they are never kept: more than `keep` slots before them are
+  // at least as high, and equal ones are taken from the lowest slot up.
+  // A slot without a page reads the pool's first one and gets key 0 too.
+  auto load = [&](int seg) {
+    if (p.src.n_pages == 0) {
+#pragma unroll
+      for (int j = 0; j < QUADS; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) key[j][e] = 0;
+      return;
+    }
+    const int32_t* table = p.src.page_table + (int64_t)b * p.src.max_pages;
+    int page[QUADS];
+#pragma unroll
+    for (int j = 0; j < QUADS; ++j) {
+      const int s = min(seg * kSeg + (j * kSelThreads + tid) * 4, n - 1);
+      page[j] = table[page_index(s >> 5, p.src_mul)];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    constexpr int kBatch = QUADS < 4 ? QUADS : 4;  // loads in flight: two a quad
+#pragma unroll
+    for (int j0 = 0; j0 < QUADS; j0 += kBatch) {
+      v4i pos[kBatch];
+      v4f acc[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int s = min(seg * kSeg + ((j0 + j) * kSelThreads + tid) * 4, (n - 1) & ~3);
+        const int64_t row = (unsigned)page[j0 + j] < (unsigned)p.src.n_pages ? (int64_t)page[j0 + j] * p.src.n_heads + h : h;
+        const int64_t i = row * p.src.page + s - page_index(s >> 5, p.src_mul) * p.src.page;
+        if (p.vec) {
+          pos[j] = *reinterpret_cast<const v4i*>(p.src.pos + i);
+          acc[j] = *reinterpret_cast<const v4f*>(p.src.acc + i);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pos[j][e] = p.src.pos[i + e], acc[j][e] = p.src.acc[i + e];
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int s = seg * kSeg + ((j0 + j) * kSelThreads + tid) * 4;
+        const bool there = (unsigned)page[j0 + j] < (unsigned)p.src.n_pages;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          key[j0 + j][e] = there && s + e < n ? order_key(pos[j][e], acc[j][e], newest) : 0u;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  uint32_t prefix = 0, want = (uint32_t)p.keep;
+#pragma nounroll
+  for (int round = 0; round < 3; ++round) {
+    const int shift = round == 0 ? 21 : round == 1 ? 10 : 0;
+    const uint32_t digits = round == 2 ? 1023u : 2047u;
+    const uint32_t known = round == 0 ? 0u : round == 1 ? ~0u << 21 : ~0u << 10;
+    for (int i = tid; i < 2048; i += kSelThreads) hist[i] = 0;
+    __syncthreads();
+    for (int seg = 0; seg < segs; ++seg) {
+      if (round == 0 || segs > 1) load(seg);
+#pragma unroll
+      for (int j = 0; j < QUADS; ++j) {
+        if (seg * kSeg + j * 4 * kSelThreads >= n) break;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (((key[j][e] ^ prefix) & known) == 0) atomicAdd(&hist[key[j][e] >> shift & digits], 1u);
+      }
+    }
+    __syncthreads();
+    // two bins a thread, from the top
+    const int bin = 2047 - 2 * tid;
+    const uint32_t c1 = hist[bin], c0 = hist[bin - 1];
+    uint32_t all;
+    const uint32_t before = scan_threads(c1 + c0, waves, all);
+    if (before < want && want <= before + c1 + c0) {
+      const bool upper = want <= before + c1;
+      found[0] = (uint32_t)(upper ? bin : bin - 1);
+      found[1] = want - before - (upper ? 0 : c1);
+    }
+    __syncthreads();
+    prefix |= (uint32_t)__builtin_amdgcn_readfirstlane((int)found[0]) << shift;
+    want = (uint32_t)__builtin_amdgcn_readfirstlane((int)found[1]);
+  }
+
+  uint32_t base_above = 0, base_equal = 0;
+  for (int seg = 0; seg < segs; ++seg) {
+    if (segs > 1) load(seg);
+    // Counts, keys above the threshold in the low half and equal ones in the
+    // high half: of the lanes before in 256 neighbouring slots, then of the
+    // wavefronts and quads before.
+    uint32_t lanes[QUADS];
+#pragma unroll
+    for (int j = 0; j < QUADS; ++j) {
+      uint32_t c = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c += (key[j][e] > prefix ? 1u : 0u) + (key[j][e] == prefix ? 0x10000u : 0u);
+      const uint32_t sum = scan_lanes(c);
+      lanes[j] = sum - c;
+      if (lane == 63) sums[0][j * kSelWaves + wave] = sum & 0xffffu, sums[1][j * kSelWaves + wave] = sum >> 16;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();
+    const uint32_t xa = tid < QUADS * kSelWaves ? sums[0][tid] : 0, xe = tid < QUADS * kSelWaves ? sums[1][tid] : 0;
+    uint32_t all_a, all_e;
+    const uint32_t sa = scan_threads(xa, waves, all_a);
+    const uint32_t se = scan_threads(xe, waves, all_e);
+    if (tid < QUADS * kSelWaves) sums[0][tid] = sa, sums[1][tid] = se;
+    __syncthreads();
+    // (the same number again, so that the compiler compares once more rather
+    // than keep the results of all comparisons)
+    uint32_t limit = prefix;
+    asm volatile("" : "+s"(limit));
+#pragma unroll
+    for (int j = 0; j < QUADS; ++j) {
+      const int s = seg * kSeg + (j * kSelThreads + tid) * 4;
+      uint32_t na = base_above + sums[0][j * kSelWaves + wave] + (lanes[j] & 0xffffu);
+      uint32_t ne = base_equal + sums[1][j * kSelWaves + wave] + (lanes[j] >> 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool up = key[j][e] > limit, eq = key[j][e] == limit;
+        if (up || (eq && ne < want)) kept[na + min(ne, want)] = s + e;
+        na += up;
+        ne += eq;
+      }
+    }
+    base_above += all_a;
+    base_equal += all_e;
+    __syncthreads();
+  }
 }
 
 // The kept tokens to dst, one workgroup per (sequence, head, block of 32 slots
-// of dst).  K words, scales, positions and weights move as they are; a word of V
-// is put together from 8 tokens' nibbles.
-__global__ __launch_bounds__(256) void evict_move(EvictArgs p) {
+// of dst), everything read before anything is written.  K's words, scales,
+// positions and weights move as they are, 16 bytes to a thread; a word of V is
+// put together from 8 tokens' nibbles.  A kept token's nibbles lie in words that
+// it shares with 7 others, and its scales, position and weight in sectors that
+// it shares with 15: where few tokens stay, that is what bounds it.
+template <int DIM>
+__global__ __launch_bounds__(256, 4) void evict_move(EvictArgs p) {
+  constexpr int kWords = DIM / 8;
   __shared__ int64_t from_row[32];
   __shared__ int from_at[32];
-  const int bh = blockIdx.y, b = bh / p.src.n_heads, h = bh % p.src.n_heads;
+  const int bh = blockIdx.y, b = bh / p.src.n_heads, h = bh % p.src.n_heads, tid = threadIdx.x;
   const int first = blockIdx.x * 32;
   const int count = min(evict_length(p, b), p.keep);
   if (first >= count) return;
-  int in_page;
-  const int64_t to = token_row(p.dst, b, h, first, in_page);
+  const int to_page = page_index(first >> 5, p.dst_mul), in_page = first - to_page * p.dst.page;
+  const int64_t to = cache_row(p.dst, b, h, to_page);
   if (to < 0) return;
-  if (threadIdx.x < 32) {
-    const int j = first + threadIdx.x;
-    from_row[threadIdx.x] = -1;
-    if (j < count) {
-      int at;
-      from_row[threadIdx.x] = token_row(p.src, b, h, p.kept[(int64_t)bh * p.keep + j], at);
-      from_at[threadIdx.x] = at;
+  if (tid < 32) {
+    int64_t row = -1;
+    int at = 0;
+    if (first + tid < count) {
+      const int s = p.kept[(int64_t)bh * p.keep + first + tid];
+      const int pi = page_index(s >> 5, p.src_mul);
+      at = s - pi * p.src.page;
+      row = cache_row(p.src, b, h, pi);
     }
+    from_row[tid] = row;
+    from_at[tid] = at;
   }
   __syncthreads();
-  const int words = p.src.dim / 8, groups = p.src.dim / p.src.group;
-  for (int w = threadIdx.x; w < 32 * words; w += 256) {
-    const int s = w / words, c = w % words;
-    if (from_row[s] >= 0)
-      p.dst.k[(to * p.dst.page + in_page + s) * words + c] =
-          p.src.k[(from_row[s] * p.src.page + from_at[s]) * words + c];
-  }
-  for (int w = threadIdx.x; w < 32 * groups; w += 256) {
-    const int s = w & 31, g = w >> 5;
-    if (from_row[s] >= 0) {
-      const int64_t i = (from_row[s] * groups + g) * p.src.page + from_at[s];
-      const int64_t o = (to * groups + g) * p.dst.page + in_page + s;
-      p.dst.k_par[o] = p.src.k_par[i];
-      p.dst.v_par[o] = p.src.v_par[i];
-    }
-  }
-  if (threadIdx.x < 32 && from_row[threadIdx.x] >= 0) {
-    const int64_t i = from_row[threadIdx.x] * p.src.page + from_at[threadIdx.x];
-    const int64_t o = to * p.dst.page + in_page + threadIdx.x;
-    p.dst.pos[o] = p.src.pos[i];
-    p.dst.acc[o] = p.src.acc[i];
-  }
-  // a word of V: channel (c, i) of slots 16 (e/4) + 4 g + e%4
-  const int dim = p.src.dim;
-  for (int w = threadIdx.x; w < 4 * dim; w += 256) {
-    const int g = w / dim, ci = w % dim;
-    uint32_t word = 0;
+  if (tid < DIM) {
+    // four words of V: channels (c, i) = 4 ci.. of slots 16 (e/4) + 4 g + e%4
+    const int g = tid / (DIM / 4), ci = tid % (DIM / 4) * 4;
+    v4u x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int s = 16 * (e >> 2) + 4 * g + (e & 3);
-      if (from_row[s] < 0) continue;
-      const int at = from_at[s] & 31;
-      const int64_t block = (from_row[s] * p.src.page + (from_at[s] & ~31)) * words;
-      const uint32_t x = p.src.v[block + ((at >> 2) & 3) * dim + ci];
-      word |= ((x >> nibble(4 * (at >> 4) + (at & 3))) & 15u) << nibble(e);
+      const int64_t row = from_row[s];
+      const int at = from_at[s];
+      x[e] = v4u{0, 0, 0, 0};
+      if (row >= 0)
+        x[e] = *reinterpret_cast<const v4u*>(p.src.v + (row * p.src.page + (at & ~31)) * kWords + (at >> 2 & 3) * DIM +
+                                             ci);
     }
-    p.dst.v[(to * p.dst.page + in_page) * words + w] = word;
+    v4u word = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int at = from_at[16 * (e >> 2) + 4 * g + (e & 3)] & 31;
+      word |= ((x[e] >> nibble(4 * (at >> 4) + (at & 3))) & 15u) << nibble(e);
+    }
+    *reinterpret_cast<v4u*>(p.dst.v + (to * p.dst.page + in_page) * kWords + g * DIM + ci) = word;
+  } else {
+    // the other threads: K's words 16 bytes each, then a word of every slot's
+    // scales, position and weight
+    const int t = tid - DIM, groups = p.src.dim / p.src.group;
+    const int others = 256 - DIM;
+    for (int i = t; i < 32 * kWords / 4; i += others) {
+      const int s = i / (kWords / 4), w = i % (kWords / 4) * 4;
+      if (from_row[s] >= 0)
+        *reinterpret_cast<v4u*>(p.dst.k + (to * p.dst.page + in_page + s) * kWords + w) =
+            *reinterpret_cast<const v4u*>(p.src.k + (from_row[s] * p.src.page + from_at[s]) * kWords + w);
+    }
+    for (int i = t; i < 32 * (2 * groups + 2); i += others) {
+      const int s = i & 31, what = i >> 5, g = what >> 1;
+      if (from_row[s] < 0) continue;
+      if (g < groups) {
+        const int64_t f = (from_row[s] * groups + g) * p.src.page + from_at[s];
+        const int64_t o = (to * groups + g) * p.dst.page + in_page + s;
+        if (what & 1)
+          p.dst.v_par[o] = p.src.v_par[f];
+        else
+          p.dst.k_par[o] = p.src.k_par[f];
+      } else {
+        const int64_t f = from_row[s] * p.src.page + from_at[s], o = to * p.dst.page + in_page + s;
+        if (what & 1)
+          p.dst.acc[o] = p.src.acc[f];
+        else
+          p.dst.pos[o] = p.src.pos[f];
+      }
+    }
   }
 }
 
@@ -385,12 +525,24 @@ int as_cache_evict(const as_cache_t* src, const as_cache_t* dst, const int32_t* 
   if (workspace_bytes < need || !workspace || !aligned(workspace, 256))
     return fail(AS_E_INVALID_ARG, "cache_evict: workspace of %lld bytes, %lld needed (aligned to 256)",
                 (long long)workspace_bytes, (long long)need);
-  const EvictArgs p{cache_args(src), cache_args(dst), length, total, out_length,
-                    reinterpret_cast<int32_t*>(workspace), keep, recent};
+  const EvictArgs p{cache_args(src), cache_args(dst), length, total, out_length, reinterpret_cast<int32_t*>(workspace),
+                    keep, recent, page_magic(src->page), page_magic(dst->page),
+                    aligned(src->pos, 16) && aligned(src->acc, 16)};
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const unsigned rows = (unsigned)(src->n_seqs * src->n_heads);
-  hipLaunchKernelGGL(evict_select, dim3(rows), dim3(kSelThreads), 0, s, p);
-  hipLaunchKernelGGL(evict_move, dim3((unsigned)((keep + 31) / 32), rows), dim3(256), 0, s, p);
+  const int64_t cap = (int64_t)src->max_pages * src->page;
+  // registers for the longest sequence that the table has room for
+  if (cap <= 4 * kSelThreads)
+    hipLaunchKernelGGL((evict_select<1>), dim3(rows), dim3(kSelThreads), 0, s, p);
+  else if (cap <= 16 * kSelThreads)
+    hipLaunchKernelGGL((evict_select<4>), dim3(rows), dim3(kSelThreads), 0, s, p);
+  else
+    hipLaunchKernelGGL((evict_select<16>), dim3(rows), dim3(kSelThreads), 0, s, p);
+  const dim3 g((unsigned)((keep + 31) / 32), rows);
+  if (src->dim == 64)
+    hipLaunchKernelGGL((evict_move<64>), g, dim3(256), 0, s, p);
+  else
+    hipLaunchKernelGGL((evict_move<128>), g, dim3(256), 0, s, p);
   return launched("cache_evict");
 }
 

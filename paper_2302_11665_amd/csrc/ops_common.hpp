@@ -82,11 +82,22 @@ struct CacheArgs {
 };
 CacheArgs cache_args(const as_cache_t* c);
 
-// Index of the (page, head) row of `slot`, or -1 where the table has no such
-// page; word offsets follow by multiplication with the row's length.
-__device__ __forceinline__ int64_t cache_row(const CacheArgs& c, int b, int h, int page_index) {
-  if ((unsigned)page_index >= (unsigned)c.max_pages) return -1;
-  const int p = c.page_table[(int64_t)b * c.max_pages + page_index];
+// Division of a block of 32 slots' number (below 2^25) by a page's blocks (at
+// most 128): the high half of a product with ceil(2^32 / blocks), which is off
+// by less than blocks, so that the error stays below 2^32.
+__host__ __forceinline__ uint32_t page_magic(int page) {
+  const uint32_t blocks = (uint32_t)page / 32;
+  return blocks > 1 ? (uint32_t)((((uint64_t)1 << 32) + blocks - 1) / blocks) : 0;
+}
+__device__ __forceinline__ int page_index(int block, uint32_t magic) {
+  return magic ? (int)__umulhi((uint32_t)block, magic) : block;
+}
+
+// Index of the (page, head) row of a page of a sequence, or -1 where the table
+// has no such page; word offsets follow by multiplication with the row's length.
+__device__ __forceinline__ int64_t cache_row(const CacheArgs& c, int b, int h, int index) {
+  if ((unsigned)index >= (unsigned)c.max_pages) return -1;
+  const int p = c.page_table[(int64_t)b * c.max_pages + index];
   if ((unsigned)p >= (unsigned)c.n_pages) return -1;
   return (int64_t)p * c.n_heads + h;
 }
