@@ -33,16 +33,16 @@ struct AttArgs {
   int64_t q_seq, q_token;
   const int32_t* length;
   void* out;
-  float* part_o;   // [n_seqs * n_heads][splits][rows][dim], not normalised
-  float* part_ml;  // [n_seqs * n_heads][splits][rows][2]: maximum (log2 units), sum
+  float* part_o;   // [workgroups][2][16 tiles][dim], not normalised
+  float* part_ml;  // [workgroups][2][16 tiles][2]: maximum (log2 units), sum
   float* row_ml;   // [n_seqs * n_heads][rows][2] for the weights: maximum, 1 / sum
   const float* acc_in;
   float* acc_out;
   float c_log2;      // scale * log2(e)
   uint32_t page_mul; // page_magic of the cache's pages
-  int32_t n_queries, per, rows, splits, row_groups;
-  int32_t chunk, row_span;  // blocks of 32 slots and query rows of a workgroup of attend
-  int32_t weigh_chunk;      // blocks of a workgroup of weigh
+  int32_t n_queries, per, rows;
+  int32_t row_groups, row_span;  // parts of 16 tiles query rows
+  int32_t workgroups, weigh_workgroups;
 };
 
 // ---------------------------------------------------------------- 4-bit codes
@@ -354,18 +354,158 @@ __device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int lane
   }
 }
 
-// Blocks of 32 slots that the query rows row0.. (`count` of them) see, and the
-// slots that the first of them sees.
-__device__ __forceinline__ int seen_blocks(const AttArgs& p, int n, int row0, int count, int& least) {
-  const int last = min(n, n - p.n_queries + min(row0 + count - 1, p.rows - 1) / p.per + 1);
+// ----------------------------------------------------------------- the shares
+
+// A segment is what 16 NT query rows of one head see of one sequence, in blocks
+// of 32 slots; the segments of all sequences, heads and row groups, one after
+// the other, are dealt to the workgroups in shares of one size, whatever the
+// lengths.  All workgroups run at once: there is no tail, and none is started for
+// slots that a table has room for but a sequence does not use.  A segment that
+// lies within a share is finished there; of another one, each workgroup leaves
+// its part: in place 1 the one that begins it, in place 0 the others.
+struct Segment {
+  int b, h, rg, n;
+  int blk, seen;  // first block of the share, blocks of the segment
+};
+
+// Blocks that the rows of group rg see; least: slots that the first row sees.
+__device__ __forceinline__ int seen_blocks(const AttArgs& p, int n, int rg, int& least) {
+  const int row0 = rg * p.row_span;
+  const int last = min(n, n - p.n_queries + min(row0 + p.row_span - 1, p.rows - 1) / p.per + 1);
   least = n - p.n_queries + row0 / p.per + 1;
   return max(0, (last + 31) / 32);
 }
 
-// One workgroup per (sequence, head, run of p.chunk blocks of 32 slots, 16 NT
-// query rows); its four wavefronts take the blocks in turn, each with a ring of
-// its own in LDS so that none waits for another, and join their results at the
-// end.
+// Blocks of all segments of one head of a sequence.  WEIGH: one segment of all
+// rows.
+template <bool WEIGH>
+__device__ __forceinline__ uint32_t head_blocks(const AttArgs& p, int n) {
+  if (WEIGH || p.row_groups == 1) return (uint32_t)(n + 31) / 32;
+  uint32_t sum = 0;
+  int least;
+  for (int rg = 0; rg < p.row_groups; ++rg) sum += (uint32_t)seen_blocks(p, n, rg, least);
+  return sum;
+}
+
+// 64 sequences from b0 on: the lane's length, and the sum of the blocks of the
+// sequences up to and with the lane's.
+struct Sequences {
+  int n;
+  uint32_t sum;
+};
+template <bool WEIGH>
+__device__ __forceinline__ Sequences scan_sequences(const AttArgs& p, int b0, int lane) {
+  const int b = b0 + lane;
+  Sequences s;
+  s.n = b < p.c.n_seqs ? clamped_length(p, b) : 0;
+  s.sum = scan_lanes(head_blocks<WEIGH>(p, s.n) * (uint32_t)p.c.n_heads);
+  return s;
+}
+__device__ __forceinline__ uint32_t all_blocks(const Sequences& s) {
+  return (uint32_t)__builtin_amdgcn_readlane((int)s.sum, 63);
+}
+
+// Blocks in all, and the size of a share: at least a block for each of a
+// workgroup's wavefronts where segments are that long.  first: the scan of the
+// first 64 sequences.
+template <bool WEIGH>
+__device__ __forceinline__ uint32_t share_size(const AttArgs& p, int lane, Sequences& first, uint32_t& total) {
+  first = scan_sequences<WEIGH>(p, 0, lane);
+  total = all_blocks(first);
+  for (int b0 = 64; b0 < p.c.n_seqs; b0 += 64) total += all_blocks(scan_sequences<WEIGH>(p, b0, lane));
+  const uint32_t segments = (uint32_t)(p.c.n_seqs * p.c.n_heads) * (WEIGH ? 1u : (uint32_t)p.row_groups);
+  const uint32_t groups = (uint32_t)(WEIGH ? p.weigh_workgroups : p.workgroups);
+  uint32_t least = 1;  // min(mean length of a segment, kWaves)
+#pragma unroll
+  for (int w = 2; w <= kWaves; ++w) least += total > (uint64_t)segments * (w - 1);
+  return max((total + groups - 1) / groups, least);
+}
+
+// This workgroup's share's number, or -1.  Neighbouring workgroup numbers go to
+// different XCDs; each XCD gets a run of shares, which mostly read the same
+// slots where a head has several row groups.
+__device__ __forceinline__ int64_t share_number(uint32_t total, uint32_t size) {
+  const uint32_t shares = (total + size - 1) / size, per_xcd = (shares + 7) / 8;
+  const uint32_t at = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  return (blockIdx.x >> 3) < per_xcd && at < shares ? (int64_t)at : -1;
+}
+
+// The segment that holds block `unit` of all.
+template <bool WEIGH>
+__device__ __forceinline__ Segment locate(const AttArgs& p, uint32_t unit, int lane, const Sequences& first) {
+  uint32_t before = 0;
+  Sequences q = first;
+  int b0 = 0;
+  while (unit >= before + all_blocks(q) && b0 + 64 < p.c.n_seqs) {
+    before += all_blocks(q);
+    q = scan_sequences<WEIGH>(p, b0 += 64, lane);
+  }
+  const uint64_t past = __ballot(before + q.sum > unit);
+  const int i = past ? __builtin_ctzll(past) : 0;
+  if (i > 0) before += (uint32_t)__builtin_amdgcn_readlane((int)q.sum, i - 1);
+  Segment s;
+  s.b = b0 + i;
+  s.n = __builtin_amdgcn_readlane(q.n, i);
+  const uint32_t per_head = max(1u, head_blocks<WEIGH>(p, s.n));
+  uint32_t off = unit - before;
+  s.h = (int)(off / per_head);
+  off -= (uint32_t)s.h * per_head;
+  s.rg = 0;
+  int least;
+  s.seen = WEIGH ? (s.n + 31) / 32 : seen_blocks(p, s.n, 0, least);
+  while (!WEIGH && s.rg + 1 < p.row_groups && off >= (uint32_t)s.seen) {
+    off -= (uint32_t)s.seen;
+    s.seen = seen_blocks(p, s.n, ++s.rg, least);
+  }
+  s.blk = (int)off;
+  return s;
+}
+
+// The next segment that is not empty; there is one.
+template <bool WEIGH>
+__device__ __forceinline__ void advance(const AttArgs& p, Segment& s) {
+  int least;
+  do {
+    if (WEIGH || ++s.rg == p.row_groups) {
+      s.rg = 0;
+      if (++s.h == p.c.n_heads) {
+        s.h = 0;
+        if (++s.b >= p.c.n_seqs) return;
+        s.n = clamped_length(p, s.b);
+      }
+    }
+    s.seen = WEIGH ? (s.n + 31) / 32 : seen_blocks(p, s.n, s.rg, least);
+  } while (s.seen == 0);
+  s.blk = 0;
+}
+
+// ------------------------------------------------------------------ the kernels
+
+// Where a row's output is.
+__device__ __forceinline__ int64_t out_index(const AttArgs& p, int b, int h, int row, int dim) {
+  const int t = row / p.per;
+  return (((int64_t)b * p.n_queries + t) * p.c.n_heads * p.per + h * p.per + row - t * p.per) * dim;
+}
+
+template <int TYPE>
+__device__ __forceinline__ void store_row(const AttArgs& p, int64_t at, v4f x, float l) {
+  const float inv = 1.0f / l;
+  uint16_t* out = reinterpret_cast<uint16_t*>(p.out) + at;
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float lo = l == 0.0f ? 0.0f : x[2 * i] * inv, hi = l == 0.0f ? 0.0f : x[2 * i + 1] * inv;
+    w[i] = (uint32_t)from_f32<TYPE>(lo) | (uint32_t)from_f32<TYPE>(hi) << 16;
+  }
+  *reinterpret_cast<v2u*>(out) = v2u{w[0], w[1]};
+}
+
+__device__ __forceinline__ void store_row_ml(const AttArgs& p, int b, int h, int row, float m, float l) {
+  float* to = p.row_ml + (((int64_t)b * p.c.n_heads + h) * p.rows + row) * 2;
+  to[0] = m;
+  to[1] = l == 0.0f ? 0.0f : 1.0f / l;
+}
+
 constexpr int kStages = 2;
 template <int DIM, int GROUP>
 constexpr int attend_lds() {
@@ -374,27 +514,14 @@ constexpr int attend_lds() {
 }
 
 template <int TYPE, int DIM, int GROUP, int NT>
-__global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : 2) - (DIM == 4 * GROUP)) void attend(AttArgs p) {
+__device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& s, int take, int share, int lane,
+                                               int wave, uint8_t* lds, float (*ml)[16][2]) {
   constexpr int NG = DIM / GROUP;
   typedef Stage<DIM, GROUP, true> S;
   constexpr int kRing = kStages * S::kBytes;
-  __shared__ float ml[kWaves][16][2];
-  extern __shared__ __align__(16) uint8_t lds[];  // the rings, then the parts to be joined
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // Neighbouring workgroup numbers go to different XCDs: the row groups of one
-  // part, which read the same slots, are a multiple of 8 apart.
-  const int unit = (int)(blockIdx.x / (8 * p.row_groups)) * 8 + (int)(blockIdx.x & 7);
-  const int rg = (int)(blockIdx.x / 8) % p.row_groups;
-  const int bh = unit / p.splits, split = unit % p.splits;
-  if (bh >= p.c.n_seqs * p.c.n_heads) return;
-  const int b = bh / p.c.n_heads, h = bh % p.c.n_heads;
-  const int n = clamped_length(p, b);
-  const int row0 = rg * 16 * NT;
+  const int b = s.b, h = s.h, n = s.n, row0 = s.rg * 16 * NT, end = s.blk + take;
   int least;
-  const int seen = seen_blocks(p, n, row0, 16 * NT, least);
-  const int end = min((split + 1) * p.chunk, seen);
-  if (p.splits > 1 && split * p.chunk >= seen) return;
-
+  seen_blocks(p, n, s.rg, least);
   uint8_t* ring = lds + wave * kRing;
   Queries<TYPE, DIM, GROUP> q[NT];
   Sums<DIM, GROUP, NT> a;
@@ -411,7 +538,7 @@ __global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : 2) - (DIM == 4 * GROUP)
 
   const Expand<TYPE> key_codes;
   const Expand<AS_BF16> value_codes;
-  int blk = split * p.chunk + wave;
+  int blk = s.blk + wave;
   uint32_t valid = 0;  // bit j: the block j turns on has a page
 #pragma unroll
   for (int j = 0; j < kStages; ++j) {
@@ -483,118 +610,136 @@ __global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : 2) - (DIM == 4 * GROUP)
       }
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) l += ml[w][r][1] * __builtin_amdgcn_exp2f(ml[w][r][0] - top);
-      const int64_t at = ((int64_t)bh * p.splits + split) * p.rows + row;
-      if (p.splits > 1) *reinterpret_cast<v4f*>(p.part_o + at * DIM + d) = x;
-      if (p.part_ml && d == 0) {
-        p.part_ml[at * 2] = top;
-        p.part_ml[at * 2 + 1] = l;
-      }
-      if (p.splits == 1) {
-        const int t = row / p.per;
-        uint16_t* out = reinterpret_cast<uint16_t*>(p.out) +
-                        (((int64_t)b * p.n_queries + t) * p.c.n_heads * p.per + h * p.per + row - t * p.per) * DIM + d;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) out[e] = from_f32<TYPE>(l == 0.0f ? 0.0f : x[e] / l);
+      if (take == s.seen) {
+        store_row<TYPE>(p, out_index(p, b, h, row, DIM) + d, x, l);
+        if (p.row_ml && d == 0) store_row_ml(p, b, h, row, top, l);
+      } else {
+        const int64_t at = ((int64_t)share * 2 + (s.blk == 0)) * (16 * NT) + 16 * u + r;
+        *reinterpret_cast<v4f*>(p.part_o + at * DIM + d) = x;
+        if (d == 0) *reinterpret_cast<float2*>(p.part_ml + at * 2) = make_float2(top, l);
       }
     }
   }
+  __syncthreads();  // the next segment's rings
 }
 
-// Joins the splits, one workgroup per row: every split's factor first, then
-// their sums, four channels to a thread and several splits side by side.
-constexpr int kMaxSplits = 1024;
+// One workgroup per share; its four wavefronts take a segment's blocks in turn,
+// each with a ring of its own in LDS so that none waits for another, and join
+// their results at the segment's end.
+template <int TYPE, int DIM, int GROUP, int NT>
+__global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : 2) - (DIM == 4 * GROUP)) void attend(AttArgs p) {
+  __shared__ float ml[kWaves][16][2];
+  extern __shared__ __align__(16) uint8_t lds[];  // the rings, then the parts to be joined
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Sequences first;
+  uint32_t total;
+  const uint32_t size = share_size<false>(p, lane, first, total);
+  const int64_t share = share_number(total, size);
+  if (share < 0) return;
+  const uint32_t unit = (uint32_t)share * size;
+  int left = (int)min(size, total - unit);
+  Segment g = locate<false>(p, unit, lane, first);
+  for (;;) {
+    const int take = min(left, g.seen - g.blk);
+    attend_segment<TYPE, DIM, GROUP, NT>(p, g, take, (int)share, lane, wave, lds, ml);
+    left -= take;
+    if (left == 0) return;
+    advance<false>(p, g);
+  }
+}
 
-template <int TYPE, int DIM>
+// Joins the parts of the segments that several workgroups had, four channels to
+// a thread.  ROWS = 1: a workgroup joins one row, its parts side by side (few
+// rows, and a long segment may have hundreds of parts); otherwise a workgroup
+// joins a whole segment, ROWS rows at a time.
+constexpr int kMaxParts = 2048;
+
+template <int TYPE, int DIM, int ROWS>
 __global__ __launch_bounds__(256) void join(AttArgs p) {
-  constexpr int kSide = 256 / (DIM / 4);
-  __shared__ float factor[kMaxSplits];
-  __shared__ float red[2][4];
+  constexpr int kSide = 256 / (DIM / 4) / ROWS;
+  __shared__ float mls[kSide][2];
   __shared__ v4f sums[kSide][DIM / 4];
-  const int row = blockIdx.x % p.rows, bh = blockIdx.x / p.rows;
-  const int b = bh / p.c.n_heads, h = bh % p.c.n_heads, tid = threadIdx.x;
-  const int rows_wg = p.row_span;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int across = ROWS == 1 ? p.rows : p.row_groups;
+  const int bh = blockIdx.x / across, in = blockIdx.x % across;
+  const int rg = ROWS == 1 ? in / p.row_span : in;
+  const int b = bh / p.c.n_heads, h = bh % p.c.n_heads;
+  const int n = clamped_length(p, b);
   int least;
-  const int seen = seen_blocks(p, clamped_length(p, b), row / rows_wg * rows_wg, rows_wg, least);
-  const int live = p.splits > 1 ? (seen + p.chunk - 1) / p.chunk : 1;
-  const int64_t base = (int64_t)bh * p.splits * p.rows + row;
-  float m = kFloor;
-  for (int s = tid; s < live; s += 256) m = fmaxf(m, p.part_ml[(base + (int64_t)s * p.rows) * 2]);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if ((tid & 63) == 0) red[0][tid >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-  float l = 0.0f;
-  for (int s = tid; s < live; s += 256) {
-    const float* ml = p.part_ml + (base + (int64_t)s * p.rows) * 2;
-    const float f = __builtin_amdgcn_exp2f(ml[0] - m);
-    factor[s] = f;
-    l += f * ml[1];
+  const int seen = seen_blocks(p, n, rg, least);
+  const int d = tid % (DIM / 4), side = tid / (DIM / 4) % kSide;
+  int row = ROWS == 1 ? in : rg * p.row_span + tid / (DIM / 4);
+  const int end = ROWS == 1 ? in + 1 : min(p.rows, (rg + 1) * p.row_span);
+  if (seen == 0) {  // in no workgroup's share
+    if (side) return;
+    for (; row < end; row += ROWS) {
+      store_row<TYPE>(p, out_index(p, b, h, row, DIM) + 4 * d, v4f{0, 0, 0, 0}, 0.0f);
+      if (p.row_ml && d == 0) store_row_ml(p, b, h, row, kFloor, 0.0f);
+    }
+    return;
   }
-#pragma unroll
-  for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
-  if ((tid & 63) == 0) red[1][tid >> 6] = l;
-  __syncthreads();
-  l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
-  if (p.row_ml && tid == 0) {
-    p.row_ml[((int64_t)bh * p.rows + row) * 2] = m;
-    p.row_ml[((int64_t)bh * p.rows + row) * 2 + 1] = l == 0.0f ? 0.0f : 1.0f / l;
+  // the segment's first block among all
+  Sequences first;
+  uint32_t total;
+  const uint32_t size = share_size<false>(p, lane, first, total);
+  uint32_t start = 0;
+  for (int b0 = 0; b0 < b; b0 += 64) {
+    if (b0) first = scan_sequences<false>(p, b0, lane);
+    start += (uint32_t)__builtin_amdgcn_readlane((int)first.sum, min(63, b - 1 - b0));
   }
-  if (p.splits == 1) return;
-  const int d = tid % (DIM / 4), side = tid / (DIM / 4);
-  v4f x = {0, 0, 0, 0};
+  start += (uint32_t)h * head_blocks<false>(p, n);
+  for (int r = 0; r < rg; ++r) start += (uint32_t)seen_blocks(p, n, r, least);
+  const int share = (int)(start / size), parts = (int)((start + seen - 1) / size) - share + 1;
+  if (parts == 1) return;  // finished where it was
+  for (; row < end; row += ROWS) {
+    auto at = [&](int s) { return ((int64_t)(share + s) * 2 + (s == 0)) * p.row_span + row - rg * p.row_span; };
+    float m = kFloor, l = 0.0f;
+    v4f x = {0, 0, 0, 0};
 #pragma unroll 4
-  for (int s = side; s < live; s += kSide)
-    x += *reinterpret_cast<const v4f*>(p.part_o + (base + (int64_t)s * p.rows) * DIM + 4 * d) * factor[s];
-  sums[side][d] = x;
-  __syncthreads();
-  if (side) return;
+    for (int s = side; s < parts; s += kSide) {
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at(s) * 2);
+      const v4f o = *reinterpret_cast<const v4f*>(p.part_o + at(s) * DIM + 4 * d);
+      const float top = fmaxf(m, ml.x), was = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(ml.x - top);
+      m = top;
+      l = fmaf(l, was, ml.y * f);
+      x = x * was + o * f;
+    }
+    if (kSide > 1) {
+      if (d == 0) mls[side][0] = m, mls[side][1] = l;
+      sums[side][d] = x;
+      __syncthreads();
+      if (side) return;  // (one row to a workgroup)
 #pragma unroll
-  for (int s = 1; s < kSide; ++s) x += sums[s][d];
-  const int t = row / p.per;
-  uint16_t* out = reinterpret_cast<uint16_t*>(p.out) +
-                  (((int64_t)b * p.n_queries + t) * p.c.n_heads * p.per + h * p.per + row - t * p.per) * DIM + 4 * d;
+      for (int s = 1; s < kSide; ++s) m = fmaxf(m, mls[s][0]);
+      l = 0.0f;
+      x = v4f{0, 0, 0, 0};
 #pragma unroll
-  for (int e = 0; e < 4; ++e) out[e] = from_f32<TYPE>(l == 0.0f ? 0.0f : x[e] / l);
-}
-
-// The sum of x over the 16 lanes of a row, in every one of them.
-__device__ __forceinline__ float sum_in_row(float x) {
-  x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x128, 0xf, 0xf, false));  // row_ror:8
-  x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x124, 0xf, 0xf, false));
-  x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x122, 0xf, 0xf, false));
-  x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x121, 0xf, 0xf, false));
-  return x;
+      for (int s = 0; s < kSide; ++s) {
+        const float f = __builtin_amdgcn_exp2f(mls[s][0] - m);
+        l = fmaf(mls[s][1], f, l);
+        x += sums[s][d] * f;
+      }
+    }
+    store_row<TYPE>(p, out_index(p, b, h, row, DIM) + 4 * d, x, l);
+    if (p.row_ml && d == 0) store_row_ml(p, b, h, row, m, l);
+  }
 }
 
 // The tokens' weights, from the keys once more now that every query's maximum
-// and sum are known: one workgroup per run of blocks, whose wavefronts take them
-// in turn, all queries of the head.  With at most 16 rows the queries stay in
-// registers.
+// and sum are known; shares as before, all rows of a head in one segment.  The
+// product is q K^T here, so that a lane has one slot and four queries: a slot's
+// sum over the queries stays in the lane but for two steps across rows of lanes.
 constexpr int kWeighStages = 3;
 
 template <int TYPE, int DIM, int GROUP>
-__global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 2 : 3) void weigh(AttArgs p) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int bh = blockIdx.y, b = bh / p.c.n_heads, h = bh % p.c.n_heads;
-  const int n = clamped_length(p, b);
-  const int end = min((int)(blockIdx.x + 1) * p.weigh_chunk, (n + 31) / 32);
-  int blk = (int)blockIdx.x * p.weigh_chunk + wave;
-  if (blk >= end) return;
-  const Expand<TYPE> key_codes;
-  Queries<TYPE, DIM, GROUP> q;
-  float m = 0.0f, inv = 0.0f;
-  auto queries = [&](int r0) {
-    const int r = r0 + (lane & 15);
-    load_queries<TYPE, DIM, GROUP>(p, b, h, r, n, lane, q);
-    if (r >= p.rows) q.limit = 0;
-    const float* ml = p.row_ml + ((int64_t)bh * p.rows + min(r, p.rows - 1)) * 2;
-    m = ml[0], inv = ml[1];
-  };
-  queries(0);
+__device__ __forceinline__ void weigh_segment(const AttArgs& p, const Segment& s, int take, int lane, int wave,
+                                              uint8_t* lds) {
+  constexpr int NG = DIM / GROUP;
   typedef Stage<DIM, GROUP, false> S;
-  extern __shared__ __align__(16) uint8_t lds[];
   constexpr int kStage = S::kBytes + 128;
+  const int b = s.b, h = s.h, n = s.n, end = s.blk + take, g = lane >> 4;
+  int blk = s.blk + wave;
+  const Expand<TYPE> key_codes;
   uint8_t* ring = lds + wave * kWeighStages * kStage;
   int64_t rows[kWeighStages];
   int places[kWeighStages];
@@ -615,6 +760,33 @@ __global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 2 : 3) void weigh(A
     rows[j] = block_row(p, b, h, blk + j * kWaves, places[j]);
     if (p.c.n_pages > 0) bring(j);
   }
+  // Queries r0.. : the operand, and of the lane's four rows 4 g + r the sums
+  // over the groups, the maximum, 1 / sum (0 for rows beyond the last) and the
+  // slots that it sees.
+  v4u q[DIM / 32];
+  v4f start[NG], qsum[NG];
+  float m[4], inv[4];
+  int limit[4];
+  auto queries = [&](int r0) {
+    Queries<TYPE, DIM, GROUP> x;
+    load_queries<TYPE, DIM, GROUP>(p, b, h, r0 + (lane & 15), n, lane, x);
+#pragma unroll
+    for (int i = 0; i < DIM / 32; ++i) q[i] = x.q[i];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int row = r0 + 4 * g + r;
+      const float* ml = p.row_ml + (((int64_t)b * p.c.n_heads + h) * p.rows + min(row, p.rows - 1)) * 2;
+      m[r] = ml[0];
+      inv[r] = row < p.rows ? ml[1] : 0.0f;
+      limit[r] = row < p.rows ? n - p.n_queries + row / p.per + 1 : 0;
+#pragma unroll
+      for (int k = 0; k < NG; ++k) {
+        qsum[k][r] = __shfl(x.sum[k], 4 * g + r);
+        start[k][r] = -16.0f * qsum[k][r];
+      }
+    }
+  };
+  queries(0);
   while (blk < end) {
 #pragma unroll
     for (int z = 0; z < kWeighStages; ++z) {
@@ -628,68 +800,91 @@ __global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 2 : 3) void weigh(A
         wait_loads<(kWeighStages - 1) * (S::kLoads + 1)>();
       else
         wait_loads<0>();
-      uint32_t k[2][DIM / 32];
-      v4u par[2][DIM / GROUP];
+      uint32_t k[2][DIM / 32], par[2][NG];
+      const uint8_t* at = ring + z * kStage;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        S::keys(ring + z * kStage, lane, t, k[t]);
+        S::keys(at, lane, t, k[t]);
 #pragma unroll
-        for (int g = 0; g < DIM / GROUP; ++g) par[t][g] = S::key_scales(ring + z * kStage, lane, t, g);
+        for (int i = 0; i < NG; ++i)
+          par[t][i] = *reinterpret_cast<const uint32_t*>(at + S::kParAt + i * 128 + (16 * t + (lane & 15)) * 4);
       }
-      const int e8 = lane & 15, s8 = 16 * (e8 >> 2) + (lane >> 4) * 4 + (e8 & 3);  // the slot that lanes e8 < 8 store
-      const float was = e8 < 8 ? *reinterpret_cast<const float*>(ring + z * kStage + S::kBytes + s8 * 4) : 0.0f;
+      const float was = *reinterpret_cast<const float*>(at + S::kBytes + (lane & 31) * 4);
       if (more) {
         wait_reads();
         if (p.c.n_pages > 0) bring(z);
       }
       if (here >= 0) {
+        float w[2] = {0.0f, 0.0f};
         v4u kf[2][DIM / 32];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < DIM / 32; ++i) kf[t][i] = key_codes(k[t][i]);
-        float w[8] = {};
-        const int slot0 = blk * 32 + (lane >> 4) * 4;
         for (int r0 = 0; r0 < p.rows; r0 += 16) {
           if (p.rows > 16) queries(r0);
+          const bool ragged = blk * 32 + 32 > n - p.n_queries + 1;
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             float x[4];
-            scores<TYPE, DIM, GROUP>(kf[t], par[t], q, x);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (slot0 + 16 * t + e < q.limit) w[4 * t + e] += __builtin_amdgcn_exp2f(fmaf(x[e], p.c_log2, -m)) * inv;
+            for (int i = 0; i < NG; ++i) {
+              v4f a = start[i];
+#pragma unroll
+              for (int c = i * (GROUP / 32); c < (i + 1) * (GROUP / 32); ++c) a = mfma<TYPE>(q[c], kf[t][c], a);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                x[r] = fma_m(qsum[i][r], par[t][i], i == 0 ? 0.0f : x[r]);
+                x[r] = fma_d(a[r], par[t][i], x[r]);
+              }
+            }
+            const int slot = blk * 32 + 16 * t + (lane & 15);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              float e = __builtin_amdgcn_exp2f(fmaf(x[r], p.c_log2, -m[r])) * inv[r];
+              // (rows beyond the last have 0 / sum, but may be NaN)
+              if (ragged || p.rows % 16) e = slot < limit[r] ? e : 0.0f;
+              w[t] += e;
+            }
           }
         }
-        // lane e of each row of 16 stores its slot e
-        float x = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float y = sum_in_row(w[e]);
-          x = (lane & 15) == e ? y : x;
-        }
-        if (e8 < 8 && blk * 32 + s8 < n) p.acc_out[here * p.c.page + place + s8] = (p.acc_in ? was : 0.0f) + x;
+        const float w0 = sum_over_rows(w[0]), w1 = sum_over_rows(w[1]);
+        const float x = (lane & 16) ? w1 : w0;
+        const int place_s = place + (lane & 31);
+        if (lane < 32 && blk * 32 + (lane & 31) < n) p.acc_out[here * p.c.page + place_s] = (p.acc_in ? was : 0.0f) + x;
       }
       blk += kWaves;
     }
   }
 }
 
+template <int TYPE, int DIM, int GROUP>
+__global__ __launch_bounds__(64 * kWaves, 3) void weigh(AttArgs p) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Sequences first;
+  uint32_t total;
+  const uint32_t size = share_size<true>(p, lane, first, total);
+  const int64_t share = share_number(total, size);
+  if (share < 0) return;
+  const uint32_t unit = (uint32_t)share * size;
+  int left = (int)min(size, total - unit);
+  Segment g = locate<true>(p, unit, lane, first);
+  for (;;) {
+    const int take = min(left, g.seen - g.blk);
+    weigh_segment<TYPE, DIM, GROUP>(p, g, take, lane, wave, lds);
+    left -= take;
+    if (left == 0) return;
+    advance<true>(p, g);
+  }
+}
+
 struct Plan {
-  int per, rows, tiles, row_groups, splits, chunk, weigh_chunk, weigh_groups;
+  int per, rows, tiles, row_groups, workgroups, weigh_workgroups;
   int64_t o_bytes, ml_bytes, row_bytes;
 };
 
-// Blocks of 32 slots to a workgroup of four wavefronts: at least two for each
-// wavefront, and more where that still leaves about 2048 workgroups.  Runs of one
-// length balance ragged sequences: those beyond a sequence's end return at once.
-int choose_chunk(int64_t blocks, int64_t units, int64_t target) {
-  int64_t c = blocks * units / target;
-  c = c < 8 ? 8 : round_up(c, 8);
-  const int64_t least = (blocks + kMaxSplits - 1) / kMaxSplits;
-  return (int)(c > least ? c : round_up(least, 8));
-}
-
+// Workgroups that a compute unit runs at once: the launch bounds of the kernels.
 Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) {
   Plan pl;
   pl.per = n_q_heads / c->n_heads;
@@ -697,16 +892,20 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   pl.tiles = pl.rows > 16 ? 2 : 1;
   pl.row_groups = (pl.rows + 16 * pl.tiles - 1) / (16 * pl.tiles);
   const int64_t heads = (int64_t)c->n_seqs * c->n_heads;
-  int64_t blocks = (int64_t)c->max_pages * c->page / 32;
-  if (blocks < 1) blocks = 1;
-  pl.chunk = choose_chunk(blocks, heads * pl.row_groups, 2048);
-  pl.splits = (int)((blocks + pl.chunk - 1) / pl.chunk);
-  pl.weigh_chunk = choose_chunk(blocks, heads, 2048);
-  pl.weigh_groups = (int)((blocks + pl.weigh_chunk - 1) / pl.weigh_chunk);
-  const int64_t rows = heads * pl.rows;
-  pl.o_bytes = pl.splits > 1 ? round_up(rows * pl.splits * c->dim * 4, 256) : 0;
-  pl.ml_bytes = pl.splits > 1 || weights ? round_up(rows * pl.splits * 8, 256) : 0;
-  pl.row_bytes = weights ? round_up(rows * 8, 256) : 0;
+  const int64_t blocks = (int64_t)c->max_pages * c->page / 32;
+  const int wide = c->dim == 4 * c->group;
+  auto groups = [&](int64_t all, int64_t resident) {
+    const int64_t g = all < resident ? all : resident;
+    return (int)round_up(g < 1 ? 1 : g, 8);
+  };
+  int cus = as_host::compute_units();
+  if (cus > kMaxParts / 4) cus = kMaxParts / 4;
+  pl.workgroups = groups(heads * pl.row_groups * blocks, (int64_t)cus * ((pl.tiles == 1 ? 4 : 2) - wide));
+  pl.weigh_workgroups = groups(heads * blocks, (int64_t)cus * 3);
+  const int64_t parts = (int64_t)pl.workgroups * 2 * 16 * pl.tiles;
+  pl.o_bytes = round_up(parts * c->dim * 4, 256);
+  pl.ml_bytes = round_up(parts * 8, 256);
+  pl.row_bytes = weights ? round_up(heads * pl.rows * 8, 256) : 0;
   return pl;
 }
 
@@ -721,25 +920,28 @@ int check_queries(const as_cache_t* c, int32_t n_queries, int32_t n_q_heads) {
   if ((int64_t)c->n_seqs * n_queries * n_q_heads > (1 << 26))
     return fail(AS_E_LIMITS, "attention_kv4: %d sequences, %d queries, %d heads (at most 2^26 rows in all)", c->n_seqs,
                 n_queries, n_q_heads);
+  const int64_t spans = ((int64_t)n_q_heads / c->n_heads * n_queries + 15) / 16;
+  if ((int64_t)c->n_seqs * c->n_heads * spans * ((int64_t)c->max_pages * c->page / 32) > 0x7fffffff)
+    return fail(AS_E_LIMITS, "attention_kv4: at most 2^31 blocks of 32 slots over all sequences, heads and 16 rows");
   return AS_OK;
 }
 
 template <int TYPE, int DIM, int GROUP>
 int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
-  const int64_t units = round_up((int64_t)p.c.n_seqs * p.c.n_heads * pl.splits, 8) * pl.row_groups;
-  const dim3 g((unsigned)units), t(64 * kWaves);
+  const dim3 g((unsigned)pl.workgroups), t(64 * kWaves);
   const size_t lds = attend_lds<DIM, GROUP>();
   if (pl.tiles == 1)
     hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 1>), g, t, lds, s, p);
   else
     hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 2>), g, t, lds, s, p);
-  if (pl.splits > 1 || p.acc_out)
-    hipLaunchKernelGGL((join<TYPE, DIM>), dim3((unsigned)((int64_t)p.c.n_seqs * p.c.n_heads * p.rows)), dim3(256), 0,
-                       s, p);
+  const int64_t heads = (int64_t)p.c.n_seqs * p.c.n_heads;
+  if (p.row_groups == 1)
+    hipLaunchKernelGGL((join<TYPE, DIM, 1>), dim3((unsigned)(heads * p.rows)), dim3(256), 0, s, p);
+  else
+    hipLaunchKernelGGL((join<TYPE, DIM, 1024 / DIM>), dim3((unsigned)(heads * p.row_groups)), dim3(256), 0, s, p);
   typedef Stage<DIM, GROUP, false> KeyStage;
   if (p.acc_out)
-    hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP>),
-                       dim3((unsigned)pl.weigh_groups, (unsigned)(p.c.n_seqs * p.c.n_heads)), t,
+    hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP>), dim3((unsigned)pl.weigh_workgroups), t,
                        (size_t)kWaves * kWeighStages * (KeyStage::kBytes + 128), s, p);
   return launched("attention_kv4");
 }
@@ -778,8 +980,8 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
   if (!(scale > 0.0f) || scale > 3.0e38f) return fail(AS_E_INVALID_ARG, "attention_kv4: scale %g", (double)scale);
   if (cache->n_seqs == 0 || n_queries == 0) return as_host::ok();
   if (!q || !length || !out) return fail(AS_E_INVALID_ARG, "attention_kv4: null pointer");
-  if (!aligned(q, 16) || q_seq % 8 || q_token % 8)
-    return fail(AS_E_INVALID_ARG, "attention_kv4: queries have to be aligned to 16 bytes, strides a multiple of 8");
+  if (!aligned(q, 16) || !aligned(out, 8) || q_seq % 8 || q_token % 8)
+    return fail(AS_E_INVALID_ARG, "attention_kv4: queries (and outputs, to 8) have to be aligned to 16 bytes, strides a multiple of 8");
   const Plan pl = make_plan(cache, n_queries, n_q_heads, acc_out != nullptr);
   const int64_t need = pl.o_bytes + pl.ml_bytes + pl.row_bytes;
   if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 256))))
@@ -793,8 +995,8 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
   p.length = length;
   p.out = out;
   char* ws = reinterpret_cast<char*>(workspace);
-  p.part_o = pl.o_bytes ? reinterpret_cast<float*>(ws) : nullptr;
-  p.part_ml = pl.ml_bytes ? reinterpret_cast<float*>(ws + pl.o_bytes) : nullptr;
+  p.part_o = reinterpret_cast<float*>(ws);
+  p.part_ml = reinterpret_cast<float*>(ws + pl.o_bytes);
   p.row_ml = pl.row_bytes ? reinterpret_cast<float*>(ws + pl.o_bytes + pl.ml_bytes) : nullptr;
   p.acc_in = acc_in;
   p.acc_out = acc_out;
@@ -803,11 +1005,10 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
   p.n_queries = n_queries;
   p.per = pl.per;
   p.rows = pl.rows;
-  p.splits = pl.splits;
   p.row_groups = pl.row_groups;
-  p.chunk = pl.chunk;
   p.row_span = 16 * pl.tiles;
-  p.weigh_chunk = pl.weigh_chunk;
+  p.workgroups = pl.workgroups;
+  p.weigh_workgroups = pl.weigh_workgroups;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return type == AS_BF16 ? launch_by_shape<AS_BF16>(p, pl, s) : launch_by_shape<AS_F16>(p, pl, s);
 }

@@ -204,20 +204,6 @@ __device__ __forceinline__ int evict_length(const EvictArgs& p, int b) {
 // wavefronts before it give.
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 
-// Sum over the lanes up to and with this one: four steps within rows of 16
-// lanes, then the rows' last lanes to the rows after them.
-__device__ __forceinline__ uint32_t scan_lanes(uint32_t x) {
-#define AS_ADD_DPP(ctrl, rows) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false)
-  AS_ADD_DPP(0x111, 0xf);  // row_shr:1
-  AS_ADD_DPP(0x112, 0xf);
-  AS_ADD_DPP(0x114, 0xf);
-  AS_ADD_DPP(0x118, 0xf);
-  AS_ADD_DPP(0x142, 0xa);  // row_bcast:15
-  AS_ADD_DPP(0x143, 0xc);  // row_bcast:31
-#undef AS_ADD_DPP
-  return x;
-}
-
 // Exclusive sum over the workgroup of one number a thread; total: of all.
 __device__ __forceinline__ uint32_t scan_threads(uint32_t x, uint32_t* waves, uint32_t& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

@@ -57,6 +57,20 @@ __device__ __forceinline__ float sum_over_rows(float x) {
   return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
+// Sum over the lanes up to and with this one: four steps within rows of 16
+// lanes, then the rows' last lanes to the rows after them.
+__device__ __forceinline__ uint32_t scan_lanes(uint32_t x) {
+#define AS_ADD_DPP(ctrl, rows) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false)
+  AS_ADD_DPP(0x111, 0xf);  // row_shr:1
+  AS_ADD_DPP(0x112, 0xf);
+  AS_ADD_DPP(0x114, 0xf);
+  AS_ADD_DPP(0x118, 0xf);
+  AS_ADD_DPP(0x142, 0xa);  // row_bcast:15
+  AS_ADD_DPP(0x143, 0xc);  // row_bcast:31
+#undef AS_ADD_DPP
+  return x;
+}
+
 __host__ __device__ __forceinline__ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 inline bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
