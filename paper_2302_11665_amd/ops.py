@@ -141,10 +141,12 @@ def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
     if x2.stride(1) != 1 and w.n_in > 1:
         x2 = x2.contiguous()
     t = x2.shape[0]
-    _need(w.codes, "weight codes", (torch.int8, torch.uint8), device=dev)
-    _need(w.scale, "weight scale", (torch.float32,), device=dev)
-    if w.codes.numel() != L.as_i8_bytes(w.n_out, w.n_in) or w.scale.numel() != w.n_out:
-        _bad(f"linear_i8: {w.codes.numel()} codes and {w.scale.numel()} scales for {w.n_out} x {w.n_in} weights")
+    codes, scale = w.codes, w.scale
+    if not (codes.device == scale.device == dev and codes.dtype in (torch.int8, torch.uint8)
+            and scale.dtype is torch.float32 and codes.is_contiguous() and scale.is_contiguous()
+            and codes.numel() == L.as_i8_bytes(w.n_out, w.n_in) and scale.numel() == w.n_out):
+        _bad(f"linear_i8: {codes.numel()} codes {codes.dtype} on {codes.device} and {scale.numel()} scales for "
+             f"{w.n_out} x {w.n_in} weights")
     if bias is not None and _need(bias, "bias", (torch.float32,), device=dev).numel() != w.n_out:
         _bad(f"linear_i8: {bias.numel()} biases for {w.n_out} outputs")
     if out is None:
@@ -181,29 +183,33 @@ class Cache:
     page_table: torch.Tensor
 
     def __post_init__(self):
-        dev = self.k.device
-        i32 = (torch.int32,)
-        _need(self.k, "cache.k", i32, 5)
-        _need(self.v, "cache.v", i32, 6, dev)
-        pages, heads, page, four, words = self.k.shape
-        dim = words * 32
-        _need(self.k_par, "cache.k_par", (torch.float16,), 5, dev)
-        _need(self.v_par, "cache.v_par", (torch.float16,), 5, dev)
-        groups = self.k_par.shape[2]
-        want = (pages, heads, groups, page, 2)
-        if four != 4 or groups < 1 or tuple(self.k_par.shape) != want or tuple(self.v_par.shape) != want or tuple(
-                self.v.shape) != (pages, heads, page // 32, 4, 16, dim // 16) or page % 32 or dim % groups:
-            _bad(f"cache: arrays of {tuple(self.k.shape)}, {tuple(self.v.shape)}, {tuple(self.k_par.shape)} and "
-                 f"{tuple(self.v_par.shape)} do not belong together")
-        for name, x, kind in (("pos", self.pos, torch.int32), ("acc", self.acc, torch.float32)):
-            if x is not None and tuple(_need(x, "cache." + name, (kind,), 3, dev).shape) != (pages, heads, page):
-                _bad(f"cache.{name}: {tuple(x.shape)}")
-        _need(self.page_table, "cache.page_table", i32, 2, dev)
-        ptr = lambda x: None if x is None else x.data_ptr()  # noqa: E731
-        self._c = as_cache_t(pages, heads, dim, dim // groups, page, self.page_table.shape[0],
-                             self.page_table.shape[1], 0, self.k.data_ptr(), self.v.data_ptr(),
-                             self.k_par.data_ptr(), self.v_par.data_ptr(), ptr(self.pos), ptr(self.acc),
-                             self.page_table.data_ptr())
+        # one cheap look at everything first: a step may make its handles anew
+        k, v, kp, vp, pos, acc, table = self.k, self.v, self.k_par, self.v_par, self.pos, self.acc, self.page_table
+        try:
+            pages, heads, page, four, words = k.shape
+            groups = kp.shape[2]
+            rows, par = (pages, heads, page), (pages, heads, groups, page, 2)
+            dev, i32 = k.device, torch.int32
+            dim = words * 32
+            fine = (k.is_cuda and k.dtype is i32 and v.dtype is i32 and kp.dtype is vp.dtype is torch.float16
+                    and table.dtype is i32 and four == 4 and kp.shape == par and vp.shape == par
+                    and v.shape == (pages, heads, page // 32, 4, 16, words * 2) and page % 32 == 0
+                    and dim % groups == 0 and table.dim() == 2 and k.is_contiguous() and v.is_contiguous()
+                    and kp.is_contiguous() and vp.is_contiguous() and table.is_contiguous()
+                    and v.device == kp.device == vp.device == table.device == dev
+                    and (pos is None or (pos.shape == rows and pos.dtype is i32 and pos.is_contiguous()
+                                         and pos.device == dev))
+                    and (acc is None or (acc.shape == rows and acc.dtype is torch.float32 and acc.is_contiguous()
+                                         and acc.device == dev)))
+        except (AttributeError, ValueError, IndexError, ZeroDivisionError):
+            fine = False
+        if not fine:
+            what = [None if x is None else (tuple(x.shape), x.dtype, str(x.device)) if isinstance(x, torch.Tensor)
+                    else type(x) for x in (k, v, kp, vp, pos, acc, table)]
+            _bad(f"cache: contiguous CUDA arrays of one cache are needed, not {what}")
+        self._c = as_cache_t(pages, heads, dim, dim // groups, page, table.shape[0], table.shape[1], 0, k.data_ptr(),
+                             v.data_ptr(), kp.data_ptr(), vp.data_ptr(), None if pos is None else pos.data_ptr(),
+                             None if acc is None else acc.data_ptr(), table.data_ptr())
 
     @staticmethod
     def empty(n_pages, n_heads, dim, page_table, group=64, page=64, device="cuda") -> "Cache":
@@ -224,18 +230,19 @@ class Cache:
 
 
 def _counts(x, name, cache):
-    if _need(x, name, (torch.int32,), 1, cache.k.device).shape[0] != cache._c.n_seqs:
-        _bad(f"{name}: {x.shape[0]} entries for {cache._c.n_seqs} sequences")
+    if not (x.dtype is torch.int32 and x.shape == (cache._c.n_seqs,) and x.device == cache.k.device
+            and x.is_contiguous()):
+        _bad(f"{name}: {tuple(x.shape)} {x.dtype} on {x.device} for {cache._c.n_seqs} sequences (int32)")
     return x.data_ptr()
 
 
 def _tokens(x, name, cache, heads):
     """x [seqs, tokens, heads, dim] with its last two dimensions contiguous."""
-    _need(x, name, _16, 4, cache.k.device, contiguous=False)
-    if x.shape[0] != cache._c.n_seqs or x.shape[3] != cache._c.dim or (heads and x.shape[2] != heads):
-        _bad(f"{name}: {tuple(x.shape)}")
-    dim = x.shape[3]
-    if x.stride(3) != 1 or (x.shape[2] > 1 and x.stride(2) != dim):
+    c = cache._c
+    if x.dim() != 4 or x.dtype not in _16 or x.device != cache.k.device or x.shape[0] != c.n_seqs or x.shape[
+            3] != c.dim or (heads and x.shape[2] != heads):
+        _bad(f"{name}: {tuple(x.shape)} {x.dtype} on {x.device}")
+    if not x.is_contiguous() and (x.stride(3) != 1 or (x.shape[2] > 1 and x.stride(2) != c.dim)):
         x = x.contiguous()
     return x
 
@@ -251,8 +258,10 @@ def cache_append(cache: Cache, k, v, start, first_pos=None, held=False):
         _bad(f"cache_append: k has {tuple(k.shape)} {k.dtype}, v {tuple(v.shape)} {v.dtype}")
     at = _counts(start, "start", cache)
     pos = None if first_pos is None else _counts(first_pos, "first_pos", cache)
-    hk = torch.empty(k.shape, dtype=torch.float32, device=k.device) if held else None
-    hv = torch.empty(k.shape, dtype=torch.float32, device=k.device) if held else None
+    hk = hv = None
+    if held:
+        hk = torch.empty_like(k, dtype=torch.float32, memory_format=torch.contiguous_format)
+        hv = torch.empty_like(hk)
     _call(lib().as_cache_append, k.device, cache._c, k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], k.shape[1],
           k.stride(0), k.stride(1), v.stride(0), v.stride(1), at, pos, hk.data_ptr() if held else None,
           hv.data_ptr() if held else None)
@@ -272,13 +281,15 @@ def attention_kv4(q, cache: Cache, length, scale=None, acc_in=None, acc_out=None
             q = q.clone(memory_format=torch.contiguous_format)
     n = _counts(length, "length", cache)
     c = cache._c
-    rows = (c.n_pages, c.n_heads, c.page)
-    for name, x in (("acc_in", acc_in), ("acc_out", acc_out)):
-        if x is not None and tuple(_need(x, name, (torch.float32,), 3, q.device).shape) != rows:
-            _bad(f"{name}: {tuple(x.shape)}")
-    if acc_in is not None and acc_out is None:
+    if acc_out is not None:
+        rows = (c.n_pages, c.n_heads, c.page)
+        for name, x in (("acc_in", acc_in), ("acc_out", acc_out)):
+            if x is not None and (x.shape != rows or x.dtype is not torch.float32 or x.device != q.device
+                                  or not x.is_contiguous()):
+                _bad(f"{name}: {tuple(x.shape)} {x.dtype} on {x.device}")
+    elif acc_in is not None:
         _bad("attention_kv4: acc_in without acc_out")
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    out = torch.empty_like(q, memory_format=torch.contiguous_format)
     heads = q.shape[2]
     L = lib()
     need = L.as_attention_kv4_workspace(c, q.shape[1], heads, 0 if acc_out is None else 1)
