@@ -508,12 +508,12 @@ __device__ __forceinline__ void store_row_ml(const AttArgs& p, int b, int h, int
 
 constexpr int kStages = 2;
 template <int DIM, int GROUP>
-constexpr int attend_lds() {
+constexpr int attend_lds(int waves) {
   constexpr int ring = kStages * Stage<DIM, GROUP, true>::kBytes, part = 16 * (DIM + 4) * 4;
-  return kWaves * (ring > part ? ring : part);
+  return waves * (ring > part ? ring : part);
 }
 
-template <int TYPE, int DIM, int GROUP, int NT>
+template <int TYPE, int DIM, int GROUP, int NT, int NW>
 __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& s, int take, int share, int lane,
                                                int wave, uint8_t* lds, float (*ml)[16][2]) {
   constexpr int NG = DIM / GROUP;
@@ -542,21 +542,21 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
   uint32_t valid = 0;  // bit j: the block j turns on has a page
 #pragma unroll
   for (int j = 0; j < kStages; ++j) {
-    if (blk + j * kWaves >= end) break;
+    if (blk + j * NW >= end) break;
     int at;
-    const int64_t row = block_row(p, b, h, blk + j * kWaves, at);
+    const int64_t row = block_row(p, b, h, blk + j * NW, at);
     valid |= (uint32_t)(row >= 0) << j;
     if (p.c.n_pages > 0) S::bring(p, row, at, lane, ring + j * S::kBytes);
   }
   int slot = 0;
   // Blocks up to `to`, all of one kind.
   auto blocks = [&](int to, auto ragged) {
-    for (; blk < to; blk += kWaves) {
+    for (; blk < to; blk += NW) {
       int at = 0;
       int64_t row = -1;
-      const bool more = blk + kStages * kWaves < end;
-      if (more) row = block_row(p, b, h, blk + kStages * kWaves, at);
-      if (blk + (kStages - 1) * kWaves < end)
+      const bool more = blk + kStages * NW < end;
+      if (more) row = block_row(p, b, h, blk + kStages * NW, at);
+      if (blk + (kStages - 1) * NW < end)
         wait_loads<(kStages - 1) * S::kLoads>();
       else
         wait_loads<0>();
@@ -575,7 +575,7 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
   blocks(end, std::true_type());
 
   // Join the wavefronts, 16 rows at a time.
-  float* part = reinterpret_cast<float*>(lds);  // [kWaves][16][DIM + 4]
+  float* part = reinterpret_cast<float*>(lds);  // [NW][16][DIM + 4]
 #pragma unroll
   for (int u = 0; u < NT; ++u) {
     const float total = sum_over_rows(a.sum[u]);
@@ -587,7 +587,7 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
     __syncthreads();
     float m = kFloor;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[w][lane & 15][0]);
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, ml[w][lane & 15][0]);
     const float f = __builtin_amdgcn_exp2f(a.mref[u] - m);
     float add[NG];
 #pragma unroll
@@ -597,19 +597,19 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
       *reinterpret_cast<v4f*>(part + (wave * 16 + (lane & 15)) * (DIM + 4) + 16 * i + (lane >> 4) * 4) =
           (a.o[u][i] + add[i * 16 / GROUP]) * f;
     __syncthreads();
-    for (int j = threadIdx.x; j < 16 * DIM / 4; j += 64 * kWaves) {
+    for (int j = threadIdx.x; j < 16 * DIM / 4; j += 64 * NW) {
       const int r = j / (DIM / 4), d = j % (DIM / 4) * 4;
       const int row = row0 + 16 * u + r;
       if (row >= p.rows) continue;
       v4f x = {0, 0, 0, 0};
       float top = kFloor, l = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < NW; ++w) {
         x += *reinterpret_cast<const v4f*>(part + (w * 16 + r) * (DIM + 4) + d);
         top = fmaxf(top, ml[w][r][0]);
       }
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) l += ml[w][r][1] * __builtin_amdgcn_exp2f(ml[w][r][0] - top);
+      for (int w = 0; w < NW; ++w) l += ml[w][r][1] * __builtin_amdgcn_exp2f(ml[w][r][0] - top);
       if (take == s.seen) {
         store_row<TYPE>(p, out_index(p, b, h, row, DIM) + d, x, l);
         if (p.row_ml && d == 0) store_row_ml(p, b, h, row, top, l);
@@ -641,7 +641,7 @@ __global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : 2) - (DIM == 4 * GROUP)
   Segment g = locate<false>(p, unit, lane, first);
   for (;;) {
     const int take = min(left, g.seen - g.blk);
-    attend_segment<TYPE, DIM, GROUP, NT>(p, g, take, (int)share, lane, wave, lds, ml);
+    attend_segment<TYPE, DIM, GROUP, NT, kWaves>(p, g, take, (int)share, lane, wave, lds, ml);
     left -= take;
     if (left == 0) return;
     advance<false>(p, g);
@@ -731,7 +731,7 @@ __global__ __launch_bounds__(256) void join(AttArgs p) {
 // sum over the queries stays in the lane but for two steps across rows of lanes.
 constexpr int kWeighStages = 3;
 
-template <int TYPE, int DIM, int GROUP>
+template <int TYPE, int DIM, int GROUP, int NW>
 __device__ __forceinline__ void weigh_segment(const AttArgs& p, const Segment& s, int take, int lane, int wave,
                                               uint8_t* lds) {
   constexpr int NG = DIM / GROUP;
@@ -756,8 +756,8 @@ __device__ __forceinline__ void weigh_segment(const AttArgs& p, const Segment& s
 #pragma unroll
   for (int j = 0; j < kWeighStages; ++j) {
     rows[j] = -1;
-    if (blk + j * kWaves >= end) continue;
-    rows[j] = block_row(p, b, h, blk + j * kWaves, places[j]);
+    if (blk + j * NW >= end) continue;
+    rows[j] = block_row(p, b, h, blk + j * NW, places[j]);
     if (p.c.n_pages > 0) bring(j);
   }
   // Queries r0.. : the operand, and of the lane's four rows 4 g + r the sums
@@ -793,10 +793,10 @@ __device__ __forceinline__ void weigh_segment(const AttArgs& p, const Segment& s
       if (blk >= end) break;
       const int64_t here = rows[z];
       const int place = places[z];
-      const bool more = blk + kWeighStages * kWaves < end;
-      if (more) rows[z] = block_row(p, b, h, blk + kWeighStages * kWaves, places[z]);
+      const bool more = blk + kWeighStages * NW < end;
+      if (more) rows[z] = block_row(p, b, h, blk + kWeighStages * NW, places[z]);
       // (a store of weights after those loads only makes this wait longer)
-      if (blk + (kWeighStages - 1) * kWaves < end)
+      if (blk + (kWeighStages - 1) * NW < end)
         wait_loads<(kWeighStages - 1) * (S::kLoads + 1)>();
       else
         wait_loads<0>();
@@ -853,7 +853,7 @@ __device__ __forceinline__ void weigh_segment(const AttArgs& p, const Segment& s
         const int place_s = place + (lane & 31);
         if (lane < 32 && blk * 32 + (lane & 31) < n) p.acc_out[here * p.c.page + place_s] = (p.acc_in ? was : 0.0f) + x;
       }
-      blk += kWaves;
+      blk += NW;
     }
   }
 }
@@ -872,17 +872,52 @@ __global__ __launch_bounds__(64 * kWaves, 3) void weigh(AttArgs p) {
   Segment g = locate<true>(p, unit, lane, first);
   for (;;) {
     const int take = min(left, g.seen - g.blk);
-    weigh_segment<TYPE, DIM, GROUP>(p, g, take, lane, wave, lds);
+    weigh_segment<TYPE, DIM, GROUP, kWaves>(p, g, take, lane, wave, lds);
     left -= take;
     if (left == 0) return;
     advance<true>(p, g);
   }
 }
 
+// Short sequences: a workgroup of more wavefronts has a whole segment, so that
+// nothing is left to be joined, and the weights too, where all rows are in one
+// segment: one launch, where a launch costs more than the work.
+template <int DIM, int GROUP, int NT>
+constexpr int whole_waves() {
+  return NT == 1 && DIM < 4 * GROUP ? 16 : 8;  // as many as their registers allow
+}
+
+template <int TYPE, int DIM, int GROUP, int NT, int NW>
+__global__ __launch_bounds__(64 * NW) void attend_whole(AttArgs p) {
+  __shared__ float ml[NW][16][2];
+  extern __shared__ __align__(16) uint8_t lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Segment s;
+  const int bh = blockIdx.x / p.row_groups;
+  s.rg = blockIdx.x % p.row_groups;
+  s.b = bh / p.c.n_heads, s.h = bh % p.c.n_heads;
+  s.n = clamped_length(p, s.b);
+  s.blk = 0;
+  int least;
+  s.seen = seen_blocks(p, s.n, s.rg, least);
+  attend_segment<TYPE, DIM, GROUP, NT, NW>(p, s, s.seen, 0, lane, wave, lds, ml);
+  if (!p.acc_out) return;
+  s.seen = (s.n + 31) / 32;
+  weigh_segment<TYPE, DIM, GROUP, NW>(p, s, s.seen, lane, wave, lds);
+}
+
 struct Plan {
+  bool whole;
   int per, rows, tiles, row_groups, workgroups, weigh_workgroups;
   int64_t o_bytes, ml_bytes, row_bytes;
 };
+
+// Tables of up to so many blocks, with a compute unit for each segment, go to
+// attend_whole.  One compute unit works 0.2 us at a block: 12 heads of up to 60
+// blocks with weights took 17 us on the device there, 17 us in three launches
+// otherwise, and 22 us a step against 35; 8 heads of 129 blocks 28 us there and
+// 14 us in shares.
+constexpr int kWholeBlocks = 64;
 
 // Workgroups that a compute unit runs at once: the launch bounds of the kernels.
 Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) {
@@ -894,6 +929,8 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   const int64_t heads = (int64_t)c->n_seqs * c->n_heads;
   const int64_t blocks = (int64_t)c->max_pages * c->page / 32;
   const int wide = c->dim == 4 * c->group;
+  pl.whole = blocks <= kWholeBlocks && heads * pl.row_groups <= as_host::compute_units() &&
+             (!weights || pl.row_groups == 1);
   auto groups = [&](int64_t all, int64_t resident) {
     const int64_t g = all < resident ? all : resident;
     return (int)round_up(g < 1 ? 1 : g, 8);
@@ -903,8 +940,8 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   pl.workgroups = groups(heads * pl.row_groups * blocks, (int64_t)cus * ((pl.tiles == 1 ? 4 : 2) - wide));
   pl.weigh_workgroups = groups(heads * blocks, (int64_t)cus * 3);
   const int64_t parts = (int64_t)pl.workgroups * 2 * 16 * pl.tiles;
-  pl.o_bytes = round_up(parts * c->dim * 4, 256);
-  pl.ml_bytes = round_up(parts * 8, 256);
+  pl.o_bytes = pl.whole ? 0 : round_up(parts * c->dim * 4, 256);
+  pl.ml_bytes = pl.whole ? 0 : round_up(parts * 8, 256);
   pl.row_bytes = weights ? round_up(heads * pl.rows * 8, 256) : 0;
   return pl;
 }
@@ -926,10 +963,26 @@ int check_queries(const as_cache_t* c, int32_t n_queries, int32_t n_q_heads) {
   return AS_OK;
 }
 
+template <int TYPE, int DIM, int GROUP, int NT>
+int launch_whole(const AttArgs& p, hipStream_t s) {
+  constexpr int NW = whole_waves<DIM, GROUP, NT>();
+  typedef Stage<DIM, GROUP, false> KeyStage;
+  size_t lds = attend_lds<DIM, GROUP>(NW);
+  const size_t weigh_lds = (size_t)NW * kWeighStages * (KeyStage::kBytes + 128);
+  if (p.acc_out && weigh_lds > lds) lds = weigh_lds;
+  const int rc = allow_lds<&attend_whole<TYPE, DIM, GROUP, NT, NW>>(lds, "attention_kv4");
+  if (rc != AS_OK) return rc;
+  hipLaunchKernelGGL((attend_whole<TYPE, DIM, GROUP, NT, NW>),
+                     dim3((unsigned)(p.c.n_seqs * p.c.n_heads * p.row_groups)), dim3(64 * NW), lds, s, p);
+  return launched("attention_kv4");
+}
+
 template <int TYPE, int DIM, int GROUP>
 int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
+  if (pl.whole)
+    return pl.tiles == 1 ? launch_whole<TYPE, DIM, GROUP, 1>(p, s) : launch_whole<TYPE, DIM, GROUP, 2>(p, s);
   const dim3 g((unsigned)pl.workgroups), t(64 * kWaves);
-  const size_t lds = attend_lds<DIM, GROUP>();
+  const size_t lds = attend_lds<DIM, GROUP>(kWaves);
   if (pl.tiles == 1)
     hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 1>), g, t, lds, s, p);
   else

@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "alpaserve_ops.h"
 #include "sim_internal.hpp"
 
@@ -80,6 +82,22 @@ inline int launched(const char* what) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return as_host::fail(AS_E_HIP, "%s: kernel launch failed: %s", what, hipGetErrorString(e));
   return as_host::ok();
+}
+
+// Lets a kernel have more than 64 KiB of LDS; once on each device (F is one
+// kernel's type and address, so the flags are its own).
+template <auto F>
+int allow_lds(size_t bytes, const char* what) {
+  static std::atomic<uint64_t> done{0};
+  if (bytes <= 64 * 1024) return AS_OK;
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev > 63) dev = 63;
+  if (done.load(std::memory_order_relaxed) >> dev & 1) return AS_OK;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(F), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           156 * 1024);  // of 160: 4 KiB for static arrays
+  if (e != hipSuccess) return as_host::fail(AS_E_HIP, "%s: %s", what, hipGetErrorString(e));
+  if (dev < 63) done.fetch_or((uint64_t)1 << dev, std::memory_order_relaxed);
+  return AS_OK;
 }
 
 // Checks of a cache's sizes and pointers; AS_OK or the error recorded.

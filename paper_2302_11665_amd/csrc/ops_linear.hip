@@ -5,8 +5,6 @@
 // takes them: a tile of 16 rows x 64 columns is 1 KiB in which lane l's 16
 // bytes (row l%16, columns 16 (l/16)..+15) lie at 16 l, so a wavefront's load of
 // an operand is one contiguous KiB.
-#include <atomic>
-
 #include "ops_common.hpp"
 
 using as_host::fail;
@@ -401,27 +399,11 @@ __global__ __launch_bounds__(64 * WC * WT) void product_many(LinArgs p) {
   }
 }
 
-// Lets a kernel have more than 64 KiB of LDS; once on each device (F is one
-// kernel's type and address, so the flags are its own).
-template <auto F>
-int allow_lds(size_t bytes) {
-  static std::atomic<uint64_t> done{0};
-  if (bytes <= 64 * 1024) return AS_OK;
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev > 63) dev = 63;
-  if (done.load(std::memory_order_relaxed) >> dev & 1) return AS_OK;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(F), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                           160 * 1024);
-  if (e != hipSuccess) return fail(AS_E_HIP, "linear_i8: %s", hipGetErrorString(e));
-  if (dev < 63) done.fetch_or((uint64_t)1 << dev, std::memory_order_relaxed);
-  return AS_OK;
-}
-
 template <int YTYPE, int TC, int TT, int WC, int WT>
 int launch_many(const LinArgs& p, hipStream_t s) {
   const int64_t gc = ((p.n_out + 15) / 16 + TC - 1) / TC, gt = ((p.n_tokens + 15) / 16 + TT - 1) / TT;
   const size_t lds = (size_t)2 * (TC + TT) * 2 * 1024;
-  const int rc = allow_lds<&product_many<YTYPE, TC, TT, WC, WT>>(lds);
+  const int rc = allow_lds<&product_many<YTYPE, TC, TT, WC, WT>>(lds, "linear_i8");
   if (rc != AS_OK) return rc;
   hipLaunchKernelGGL((product_many<YTYPE, TC, TT, WC, WT>), dim3((unsigned)(gc * gt)), dim3(64 * WC * WT), lds, s, p);
   return launched("linear_i8");
@@ -432,7 +414,7 @@ int launch_few(const LinArgs& p, hipStream_t s) {
   const int n_ct = (p.n_out + 15) / 16;
   size_t lds = (size_t)TT * CT * 1024 + 64;
   if (FUSED) lds += (size_t)p.n_tokens * (p.k_tiles * 64 + 16);
-  const int rc = allow_lds<&product_few<YTYPE, XTYPE, CT, TT, FUSED>>(lds);
+  const int rc = allow_lds<&product_few<YTYPE, XTYPE, CT, TT, FUSED>>(lds, "linear_i8");
   if (rc != AS_OK) return rc;
   hipLaunchKernelGGL((product_few<YTYPE, XTYPE, CT, TT, FUSED>), dim3((unsigned)((n_ct + CT - 1) / CT)),
                      dim3(64 * kFewWaves), lds, s, p);

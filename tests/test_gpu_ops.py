@@ -211,6 +211,21 @@ ATTEND = [
 ]
 
 
+# Tables too long, or heads too many, for one workgroup to a head: the slots
+# are dealt out in shares.
+ATTEND += [
+    ([5200], 1, 8, 2, 64, 32, 32),
+    ([6000, 0, 1, 5300, 33], 1, 16, 2, 128, 64, 64),
+    ([40, 7000], 1, 5, 1, 128, 128, 96),
+    ([5500, 3, 90], 4, 6, 2, 64, 64, 128),
+    ([5400, 60], 25, 2, 1, 128, 32, 64),       # 50 rows, several groups
+    ([1500, 5200], 70, 3, 3, 64, 64, 32),
+    ([31 + 7 * i for i in range(70)], 1, 4, 4, 64, 64, 32),  # more than 64 sequences
+    ([0] * 66 + [100, 0, 0, 64], 2, 8, 4, 128, 64, 32),
+    ([20] * 90, 20, 6, 3, 64, 32, 32),
+]
+
+
 @pytest.mark.parametrize("case", ATTEND, ids=[str(i) for i in range(len(ATTEND))])
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("weights", [False, True])
