@@ -173,21 +173,6 @@ struct Stage {
   }
 };
 
-// Wait until at most N of the wavefront's loads are on their way; what is read
-// from LDS afterwards is read afterwards.
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-  static_assert(N < 64, "six bits");
-  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
-  asm volatile("" ::: "memory");
-}
-// Wait for the wavefront's LDS reads: their place may be written again.
-__device__ __forceinline__ void wait_reads() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0), nothing else
-  asm volatile("" ::: "memory");
-}
-
 // Sixteen queries as the second operand of K q^T: lane's channels 32 i + 8 g +
 // 0..7 of query row lane % 16; the sums over each group's channels.
 template <int TYPE, int DIM, int GROUP>

@@ -73,6 +73,21 @@ __device__ __forceinline__ uint32_t scan_lanes(uint32_t x) {
   return x;
 }
 
+// Wait until at most N of the wavefront's loads are on their way; what is read
+// from LDS afterwards is read afterwards.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "six bits");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
+  asm volatile("" ::: "memory");
+}
+// Wait for the wavefront's LDS reads: their place may be written again.
+__device__ __forceinline__ void wait_reads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0), nothing else
+  asm volatile("" ::: "memory");
+}
+
 __host__ __device__ __forceinline__ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 inline bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }

@@ -21,24 +21,26 @@ __device__ __forceinline__ float load_one(const void* x, int64_t i) {
   return to_f32<TYPE>(reinterpret_cast<const uint16_t*>(x)[i]);
 }
 
-// 16 values from column c of a row; columns beyond n_cols are 0.  VEC: the row
-// is aligned to 16 bytes.
-template <int TYPE, bool VEC>
+// 16 values from column c of a row; columns beyond n_cols are 0.  Rows may start
+// anywhere: memory takes unaligned loads of 16 bytes.
+template <int TYPE>
 __device__ __forceinline__ void load16(const void* x, int64_t row, int64_t c, int64_t n_cols, float (&f)[16]) {
-  if (VEC && c + 16 <= n_cols) {
+  if (c + 16 <= n_cols) {
     if (TYPE == AS_F32) {
-      const v4f* p = reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(x) + row + c);
+      const float* p = reinterpret_cast<const float*>(x) + row + c;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const v4f v = p[i];
+        v4f v;
+        __builtin_memcpy(&v, p + 4 * i, 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j) f[4 * i + j] = v[j];
       }
     } else {
-      const v4u* p = reinterpret_cast<const v4u*>(reinterpret_cast<const uint16_t*>(x) + row + c);
+      const uint16_t* p = reinterpret_cast<const uint16_t*>(x) + row + c;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const v4u v = p[i];
+        v4u v;
+        __builtin_memcpy(&v, p + 8 * i, 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           f[8 * i + 2 * j] = to_f32<TYPE>(v[j] & 0xffffu);
@@ -56,37 +58,49 @@ __device__ __forceinline__ void load16(const void* x, int64_t row, int64_t c, in
 // them, so that one integer maximum finds both.
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// Codes of the N values of one row whose largest magnitude is top.  127 x is
-// exact for 16-bit x, and its quotient by top cannot round to a tie that it is
-// not, so rint(127 x / top) is the code of exact arithmetic.  The quotient is
-// first taken with a reciprocal; the remainder 127 x - code * top, exact in one
-// fma, shows whether the code is the nearest, and where a remainder is half of
-// top or more (a tie, or a reciprocal that misled) all N are divided.
-template <int N>
-__device__ __forceinline__ void codes_of(const float (&f)[N], float top, float inv, uint32_t (&out)[N / 4]) {
-  float q[N], worst = 0.0f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    q[i] = rintf(f[i] * inv);
-    worst = fmaxf(worst, fabsf(fmaf(-q[i], top, f[i] * 127.0f)));
+// How a row is quantised, from its largest magnitude.  A power of two takes
+// rows of very large or small numbers away from the ends of fp32's range.
+template <int TYPE>
+struct Quantiser {
+  float by, top, inv;  // 127 and the largest magnitude, scaled; 1 / top
+  bool none;           // all codes are 0
+  __device__ __forceinline__ Quantiser(float a, bool finite) {
+    none = !finite || a == 0.0f;
+    const float scale = a > 0x1p100f ? 0x1p-64f : a < 0x1p-64f ? 0x1p64f : 1.0f;
+    by = 127.0f * scale;
+    top = none ? 1.0f : a * scale;
+    inv = 1.0f / top;
   }
-  if (!(worst + worst < top)) {
+  // Codes of four values.  127 x is exact for 16-bit x.  Its quotient by top is
+  // taken with the reciprocal and corrected once by the exact remainder: off by
+  // 2^-46 of itself before the last rounding, so a quotient that ties between
+  // two codes comes out exactly, and no other one can reach a tie (the nearest
+  // is 2^-19 away).  The codes are therefore those of exact arithmetic.  fp32
+  // values are divided.  Adding 1.5 * 2^23 rounds to whole numbers, ties to
+  // even, and leaves the code in the low byte.
+  __device__ __forceinline__ uint32_t codes4(const float* f) const {
+    uint32_t u[4];
 #pragma unroll
-    for (int i = 0; i < N; ++i) q[i] = rintf(f[i] * 127.0f / top);
+    for (int i = 0; i < 4; ++i) {
+      const float x = f[i] * by;
+      float q;
+      if (TYPE == AS_F32) {
+        q = x / top;
+      } else {
+        q = x * inv;
+        q = fmaf(fmaf(-q, top, x), inv, q);
+      }
+      u[i] = __float_as_uint(q + 12582912.0f);
+    }
+    const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(u[3], u[2], 0x04000c0cu);
+    return none ? 0u : lo | hi;
   }
-#pragma unroll
-  for (int i = 0; i < N / 4; ++i) {
-    uint32_t w = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w |= ((uint32_t)(int)q[4 * i + j] & 0xffu) << (8 * j);
-    out[i] = w;
-  }
-}
+};
 
 // One workgroup per row: its largest magnitude, then its codes; the second
 // reading comes from the caches.  Bound by latency for few rows, by the bytes
 // of x for many.
-template <int TYPE, bool VEC>
+template <int TYPE>
 __global__ __launch_bounds__(kQThreads) void quantize_rows(const void* __restrict__ x, int64_t n_cols,
                                                            int64_t row_stride, int64_t padded,
                                                            uint8_t* __restrict__ codes, float* __restrict__ scale) {
@@ -96,7 +110,7 @@ __global__ __launch_bounds__(kQThreads) void quantize_rows(const void* __restric
   uint32_t top = 0;
   for (int64_t c = (int64_t)threadIdx.x * 16; c < n_cols; c += kQThreads * 16) {
     float f[16];
-    load16<TYPE, VEC>(x, row, c, n_cols, f);
+    load16<TYPE>(x, row, c, n_cols, f);
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = max(top, magnitude(f[i]));
   }
@@ -107,20 +121,82 @@ __global__ __launch_bounds__(kQThreads) void quantize_rows(const void* __restric
 #pragma unroll
   for (int w = 0; w < kQThreads / 64; ++w) top = max(top, part[w]);
   const bool finite = top < 0x7f800000u;
-  const float a = __uint_as_float(top), inv = 127.0f / a;
+  const float a = __uint_as_float(top);
+  const Quantiser<TYPE> quantiser(a, finite);
   if (threadIdx.x == 0) scale[r] = finite ? a / 127.0f : __builtin_nanf("");
   // byte offset of column c: tiles of 1 KiB, 256 bytes for each 16 columns
   uint8_t* out = codes + (r >> 4) * (padded >> 6) * 1024 + (r & 15) * 16;
   for (int64_t c = (int64_t)threadIdx.x * 16; c < padded; c += kQThreads * 16) {
     v4u q = {0, 0, 0, 0};
-    if (finite && top != 0 && c < n_cols) {
+    if (!quantiser.none && c < n_cols) {
       float f[16];
-      load16<TYPE, VEC>(x, row, c, n_cols, f);
-      uint32_t w[4];
-      codes_of<16>(f, a, inv, w);
-      q = v4u{w[0], w[1], w[2], w[3]};
+      load16<TYPE>(x, row, c, n_cols, f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = quantiser.codes4(f + 4 * i);
     }
     *reinterpret_cast<v4u*>(out + (c >> 4) * 256) = q;
+  }
+}
+
+// Many rows of 16-bit values: a workgroup of 16 wavefronts per 16 rows, a lane of
+// which has 16 columns of one row of every 64 x 16th tile and keeps them in
+// registers, so that x is read once and the codes are written as contiguous
+// tiles.  Bound by the bytes: 4096 rows of 8192 took 47 us with a workgroup per
+// row, 32 us with a wavefront per row, whose codes go out 16 bytes at a time.
+template <int TYPE, int TILES>
+__global__ __launch_bounds__(1024) void quantize_tiles(const uint16_t* __restrict__ x, int64_t n_rows, int n_cols,
+                                                       int64_t row_stride, int k_tiles, uint8_t* __restrict__ codes,
+                                                       float* __restrict__ scale) {
+  __shared__ uint32_t tops[16][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in = lane & 15;
+  const int64_t r = (int64_t)blockIdx.x * 16 + in;
+  const uint16_t* row = x + min(r, n_rows - 1) * row_stride;
+  v4u raw[TILES][2];
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) {
+    const int c = (i * 16 + wave) * 64 + (lane >> 4) * 16;
+    raw[i][0] = raw[i][1] = v4u{0, 0, 0, 0};
+    if (c + 16 <= n_cols) {
+      __builtin_memcpy(&raw[i][0], row + c, 16);
+      __builtin_memcpy(&raw[i][1], row + c + 8, 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (c + e < n_cols) raw[i][e >> 3][(e >> 1) & 3] |= (uint32_t)row[c + e] << (16 * (e & 1));
+    }
+  }
+  // magnitudes of 16-bit values are ordered as their bits without the sign
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < TILES; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t w = raw[i][j >> 2][j & 3] & 0x7fff7fffu;
+      top = max(top, max(w & 0xffffu, w >> 16));
+    }
+  top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+  if (lane < 16) tops[wave][in] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 16; ++w) top = max(top, tops[w][in]);
+  const float a = to_f32<TYPE>(top);
+  const bool finite = top < (TYPE == AS_BF16 ? 0x7f80u : 0x7c00u);
+  const Quantiser<TYPE> quantiser(a, finite);
+  if (threadIdx.x < 16 && r < n_rows) scale[r] = finite ? a / 127.0f : __builtin_nanf("");
+  uint8_t* out = codes + (int64_t)blockIdx.x * k_tiles * 1024 + lane * 16;
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) {
+    const int tile = i * 16 + wave;
+    if (tile >= k_tiles) break;
+    float f[16];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      f[2 * j] = to_f32<TYPE>(raw[i][j >> 2][j & 3] & 0xffffu);
+      f[2 * j + 1] = to_f32<TYPE>(raw[i][j >> 2][j & 3] >> 16);
+    }
+    *reinterpret_cast<v4u*>(out + (int64_t)tile * 1024) =
+        v4u{quantiser.codes4(f), quantiser.codes4(f + 4), quantiser.codes4(f + 8), quantiser.codes4(f + 12)};
   }
 }
 
@@ -128,13 +204,27 @@ template <int TYPE>
 void launch_quantize(const void* x, int64_t rows, int64_t cols, int64_t stride, void* codes, float* scale,
                      hipStream_t s) {
   const int64_t padded = round_up(cols, 128);
-  const int elt = TYPE == AS_F32 ? 4 : 2;
-  const bool vec = aligned(x, 16) && (stride * elt) % 16 == 0;
-  const dim3 g((unsigned)rows), t(kQThreads);
-  if (vec)
-    hipLaunchKernelGGL((quantize_rows<TYPE, true>), g, t, 0, s, x, cols, stride, padded, (uint8_t*)codes, scale);
-  else
-    hipLaunchKernelGGL((quantize_rows<TYPE, false>), g, t, 0, s, x, cols, stride, padded, (uint8_t*)codes, scale);
+  if constexpr (TYPE != AS_F32) {
+    // enough rows for half the compute units, 16 to each; rows that fit the registers
+    if (rows >= 2048 && cols <= 8192) {
+      auto tiles = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 15) / 16)), dim3(1024), 0, s,
+                           reinterpret_cast<const uint16_t*>(x), rows, (int)cols, stride, (int)(padded / 64),
+                           (uint8_t*)codes, scale);
+      };
+      if (cols <= 1024)
+        tiles(quantize_tiles<TYPE, 1>);
+      else if (cols <= 2048)
+        tiles(quantize_tiles<TYPE, 2>);
+      else if (cols <= 4096)
+        tiles(quantize_tiles<TYPE, 4>);
+      else
+        tiles(quantize_tiles<TYPE, 8>);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((quantize_rows<TYPE>), dim3((unsigned)rows), dim3(kQThreads), 0, s, x, cols, stride, padded,
+                     (uint8_t*)codes, scale);
 }
 
 // ------------------------------------------------------------------ product
@@ -153,7 +243,6 @@ struct LinArgs {
   const void* x;
   int64_t x_stride;
   int32_t n_in;
-  bool x_aligned;        // rows aligned to 16 bytes
 };
 
 template <int YTYPE>
@@ -177,9 +266,10 @@ __device__ __forceinline__ void store_four(void* y, int64_t i, const float (&v)[
 
 // 8 values from column c of a row of 16-bit values; columns beyond n are 0.
 template <int TYPE>
-__device__ __forceinline__ void load8(const uint16_t* x, int64_t row, int c, int n, bool vec, float (&f)[8]) {
-  if (vec && c + 8 <= n) {
-    const v4u v = *reinterpret_cast<const v4u*>(x + row + c);
+__device__ __forceinline__ void load8(const uint16_t* x, int64_t row, int c, int n, float (&f)[8]) {
+  if (c + 8 <= n) {
+    v4u v;
+    __builtin_memcpy(&v, x + row + c, 16);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       f[2 * j] = to_f32<TYPE>(v[j] & 0xffffu);
@@ -219,7 +309,7 @@ constexpr int kFewWaves = 8;
 template <int YTYPE, int XTYPE, int CT, int TT, bool FUSED>
 __global__ __launch_bounds__(64 * kFewWaves) void product_few(LinArgs p) {
   extern __shared__ uint8_t lds[];
-  int* sums = reinterpret_cast<int*>(lds);                       // [TT][16 tokens][CT * 16 channels]
+  int* sums = reinterpret_cast<int*>(lds);                       // [TT][CT][4][64], as the lanes have them
   uint32_t* tops = reinterpret_cast<uint32_t*>(sums + TT * CT * 256);  // [16]
   uint8_t* rows = reinterpret_cast<uint8_t*>(tops + 16);         // FUSED: [n_tokens][row_bytes]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -248,7 +338,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few(LinArgs p) {
       uint32_t top = 0;
       for (int c = tid; c < chunks; c += 64 * kFewWaves) {
         float f[8];
-        load8<XTYPE>(x, t * p.x_stride, c * 8, p.n_in, p.x_aligned, f);
+        load8<XTYPE>(x, t * p.x_stride, c * 8, p.n_in, f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = max(top, magnitude(f[i]));
       }
@@ -259,14 +349,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few(LinArgs p) {
     lds_barrier();
     for (int t = 0; t < p.n_tokens; ++t) {
       const uint32_t top = tops[t];
-      const bool zero = top == 0 || top >= 0x7f800000u;
-      const float a = zero ? 1.0f : __uint_as_float(top), inv = 127.0f / a;
+      const Quantiser<XTYPE> quantiser(__uint_as_float(top), top < 0x7f800000u);
       for (int c = tid; c < chunks; c += 64 * kFewWaves) {
         float f[8];
-        load8<XTYPE>(x, t * p.x_stride, c * 8, p.n_in, p.x_aligned, f);
-        uint32_t q[2] = {0, 0};
-        if (!zero) codes_of<8>(f, a, inv, q);
-        *reinterpret_cast<v2u*>(rows + t * row_bytes + c * 8) = v2u{q[0], q[1]};
+        load8<XTYPE>(x, t * p.x_stride, c * 8, p.n_in, f);
+        *reinterpret_cast<v2u*>(rows + t * row_bytes + c * 8) = v2u{quantiser.codes4(f), quantiser.codes4(f + 4)};
       }
     }
   }
@@ -305,7 +392,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few(LinArgs p) {
     for (int i = 0; i < CT; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        atomicAdd(&sums[(u * 16 + (lane & 15)) * (CT * 16) + i * 16 + (lane >> 4) * 4 + r], acc[i][u][r]);
+        atomicAdd(&sums[((u * CT + i) * 4 + r) * 64 + lane], acc[i][u][r]);
   lds_barrier();
   for (int j = tid; j < TT * CT * 256; j += 64 * kFewWaves) {
     const int t = j / (CT * 16), n = ct0 * 16 + j % (CT * 16);
@@ -315,21 +402,24 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few(LinArgs p) {
       s = tops[t] < 0x7f800000u ? __uint_as_float(tops[t]) / 127.0f : __builtin_nanf("");
     else
       s = p.a_scale[t];
-    finish<YTYPE>(p, t, n, sums[j], s);
+    const int i = j / 16 % CT, c = j % 16;  // channel 4 (lane / 16) + r of the tile, token lane % 16
+    finish<YTYPE>(p, t, n, sums[((t / 16 * CT + i) * 4 + (c & 3)) * 64 + (c >> 2) * 16 + (t & 15)], s);
   }
 }
 
 // Many tokens: the matrix rate bounds it.  A workgroup of WC x WT wavefronts takes
-// 16 TC channels x 16 TT tokens, two tiles of 64 columns at a time: they come
-// into one half of LDS straight from memory (a tile is a contiguous KiB there
-// and in LDS, read back without bank conflicts) while the other half is
-// multiplied.  Neighbouring workgroup numbers go to different XCDs, so each XCD
-// gets a contiguous run of tiles in an order that walks the channels in bands
-// of 8: the tiles that run together share rows of both operands in its L2.
-template <int YTYPE, int TC, int TT, int WC, int WT>
+// 16 TC channels x 16 TT tokens, KS tiles of 64 columns at a time: they come
+// into a ring of S stages in LDS straight from memory (a tile is a contiguous KiB
+// there and in LDS, read back without bank conflicts) while older ones are
+// multiplied; one barrier a stage.  Neighbouring workgroup numbers go to different
+// XCDs, so each XCD gets a contiguous run of tiles in an order that walks the
+// channels in bands of 8: the tiles that run together share rows of both
+// operands in its L2.
+template <int YTYPE, int TC, int TT, int WC, int WT, int KS, int S>
 __global__ __launch_bounds__(64 * WC * WT) void product_many(LinArgs p) {
-  constexpr int kW = WC * WT, kC = TC / WC, kT = TT / WT, kStage = (TC + TT) * 2;
-  extern __shared__ uint8_t lds[];  // [2][kStage][1024]
+  constexpr int kW = WC * WT, kC = TC / WC, kT = TT / WT, kStage = (TC + TT) * KS, kLoads = kStage / kW;
+  static_assert(kStage % kW == 0, "every wavefront brings in as many tiles");
+  extern __shared__ uint8_t lds[];  // [S][kStage][1024]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n_ct = (p.n_out + 15) / 16, n_tt = (p.n_tokens + 15) / 16;
   const int gc = (n_ct + TC - 1) / TC, gt = (n_tt + TT - 1) / TT;
@@ -340,39 +430,53 @@ __global__ __launch_bounds__(64 * WC * WT) void product_many(LinArgs p) {
   const int c0 = (band * 8 + in_band % wide) * TC, t0 = in_band / wide * TT;
   const int64_t tile_row = (int64_t)p.k_tiles * 1024;
 
-  // The tiles that this wavefront brings in: i, i + kW, ..
-  auto bring = [&](int half, int k) {
+  // The tiles of a stage that this wavefront brings in: i, i + kW, ..
+  const uint8_t* from[kLoads];
 #pragma unroll
-    for (int j = 0; j < kStage / kW; ++j) {
-      const int i = wave + j * kW, r = i >> 1;
-      const uint8_t* src = r < TC ? p.w + min(c0 + r, n_ct - 1) * tile_row : p.a + min(t0 + r - TC, n_tt - 1) * tile_row;
-      src += (int64_t)(k + (i & 1)) * 1024 + lane * 16;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                       (__attribute__((address_space(3))) void*)(lds + (half * kStage + i) * 1024), 16, 0,
-                                       0);
-    }
+  for (int j = 0; j < kLoads; ++j) {
+    const int i = wave + j * kW, r = i / KS;
+    from[j] = (r < TC ? p.w + min(c0 + r, n_ct - 1) * tile_row : p.a + min(t0 + r - TC, n_tt - 1) * tile_row) +
+              (i % KS) * 1024 + lane * 16;
+  }
+  auto bring = [&](int slot, int k) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)(from[j] + (int64_t)k * 1024),
+          (__attribute__((address_space(3))) void*)(lds + (slot * kStage + wave + j * kW) * 1024), 16, 0, 0);
   };
   const int wc = wave % WC * kC, wt = wave / WC * kT;
   v4i acc[kC][kT] = {};
-  bring(0, 0);
-  __syncthreads();
-  int half = 0;
-  for (int k = 0; k < p.k_tiles; k += 2, half ^= 1) {
-    if (k + 2 < p.k_tiles) bring(half ^ 1, k + 2);
-    const uint8_t* here = lds + half * kStage * 1024 + lane * 16;
+  const int steps = p.k_tiles / KS;
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
+  for (int j = 0; j < S - 1; ++j)
+    if (j < steps) bring(j, j * KS);
+  int slot = 0;
+  for (int i = 0; i < steps; ++i) {
+    // stage i is there for this wavefront, then for all; all are done with i - 1
+    if (i + S - 2 < steps)
+      wait_loads<(S - 2) * kLoads>();
+    else
+      wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int free = slot == 0 ? S - 1 : slot - 1;
+    if (i + S - 1 < steps) bring(free, (i + S - 1) * KS);
+    const uint8_t* here = lds + slot * kStage * 1024 + lane * 16;
+#pragma unroll
+    for (int z = 0; z < KS; ++z) {
       v4i a[kC], b[kT];
 #pragma unroll
-      for (int i = 0; i < kC; ++i) a[i] = *reinterpret_cast<const v4i*>(here + ((wc + i) * 2 + z) * 1024);
+      for (int j = 0; j < kC; ++j) a[j] = *reinterpret_cast<const v4i*>(here + ((wc + j) * KS + z) * 1024);
 #pragma unroll
-      for (int i = 0; i < kT; ++i) b[i] = *reinterpret_cast<const v4i*>(here + ((TC + wt + i) * 2 + z) * 1024);
+      for (int j = 0; j < kT; ++j) b[j] = *reinterpret_cast<const v4i*>(here + ((TC + wt + j) * KS + z) * 1024);
 #pragma unroll
-      for (int i = 0; i < kC; ++i)
+      for (int j = 0; j < kC; ++j)
 #pragma unroll
-        for (int j = 0; j < kT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[j], acc[i][j], 0, 0, 0);
+        for (int u = 0; u < kT; ++u) acc[j][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[j], b[u], acc[j][u], 0, 0, 0);
     }
-    __syncthreads();
+    wait_reads();
+    slot = slot + 1 == S ? 0 : slot + 1;
   }
 #pragma unroll
   for (int j = 0; j < kT; ++j) {
@@ -399,13 +503,13 @@ __global__ __launch_bounds__(64 * WC * WT) void product_many(LinArgs p) {
   }
 }
 
-template <int YTYPE, int TC, int TT, int WC, int WT>
+template <int YTYPE, int TC, int TT, int WC, int WT, int KS, int S>
 int launch_many(const LinArgs& p, hipStream_t s) {
   const int64_t gc = ((p.n_out + 15) / 16 + TC - 1) / TC, gt = ((p.n_tokens + 15) / 16 + TT - 1) / TT;
-  const size_t lds = (size_t)2 * (TC + TT) * 2 * 1024;
-  const int rc = allow_lds<&product_many<YTYPE, TC, TT, WC, WT>>(lds, "linear_i8");
+  const size_t lds = (size_t)S * (TC + TT) * KS * 1024;
+  const int rc = allow_lds<&product_many<YTYPE, TC, TT, WC, WT, KS, S>>(lds, "linear_i8");
   if (rc != AS_OK) return rc;
-  hipLaunchKernelGGL((product_many<YTYPE, TC, TT, WC, WT>), dim3((unsigned)(gc * gt)), dim3(64 * WC * WT), lds, s, p);
+  hipLaunchKernelGGL((product_many<YTYPE, TC, TT, WC, WT, KS, S>), dim3((unsigned)(gc * gt)), dim3(64 * WC * WT), lds, s, p);
   return launched("linear_i8");
 }
 
@@ -426,8 +530,8 @@ int launch_few(const LinArgs& p, hipStream_t s) {
 template <int YTYPE, int XTYPE, int TT, bool FUSED>
 int few_by_channels(const LinArgs& p, hipStream_t s) {
   const int n_ct = (p.n_out + 15) / 16, cus = as_host::compute_units();
-  if (n_ct >= 4 * cus) return launch_few<YTYPE, XTYPE, 4, TT, FUSED>(p, s);
-  if (n_ct >= 2 * cus) return launch_few<YTYPE, XTYPE, 2, TT, FUSED>(p, s);
+  if (n_ct >= 8 * cus) return launch_few<YTYPE, XTYPE, 4, TT, FUSED>(p, s);
+  if (n_ct >= 4 * cus) return launch_few<YTYPE, XTYPE, 2, TT, FUSED>(p, s);
   return launch_few<YTYPE, XTYPE, 1, TT, FUSED>(p, s);
 }
 
@@ -439,9 +543,9 @@ int launch_product(const LinArgs& p, hipStream_t s) {
   if (n_tt == 3) return few_by_channels<YTYPE, AS_BF16, 3, false>(p, s);
   if (n_tt == 4) return few_by_channels<YTYPE, AS_BF16, 4, false>(p, s);
   const int64_t n_ct = (p.n_out + 15) / 16, cus = as_host::compute_units();
-  if (((n_ct + 15) / 16) * ((n_tt + 15) / 16) >= cus) return launch_many<YTYPE, 16, 16, 2, 4>(p, s);
-  if (((n_ct + 7) / 8) * ((n_tt + 7) / 8) >= cus) return launch_many<YTYPE, 8, 8, 2, 2>(p, s);
-  return launch_many<YTYPE, 4, 4, 2, 2>(p, s);
+  if (((n_ct + 15) / 16) * ((n_tt + 15) / 16) >= cus) return launch_many<YTYPE, 16, 16, 2, 4, 2, 2>(p, s);
+  if (((n_ct + 7) / 8) * ((n_tt + 7) / 8) >= cus) return launch_many<YTYPE, 8, 8, 2, 2, 2, 2>(p, s);
+  return launch_many<YTYPE, 4, 4, 2, 2, 2, 4>(p, s);
 }
 
 // Whether the product quantises the activations itself: they fit one tile of
@@ -537,7 +641,6 @@ int as_linear_i8(const void* x, int32_t x_type, int64_t n_tokens, int64_t n_in, 
   p.x = x;
   p.x_stride = x_stride;
   p.n_in = (int32_t)n_in;
-  p.x_aligned = aligned(x, 16) && x_stride % 8 == 0;
   if (fuses(n_tokens, n_in)) return x_type == AS_BF16 ? launch_fused<AS_BF16>(p, y_type, s) : launch_fused<AS_F16>(p, y_type, s);
   if (x_type == AS_BF16)
     launch_quantize<AS_BF16>(x, n_tokens, n_in, x_stride, codes, scale, s);

@@ -63,7 +63,8 @@ def test_quantised_rows(rows, cols, dtype):
 
 LINEAR = [(1, 1, 1), (1, 64, 16), (1, 4096, 1024), (2, 300, 77), (7, 1000, 130), (16, 512, 256), (17, 129, 4097),
           (33, 2048, 96), (64, 1024, 1024), (100, 640, 300), (129, 256, 520), (257, 1500, 777), (1000, 200, 300),
-          (300, 4224, 640)]
+          (300, 4224, 640), (2050, 900, 33), (2049, 1500, 40), (2048, 3001, 24), (2100, 6100, 17), (2060, 8200, 20),
+          (4100, 260, 4200), (2, 9000, 60), (15, 5000, 8500), (64, 130, 9000)]
 
 
 def check_linear(x, w, u, bias, y, y_dtype):
@@ -126,6 +127,31 @@ def test_linear_strides_and_shapes(t):
     z = ops.linear_i8(x.reshape(t, 1, 300), w)
     assert z.shape == (t, 1, 50) and torch.equal(z[:, 0], y[:, :50])
     assert ops.linear_i8(x[:0], w).shape == (0, 50)
+
+
+@pytest.mark.parametrize("t", [3, 40, 2100])
+def test_linear_of_values_at_the_ends_of_the_range(t):
+    """Rows of very large and very small values, subnormal ones too, and rows
+    whose values tie between two codes."""
+    g = gen(t)
+    w = ops.pack_weight(normal(g, 24, 320))
+    codes = w.codes.cpu().numpy()[oo.tile_index(24, 320)]
+    for dtype, sizes in ((BF16, (3e38, 1e37, 1e30, 2e-38, 5e-39, 1e-40)), (F16, (6e4, 1e-4, 3e-6, 6e-8))):
+        for size in sizes:
+            x = (torch.rand(t, 320, device="cuda", generator=g) * 2 - 1) * size
+            x = x.to(dtype)
+            assert np.array_equal(ops.pack_weight(x).codes.cpu().numpy()[oo.tile_index(t, 320)],
+                                  oo.quantise_rows(f64(x))[0])
+            if not 2e-36 < size < 1e35:
+                continue  # scales that are subnormal, sums beyond fp32 once scaled
+            check_linear(x, codes, f64(w.scale), None,
+                         ops.linear_i8(x, w, dtype=F32), F32)
+    x = torch.randint(-254, 255, (t, 320), device="cuda", generator=g)  # codes k + 0.5 where odd
+    x[:, 0] = 254
+    for dtype in (BF16, F16):
+        check_linear(x.to(dtype), codes, f64(w.scale), None, ops.linear_i8(x.to(dtype), w, dtype=F32), F32)
+        check_linear((x * 0.75).to(dtype), codes, f64(w.scale), None,
+                     ops.linear_i8((x * 0.75).to(dtype), w, dtype=F32), F32)
 
 
 # -------------------------------------------------------------------- cache
