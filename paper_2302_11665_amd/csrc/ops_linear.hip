@@ -320,7 +320,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few(LinArgs p) {
   const uint8_t* w[CT];
 #pragma unroll
   for (int i = 0; i < CT; ++i) w[i] = p.w + min(ct0 + i, n_ct - 1) * tile_row + lane * 16;
-  constexpr int kAhead = CT == 1 ? 8 : CT == 2 ? 4 : 2;
+  constexpr int kAhead = CT <= 2 ? 4 : 2;
   v4i first[kAhead][CT];
 #pragma unroll
   for (int j = 0; j < kAhead; ++j)
@@ -334,9 +334,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few(LinArgs p) {
     lds_barrier();
     const int chunks = p.k_tiles * 8;  // of 8 columns
     const uint16_t* x = reinterpret_cast<const uint16_t*>(p.x);
-    for (int t = 0; t < p.n_tokens; ++t) {
+    // One or two tokens: all wavefronts at each.  More: a wavefront to a token,
+    // so that no token waits for another.
+    const bool together = p.n_tokens <= 2;
+    const int from = together ? tid : lane, step = together ? 64 * kFewWaves : 64;
+    for (int t = together ? 0 : wave; t < p.n_tokens; t += together ? 1 : kFewWaves) {
       uint32_t top = 0;
-      for (int c = tid; c < chunks; c += 64 * kFewWaves) {
+#pragma unroll 8
+      for (int c = from; c < chunks; c += step) {
         float f[8];
         load8<XTYPE>(x, t * p.x_stride, c * 8, p.n_in, f);
 #pragma unroll
@@ -347,10 +352,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few(LinArgs p) {
       if (lane == 0) atomicMax(&tops[t], top);
     }
     lds_barrier();
-    for (int t = 0; t < p.n_tokens; ++t) {
+    for (int t = together ? 0 : wave; t < p.n_tokens; t += together ? 1 : kFewWaves) {
       const uint32_t top = tops[t];
       const Quantiser<XTYPE> quantiser(__uint_as_float(top), top < 0x7f800000u);
-      for (int c = tid; c < chunks; c += 64 * kFewWaves) {
+#pragma unroll 4
+      for (int c = from; c < chunks; c += step) {
         float f[8];
         load8<XTYPE>(x, t * p.x_stride, c * 8, p.n_in, f);
         *reinterpret_cast<v2u*>(rows + t * row_bytes + c * 8) = v2u{quantiser.codes4(f), quantiser.codes4(f + 4)};
@@ -544,8 +550,12 @@ int launch_product(const LinArgs& p, hipStream_t s) {
   if (n_tt == 4) return few_by_channels<YTYPE, AS_BF16, 4, false>(p, s);
   const int64_t n_ct = (p.n_out + 15) / 16, cus = as_host::compute_units();
   if (((n_ct + 15) / 16) * ((n_tt + 15) / 16) >= cus) return launch_many<YTYPE, 16, 16, 2, 4, 2, 2>(p, s);
-  if (((n_ct + 7) / 8) * ((n_tt + 7) / 8) >= cus) return launch_many<YTYPE, 8, 8, 2, 2, 2, 2>(p, s);
-  return launch_many<YTYPE, 4, 4, 2, 2, 2, 4>(p, s);
+  if (((n_ct + 7) / 8) * ((n_tt + 7) / 8) >= cus) return launch_many<YTYPE, 8, 8, 2, 4, 2, 2>(p, s);
+  // Two workgroups of either of these run on a compute unit; the smaller tiles
+  // where all of them run at once (333 tokens 1500 -> 2777: 264 tiles of 64 x 64 took
+  // 12.6 us, 484 of 64 x 32 took 9.8).
+  if (((n_ct + 3) / 4) * ((n_tt + 1) / 2) > 2 * cus) return launch_many<YTYPE, 4, 4, 2, 2, 2, 4>(p, s);
+  return launch_many<YTYPE, 4, 2, 4, 1, 2, 6>(p, s);
 }
 
 // Whether the product quantises the activations itself: they fit one tile of
