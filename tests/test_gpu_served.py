@@ -1,0 +1,82 @@
+"""A served block's steps, its caches' cuts, and the placement from its profile."""
+import numpy as np
+import pytest
+
+import oracle
+from oracle import greedy as ogreedy
+from gpu_common import say
+
+pytestmark = pytest.mark.gpu
+
+
+def small(**over):
+    from paper_2302_11665_amd.served import Shape
+    f = dict(layers=2, hidden=256, heads=4, kv_heads=2, dim=64, inner=512, budget=40, slack=24, recent=8, page=32)
+    f.update(over)
+    return Shape(**f)
+
+
+def run(shape, steps, seqs=3):
+    import torch
+    from paper_2302_11665_amd import served
+    block = served.Block(shape, seed=3)
+    caches = served.Caches(shape, seqs)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    outs = []
+    for _ in range(steps):
+        x = torch.randn(seqs, shape.hidden, device="cuda", generator=g).to(torch.bfloat16)
+        outs.append(block.step(x, caches))
+    return torch.stack(outs), caches
+
+
+def positions(caches):
+    """pos [seqs, heads, length] on the host."""
+    table, page = caches.now.page_table.cpu().numpy(), caches.shape.page
+    pos = caches.now.pos.cpu().numpy()
+    slot = np.arange(caches.held)
+    return np.stack([pos[row[slot // page], :, slot % page].T for row in table])
+
+
+def test_caches_are_cut_to_the_budget():
+    shape = small()
+    out, caches = run(shape, 150)
+    say("steps run")
+    import torch
+    assert torch.isfinite(out).all()
+    assert caches.length.tolist() == [caches.held] * 3 and caches.total.tolist() == [150] * 3
+    assert shape.budget < caches.held <= shape.budget + shape.slack
+    pos = positions(caches)
+    assert (np.diff(pos, axis=-1) > 0).all()  # in the order of the tokens
+    since = caches.held - shape.budget        # tokens since the last cut
+    newest = np.arange(150 - since - shape.recent, 150)
+    assert (pos[..., -len(newest):] == newest).all()
+    # a token's weight is what its queries' heads gave it: all rows of all steps
+    # gave 1 in sum, and cuts only take weight away
+    assert float(caches.now.acc.sum()) <= 150 * 3 * shape.heads * (1 + 1e-3)
+
+
+def test_a_cut_changes_nothing_before_it():
+    import torch
+    cut, _ = run(small(), 64)
+    free, caches = run(small(budget=200), 64)
+    assert torch.equal(cut, free)
+    # 64 steps of one row a head: every row gives weight 1 in sum (fp32 sums of
+    # at most 64 terms)
+    assert float(caches.now.acc.sum()) == pytest.approx(64 * 3 * 4, rel=1e-5)
+    longer, _ = run(small(), 70)
+    assert torch.equal(longer[:64], free) and torch.isfinite(longer).all()
+
+
+def test_profile_and_placement():
+    from paper_2302_11665_amd import served
+    shape = small()
+    p = served.measure(shape, tokens=16, requests=4, batch=4)
+    assert p.latency > 0 and p.slope >= 0 and p.weight_mib >= 1
+    profiles = [served.Profile(latency=0.2 + 0.05 * i, slope=0.1, weight_mib=3000 + 500 * i) for i in range(6)]
+    gp = served.placement_problem(profiles, n_devices=8, device_mem_gb=8, rate=2.0, duration=30.0)
+    r = served.place(gp)
+    best, results = ogreedy.reduced_partition_search(oracle.lib(), gp.t, gp.model, gp.d_single, gp.weight_mib,
+                                                     gp.cfg_stages, gp.stage_lat, gp.partitions, gp.slo_scale)
+    assert r["best_served"] == max(x["best_served"] for x in results)
+    assert [int(m) for m in r["best_mask"]] == [int(m) for m in results[r["best_partition"]]["best_mask"]]

@@ -48,7 +48,7 @@ def test_linear_refusals(L):
 
     for kw in (dict(x=None), dict(w=None), dict(ws=None), dict(y=None), dict(xt=2), dict(xt=9), dict(yt=3),
                dict(yt=-1), dict(t=-1), dict(k=0), dict(n=0), dict(xs=63), dict(ys=31), dict(w=0x1001),
-               dict(wb=0), dict(work=None), dict(work=0x4010)):
+               dict(t=40, wb=0), dict(t=40, work=None), dict(t=40, work=0x4010)):
         assert call(**kw) == sim.AS_E_INVALID_ARG, kw
         assert "linear_i8" in sim.as_last_error()
     assert call(k=131073, xs=131073) == sim.AS_E_LIMITS
@@ -56,6 +56,9 @@ def test_linear_refusals(L):
     assert call(n=1 << 25, ys=1 << 25) == sim.AS_E_LIMITS
     assert call(t=0, x=None, y=None, work=None, wb=0) == sim.AS_OK
     assert sim.as_last_error() == ""
+    # a few tokens need no scratch memory, the tokens' codes and scales otherwise
+    assert L.as_linear_i8_workspace(4, 64, 32) == 0
+    assert L.as_linear_i8_workspace(40, 64, 32) >= 40 * 128 + 40 * 4
 
 
 def test_quantize_refusals(L):
@@ -127,3 +130,16 @@ def test_append_and_evict_refusals(L):
                dict(dst=cache(group=32)), dict(dst=cache(n_heads=1)), dict(dst=cache(n_seqs=1))):
         assert ev(**kw) == sim.AS_E_INVALID_ARG, kw
     assert L.as_cache_evict(cache(n_seqs=0), cache(n_seqs=0), None, None, 8, 2, None, None, 0, None) == sim.AS_OK
+
+
+def test_profile_and_placement_problem():
+    from paper_2302_11665_amd import served
+    s = served.Shape(layers=10, hidden=64, heads=2, kv_heads=1, dim=64, inner=128, budget=32)
+    p = served.profile(s, tokens=100, requests=3, block_bytes=1 << 20, cache_bytes=1 << 19, one=1e-3, many=2.4e-3,
+                       batch=8)
+    assert p.latency == pytest.approx(1.0) and p.slope == pytest.approx(0.2) and p.weight_mib == 25
+    assert served.profile(s, 1, 0, 1, 0, 1e-3, 0.9e-3, 8).slope == 0.0
+    gp = served.placement_problem([p, p], n_devices=4, device_mem_gb=1, rate=1.0, duration=10.0)
+    assert [len(x["group_cfg"]) for x in gp.partitions] == [4, 2, 1]
+    assert gp.stage_lat.shape == (2, 3, 4) and gp.stage_lat[0, 0, 0] == 1.0
+    assert set(gp.model.tolist()) <= {0, 1} and (gp.weight_mib == 25).all()
