@@ -240,6 +240,54 @@ struct Sums {
   float mref[NT], sum[NT];       // reference of the exponents (log2 units), sum of p over the lane's slots
 };
 
+template <int DIM, int GROUP, int NT>
+__device__ __forceinline__ void clear(Sums<DIM, GROUP, NT>& a, int t) {
+  a.mref[t] = kFloor;
+  a.sum[t] = 0.0f;
+#pragma unroll
+  for (int g = 0; g < DIM / GROUP; ++g) a.shift[t][g] = 0.0f;
+#pragma unroll
+  for (int i = 0; i < DIM / 16; ++i) a.o[t][i] = v4f{0, 0, 0, 0};
+}
+
+// The q.k of a lane's 8 slots of a block to p, the sums so far scaled where the
+// reference moves.
+template <int TYPE, int DIM, int GROUP, int NT, bool RAGGED>
+__device__ __forceinline__ void softmax_block(const AttArgs& p, int slot0, int limit, int u, float (&s)[8],
+                                              Sums<DIM, GROUP, NT>& a) {
+  if (RAGGED) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (slot0 + 16 * (e >> 2) + (e & 3) >= limit) s[e] = -kInf;
+  }
+  const float top = p.c_log2 * fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])),
+                                     fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+  // The reference follows the maximum only where it is passed by a factor of
+  // 2^8: sums and products stay far from fp32's range, and the sums so far are
+  // hardly ever scaled.
+  if (__any(top > a.mref[u] + 8.0f)) {
+    const float m = fmaxf(a.mref[u], max_over_rows(top));
+    const float f = __builtin_amdgcn_exp2f(a.mref[u] - m);
+    a.mref[u] = m;
+    a.sum[u] *= f;
+#pragma unroll
+    for (int g = 0; g < DIM / GROUP; ++g) a.shift[u][g] *= f;
+#pragma unroll
+    for (int i = 0; i < DIM / 16; ++i) a.o[u][i] *= f;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], p.c_log2, -a.mref[u]));
+    a.sum[u] += s[e];
+  }
+}
+
+// Two numbers as pairs of bf16: the nearest, and the nearest to what it leaves.
+__device__ __forceinline__ v2u split_bf16(float x, float y) {
+  const uint32_t hi = pack_bf16(x, y);
+  return v2u{hi, pack_bf16(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u))};
+}
+
 // 32 slots more; RAGGED: some are not seen by some query.
 template <int TYPE, int DIM, int GROUP, int NT, bool RAGGED>
 __device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int lane,
@@ -268,36 +316,8 @@ __device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int lane
     phase();
   }
   const int slot0 = blk * 32 + (lane >> 4) * 4;
-  if (RAGGED) {
 #pragma unroll
-    for (int u = 0; u < NT; ++u)
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) s[u][e] = -kInf;
-  }
-#pragma unroll
-  for (int u = 0; u < NT; ++u) {
-    const float top = p.c_log2 * fmaxf(fmaxf(fmaxf(s[u][0], s[u][1]), fmaxf(s[u][2], s[u][3])),
-                                       fmaxf(fmaxf(s[u][4], s[u][5]), fmaxf(s[u][6], s[u][7])));
-    // The reference follows the maximum only where it is passed by a factor
-    // of 2^8: sums and products stay far from fp32's range, and the sums so
-    // far are hardly ever scaled.
-    if (__any(top > a.mref[u] + 8.0f)) {
-      const float m = fmaxf(a.mref[u], max_over_rows(top));
-      const float f = __builtin_amdgcn_exp2f(a.mref[u] - m);
-      a.mref[u] = m;
-      a.sum[u] *= f;
-#pragma unroll
-      for (int g = 0; g < NG; ++g) a.shift[u][g] *= f;
-#pragma unroll
-      for (int i = 0; i < DIM / 16; ++i) a.o[u][i] *= f;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      s[u][e] = __builtin_amdgcn_exp2f(fmaf(s[u][e], p.c_log2, -a.mref[u]));
-      a.sum[u] += s[u][e];
-    }
-  }
+  for (int u = 0; u < NT; ++u) softmax_block<TYPE, DIM, GROUP, NT, RAGGED>(p, slot0, q[u].limit, u, s[u], a);
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     phase();
@@ -321,8 +341,8 @@ __device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int lane
           a.shift[u][g] = fma_m(s[u][e], w, a.shift[u][g]);
           a.shift[u][g] = fmaf(-16.0f, pd[z], a.shift[u][g]);
         }
-        hi[u][j] = pack_bf16(pd[0], pd[1]);
-        lo[u][j] = pack_bf16(pd[0] - __uint_as_float(hi[u][j] << 16), pd[1] - __uint_as_float(hi[u][j] & 0xffff0000u));
+        const v2u two = split_bf16(pd[0], pd[1]);
+        hi[u][j] = two[0], lo[u][j] = two[1];
       }
     }
 #pragma unroll
@@ -513,12 +533,7 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     load_queries<TYPE, DIM, GROUP>(p, b, h, row0 + 16 * t + (lane & 15), n, lane, q[t]);
-    a.mref[t] = kFloor;
-    a.sum[t] = 0.0f;
-#pragma unroll
-    for (int g = 0; g < NG; ++g) a.shift[t][g] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < DIM / 16; ++i) a.o[t][i] = v4f{0, 0, 0, 0};
+    clear(a, t);
   }
 
   const Expand<TYPE> key_codes;
@@ -612,7 +627,7 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
 // each with a ring of its own in LDS so that none waits for another, and join
 // their results at the segment's end.
 template <int TYPE, int DIM, int GROUP, int NT>
-__global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : 2) - (DIM == 4 * GROUP)) void attend(AttArgs p) {
+__global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : DIM == 64 ? 3 : 2) - (DIM == 4 * GROUP)) void attend(AttArgs p) {
   __shared__ float ml[kWaves][16][2];
   extern __shared__ __align__(16) uint8_t lds[];  // the rings, then the parts to be joined
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -633,10 +648,225 @@ __global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : 2) - (DIM == 4 * GROUP)
   }
 }
 
+// Many rows: every wavefront has 32 rows of its own and all slots of the
+// segment, and the four expand each block's codes together, a quarter each, into
+// operands in LDS that all of them multiply with: 128 rows share the work at the
+// codes, which otherwise takes half of the vector instructions.  The words of the
+// next block are on their way, and the operands of the one after this are written
+// while this one is multiplied; one barrier a block.  Bound by the vector
+// instructions of the softmax and of splitting p d, with the matrix
+// instructions close behind.
+constexpr int kManyRows = 128;
+
+template <int DIM, int GROUP>
+struct Operands {
+  static constexpr int kNG = DIM / GROUP, kWords = DIM / 32;  // words of a lane's quarter
+  static constexpr int kV = 2 * kWords * 1024;                // K's operands: [2][kWords], then V's [2 kWords]
+  static constexpr int kKeyPar = 2 * kV;                      // words [kNG][32]
+  static constexpr int kValuePar = kKeyPar + kNG * 128;       // words [kNG][32]
+  static constexpr int kValueMin = kValuePar + kNG * 128;     // m - 16 d, fp32 [kNG][32]
+  static constexpr int kBytes = kValueMin + kNG * 128;
+
+  uint32_t words[kWords], par;  // this wavefront's quarter of a block
+
+  __device__ __forceinline__ void fetch(const AttArgs& p, int64_t row, int at, int lane, int wave) {
+    if (row < 0) row = 0, at = 0;
+    const uint32_t* from = wave < 2 ? p.c.k + (row * p.c.page + at + 16 * wave + (lane & 15)) * (DIM / 8) + (lane >> 4) * kWords
+                                    : p.c.v + (row * p.c.page + at) * (DIM / 8) + lane * (2 * kWords) + (wave - 2) * kWords;
+    if (kWords == 4) {
+      const v4u w = *reinterpret_cast<const v4u*>(from);
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) words[i] = w[i];
+    } else {
+      const v2u w = *reinterpret_cast<const v2u*>(from);
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) words[i] = w[i];
+    }
+    const int i = (wave & 1) * 16 * kNG + lane;  // of the 32 kNG words of K's (wave < 2) or V's scales
+    if (lane < 16 * kNG)
+      par = (wave < 2 ? p.c.k_par : p.c.v_par)[(row * kNG + (i >> 5)) * p.c.page + at + (i & 31)];
+  }
+
+  template <int TYPE>
+  __device__ __forceinline__ void store(uint8_t* lds, int lane, int wave, const Expand<TYPE>& key_codes,
+                                        const Expand<AS_BF16>& value_codes) const {
+    uint8_t* to = lds + wave * kWords * 1024 + lane * 16;  // (K's tiles of 16 slots, V's halves)
+#pragma unroll
+    for (int i = 0; i < kWords; ++i)
+      *reinterpret_cast<v4u*>(to + i * 1024) = wave < 2 ? key_codes(words[i]) : value_codes(words[i]);
+    const int i = (wave & 1) * 16 * kNG + lane;
+    if (lane < 16 * kNG) {
+      *reinterpret_cast<uint32_t*>(lds + (wave < 2 ? kKeyPar : kValuePar) + i * 4) = par;
+      if (wave >= 2) *reinterpret_cast<float*>(lds + kValueMin + i * 4) = fma_m(1.0f, par, fma_d(-16.0f, par, 0.0f));
+    }
+  }
+};
+
+template <int TYPE, int DIM, int GROUP, bool RAGGED>
+__device__ __forceinline__ void many_block(const AttArgs& p, int blk, int lane,
+                                           const Queries<TYPE, DIM, GROUP> (&q)[2], const uint8_t* lds,
+                                           Sums<DIM, GROUP, 2>& a) {
+  typedef Operands<DIM, GROUP> O;
+  constexpr int NG = DIM / GROUP;
+  float s[2][8];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    v4u kf[DIM / 32], par[NG];
+#pragma unroll
+    for (int i = 0; i < DIM / 32; ++i)
+      kf[i] = *reinterpret_cast<const v4u*>(lds + (t * (DIM / 32) + i) * 1024 + lane * 16);
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+      par[g] = *reinterpret_cast<const v4u*>(lds + O::kKeyPar + g * 128 + t * 64 + (lane >> 4) * 16);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float x[4];
+      scores<TYPE, DIM, GROUP>(kf, par, q[u], x);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[u][4 * t + r] = x[r];
+    }
+  }
+  const int slot0 = blk * 32 + (lane >> 4) * 4;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) softmax_block<TYPE, DIM, GROUP, 2, RAGGED>(p, slot0, q[u].limit, u, s[u], a);
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    v4u par[2], hi[2], lo[2];
+    v4f low[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      par[t] = *reinterpret_cast<const v4u*>(lds + O::kValuePar + g * 128 + t * 64 + (lane >> 4) * 16);
+      low[t] = *reinterpret_cast<const v4f*>(lds + O::kValueMin + g * 128 + t * 64 + (lane >> 4) * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float pd[2];
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const int e = 2 * j + z;
+          uint32_t w = par[e >> 2][e & 3];
+          float m = low[e >> 2][e & 3];
+          // a slot that is not seen may hold anything, infinities and NaN too
+          if (RAGGED && slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) w = 0, m = 0.0f;
+          pd[z] = fma_d(s[u][e], w, 0.0f);
+          a.shift[u][g] = fmaf(s[u][e], m, a.shift[u][g]);
+        }
+        const v2u two = split_bf16(pd[0], pd[1]);
+        hi[u][j] = two[0], lo[u][j] = two[1];
+      }
+    // (the two products of one sum apart, so that neither waits for the other)
+    constexpr int kRun = GROUP / 16 < 4 ? GROUP / 16 : 4;
+#pragma unroll
+    for (int i0 = 0; i0 < GROUP / 16; i0 += kRun) {
+        v4u vf[kRun];
+#pragma unroll
+      for (int i = 0; i < kRun; ++i)
+        vf[i] = *reinterpret_cast<const v4u*>(lds + O::kV + (g * (GROUP / 16) + i0 + i) * 1024 + lane * 16);
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < kRun; ++i)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            v4f& o = a.o[u][g * (GROUP / 16) + i0 + i];
+            o = mfma<AS_BF16>(vf[i], half ? lo[u] : hi[u], o);
+          }
+    }
+  }
+}
+
+template <int TYPE, int DIM, int GROUP>
+__device__ __forceinline__ void many_segment(const AttArgs& p, const Segment& s, int take, int share, int lane,
+                                             int wave, uint8_t* lds) {
+  constexpr int NG = DIM / GROUP;
+  typedef Operands<DIM, GROUP> O;
+  const int b = s.b, h = s.h, n = s.n, row0 = s.rg * kManyRows + wave * 32, end = s.blk + take;
+  int least;
+  seen_blocks(p, n, s.rg, least);
+  Queries<TYPE, DIM, GROUP> q[2];
+  Sums<DIM, GROUP, 2> a;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    load_queries<TYPE, DIM, GROUP>(p, b, h, row0 + 16 * t + (lane & 15), n, lane, q[t]);
+    clear(a, t);
+  }
+  const Expand<TYPE> key_codes;
+  const Expand<AS_BF16> value_codes;
+  O quarter;
+  int blk = s.blk, half = 0;
+  bool valid[2];  // of this block and the next
+  auto fetch = [&](int i, bool& ok) {
+    int at;
+    const int64_t row = block_row(p, b, h, i, at);
+    ok = row >= 0;
+    if (p.c.n_pages > 0) quarter.fetch(p, row, at, lane, wave);
+  };
+  fetch(blk, valid[0]);
+  quarter.store(lds, lane, wave, key_codes, value_codes);
+  valid[1] = false;
+  if (blk + 1 < end) fetch(blk + 1, valid[1]);
+  lds_barrier();
+  auto blocks = [&](int to, auto ragged) {
+    for (; blk < to; ++blk, half ^= 1) {
+      const bool here = valid[0];
+      valid[0] = valid[1];
+      if (blk + 1 < end) quarter.store(lds + (half ^ 1) * O::kBytes, lane, wave, key_codes, value_codes);
+      if (blk + 2 < end) fetch(blk + 2, valid[1]);
+      if (here) many_block<TYPE, DIM, GROUP, decltype(ragged)::value>(p, blk, lane, q, lds + half * O::kBytes, a);
+      lds_barrier();
+    }
+  };
+  blocks(min(end, least >> 5), std::false_type());
+  blocks(end, std::true_type());
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int in = wave * 32 + 16 * u + (lane & 15), row = s.rg * kManyRows + in, g = lane >> 4;
+    const float l = sum_over_rows(a.sum[u]);
+    float add[NG];
+#pragma unroll
+    for (int k = 0; k < NG; ++k) add[k] = sum_over_rows(a.shift[u][k]);
+    if (row >= p.rows) continue;
+    const int64_t at = ((int64_t)share * 2 + (s.blk == 0)) * kManyRows + in;
+#pragma unroll
+    for (int i = 0; i < DIM / 16; ++i) {
+      const v4f x = a.o[u][i] + add[i * 16 / GROUP];
+      if (take == s.seen)
+        store_row<TYPE>(p, out_index(p, b, h, row, DIM) + 16 * i + 4 * g, x, l);
+      else
+        *reinterpret_cast<v4f*>(p.part_o + at * DIM + 16 * i + 4 * g) = x;
+    }
+    if (g == 0 && take == s.seen && p.row_ml) store_row_ml(p, b, h, row, a.mref[u], l);
+    if (g == 0 && take != s.seen) *reinterpret_cast<float2*>(p.part_ml + at * 2) = make_float2(a.mref[u], l);
+  }
+}
+
+template <int TYPE, int DIM, int GROUP>
+__global__ __launch_bounds__(64 * kWaves, 2) void attend_many(AttArgs p) {
+  extern __shared__ __align__(16) uint8_t lds[];  // two blocks' operands
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Sequences first;
+  uint32_t total;
+  const uint32_t size = share_size<false>(p, lane, first, total);
+  const int64_t share = share_number(total, size);
+  if (share < 0) return;
+  const uint32_t unit = (uint32_t)share * size;
+  int left = (int)min(size, total - unit);
+  Segment g = locate<false>(p, unit, lane, first);
+  for (;;) {
+    const int take = min(left, g.seen - g.blk);
+    many_segment<TYPE, DIM, GROUP>(p, g, take, (int)share, lane, wave, lds);
+    left -= take;
+    if (left == 0) return;
+    advance<false>(p, g);
+  }
+}
+
 // Joins the parts of the segments that several workgroups had, four channels to
 // a thread.  ROWS = 1: a workgroup joins one row, its parts side by side (few
 // rows, and a long segment may have hundreds of parts); otherwise a workgroup
-// joins a whole segment, ROWS rows at a time.
+// joins ROWS rows of a segment, or 16.
 constexpr int kMaxParts = 2048;
 
 template <int TYPE, int DIM, int ROWS>
@@ -645,16 +875,17 @@ __global__ __launch_bounds__(256) void join(AttArgs p) {
   __shared__ float mls[kSide][2];
   __shared__ v4f sums[kSide][DIM / 4];
   const int tid = threadIdx.x, lane = tid & 63;
-  const int across = ROWS == 1 ? p.rows : p.row_groups;
-  const int bh = blockIdx.x / across, in = blockIdx.x % across;
-  const int rg = ROWS == 1 ? in / p.row_span : in;
+  constexpr int kRun = ROWS == 1 ? 1 : 16;  // rows of a workgroup
+  const int across = (p.rows + kRun - 1) / kRun;
+  const int bh = blockIdx.x / across, in = blockIdx.x % across * kRun;
+  const int rg = in / p.row_span;
   const int b = bh / p.c.n_heads, h = bh % p.c.n_heads;
   const int n = clamped_length(p, b);
   int least;
   const int seen = seen_blocks(p, n, rg, least);
   const int d = tid % (DIM / 4), side = tid / (DIM / 4) % kSide;
-  int row = ROWS == 1 ? in : rg * p.row_span + tid / (DIM / 4);
-  const int end = ROWS == 1 ? in + 1 : min(p.rows, (rg + 1) * p.row_span);
+  int row = ROWS == 1 ? in : in + tid / (DIM / 4);
+  const int end = min(p.rows, in + kRun);
   if (seen == 0) {  // in no workgroup's share
     if (side) return;
     for (; row < end; row += ROWS) {
@@ -892,7 +1123,7 @@ __global__ __launch_bounds__(64 * NW) void attend_whole(AttArgs p) {
 }
 
 struct Plan {
-  bool whole;
+  bool whole, many;
   int per, rows, tiles, row_groups, workgroups, weigh_workgroups;
   int64_t o_bytes, ml_bytes, row_bytes;
 };
@@ -909,20 +1140,22 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   Plan pl;
   pl.per = n_q_heads / c->n_heads;
   pl.rows = pl.per * n_queries;
-  pl.tiles = pl.rows > 16 ? 2 : 1;
+  pl.many = pl.rows >= kManyRows * 3 / 4;  // three of four wavefronts have rows
+  pl.tiles = pl.many ? kManyRows / 16 : pl.rows > 16 ? 2 : 1;
   pl.row_groups = (pl.rows + 16 * pl.tiles - 1) / (16 * pl.tiles);
   const int64_t heads = (int64_t)c->n_seqs * c->n_heads;
   const int64_t blocks = (int64_t)c->max_pages * c->page / 32;
   const int wide = c->dim == 4 * c->group;
-  pl.whole = blocks <= kWholeBlocks && heads * pl.row_groups <= as_host::compute_units() &&
+  pl.whole = !pl.many && blocks <= kWholeBlocks && heads * pl.row_groups <= as_host::compute_units() &&
              (!weights || pl.row_groups == 1);
+  const int resident = pl.many ? 2 : (pl.tiles == 1 ? 4 : c->dim == 64 ? 3 : 2) - wide;
   auto groups = [&](int64_t all, int64_t resident) {
     const int64_t g = all < resident ? all : resident;
     return (int)round_up(g < 1 ? 1 : g, 8);
   };
   int cus = as_host::compute_units();
   if (cus > kMaxParts / 4) cus = kMaxParts / 4;
-  pl.workgroups = groups(heads * pl.row_groups * blocks, (int64_t)cus * ((pl.tiles == 1 ? 4 : 2) - wide));
+  pl.workgroups = groups(heads * pl.row_groups * blocks, (int64_t)cus * resident);
   pl.weigh_workgroups = groups(heads * blocks, (int64_t)cus * 3);
   const int64_t parts = (int64_t)pl.workgroups * 2 * 16 * pl.tiles;
   pl.o_bytes = pl.whole ? 0 : round_up(parts * c->dim * 4, 256);
@@ -968,7 +1201,10 @@ int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
     return pl.tiles == 1 ? launch_whole<TYPE, DIM, GROUP, 1>(p, s) : launch_whole<TYPE, DIM, GROUP, 2>(p, s);
   const dim3 g((unsigned)pl.workgroups), t(64 * kWaves);
   const size_t lds = attend_lds<DIM, GROUP>(kWaves);
-  if (pl.tiles == 1)
+  typedef Operands<DIM, GROUP> OperandSet;
+  if (pl.many)
+    hipLaunchKernelGGL((attend_many<TYPE, DIM, GROUP>), g, t, (size_t)2 * OperandSet::kBytes, s, p);
+  else if (pl.tiles == 1)
     hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 1>), g, t, lds, s, p);
   else
     hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 2>), g, t, lds, s, p);
@@ -976,7 +1212,7 @@ int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
   if (p.row_groups == 1)
     hipLaunchKernelGGL((join<TYPE, DIM, 1>), dim3((unsigned)(heads * p.rows)), dim3(256), 0, s, p);
   else
-    hipLaunchKernelGGL((join<TYPE, DIM, 1024 / DIM>), dim3((unsigned)(heads * p.row_groups)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((join<TYPE, DIM, 1024 / DIM>), dim3((unsigned)(heads * ((p.rows + 15) / 16))), dim3(256), 0, s, p);
   typedef Stage<DIM, GROUP, false> KeyStage;
   if (p.acc_out)
     hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP>), dim3((unsigned)pl.weigh_workgroups), t,

@@ -73,6 +73,14 @@ __device__ __forceinline__ uint32_t scan_lanes(uint32_t x) {
   return x;
 }
 
+// Barrier of a workgroup that orders its LDS accesses alone: loads from memory
+// stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // Wait until at most N of the wavefront's loads are on their way; what is read
 // from LDS afterwards is read afterwards.
 template <int N>

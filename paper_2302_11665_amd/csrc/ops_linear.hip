@@ -289,14 +289,6 @@ __device__ __forceinline__ void finish(const LinArgs& p, int t, int n, int sum, 
   store_one<YTYPE>(p.y, (int64_t)t * p.y_stride + n, v);
 }
 
-// Barrier of a workgroup that orders its LDS accesses alone: loads from memory
-// stay in flight across it.
-__device__ __forceinline__ void lds_barrier() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 // Few tokens: the weights' bytes bound it, each read once.  One workgroup takes
 // 16 CT channels and all tokens; its eight wavefronts share out the columns and
 // add their sums in LDS (whole numbers: the order does not matter).  Weights go

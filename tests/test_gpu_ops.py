@@ -249,6 +249,9 @@ ATTEND += [
     ([31 + 7 * i for i in range(70)], 1, 4, 4, 64, 64, 32),  # more than 64 sequences
     ([0] * 66 + [100, 0, 0, 64], 2, 8, 4, 128, 64, 32),
     ([20] * 90, 20, 6, 3, 64, 32, 32),
+    ([2500, 130], 100, 4, 1, 128, 64, 64),     # 400 rows: the codes expanded once for 128
+    ([700, 3000, 65], 65, 2, 1, 64, 64, 32),
+    ([1900], 33, 3, 1, 128, 32, 96),
 ]
 
 
