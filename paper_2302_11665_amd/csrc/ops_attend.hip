@@ -1074,8 +1074,116 @@ __device__ __forceinline__ void weigh_segment(const AttArgs& p, const Segment& s
   }
 }
 
-template <int TYPE, int DIM, int GROUP>
-__global__ __launch_bounds__(64 * kWaves, 3) void weigh(AttArgs p) {
+// More than 16 rows: a wavefront keeps the expanded keys of BLOCKS blocks in
+// registers and goes over the rows, 16 at a time; the other wavefronts of the
+// workgroup read the same rows at about the same time.  The sums of q come from
+// the matrix instructions too, as a product with ones.
+template <int TYPE, int DIM, int GROUP, int BLOCKS>
+__device__ __forceinline__ void weigh_rows(const AttArgs& p, const Segment& s, int take, int lane, int wave) {
+  constexpr int NG = DIM / GROUP;
+  const int b = s.b, h = s.h, n = s.n, end = s.blk + take, g = lane >> 4, in = lane & 15;
+  const Expand<TYPE> key_codes;
+  const uint32_t one = TYPE == AS_BF16 ? 0x3f803f80u : 0x3c003c00u;
+  const v4u ones = {one, one, one, one};
+  const float* row_ml = p.row_ml + ((int64_t)b * p.c.n_heads + h) * p.rows * 2;
+  for (int blk0 = s.blk + wave * BLOCKS; blk0 < end; blk0 += kWaves * BLOCKS) {
+    v4u kf[BLOCKS][2][DIM / 32];
+    uint32_t par[BLOCKS][2][NG];
+    int64_t slots[BLOCKS];  // of the block's first slot in a pool of one value a slot, or -1
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) {
+      slots[i] = -1;
+      if (blk0 + i >= end) continue;
+      int at;
+      const int64_t row = block_row(p, b, h, blk0 + i, at);
+      if (row < 0) continue;
+      slots[i] = row * p.c.page + at;
+      const uint32_t* k = p.c.k + (slots[i] + in) * (DIM / 8) + g * (DIM / 32);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (DIM == 128) {
+          const v4u w = *reinterpret_cast<const v4u*>(k + t * 16 * (DIM / 8));
+#pragma unroll
+          for (int c = 0; c < DIM / 32; ++c) kf[i][t][c] = key_codes(w[c]);
+        } else {
+          const v2u w = *reinterpret_cast<const v2u*>(k + t * 16 * (DIM / 8));
+#pragma unroll
+          for (int c = 0; c < DIM / 32; ++c) kf[i][t][c] = key_codes(w[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < NG; ++c) par[i][t][c] = p.c.k_par[(row * NG + c) * p.c.page + at + 16 * t + in];
+      }
+    }
+    float w[BLOCKS][2] = {};
+    const bool ragged = (blk0 + BLOCKS) * 32 > n - p.n_queries + 1;
+    for (int r0 = 0; r0 < p.rows; r0 += 16) {
+      const int row = min(r0 + in, p.rows - 1), t = row / p.per;
+      const uint16_t* from = p.q + b * p.q_seq + t * p.q_token + (int64_t)(h * p.per + row - t * p.per) * DIM + g * 8;
+      v4u q[DIM / 32];
+#pragma unroll
+      for (int c = 0; c < DIM / 32; ++c) q[c] = *reinterpret_cast<const v4u*>(from + 32 * c);
+      v4f qsum[NG], start[NG];
+      float m[4], inv[4];
+      int limit[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int at = r0 + 4 * g + r;
+        const float2 ml = *reinterpret_cast<const float2*>(row_ml + (int64_t)min(at, p.rows - 1) * 2);
+        m[r] = ml.x;
+        inv[r] = ml.y;
+      }
+      const bool masked = ragged || r0 + 16 > p.rows;
+      if (masked) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int at = r0 + 4 * g + r;
+          limit[r] = at < p.rows ? n - p.n_queries + at / p.per + 1 : 0;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < NG; ++k) {
+        qsum[k] = v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int c = k * (GROUP / 32); c < (k + 1) * (GROUP / 32); ++c) qsum[k] = mfma<TYPE>(q[c], ones, qsum[k]);
+        start[k] = qsum[k] * -16.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          float x[4];
+#pragma unroll
+          for (int k = 0; k < NG; ++k) {
+            v4f a = start[k];
+#pragma unroll
+            for (int c = k * (GROUP / 32); c < (k + 1) * (GROUP / 32); ++c) a = mfma<TYPE>(q[c], kf[i][t][c], a);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              x[r] = fma_m(qsum[k][r], par[i][t][k], k == 0 ? 0.0f : x[r]);
+              x[r] = fma_d(a[r], par[i][t][k], x[r]);
+            }
+          }
+          const int slot = (blk0 + i) * 32 + 16 * t + in;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float e = __builtin_amdgcn_exp2f(fmaf(x[r], p.c_log2, -m[r])) * inv[r];
+            if (masked) e = slot < limit[r] ? e : 0.0f;
+            w[i][t] += e;
+          }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) {
+      const float w0 = sum_over_rows(w[i][0]), w1 = sum_over_rows(w[i][1]);
+      const int slot = lane & 31;
+      if (slots[i] >= 0 && lane < 32 && (blk0 + i) * 32 + slot < n)
+        p.acc_out[slots[i] + slot] = (p.acc_in ? p.acc_in[slots[i] + slot] : 0.0f) + ((lane & 16) ? w1 : w0);
+    }
+  }
+}
+
+template <int TYPE, int DIM, int GROUP, bool MANY>
+__global__ __launch_bounds__(64 * kWaves, MANY ? 2 : 3) void weigh(AttArgs p) {
   extern __shared__ __align__(16) uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Sequences first;
@@ -1088,7 +1196,10 @@ __global__ __launch_bounds__(64 * kWaves, 3) void weigh(AttArgs p) {
   Segment g = locate<true>(p, unit, lane, first);
   for (;;) {
     const int take = min(left, g.seen - g.blk);
-    weigh_segment<TYPE, DIM, GROUP, kWaves>(p, g, take, lane, wave, lds);
+    if (MANY)
+      weigh_rows<TYPE, DIM, GROUP, 256 / DIM>(p, g, take, lane, wave);
+    else
+      weigh_segment<TYPE, DIM, GROUP, kWaves>(p, g, take, lane, wave, lds);
     left -= take;
     if (left == 0) return;
     advance<true>(p, g);
@@ -1156,7 +1267,7 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   int cus = as_host::compute_units();
   if (cus > kMaxParts / 4) cus = kMaxParts / 4;
   pl.workgroups = groups(heads * pl.row_groups * blocks, (int64_t)cus * resident);
-  pl.weigh_workgroups = groups(heads * blocks, (int64_t)cus * 3);
+  pl.weigh_workgroups = groups(heads * blocks, (int64_t)cus * (pl.rows > 16 ? 2 : 3));
   const int64_t parts = (int64_t)pl.workgroups * 2 * 16 * pl.tiles;
   pl.o_bytes = pl.whole ? 0 : round_up(parts * c->dim * 4, 256);
   pl.ml_bytes = pl.whole ? 0 : round_up(parts * 8, 256);
@@ -1214,8 +1325,10 @@ int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
   else
     hipLaunchKernelGGL((join<TYPE, DIM, 1024 / DIM>), dim3((unsigned)(heads * ((p.rows + 15) / 16))), dim3(256), 0, s, p);
   typedef Stage<DIM, GROUP, false> KeyStage;
-  if (p.acc_out)
-    hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP>), dim3((unsigned)pl.weigh_workgroups), t,
+  if (p.acc_out && p.rows > 16)
+    hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP, true>), dim3((unsigned)pl.weigh_workgroups), t, 0, s, p);
+  else if (p.acc_out)
+    hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP, false>), dim3((unsigned)pl.weigh_workgroups), t,
                        (size_t)kWaves * kWeighStages * (KeyStage::kBytes + 128), s, p);
   return launched("attention_kv4");
 }
