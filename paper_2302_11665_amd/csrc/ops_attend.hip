@@ -869,9 +869,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(AttArgs p) {
 // joins ROWS rows of a segment, or 16.
 constexpr int kMaxParts = 2048;
 
-template <int TYPE, int DIM, int ROWS>
-__global__ __launch_bounds__(256) void join(AttArgs p) {
-  constexpr int kSide = 256 / (DIM / 4) / ROWS;
+template <int TYPE, int DIM, int ROWS, int THREADS>
+__global__ __launch_bounds__(THREADS) void join(AttArgs p) {
+  constexpr int kSide = THREADS / (DIM / 4) / ROWS;
   __shared__ float mls[kSide][2];
   __shared__ v4f sums[kSide][DIM / 4];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -1206,13 +1206,11 @@ __global__ __launch_bounds__(64 * kWaves, MANY ? 2 : 3) void weigh(AttArgs p) {
   }
 }
 
-// Short sequences: a workgroup of more wavefronts has a whole segment, so that
-// nothing is left to be joined, and the weights too, where all rows are in one
-// segment: one launch, where a launch costs more than the work.
-template <int DIM, int GROUP, int NT>
-constexpr int whole_waves() {
-  return NT == 1 && DIM < 4 * GROUP ? 16 : 8;  // as many as their registers allow
-}
+// Short sequences: a workgroup has a whole segment, so that nothing is left to
+// be joined, and the weights too, where all rows are in one segment: one launch,
+// where a launch costs more than the work.  Very short ones take four
+// wavefronts, others as many as their registers allow.
+constexpr int whole_waves(int dim, int group, int nt) { return nt == 1 && dim < 4 * group ? 16 : 8; }
 
 template <int TYPE, int DIM, int GROUP, int NT, int NW>
 __global__ __launch_bounds__(64 * NW) void attend_whole(AttArgs p) {
@@ -1234,17 +1232,21 @@ __global__ __launch_bounds__(64 * NW) void attend_whole(AttArgs p) {
 }
 
 struct Plan {
-  bool whole, many;
+  bool many;
+  int whole;  // wavefronts of attend_whole, kWaves or more, or 0
   int per, rows, tiles, row_groups, workgroups, weigh_workgroups;
+  int64_t parts;  // of a segment, at most, where all have one length
   int64_t o_bytes, ml_bytes, row_bytes;
 };
 
-// Tables of up to so many blocks, with a compute unit for each segment, go to
-// attend_whole.  One compute unit works 0.2 us at a block: 12 heads of up to 60
-// blocks with weights took 17 us on the device there, 17 us in three launches
-// otherwise, and 22 us a step against 35; 8 heads of 129 blocks 28 us there and
-// 14 us in shares.
-constexpr int kWholeBlocks = 64;
+// attend_whole takes tables of up to kShortBlocks blocks with four wavefronts
+// (64 sequences of 8 heads, up to 10 blocks, with weights: 37 us on the device in
+// three launches of shares and 14 there), and of up to kWholeBlocks with more
+// wavefronts where every segment has a compute unit.  One compute unit works 0.2 us at a
+// block: 12 heads of up to 60 blocks with weights took 17 us on the device
+// there, 17 us in shares, and 22 us a step against 35; 8 heads of 129 blocks 28
+// us there and 14 us in shares.
+constexpr int kShortBlocks = 16, kWholeBlocks = 64;
 
 // Workgroups that a compute unit runs at once: the launch bounds of the kernels.
 Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) {
@@ -1257,8 +1259,13 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   const int64_t heads = (int64_t)c->n_seqs * c->n_heads;
   const int64_t blocks = (int64_t)c->max_pages * c->page / 32;
   const int wide = c->dim == 4 * c->group;
-  pl.whole = !pl.many && blocks <= kWholeBlocks && heads * pl.row_groups <= as_host::compute_units() &&
-             (!weights || pl.row_groups == 1);
+  pl.whole = 0;
+  if (!pl.many && (!weights || pl.row_groups == 1)) {
+    if (blocks <= kShortBlocks)
+      pl.whole = kWaves;
+    else if (blocks <= kWholeBlocks && heads * pl.row_groups <= as_host::compute_units())
+      pl.whole = whole_waves(c->dim, c->group, pl.tiles);
+  }
   const int resident = pl.many ? 2 : (pl.tiles == 1 ? 4 : c->dim == 64 ? 3 : 2) - wide;
   auto groups = [&](int64_t all, int64_t resident) {
     const int64_t g = all < resident ? all : resident;
@@ -1268,9 +1275,11 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   if (cus > kMaxParts / 4) cus = kMaxParts / 4;
   pl.workgroups = groups(heads * pl.row_groups * blocks, (int64_t)cus * resident);
   pl.weigh_workgroups = groups(heads * blocks, (int64_t)cus * (pl.rows > 16 ? 2 : 3));
-  const int64_t parts = (int64_t)pl.workgroups * 2 * 16 * pl.tiles;
-  pl.o_bytes = pl.whole ? 0 : round_up(parts * c->dim * 4, 256);
-  pl.ml_bytes = pl.whole ? 0 : round_up(parts * 8, 256);
+  pl.parts = pl.workgroups / (heads * pl.row_groups);
+  if (pl.parts > blocks / kWaves) pl.parts = blocks / kWaves;
+  const int64_t places = (int64_t)pl.workgroups * 2 * 16 * pl.tiles;
+  pl.o_bytes = pl.whole ? 0 : round_up(places * c->dim * 4, 256);
+  pl.ml_bytes = pl.whole ? 0 : round_up(places * 8, 256);
   pl.row_bytes = weights ? round_up(heads * pl.rows * 8, 256) : 0;
   return pl;
 }
@@ -1292,9 +1301,8 @@ int check_queries(const as_cache_t* c, int32_t n_queries, int32_t n_q_heads) {
   return AS_OK;
 }
 
-template <int TYPE, int DIM, int GROUP, int NT>
+template <int TYPE, int DIM, int GROUP, int NT, int NW>
 int launch_whole(const AttArgs& p, hipStream_t s) {
-  constexpr int NW = whole_waves<DIM, GROUP, NT>();
   typedef Stage<DIM, GROUP, false> KeyStage;
   size_t lds = attend_lds<DIM, GROUP>(NW);
   const size_t weigh_lds = (size_t)NW * kWeighStages * (KeyStage::kBytes + 128);
@@ -1308,8 +1316,12 @@ int launch_whole(const AttArgs& p, hipStream_t s) {
 
 template <int TYPE, int DIM, int GROUP>
 int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
+  if (pl.whole == kWaves)
+    return pl.tiles == 1 ? launch_whole<TYPE, DIM, GROUP, 1, kWaves>(p, s)
+                         : launch_whole<TYPE, DIM, GROUP, 2, kWaves>(p, s);
   if (pl.whole)
-    return pl.tiles == 1 ? launch_whole<TYPE, DIM, GROUP, 1>(p, s) : launch_whole<TYPE, DIM, GROUP, 2>(p, s);
+    return pl.tiles == 1 ? launch_whole<TYPE, DIM, GROUP, 1, whole_waves(DIM, GROUP, 1)>(p, s)
+                         : launch_whole<TYPE, DIM, GROUP, 2, whole_waves(DIM, GROUP, 2)>(p, s);
   const dim3 g((unsigned)pl.workgroups), t(64 * kWaves);
   const size_t lds = attend_lds<DIM, GROUP>(kWaves);
   typedef Operands<DIM, GROUP> OperandSet;
@@ -1320,10 +1332,14 @@ int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
   else
     hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 2>), g, t, lds, s, p);
   const int64_t heads = (int64_t)p.c.n_seqs * p.c.n_heads;
-  if (p.row_groups == 1)
-    hipLaunchKernelGGL((join<TYPE, DIM, 1>), dim3((unsigned)(heads * p.rows)), dim3(256), 0, s, p);
+  const dim3 by_row((unsigned)(heads * p.rows));
+  if (p.row_groups > 1)
+    hipLaunchKernelGGL((join<TYPE, DIM, 1024 / DIM, 256>), dim3((unsigned)(heads * ((p.rows + 15) / 16))), dim3(256), 0,
+                       s, p);
+  else if (pl.parts >= 64)
+    hipLaunchKernelGGL((join<TYPE, DIM, 1, 1024>), by_row, dim3(1024), 0, s, p);
   else
-    hipLaunchKernelGGL((join<TYPE, DIM, 1024 / DIM>), dim3((unsigned)(heads * ((p.rows + 15) / 16))), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((join<TYPE, DIM, 1, 256>), by_row, dim3(256), 0, s, p);
   typedef Stage<DIM, GROUP, false> KeyStage;
   if (p.acc_out && p.rows > 16)
     hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP, true>), dim3((unsigned)pl.weigh_workgroups), t, 0, s, p);
