@@ -190,14 +190,19 @@ __device__ __forceinline__ void load_queries(const AttArgs& p, int b, int h, int
   // rows beyond the last are zero and see what the last sees; they are not stored
   x.limit = n - p.n_queries + (row < p.rows ? t : p.n_queries - 1) + 1;
 #pragma unroll
+  for (int i = 0; i < DIM / 32; ++i)
+    x.q[i] = row < p.rows ? *reinterpret_cast<const v4u*>(q + 32 * i) : v4u{0, 0, 0, 0};
+}
+// The sums, once the loads are under way and others after them.
+template <int TYPE, int DIM, int GROUP>
+__device__ __forceinline__ void sum_queries(Queries<TYPE, DIM, GROUP>& x) {
+#pragma unroll
   for (int g = 0; g < DIM / GROUP; ++g) {
     float s = 0.0f;
 #pragma unroll
-    for (int i = g * (GROUP / 32); i < (g + 1) * (GROUP / 32); ++i) {
-      x.q[i] = row < p.rows ? *reinterpret_cast<const v4u*>(q + 32 * i) : v4u{0, 0, 0, 0};
+    for (int i = g * (GROUP / 32); i < (g + 1) * (GROUP / 32); ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) s += to_f32<TYPE>(x.q[i][j] & 0xffffu) + to_f32<TYPE>(x.q[i][j] >> 16);
-    }
     x.sum[g] = sum_over_rows(s);
   }
 }
@@ -531,13 +536,7 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
   Queries<TYPE, DIM, GROUP> q[NT];
   Sums<DIM, GROUP, NT> a;
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    load_queries<TYPE, DIM, GROUP>(p, b, h, row0 + 16 * t + (lane & 15), n, lane, q[t]);
-    clear(a, t);
-  }
-
-  const Expand<TYPE> key_codes;
-  const Expand<AS_BF16> value_codes;
+  for (int t = 0; t < NT; ++t) load_queries<TYPE, DIM, GROUP>(p, b, h, row0 + 16 * t + (lane & 15), n, lane, q[t]);
   int blk = s.blk + wave;
   uint32_t valid = 0;  // bit j: the block j turns on has a page
 #pragma unroll
@@ -548,6 +547,13 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
     valid |= (uint32_t)(row >= 0) << j;
     if (p.c.n_pages > 0) S::bring(p, row, at, lane, ring + j * S::kBytes);
   }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    sum_queries(q[t]);
+    clear(a, t);
+  }
+  const Expand<TYPE> key_codes;
+  const Expand<AS_BF16> value_codes;
   int slot = 0;
   // Blocks up to `to`, all of one kind.
   auto blocks = [&](int to, auto ragged) {
@@ -788,10 +794,7 @@ __device__ __forceinline__ void many_segment(const AttArgs& p, const Segment& s,
   Queries<TYPE, DIM, GROUP> q[2];
   Sums<DIM, GROUP, 2> a;
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    load_queries<TYPE, DIM, GROUP>(p, b, h, row0 + 16 * t + (lane & 15), n, lane, q[t]);
-    clear(a, t);
-  }
+  for (int t = 0; t < 2; ++t) load_queries<TYPE, DIM, GROUP>(p, b, h, row0 + 16 * t + (lane & 15), n, lane, q[t]);
   const Expand<TYPE> key_codes;
   const Expand<AS_BF16> value_codes;
   O quarter;
@@ -807,6 +810,11 @@ __device__ __forceinline__ void many_segment(const AttArgs& p, const Segment& s,
   quarter.store(lds, lane, wave, key_codes, value_codes);
   valid[1] = false;
   if (blk + 1 < end) fetch(blk + 1, valid[1]);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    sum_queries(q[t]);
+    clear(a, t);
+  }
   lds_barrier();
   auto blocks = [&](int to, auto ragged) {
     for (; blk < to; ++blk, half ^= 1) {
@@ -843,7 +851,7 @@ __device__ __forceinline__ void many_segment(const AttArgs& p, const Segment& s,
 }
 
 template <int TYPE, int DIM, int GROUP>
-__global__ __launch_bounds__(64 * kWaves, 2) void attend_many(AttArgs p) {
+__global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 1 : 2) void attend_many(AttArgs p) {
   extern __shared__ __align__(16) uint8_t lds[];  // two blocks' operands
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Sequences first;
@@ -986,6 +994,7 @@ __device__ __forceinline__ void weigh_segment(const AttArgs& p, const Segment& s
   auto queries = [&](int r0) {
     Queries<TYPE, DIM, GROUP> x;
     load_queries<TYPE, DIM, GROUP>(p, b, h, r0 + (lane & 15), n, lane, x);
+    sum_queries(x);
 #pragma unroll
     for (int i = 0; i < DIM / 32; ++i) q[i] = x.q[i];
 #pragma unroll
@@ -1038,7 +1047,7 @@ __device__ __forceinline__ void weigh_segment(const AttArgs& p, const Segment& s
 #pragma unroll
           for (int i = 0; i < DIM / 32; ++i) kf[t][i] = key_codes(k[t][i]);
         for (int r0 = 0; r0 < p.rows; r0 += 16) {
-          if (p.rows > 16) queries(r0);
+          if (p.rows > 16) queries(r0);  // (in attend_whole alone)
           const bool ragged = blk * 32 + 32 > n - p.n_queries + 1;
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
@@ -1266,15 +1275,19 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
     else if (blocks <= kWholeBlocks && heads * pl.row_groups <= as_host::compute_units())
       pl.whole = whole_waves(c->dim, c->group, pl.tiles);
   }
-  const int resident = pl.many ? 2 : (pl.tiles == 1 ? 4 : c->dim == 64 ? 3 : 2) - wide;
-  auto groups = [&](int64_t all, int64_t resident) {
-    const int64_t g = all < resident ? all : resident;
-    return (int)round_up(g < 1 ? 1 : g, 8);
+  const int resident = pl.many ? 2 - wide : (pl.tiles == 1 ? 4 : c->dim == 64 ? 3 : 2) - wide;
+  // As many as run at once, but no more than there can be shares: one of less
+  // than kWaves blocks only where segments are shorter (starting a workgroup
+  // takes about 4 ns, those without a share included).
+  auto groups = [&](int64_t segments, int64_t running) {
+    const int64_t most = (segments * blocks + kWaves - 1) / kWaves;
+    const int64_t g = most > segments ? most : segments;
+    return (int)round_up(g < running ? g : running, 8);
   };
   int cus = as_host::compute_units();
   if (cus > kMaxParts / 4) cus = kMaxParts / 4;
-  pl.workgroups = groups(heads * pl.row_groups * blocks, (int64_t)cus * resident);
-  pl.weigh_workgroups = groups(heads * blocks, (int64_t)cus * (pl.rows > 16 ? 2 : 3));
+  pl.workgroups = groups(heads * pl.row_groups, (int64_t)cus * resident);
+  pl.weigh_workgroups = groups(heads, (int64_t)cus * (pl.rows > 16 ? 2 : 3));
   pl.parts = pl.workgroups / (heads * pl.row_groups);
   if (pl.parts > blocks / kWaves) pl.parts = blocks / kWaves;
   const int64_t places = (int64_t)pl.workgroups * 2 * 16 * pl.tiles;
