@@ -43,6 +43,8 @@ struct AttArgs {
   int32_t n_queries, per, rows;
   int32_t row_groups, row_span;  // parts of 16 tiles query rows
   int32_t workgroups, weigh_workgroups;
+  int32_t round, weigh_round;  // log2 of a round's blocks
+  int32_t least;               // rounds of a share, at least
 };
 
 // ---------------------------------------------------------------- 4-bit codes
@@ -367,12 +369,16 @@ __device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int lane
 // ----------------------------------------------------------------- the shares
 
 // A segment is what 16 NT query rows of one head see of one sequence, in blocks
-// of 32 slots; the segments of all sequences, heads and row groups, one after
-// the other, are dealt to the workgroups in shares of one size, whatever the
-// lengths.  All workgroups run at once: there is no tail, and none is started for
-// slots that a table has room for but a sequence does not use.  A segment that
-// lies within a share is finished there; of another one, each workgroup leaves
-// its part: in place 1 the one that begins it, in place 0 the others.
+// of 32 slots, and a round what a workgroup does of it at once: a block for each
+// wavefront, or one block that all of them work at.  The rounds of all sequences,
+// heads and row groups, one after the other, are dealt to the workgroups in
+// shares of one size, whatever the lengths.  All workgroups run at once: there is
+// no tail, and none is started for slots that a table has room for but a sequence
+// does not use.  A segment that lies within a share is finished there; of another
+// one, each workgroup leaves its part: in place 1 the one that begins it, in
+// place 0 the others.  (Shares of blocks rather than rounds put the last block
+// of one segment and the first of the next into one share, which then takes two
+// rounds: 10 us for 8 segments of 129 blocks, a round each.)
 struct Segment {
   int b, h, rg, n;
   int blk, seen;  // first block of the share, blocks of the segment
@@ -386,18 +392,24 @@ __device__ __forceinline__ int seen_blocks(const AttArgs& p, int n, int rg, int&
   return max(0, (last + 31) / 32);
 }
 
-// Blocks of all segments of one head of a sequence.  WEIGH: one segment of all
-// rows.
+// Rounds of so many blocks.  WEIGH: one segment of all rows.
 template <bool WEIGH>
-__device__ __forceinline__ uint32_t head_blocks(const AttArgs& p, int n) {
-  if (WEIGH || p.row_groups == 1) return (uint32_t)(n + 31) / 32;
+__device__ __forceinline__ uint32_t rounds(const AttArgs& p, int blocks) {
+  const int log2 = WEIGH ? p.weigh_round : p.round;
+  return (uint32_t)(blocks + (1 << log2) - 1) >> log2;
+}
+
+// Rounds of all segments of one head of a sequence.
+template <bool WEIGH>
+__device__ __forceinline__ uint32_t head_rounds(const AttArgs& p, int n) {
+  if (WEIGH || p.row_groups == 1) return rounds<WEIGH>(p, (n + 31) / 32);
   uint32_t sum = 0;
   int least;
-  for (int rg = 0; rg < p.row_groups; ++rg) sum += (uint32_t)seen_blocks(p, n, rg, least);
+  for (int rg = 0; rg < p.row_groups; ++rg) sum += rounds<false>(p, seen_blocks(p, n, rg, least));
   return sum;
 }
 
-// 64 sequences from b0 on: the lane's length, and the sum of the blocks of the
+// 64 sequences from b0 on: the lane's length, and the sum of the rounds of the
 // sequences up to and with the lane's.
 struct Sequences {
   int n;
@@ -408,27 +420,22 @@ __device__ __forceinline__ Sequences scan_sequences(const AttArgs& p, int b0, in
   const int b = b0 + lane;
   Sequences s;
   s.n = b < p.c.n_seqs ? clamped_length(p, b) : 0;
-  s.sum = scan_lanes(head_blocks<WEIGH>(p, s.n) * (uint32_t)p.c.n_heads);
+  s.sum = scan_lanes(head_rounds<WEIGH>(p, s.n) * (uint32_t)p.c.n_heads);
   return s;
 }
-__device__ __forceinline__ uint32_t all_blocks(const Sequences& s) {
+__device__ __forceinline__ uint32_t all_rounds(const Sequences& s) {
   return (uint32_t)__builtin_amdgcn_readlane((int)s.sum, 63);
 }
 
-// Blocks in all, and the size of a share: at least a block for each of a
-// workgroup's wavefronts where segments are that long.  first: the scan of the
-// first 64 sequences.
+// Rounds in all, and the size of a share.  first: the scan of the first 64
+// sequences.
 template <bool WEIGH>
 __device__ __forceinline__ uint32_t share_size(const AttArgs& p, int lane, Sequences& first, uint32_t& total) {
   first = scan_sequences<WEIGH>(p, 0, lane);
-  total = all_blocks(first);
-  for (int b0 = 64; b0 < p.c.n_seqs; b0 += 64) total += all_blocks(scan_sequences<WEIGH>(p, b0, lane));
-  const uint32_t segments = (uint32_t)(p.c.n_seqs * p.c.n_heads) * (WEIGH ? 1u : (uint32_t)p.row_groups);
+  total = all_rounds(first);
+  for (int b0 = 64; b0 < p.c.n_seqs; b0 += 64) total += all_rounds(scan_sequences<WEIGH>(p, b0, lane));
   const uint32_t groups = (uint32_t)(WEIGH ? p.weigh_workgroups : p.workgroups);
-  uint32_t least = 1;  // min(mean length of a segment, kWaves)
-#pragma unroll
-  for (int w = 2; w <= kWaves; ++w) least += total > (uint64_t)segments * (w - 1);
-  return max((total + groups - 1) / groups, least);
+  return max((total + groups - 1) / groups, WEIGH ? 1u : (uint32_t)p.least);
 }
 
 // This workgroup's share's number, or -1.  Neighbouring workgroup numbers go to
@@ -440,14 +447,14 @@ __device__ __forceinline__ int64_t share_number(uint32_t total, uint32_t size) {
   return (blockIdx.x >> 3) < per_xcd && at < shares ? (int64_t)at : -1;
 }
 
-// The segment that holds block `unit` of all.
+// The segment that holds round `unit` of all.
 template <bool WEIGH>
 __device__ __forceinline__ Segment locate(const AttArgs& p, uint32_t unit, int lane, const Sequences& first) {
   uint32_t before = 0;
   Sequences q = first;
   int b0 = 0;
-  while (unit >= before + all_blocks(q) && b0 + 64 < p.c.n_seqs) {
-    before += all_blocks(q);
+  while (unit >= before + all_rounds(q) && b0 + 64 < p.c.n_seqs) {
+    before += all_rounds(q);
     q = scan_sequences<WEIGH>(p, b0 += 64, lane);
   }
   const uint64_t past = __ballot(before + q.sum > unit);
@@ -456,18 +463,18 @@ __device__ __forceinline__ Segment locate(const AttArgs& p, uint32_t unit, int l
   Segment s;
   s.b = b0 + i;
   s.n = __builtin_amdgcn_readlane(q.n, i);
-  const uint32_t per_head = max(1u, head_blocks<WEIGH>(p, s.n));
+  const uint32_t per_head = max(1u, head_rounds<WEIGH>(p, s.n));
   uint32_t off = unit - before;
   s.h = (int)(off / per_head);
   off -= (uint32_t)s.h * per_head;
   s.rg = 0;
   int least;
   s.seen = WEIGH ? (s.n + 31) / 32 : seen_blocks(p, s.n, 0, least);
-  while (!WEIGH && s.rg + 1 < p.row_groups && off >= (uint32_t)s.seen) {
-    off -= (uint32_t)s.seen;
+  while (!WEIGH && s.rg + 1 < p.row_groups && off >= rounds<false>(p, s.seen)) {
+    off -= rounds<false>(p, s.seen);
     s.seen = seen_blocks(p, s.n, ++s.rg, least);
   }
-  s.blk = (int)off;
+  s.blk = (int)(off << (WEIGH ? p.weigh_round : p.round));
   return s;
 }
 
@@ -646,9 +653,9 @@ __global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : DIM == 64 ? 3 : 2) - (D
   int left = (int)min(size, total - unit);
   Segment g = locate<false>(p, unit, lane, first);
   for (;;) {
-    const int take = min(left, g.seen - g.blk);
+    const int take = min(left << p.round, g.seen - g.blk);
     attend_segment<TYPE, DIM, GROUP, NT, kWaves>(p, g, take, (int)share, lane, wave, lds, ml);
-    left -= take;
+    left -= (int)rounds<false>(p, take);
     if (left == 0) return;
     advance<false>(p, g);
   }
@@ -863,9 +870,9 @@ __global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 1 : 2) void attend_
   int left = (int)min(size, total - unit);
   Segment g = locate<false>(p, unit, lane, first);
   for (;;) {
-    const int take = min(left, g.seen - g.blk);
+    const int take = min(left << p.round, g.seen - g.blk);
     many_segment<TYPE, DIM, GROUP>(p, g, take, (int)share, lane, wave, lds);
-    left -= take;
+    left -= (int)rounds<false>(p, take);
     if (left == 0) return;
     advance<false>(p, g);
   }
@@ -902,7 +909,7 @@ __global__ __launch_bounds__(THREADS) void join(AttArgs p) {
     }
     return;
   }
-  // the segment's first block among all
+  // the segment's first round among all
   Sequences first;
   uint32_t total;
   const uint32_t size = share_size<false>(p, lane, first, total);
@@ -911,9 +918,9 @@ __global__ __launch_bounds__(THREADS) void join(AttArgs p) {
     if (b0) first = scan_sequences<false>(p, b0, lane);
     start += (uint32_t)__builtin_amdgcn_readlane((int)first.sum, min(63, b - 1 - b0));
   }
-  start += (uint32_t)h * head_blocks<false>(p, n);
-  for (int r = 0; r < rg; ++r) start += (uint32_t)seen_blocks(p, n, r, least);
-  const int share = (int)(start / size), parts = (int)((start + seen - 1) / size) - share + 1;
+  start += (uint32_t)h * head_rounds<false>(p, n);
+  for (int r = 0; r < rg; ++r) start += rounds<false>(p, seen_blocks(p, n, r, least));
+  const int share = (int)(start / size), parts = (int)((start + rounds<false>(p, seen) - 1) / size) - share + 1;
   if (parts == 1) return;  // finished where it was
   for (; row < end; row += ROWS) {
     auto at = [&](int s) { return ((int64_t)(share + s) * 2 + (s == 0)) * p.row_span + row - rg * p.row_span; };
@@ -1204,12 +1211,12 @@ __global__ __launch_bounds__(64 * kWaves, MANY ? 2 : 3) void weigh(AttArgs p) {
   int left = (int)min(size, total - unit);
   Segment g = locate<true>(p, unit, lane, first);
   for (;;) {
-    const int take = min(left, g.seen - g.blk);
+    const int take = min(left << p.weigh_round, g.seen - g.blk);
     if (MANY)
       weigh_rows<TYPE, DIM, GROUP, 256 / DIM>(p, g, take, lane, wave);
     else
       weigh_segment<TYPE, DIM, GROUP, kWaves>(p, g, take, lane, wave, lds);
-    left -= take;
+    left -= (int)rounds<true>(p, take);
     if (left == 0) return;
     advance<true>(p, g);
   }
@@ -1244,6 +1251,7 @@ struct Plan {
   bool many;
   int whole;  // wavefronts of attend_whole, kWaves or more, or 0
   int per, rows, tiles, row_groups, workgroups, weigh_workgroups;
+  int round, weigh_round, least;  // as in AttArgs
   int64_t parts;  // of a segment, at most, where all have one length
   int64_t o_bytes, ml_bytes, row_bytes;
 };
@@ -1276,18 +1284,20 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
       pl.whole = whole_waves(c->dim, c->group, pl.tiles);
   }
   const int resident = pl.many ? 2 - wide : (pl.tiles == 1 ? 4 : c->dim == 64 ? 3 : 2) - wide;
-  // As many as run at once, but no more than there can be shares: one of less
-  // than kWaves blocks only where segments are shorter (starting a workgroup
-  // takes about 4 ns, those without a share included).
-  auto groups = [&](int64_t segments, int64_t running) {
-    const int64_t most = (segments * blocks + kWaves - 1) / kWaves;
-    const int64_t g = most > segments ? most : segments;
-    return (int)round_up(g < running ? g : running, 8);
+  pl.round = pl.many ? 0 : 2;
+  pl.least = pl.many ? kWaves : 1;
+  pl.weigh_round = pl.rows <= 16 ? 2 : c->dim == 128 ? 3 : 4;
+  static_assert(kWaves == 4, "rounds");
+  // As many as run at once, but no more than there can be shares (starting a
+  // workgroup takes about 4 ns, those without a share included).
+  auto groups = [&](int64_t segments, int64_t in_share, int64_t running) {
+    const int64_t most = segments * ((blocks + in_share - 1) / in_share);
+    return (int)round_up(most > running ? running : most < 1 ? 1 : most, 8);
   };
   int cus = as_host::compute_units();
   if (cus > kMaxParts / 4) cus = kMaxParts / 4;
-  pl.workgroups = groups(heads * pl.row_groups, (int64_t)cus * resident);
-  pl.weigh_workgroups = groups(heads, (int64_t)cus * (pl.rows > 16 ? 2 : 3));
+  pl.workgroups = groups(heads * pl.row_groups, kWaves, (int64_t)cus * resident);
+  pl.weigh_workgroups = groups(heads, 1 << pl.weigh_round, (int64_t)cus * (pl.rows > 16 ? 2 : 3));
   pl.parts = pl.workgroups / (heads * pl.row_groups);
   if (pl.parts > blocks / kWaves) pl.parts = blocks / kWaves;
   const int64_t places = (int64_t)pl.workgroups * 2 * 16 * pl.tiles;
@@ -1425,6 +1435,9 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
   p.row_span = 16 * pl.tiles;
   p.workgroups = pl.workgroups;
   p.weigh_workgroups = pl.weigh_workgroups;
+  p.round = pl.round;
+  p.weigh_round = pl.weigh_round;
+  p.least = pl.least;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return type == AS_BF16 ? launch_by_shape<AS_BF16>(p, pl, s) : launch_by_shape<AS_F16>(p, pl, s);
 }
