@@ -238,7 +238,6 @@ struct LinArgs {
   void* y;
   int64_t y_stride;
   int32_t n_tokens, n_out, k_tiles;
-  bool y_vec;            // four neighbouring channels can be stored at once
   // activations, where the product quantises them
   const void* x;
   int64_t x_stride;
@@ -253,14 +252,16 @@ __device__ __forceinline__ void store_one(void* y, int64_t i, float v) {
     reinterpret_cast<uint16_t*>(y)[i] = from_f32<YTYPE>(v);
 }
 
+// (rows of an odd length are at any address: one store all the same)
 template <int YTYPE>
 __device__ __forceinline__ void store_four(void* y, int64_t i, const float (&v)[4]) {
   if (YTYPE == AS_F32) {
-    *reinterpret_cast<v4f*>(reinterpret_cast<float*>(y) + i) = v4f{v[0], v[1], v[2], v[3]};
+    __builtin_memcpy(reinterpret_cast<float*>(y) + i, v, 16);
   } else {
     const uint32_t lo = from_f32<YTYPE>(v[0]) | (uint32_t)from_f32<YTYPE>(v[1]) << 16;
     const uint32_t hi = from_f32<YTYPE>(v[2]) | (uint32_t)from_f32<YTYPE>(v[3]) << 16;
-    *reinterpret_cast<v2u*>(reinterpret_cast<uint16_t*>(y) + i) = v2u{lo, hi};
+    const v2u two = {lo, hi};
+    __builtin_memcpy(reinterpret_cast<uint16_t*>(y) + i, &two, 8);
   }
 }
 
@@ -476,26 +477,36 @@ __global__ __launch_bounds__(64 * WC * WT) void product_many(LinArgs p) {
     wait_reads();
     slot = slot + 1 == S ? 0 : slot + 1;
   }
+  float s[kT];
 #pragma unroll
-  for (int j = 0; j < kT; ++j) {
-    const int t = (t0 + wt + j) * 16 + (lane & 15);
-    if (t >= p.n_tokens) continue;
-    const float s = p.a_scale[t];
+  for (int j = 0; j < kT; ++j) s[j] = p.a_scale[min((t0 + wt + j) * 16 + (lane & 15), p.n_tokens - 1)];
 #pragma unroll
-    for (int i = 0; i < kC; ++i) {
-      const int n = (c0 + wc + i) * 16 + (lane >> 4) * 4;
-      if (p.y_vec && n + 4 <= p.n_out) {
+  for (int i = 0; i < kC; ++i) {
+    const int n = (c0 + wc + i) * 16 + (lane >> 4) * 4;
+    if (n + 4 <= p.n_out) {
+      float u[4], bias[4] = {};
+      __builtin_memcpy(u, p.w_scale + n, 16);
+      if (p.bias) __builtin_memcpy(bias, p.bias + n, 16);
+#pragma unroll
+      for (int j = 0; j < kT; ++j) {
+        const int t = (t0 + wt + j) * 16 + (lane & 15);
+        if (t >= p.n_tokens) continue;
         float v[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          v[r] = (float)acc[i][j][r] * s * p.w_scale[n + r];
-          if (p.bias) v[r] += p.bias[n + r];
+          v[r] = (float)acc[i][j][r] * s[j] * u[r];
+          if (p.bias) v[r] += bias[r];
         }
         store_four<YTYPE>(p.y, (int64_t)t * p.y_stride + n, v);
-      } else {
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kT; ++j) {
+        const int t = (t0 + wt + j) * 16 + (lane & 15);
+        if (t >= p.n_tokens) continue;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (n + r < p.n_out) finish<YTYPE>(p, t, n + r, acc[i][j][r], s);
+          if (n + r < p.n_out) finish<YTYPE>(p, t, n + r, acc[i][j][r], s[j]);
       }
     }
   }
@@ -627,7 +638,6 @@ int as_linear_i8(const void* x, int32_t x_type, int64_t n_tokens, int64_t n_in, 
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   uint8_t* codes = reinterpret_cast<uint8_t*>(workspace);
   float* scale = reinterpret_cast<float*>(codes + as_i8_bytes(n_tokens, n_in));
-  const int y_bytes = y_type == AS_F32 ? 4 : 2;
   LinArgs p{};
   p.a = codes;
   p.a_scale = scale;
@@ -639,7 +649,6 @@ int as_linear_i8(const void* x, int32_t x_type, int64_t n_tokens, int64_t n_in, 
   p.n_tokens = (int32_t)n_tokens;
   p.n_out = (int32_t)n_out;
   p.k_tiles = (int32_t)(round_up(n_in, 128) / 64);
-  p.y_vec = aligned(y, 4 * y_bytes) && y_stride % 4 == 0;
   p.x = x;
   p.x_stride = x_stride;
   p.n_in = (int32_t)n_in;
