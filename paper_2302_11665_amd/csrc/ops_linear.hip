@@ -265,6 +265,17 @@ __device__ __forceinline__ void store_four(void* y, int64_t i, const float (&v)[
   }
 }
 
+// a's upper 32 lanes and b's lower ones change places; then, of each 32 lanes,
+// a's upper 16 and b's lower ones.
+__device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
+  const v2u p = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = p[0], b = p[1];
+}
+__device__ __forceinline__ void swap_rows(uint32_t& a, uint32_t& b) {
+  const v2u p = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  a = p[0], b = p[1];
+}
+
 // 8 values from column c of a row of 16-bit values; columns beyond n are 0.
 template <int TYPE>
 __device__ __forceinline__ void load8(const uint16_t* x, int64_t row, int c, int n, float (&f)[8]) {
@@ -480,6 +491,53 @@ __global__ __launch_bounds__(64 * WC * WT) void product_many(LinArgs p) {
   float s[kT];
 #pragma unroll
   for (int j = 0; j < kT; ++j) s[j] = p.a_scale[min((t0 + wt + j) * 16 + (lane & 15), p.n_tokens - 1)];
+  // Where the wavefront has 64 channels side by side, the four lanes of a token
+  // exchange theirs: 32 bytes a lane, 128 side by side, not four times 32.
+  constexpr bool kSwap = YTYPE != AS_F32 && kC % 4 == 0;
+  if (kSwap && (c0 + wc + kC) * 16 <= p.n_out) {
+#pragma unroll
+    for (int i = 0; i < kC; i += 4) {
+      const int n = (c0 + wc + i) * 16 + (lane >> 4) * 4;
+      float u[4][4], bias[4][4] = {};
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        __builtin_memcpy(u[z], p.w_scale + n + 16 * z, 16);
+        if (p.bias) __builtin_memcpy(bias[z], p.bias + n + 16 * z, 16);
+      }
+#pragma unroll
+      for (int j = 0; j < kT; ++j) {
+        const int t = (t0 + wt + j) * 16 + (lane & 15);
+        uint32_t w[2][4];  // of tile z: channels 0 and 1, 2 and 3 of the lane's four
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          float v[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            v[r] = (float)acc[i + z][j][r] * s[j] * u[z][r];
+            if (p.bias) v[r] += bias[z][r];
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            w[h][z] = from_f32<YTYPE>(v[2 * h]) | (uint32_t)from_f32<YTYPE>(v[2 * h + 1]) << 16;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {  // tile z's quarter g to tile g's quarter z
+          swap_halves(w[h][0], w[h][2]);
+          swap_halves(w[h][1], w[h][3]);
+          swap_rows(w[h][0], w[h][1]);
+          swap_rows(w[h][2], w[h][3]);
+        }
+        if (t >= p.n_tokens) continue;
+        uint16_t* y = reinterpret_cast<uint16_t*>(p.y) + (int64_t)t * p.y_stride + (c0 + wc + i + (lane >> 4)) * 16;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const v4u two = {w[0][2 * h], w[1][2 * h], w[0][2 * h + 1], w[1][2 * h + 1]};
+          __builtin_memcpy(y + 8 * h, &two, 16);
+        }
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < kC; ++i) {
     const int n = (c0 + wc + i) * 16 + (lane >> 4) * 4;
@@ -551,9 +609,15 @@ int launch_product(const LinArgs& p, hipStream_t s) {
   if (n_tt == 2) return few_by_channels<YTYPE, AS_BF16, 2, false>(p, s);
   if (n_tt == 3) return few_by_channels<YTYPE, AS_BF16, 3, false>(p, s);
   if (n_tt == 4) return few_by_channels<YTYPE, AS_BF16, 4, false>(p, s);
+  // A compute unit runs one workgroup of 256 x 256 or two of 128 x 128, which take
+  // 1.15 times as long for as much work (4096 tokens 8192 -> 8192: 296 us against
+  // 268) but leave fewer units idle at the end: 1187 tokens 8192 -> 13712 take 3
+  // turns of them, 174 us, and 2 of the larger ones, each as long as 1.7 (222 us).
   const int64_t n_ct = (p.n_out + 15) / 16, cus = as_host::compute_units();
-  if (((n_ct + 15) / 16) * ((n_tt + 15) / 16) >= cus) return launch_many<YTYPE, 16, 16, 2, 4, 2, 2>(p, s);
-  if (((n_ct + 7) / 8) * ((n_tt + 7) / 8) >= cus) return launch_many<YTYPE, 8, 8, 2, 4, 2, 2>(p, s);
+  const int64_t large = ((n_ct + 15) / 16) * ((n_tt + 15) / 16), middle = ((n_ct + 7) / 8) * ((n_tt + 7) / 8);
+  const int64_t large_turns = (large + cus - 1) / cus, middle_turns = (middle + 2 * cus - 1) / (2 * cus);
+  if (large >= cus && large_turns * 200 <= middle_turns * 115) return launch_many<YTYPE, 16, 16, 2, 4, 2, 2>(p, s);
+  if (middle >= cus) return launch_many<YTYPE, 8, 8, 2, 4, 2, 2>(p, s);
   // Two workgroups of either of these run on a compute unit; the smaller tiles
   // where all of them run at once (333 tokens 1500 -> 2777: 264 tiles of 64 x 64 took
   // 12.6 us, 484 of 64 x 32 took 9.8).
