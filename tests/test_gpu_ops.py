@@ -113,6 +113,21 @@ def test_linear_rows_that_are_not_finite():
     assert torch.isnan(y[0]).all() and torch.isnan(y[7]).all() and (y[19] == 0).all()
 
 
+@pytest.mark.parametrize("t,k,n", [(4090, 130, 4081), (4096, 256, 4096), (2050, 200, 4097), (1111, 130, 2111), (200, 130, 610)])
+@pytest.mark.parametrize("x_dtype,y_dtype,bias", [(BF16, BF16, True), (F16, F16, False), (BF16, F32, True)])
+def test_linear_tiles_to_outputs_at_odd_places(t, k, n, x_dtype, y_dtype, bias):
+    say("linear tiles", t, k, n, x_dtype, y_dtype, bias)
+    g = gen(t + k + n)
+    x = normal(g, t, k, dtype=x_dtype)
+    w = ops.pack_weight(normal(g, n, k))
+    b = normal(g, n) if bias else None
+    y = torch.full((t, n + 3), 7.0, device="cuda", dtype=y_dtype)
+    ops.linear_i8(x, w, bias=b, out=y[:, 1:n + 1])
+    assert (y[:, 0] == 7.0).all() and (y[:, n + 1:] == 7.0).all()
+    codes = w.codes.cpu().numpy()[oo.tile_index(n, k)]
+    check_linear(x, codes, f64(w.scale), f64(b) if bias else None, y[:, 1:n + 1], y_dtype)
+
+
 @pytest.mark.parametrize("t", [1, 5, 40, 300])
 def test_linear_strides_and_shapes(t):
     g = gen(t)
