@@ -639,8 +639,11 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
 // One workgroup per share; its four wavefronts take a segment's blocks in turn,
 // each with a ring of its own in LDS so that none waits for another, and join
 // their results at the segment's end.
-template <int TYPE, int DIM, int GROUP, int NT>
-__global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : DIM == 64 ? 3 : 2) - (DIM == 4 * GROUP)) void attend(AttArgs p) {
+// (Segments of 32 rows, so that codes are expanded once for both halves, took as
+// long, 77 us for 9 sequences of up to 90,000 slots, 2 heads of 20 rows each, or
+// longer: 57 us, 49 in segments of 16, for 40 rows; they leave half the wavefronts.)
+template <int TYPE, int DIM, int GROUP>
+__global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 3 : 4) void attend(AttArgs p) {
   __shared__ float ml[kWaves][16][2];
   extern __shared__ __align__(16) uint8_t lds[];  // the rings, then the parts to be joined
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -654,7 +657,7 @@ __global__ __launch_bounds__(64 * kWaves, (NT == 1 ? 4 : DIM == 64 ? 3 : 2) - (D
   Segment g = locate<false>(p, unit, lane, first);
   for (;;) {
     const int take = min(left << p.round, g.seen - g.blk);
-    attend_segment<TYPE, DIM, GROUP, NT, kWaves>(p, g, take, (int)share, lane, wave, lds, ml);
+    attend_segment<TYPE, DIM, GROUP, 1, kWaves>(p, g, take, (int)share, lane, wave, lds, ml);
     left -= (int)rounds<false>(p, take);
     if (left == 0) return;
     advance<false>(p, g);
@@ -1271,8 +1274,11 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   pl.per = n_q_heads / c->n_heads;
   pl.rows = pl.per * n_queries;
   pl.many = pl.rows >= kManyRows * 3 / 4;  // three of four wavefronts have rows
-  pl.tiles = pl.many ? kManyRows / 16 : pl.rows > 16 ? 2 : 1;
-  pl.row_groups = (pl.rows + 16 * pl.tiles - 1) / (16 * pl.tiles);
+  auto set_tiles = [&](int tiles) {
+    pl.tiles = tiles;
+    pl.row_groups = (pl.rows + 16 * tiles - 1) / (16 * tiles);
+  };
+  set_tiles(pl.many ? kManyRows / 16 : pl.rows > 16 ? 2 : 1);
   const int64_t heads = (int64_t)c->n_seqs * c->n_heads;
   const int64_t blocks = (int64_t)c->max_pages * c->page / 32;
   const int wide = c->dim == 4 * c->group;
@@ -1283,7 +1289,8 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
     else if (blocks <= kWholeBlocks && heads * pl.row_groups <= as_host::compute_units())
       pl.whole = whole_waves(c->dim, c->group, pl.tiles);
   }
-  const int resident = pl.many ? 2 - wide : (pl.tiles == 1 ? 4 : c->dim == 64 ? 3 : 2) - wide;
+  if (!pl.many && !pl.whole) set_tiles(1);
+  const int resident = (pl.many ? 2 : 4) - wide;
   pl.round = pl.many ? 0 : 2;
   pl.least = pl.many ? kWaves : 1;
   pl.weigh_round = pl.rows <= 16 ? 2 : c->dim == 128 ? 3 : 4;
@@ -1350,13 +1357,11 @@ int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
   typedef Operands<DIM, GROUP> OperandSet;
   if (pl.many)
     hipLaunchKernelGGL((attend_many<TYPE, DIM, GROUP>), g, t, (size_t)2 * OperandSet::kBytes, s, p);
-  else if (pl.tiles == 1)
-    hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 1>), g, t, lds, s, p);
   else
-    hipLaunchKernelGGL((attend<TYPE, DIM, GROUP, 2>), g, t, lds, s, p);
+    hipLaunchKernelGGL((attend<TYPE, DIM, GROUP>), g, t, lds, s, p);
   const int64_t heads = (int64_t)p.c.n_seqs * p.c.n_heads;
   const dim3 by_row((unsigned)(heads * p.rows));
-  if (p.row_groups > 1)
+  if (pl.many || pl.parts < 8)
     hipLaunchKernelGGL((join<TYPE, DIM, 1024 / DIM, 256>), dim3((unsigned)(heads * ((p.rows + 15) / 16))), dim3(256), 0,
                        s, p);
   else if (pl.parts >= 64)
