@@ -861,7 +861,7 @@ __device__ __forceinline__ void many_segment(const AttArgs& p, const Segment& s,
 }
 
 template <int TYPE, int DIM, int GROUP>
-__global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 1 : 2) void attend_many(AttArgs p) {
+__global__ __launch_bounds__(64 * kWaves, 2) void attend_many(AttArgs p) {
   extern __shared__ __align__(16) uint8_t lds[];  // two blocks' operands
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Sequences first;
@@ -1273,7 +1273,13 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   Plan pl;
   pl.per = n_q_heads / c->n_heads;
   pl.rows = pl.per * n_queries;
-  pl.many = pl.rows >= kManyRows * 3 / 4;  // three of four wavefronts have rows
+  // attend_many takes 4/5 as long for a row, empty ones of its 128 included (128
+  // channels in groups of 64, 9 sequences of up to 30,000 slots, 2 heads: 78 us
+  // against 86 for 100 rows, 140 against 106 for 130, 206 against 191 for 260), but
+  // longer with groups of a fourth of the channels, whose sums leave room for one
+  // wavefront a SIMD: 390 us against 261 for 260 rows.
+  const bool wide = c->dim == 4 * c->group;
+  pl.many = !wide && round_up(pl.rows, kManyRows) * 4 <= round_up(pl.rows, 16) * 5;
   auto set_tiles = [&](int tiles) {
     pl.tiles = tiles;
     pl.row_groups = (pl.rows + 16 * tiles - 1) / (16 * tiles);
@@ -1281,7 +1287,6 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   set_tiles(pl.many ? kManyRows / 16 : pl.rows > 16 ? 2 : 1);
   const int64_t heads = (int64_t)c->n_seqs * c->n_heads;
   const int64_t blocks = (int64_t)c->max_pages * c->page / 32;
-  const int wide = c->dim == 4 * c->group;
   pl.whole = 0;
   if (!pl.many && (!weights || pl.row_groups == 1)) {
     if (blocks <= kShortBlocks)
@@ -1290,7 +1295,7 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
       pl.whole = whole_waves(c->dim, c->group, pl.tiles);
   }
   if (!pl.many && !pl.whole) set_tiles(1);
-  const int resident = (pl.many ? 2 : 4) - wide;
+  const int resident = pl.many ? 2 : wide ? 3 : 4;
   pl.round = pl.many ? 0 : 2;
   pl.least = pl.many ? kWaves : 1;
   pl.weigh_round = pl.rows <= 16 ? 2 : c->dim == 128 ? 3 : 4;
@@ -1355,10 +1360,11 @@ int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
   const dim3 g((unsigned)pl.workgroups), t(64 * kWaves);
   const size_t lds = attend_lds<DIM, GROUP>(kWaves);
   typedef Operands<DIM, GROUP> OperandSet;
-  if (pl.many)
-    hipLaunchKernelGGL((attend_many<TYPE, DIM, GROUP>), g, t, (size_t)2 * OperandSet::kBytes, s, p);
-  else
-    hipLaunchKernelGGL((attend<TYPE, DIM, GROUP>), g, t, lds, s, p);
+  if constexpr (DIM < 4 * GROUP) {
+    if (pl.many)
+      hipLaunchKernelGGL((attend_many<TYPE, DIM, GROUP>), g, t, (size_t)2 * OperandSet::kBytes, s, p);
+  }
+  if (!pl.many) hipLaunchKernelGGL((attend<TYPE, DIM, GROUP>), g, t, lds, s, p);
   const int64_t heads = (int64_t)p.c.n_seqs * p.c.n_heads;
   const dim3 by_row((unsigned)(heads * p.rows));
   if (pl.many || pl.parts < 8)
