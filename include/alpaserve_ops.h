@@ -144,11 +144,14 @@ int as_cache_append(const as_cache_t* cache, const void* k, const void* v, int32
  *            elements (multiples of 8), aligned to 16 bytes
  *   length   [n_seqs]
  *   scale    finite, > 0
- *   out      [n_seqs][n_queries][n_q_heads][dim] of `type`, contiguous
+ *   out      [n_seqs][n_queries][n_q_heads][dim] of `type`, contiguous, aligned
+ *            to 8 bytes
  *   acc_in, acc_out  laid out as cache->acc: for every slot s below the
  *            length, acc_out = acc_in + sum of p_is over the queries and heads
  *            that read the key/value head (acc_in NULL: 0; the two may be the
  *            same array); other slots are not written.  acc_out NULL: no weights
+ * At most 2^26 query rows, 65,535 sequences times heads, and 2^31 blocks of 32
+ * slots over all sequences, heads and 16 rows (AS_E_LIMITS).
  * Products of codes and 16-bit numbers with fp32 sums; softmax in fp32; p times
  * a value's scale enters its product as two bf16 numbers (17 bits).
  */

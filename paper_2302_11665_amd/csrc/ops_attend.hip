@@ -638,7 +638,11 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
 
 // One workgroup per share; its four wavefronts take a segment's blocks in turn,
 // each with a ring of its own in LDS so that none waits for another, and join
-// their results at the segment's end.
+// their results at the segment's end.  Bound by memory where rows are few (128
+// channels in groups of 64, 8 rows: 1.04 GB of long contexts in 204 us, 5.1 TB/s;
+// 403 MB of 40 ragged ones in 95 us, 4.2), by the vector instructions of codes and
+// softmax above some 16 rows, and by a round's latency, 8 us, for one short
+// sequence.
 // (Segments of 32 rows, so that codes are expanded once for both halves, took as
 // long, 77 us for 9 sequences of up to 90,000 slots, 2 heads of 20 rows each, or
 // longer: 57 us, 49 in segments of 16, for 40 rows; they leave half the wavefronts.)
@@ -671,7 +675,9 @@ __global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 3 : 4) void attend(
 // next block are on their way, and the operands of the one after this are written
 // while this one is multiplied; one barrier a block.  Bound by the vector
 // instructions of the softmax and of splitting p d, with the matrix
-// instructions close behind.
+// instructions close behind: 1200 rows a head of two sequences of up to 12,000
+// slots take 184 us, 0.52 PFLOP/s as the formula counts, 0.78 with V's second
+// product.
 constexpr int kManyRows = 128;
 
 template <int DIM, int GROUP>
@@ -884,7 +890,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(AttArgs p) {
 // Joins the parts of the segments that several workgroups had, four channels to
 // a thread.  ROWS = 1: a workgroup joins one row, its parts side by side (few
 // rows, and a long segment may have hundreds of parts); otherwise a workgroup
-// joins ROWS rows of a segment, or 16.
+// joins ROWS rows of a segment, or 16.  Bound by latency: 3.6 us for 32 rows of 33
+// parts, 5.4 for 320 segments of 3 parts (7.6 with a workgroup to a row), 14 for
+// 1200 rows of 16 heads.
 constexpr int kMaxParts = 2048;
 
 template <int TYPE, int DIM, int ROWS, int THREADS>
@@ -963,6 +971,9 @@ __global__ __launch_bounds__(THREADS) void join(AttArgs p) {
 // and sum are known; shares as before, all rows of a head in one segment.  The
 // product is q K^T here, so that a lane has one slot and four queries: a slot's
 // sum over the queries stays in the lane but for two steps across rows of lanes.
+// 61 us for 225 MB of keys and weights (40 sequences of 8 heads, 8 rows): 3.7 TB/s,
+// memory and vector instructions about even; three blocks on their way to each
+// wavefront, three workgroups a compute unit (four spill: 64 us).
 constexpr int kWeighStages = 3;
 
 template <int TYPE, int DIM, int GROUP, int NW>
@@ -1096,7 +1107,8 @@ __device__ __forceinline__ void weigh_segment(const AttArgs& p, const Segment& s
 // More than 16 rows: a wavefront keeps the expanded keys of BLOCKS blocks in
 // registers and goes over the rows, 16 at a time; the other wavefronts of the
 // workgroup read the same rows at about the same time.  The sums of q come from
-// the matrix instructions too, as a product with ones.
+// the matrix instructions too, as a product with ones.  Bound by the exponentials
+// and sums, 1200 rows over two sequences of up to 12,000 slots take 180 us.
 template <int TYPE, int DIM, int GROUP, int BLOCKS>
 __device__ __forceinline__ void weigh_rows(const AttArgs& p, const Segment& s, int take, int lane, int wave) {
   constexpr int NG = DIM / GROUP;

@@ -99,7 +99,7 @@ struct Quantiser {
 
 // One workgroup per row: its largest magnitude, then its codes; the second
 // reading comes from the caches.  Bound by latency for few rows, by the bytes
-// of x for many.
+// of x for many: 48 rows of 4096 take 3.3 us, 1187 of 282 5.6 us.
 template <int TYPE>
 __global__ __launch_bounds__(kQThreads) void quantize_rows(const void* __restrict__ x, int64_t n_cols,
                                                            int64_t row_stride, int64_t padded,
@@ -142,7 +142,8 @@ __global__ __launch_bounds__(kQThreads) void quantize_rows(const void* __restric
 // which has 16 columns of one row of every 64 x 16th tile and keeps them in
 // registers, so that x is read once and the codes are written as contiguous
 // tiles.  Bound by the bytes: 4096 rows of 8192 took 47 us with a workgroup per
-// row, 32 us with a wavefront per row, whose codes go out 16 bytes at a time.
+// row, 32 us with a wavefront per row, whose codes go out 16 bytes at a time, and
+// take 21 us so (67 MB read, 34 written: 4.7 TB/s).
 template <int TYPE, int TILES>
 __global__ __launch_bounds__(1024) void quantize_tiles(const uint16_t* __restrict__ x, int64_t n_rows, int n_cols,
                                                        int64_t row_stride, int k_tiles, uint8_t* __restrict__ codes,
@@ -307,7 +308,9 @@ __device__ __forceinline__ void finish(const LinArgs& p, int t, int n, int sum, 
 // from memory to registers, 1 KiB a load, several in flight.
 // FUSED (at most 16 tokens): the workgroup quantises the activations itself,
 // into LDS, with its first weights already on their way; this repeats little
-// work in every workgroup and saves a launch.
+// work in every workgroup and saves a launch.  1 token 4096 -> 4096: 5.0 us (3.3
+// TB/s of weights: a launch, two passes over the token and the last sums are half
+// of it), 8.4 us a call by the host; 48 tokens 4096 -> 16384: 16.7 us, 4.0 TB/s.
 constexpr int kFewWaves = 8;
 
 template <int YTYPE, int XTYPE, int CT, int TT, bool FUSED>
@@ -424,7 +427,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void product_few(LinArgs p) {
 // multiplied; one barrier a stage.  Neighbouring workgroup numbers go to different
 // XCDs, so each XCD gets a contiguous run of tiles in an order that walks the
 // channels in bands of 8: the tiles that run together share rows of both
-// operands in its L2.
+// operands in its L2.  4096 tokens 8192 -> 8192: 218 us in tiles of 256 x 256, 2.5
+// POP/s; 333 tokens 1500 -> 2777: 7 us.
 template <int YTYPE, int TC, int TT, int WC, int WT, int KS, int S>
 __global__ __launch_bounds__(64 * WC * WT) void product_many(LinArgs p) {
   constexpr int kW = WC * WT, kC = TC / WC, kT = TT / WT, kStage = (TC + TT) * KS, kLoads = kStage / kW;
