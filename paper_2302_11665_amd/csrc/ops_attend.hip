@@ -45,6 +45,7 @@ struct AttArgs {
   int32_t workgroups, weigh_workgroups;
   int32_t round, weigh_round;  // log2 of a round's blocks
   int32_t least;               // rounds of a share, at least
+  int32_t alone;               // attend_many: a segment to a workgroup
 };
 
 // ---------------------------------------------------------------- 4-bit codes
@@ -822,9 +823,11 @@ __device__ __forceinline__ void many_segment(const AttArgs& p, const Segment& s,
     ok = row >= 0;
     if (p.c.n_pages > 0) quarter.fetch(p, row, at, lane, wave);
   };
-  fetch(blk, valid[0]);
-  quarter.store(lds, lane, wave, key_codes, value_codes);
-  valid[1] = false;
+  valid[0] = valid[1] = false;
+  if (blk < end) {
+    fetch(blk, valid[0]);
+    quarter.store(lds, lane, wave, key_codes, value_codes);
+  }
   if (blk + 1 < end) fetch(blk + 1, valid[1]);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
@@ -870,17 +873,32 @@ template <int TYPE, int DIM, int GROUP>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(AttArgs p) {
   extern __shared__ __align__(16) uint8_t lds[];  // two blocks' operands
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Sequences first;
-  uint32_t total;
-  const uint32_t size = share_size<false>(p, lane, first, total);
-  const int64_t share = share_number(total, size);
-  if (share < 0) return;
-  const uint32_t unit = (uint32_t)share * size;
-  int left = (int)min(size, total - unit);
-  Segment g = locate<false>(p, unit, lane, first);
+  Segment g;
+  int64_t share = 0;
+  int left = 0;
+  if (p.alone) {
+    // the longest segments, which a step's last rows have, first
+    const int heads = p.c.n_seqs * p.c.n_heads, bh = blockIdx.x % heads;
+    g.rg = p.row_groups - 1 - blockIdx.x / heads;
+    g.b = bh / p.c.n_heads, g.h = bh % p.c.n_heads;
+    g.n = clamped_length(p, g.b);
+    g.blk = 0;
+    int least;
+    g.seen = seen_blocks(p, g.n, g.rg, least);
+  } else {
+    Sequences first;
+    uint32_t total;
+    const uint32_t size = share_size<false>(p, lane, first, total);
+    share = share_number(total, size);
+    if (share < 0) return;
+    const uint32_t unit = (uint32_t)share * size;
+    left = (int)min(size, total - unit);
+    g = locate<false>(p, unit, lane, first);
+  }
   for (;;) {
-    const int take = min(left << p.round, g.seen - g.blk);
+    const int take = p.alone ? g.seen : min(left << p.round, g.seen - g.blk);
     many_segment<TYPE, DIM, GROUP>(p, g, take, (int)share, lane, wave, lds);
+    if (p.alone) return;
     left -= (int)rounds<false>(p, take);
     if (left == 0) return;
     advance<false>(p, g);
@@ -1257,14 +1275,15 @@ __global__ __launch_bounds__(64 * NW) void attend_whole(AttArgs p) {
   int least;
   s.seen = seen_blocks(p, s.n, s.rg, least);
   attend_segment<TYPE, DIM, GROUP, NT, NW>(p, s, s.seen, 0, lane, wave, lds, ml);
-  if (!p.acc_out) return;
+  if (!p.acc_out || p.row_groups > 1) return;
   s.seen = (s.n + 31) / 32;
   weigh_segment<TYPE, DIM, GROUP, NW>(p, s, s.seen, lane, wave, lds);
 }
 
 struct Plan {
   bool many;
-  int whole;  // wavefronts of attend_whole, kWaves or more, or 0
+  int whole;   // wavefronts of attend_whole, kWaves or more, or 0
+  bool alone;  // as in AttArgs
   int per, rows, tiles, row_groups, workgroups, weigh_workgroups;
   int round, weigh_round, least;  // as in AttArgs
   int64_t parts;  // of a segment, at most, where all have one length
@@ -1300,13 +1319,19 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   const int64_t heads = (int64_t)c->n_seqs * c->n_heads;
   const int64_t blocks = (int64_t)c->max_pages * c->page / 32;
   pl.whole = 0;
-  if (!pl.many && (!weights || pl.row_groups == 1)) {
+  if (!pl.many) {
     if (blocks <= kShortBlocks)
       pl.whole = kWaves;
     else if (blocks <= kWholeBlocks && heads * pl.row_groups <= as_host::compute_units())
       pl.whole = whole_waves(c->dim, c->group, pl.tiles);
   }
   if (!pl.many && !pl.whole) set_tiles(1);
+  // Many rows of short tables: shares would only add parts to be joined, unless
+  // some segments are long and there are few.  226 new tokens of 15 sequences, 20
+  // heads of 64 channels: 17 us so, 57 in shares and joined; 300 tokens of 2 and of
+  // 15 sequences of up to 500 slots, 32 heads of 128: 34 us against 44, 82 against 152.
+  pl.alone = pl.many && (blocks <= kShortBlocks ||
+                         (blocks <= kWholeBlocks && heads * pl.row_groups >= 2 * (int64_t)as_host::compute_units()));
   const int resident = pl.many ? 2 : wide ? 3 : 4;
   pl.round = pl.many ? 0 : 2;
   pl.least = pl.many ? kWaves : 1;
@@ -1325,8 +1350,8 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   pl.parts = pl.workgroups / (heads * pl.row_groups);
   if (pl.parts > blocks / kWaves) pl.parts = blocks / kWaves;
   const int64_t places = (int64_t)pl.workgroups * 2 * 16 * pl.tiles;
-  pl.o_bytes = pl.whole ? 0 : round_up(places * c->dim * 4, 256);
-  pl.ml_bytes = pl.whole ? 0 : round_up(places * 8, 256);
+  pl.o_bytes = pl.whole || pl.alone ? 0 : round_up(places * c->dim * 4, 256);
+  pl.ml_bytes = pl.whole || pl.alone ? 0 : round_up(places * 8, 256);
   pl.row_bytes = weights ? round_up(heads * pl.rows * 8, 256) : 0;
   return pl;
 }
@@ -1363,29 +1388,38 @@ int launch_whole(const AttArgs& p, hipStream_t s) {
 
 template <int TYPE, int DIM, int GROUP>
 int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
-  if (pl.whole == kWaves)
-    return pl.tiles == 1 ? launch_whole<TYPE, DIM, GROUP, 1, kWaves>(p, s)
-                         : launch_whole<TYPE, DIM, GROUP, 2, kWaves>(p, s);
-  if (pl.whole)
-    return pl.tiles == 1 ? launch_whole<TYPE, DIM, GROUP, 1, whole_waves(DIM, GROUP, 1)>(p, s)
-                         : launch_whole<TYPE, DIM, GROUP, 2, whole_waves(DIM, GROUP, 2)>(p, s);
-  const dim3 g((unsigned)pl.workgroups), t(64 * kWaves);
-  const size_t lds = attend_lds<DIM, GROUP>(kWaves);
-  typedef Operands<DIM, GROUP> OperandSet;
-  if constexpr (DIM < 4 * GROUP) {
-    if (pl.many)
-      hipLaunchKernelGGL((attend_many<TYPE, DIM, GROUP>), g, t, (size_t)2 * OperandSet::kBytes, s, p);
-  }
-  if (!pl.many) hipLaunchKernelGGL((attend<TYPE, DIM, GROUP>), g, t, lds, s, p);
   const int64_t heads = (int64_t)p.c.n_seqs * p.c.n_heads;
-  const dim3 by_row((unsigned)(heads * p.rows));
-  if (pl.many || pl.parts < 8)
-    hipLaunchKernelGGL((join<TYPE, DIM, 1024 / DIM, 256>), dim3((unsigned)(heads * ((p.rows + 15) / 16))), dim3(256), 0,
-                       s, p);
-  else if (pl.parts >= 64)
-    hipLaunchKernelGGL((join<TYPE, DIM, 1, 1024>), by_row, dim3(1024), 0, s, p);
-  else
-    hipLaunchKernelGGL((join<TYPE, DIM, 1, 256>), by_row, dim3(256), 0, s, p);
+  const dim3 t(64 * kWaves);
+  if (pl.whole) {
+    int rc;
+    if (pl.whole == kWaves)
+      rc = pl.tiles == 1 ? launch_whole<TYPE, DIM, GROUP, 1, kWaves>(p, s)
+                         : launch_whole<TYPE, DIM, GROUP, 2, kWaves>(p, s);
+    else
+      rc = pl.tiles == 1 ? launch_whole<TYPE, DIM, GROUP, 1, whole_waves(DIM, GROUP, 1)>(p, s)
+                         : launch_whole<TYPE, DIM, GROUP, 2, whole_waves(DIM, GROUP, 2)>(p, s);
+    if (rc != AS_OK || p.row_groups == 1) return rc;
+  } else {
+    typedef Operands<DIM, GROUP> OperandSet;
+    if constexpr (DIM < 4 * GROUP) {
+      const dim3 g((unsigned)(pl.alone ? heads * p.row_groups : pl.workgroups));
+      if (pl.many)
+        hipLaunchKernelGGL((attend_many<TYPE, DIM, GROUP>), g, t, (size_t)2 * OperandSet::kBytes, s, p);
+    }
+    const size_t lds = attend_lds<DIM, GROUP>(kWaves);
+    if (!pl.many)
+      hipLaunchKernelGGL((attend<TYPE, DIM, GROUP>), dim3((unsigned)pl.workgroups), t, lds, s, p);
+  }
+  if (!pl.whole && !pl.alone) {
+    const dim3 by_row((unsigned)(heads * p.rows));
+    if (pl.many || pl.parts < 8)
+      hipLaunchKernelGGL((join<TYPE, DIM, 1024 / DIM, 256>), dim3((unsigned)(heads * ((p.rows + 15) / 16))), dim3(256),
+                         0, s, p);
+    else if (pl.parts >= 64)
+      hipLaunchKernelGGL((join<TYPE, DIM, 1, 1024>), by_row, dim3(1024), 0, s, p);
+    else
+      hipLaunchKernelGGL((join<TYPE, DIM, 1, 256>), by_row, dim3(256), 0, s, p);
+  }
   typedef Stage<DIM, GROUP, false> KeyStage;
   if (p.acc_out && p.rows > 16)
     hipLaunchKernelGGL((weigh<TYPE, DIM, GROUP, true>), dim3((unsigned)pl.weigh_workgroups), t, 0, s, p);
@@ -1461,6 +1495,7 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
   p.round = pl.round;
   p.weigh_round = pl.weigh_round;
   p.least = pl.least;
+  p.alone = pl.alone;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return type == AS_BF16 ? launch_by_shape<AS_BF16>(p, pl, s) : launch_by_shape<AS_F16>(p, pl, s);
 }

@@ -302,6 +302,21 @@ def test_attention(case, dtype, weights):
     assert torch.all((again[live] >= 0) & (again[live] <= t * hq / heads * (1 + 1e-3)))
 
 
+# Many rows over short tables, a segment to a workgroup, with weights or not; some
+# of one unseen sequence, of tables without pages, of rows that see nothing, and
+# of more segments than two to a compute unit over tables of up to 2048 slots.
+SHORT = [([0, 1, 40, 226], 33, 10, 2, 64, 64, 64), ([0, 0], 120, 2, 2, 64, 64, 32), ([300, 7], 128, 8, 8, 128, 64, 128),
+         ([129, 130, 500], 100, 4, 2, 128, 128, 256), ([64, 81, 3], 64, 10, 2, 128, 32, 64), ([96], 25, 4, 2, 64, 32, 32),
+         ([700, 10, 333, 0, 1500, 901, 64, 65], 96, 128, 16, 64, 64, 64)]
+
+
+@pytest.mark.parametrize("case", SHORT, ids=[str(i) for i in range(len(SHORT))])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("weights", [False, True])
+def test_attention_of_many_rows_over_short_tables(case, dtype, weights):
+    test_attention(case, dtype, weights)
+
+
 def test_attention_ignores_what_it_does_not_see():
     """Slots beyond a length, and slots after a query, may hold infinities and
     NaN; pages that do not exist hold no slots."""
