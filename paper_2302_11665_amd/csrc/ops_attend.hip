@@ -45,7 +45,6 @@ struct AttArgs {
   int32_t workgroups, weigh_workgroups;
   int32_t round, weigh_round;  // log2 of a round's blocks
   int32_t least;               // rounds of a share, at least
-  int32_t alone;               // attend_many: a segment to a workgroup
 };
 
 // ---------------------------------------------------------------- 4-bit codes
@@ -869,36 +868,35 @@ __device__ __forceinline__ void many_segment(const AttArgs& p, const Segment& s,
   }
 }
 
-template <int TYPE, int DIM, int GROUP>
+// ALONE: a segment to a workgroup.
+template <int TYPE, int DIM, int GROUP, bool ALONE>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(AttArgs p) {
   extern __shared__ __align__(16) uint8_t lds[];  // two blocks' operands
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  Segment g;
-  int64_t share = 0;
-  int left = 0;
-  if (p.alone) {
+  if (ALONE) {
     // the longest segments, which a step's last rows have, first
     const int heads = p.c.n_seqs * p.c.n_heads, bh = blockIdx.x % heads;
+    Segment g;
     g.rg = p.row_groups - 1 - blockIdx.x / heads;
     g.b = bh / p.c.n_heads, g.h = bh % p.c.n_heads;
     g.n = clamped_length(p, g.b);
     g.blk = 0;
     int least;
     g.seen = seen_blocks(p, g.n, g.rg, least);
-  } else {
-    Sequences first;
-    uint32_t total;
-    const uint32_t size = share_size<false>(p, lane, first, total);
-    share = share_number(total, size);
-    if (share < 0) return;
-    const uint32_t unit = (uint32_t)share * size;
-    left = (int)min(size, total - unit);
-    g = locate<false>(p, unit, lane, first);
+    many_segment<TYPE, DIM, GROUP>(p, g, g.seen, 0, lane, wave, lds);
+    return;
   }
+  Sequences first;
+  uint32_t total;
+  const uint32_t size = share_size<false>(p, lane, first, total);
+  const int64_t share = share_number(total, size);
+  if (share < 0) return;
+  const uint32_t unit = (uint32_t)share * size;
+  int left = (int)min(size, total - unit);
+  Segment g = locate<false>(p, unit, lane, first);
   for (;;) {
-    const int take = p.alone ? g.seen : min(left << p.round, g.seen - g.blk);
+    const int take = min(left << p.round, g.seen - g.blk);
     many_segment<TYPE, DIM, GROUP>(p, g, take, (int)share, lane, wave, lds);
-    if (p.alone) return;
     left -= (int)rounds<false>(p, take);
     if (left == 0) return;
     advance<false>(p, g);
@@ -1283,7 +1281,7 @@ __global__ __launch_bounds__(64 * NW) void attend_whole(AttArgs p) {
 struct Plan {
   bool many;
   int whole;   // wavefronts of attend_whole, kWaves or more, or 0
-  bool alone;  // as in AttArgs
+  bool alone;  // attend_many with a segment to a workgroup
   int per, rows, tiles, row_groups, workgroups, weigh_workgroups;
   int round, weigh_round, least;  // as in AttArgs
   int64_t parts;  // of a segment, at most, where all have one length
@@ -1328,8 +1326,8 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   if (!pl.many && !pl.whole) set_tiles(1);
   // Many rows of short tables: shares would only add parts to be joined, unless
   // some segments are long and there are few.  226 new tokens of 15 sequences, 20
-  // heads of 64 channels: 17 us so, 57 in shares and joined; 300 tokens of 2 and of
-  // 15 sequences of up to 500 slots, 32 heads of 128: 34 us against 44, 82 against 152.
+  // heads of 64 channels: 16 us so, 57 in shares and joined; 300 tokens of 2 and of
+  // 15 sequences of up to 500 slots, 32 heads of 128: 34 us against 44, 75 against 152.
   pl.alone = pl.many && (blocks <= kShortBlocks ||
                          (blocks <= kWholeBlocks && heads * pl.row_groups >= 2 * (int64_t)as_host::compute_units()));
   const int resident = pl.many ? 2 : wide ? 3 : 4;
@@ -1402,9 +1400,11 @@ int launch_attention(const AttArgs& p, const Plan& pl, hipStream_t s) {
   } else {
     typedef Operands<DIM, GROUP> OperandSet;
     if constexpr (DIM < 4 * GROUP) {
-      const dim3 g((unsigned)(pl.alone ? heads * p.row_groups : pl.workgroups));
-      if (pl.many)
-        hipLaunchKernelGGL((attend_many<TYPE, DIM, GROUP>), g, t, (size_t)2 * OperandSet::kBytes, s, p);
+      const size_t lds = 2 * OperandSet::kBytes;
+      if (pl.alone)
+        hipLaunchKernelGGL((attend_many<TYPE, DIM, GROUP, true>), dim3((unsigned)(heads * p.row_groups)), t, lds, s, p);
+      else if (pl.many)
+        hipLaunchKernelGGL((attend_many<TYPE, DIM, GROUP, false>), dim3((unsigned)pl.workgroups), t, lds, s, p);
     }
     const size_t lds = attend_lds<DIM, GROUP>(kWaves);
     if (!pl.many)
@@ -1495,7 +1495,6 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
   p.round = pl.round;
   p.weigh_round = pl.weigh_round;
   p.least = pl.least;
-  p.alone = pl.alone;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   return type == AS_BF16 ? launch_by_shape<AS_BF16>(p, pl, s) : launch_by_shape<AS_F16>(p, pl, s);
 }
