@@ -6,9 +6,16 @@
 //   sum p v = sum over tokens of  (p d) c + p m
 // and the codes enter v_mfma_f32_16x16x32 as 16 + c, which a shift, a mask and
 // an or make of 4 bits (bf16 holds 16..31 in steps of 1/8, fp16 in steps of
-// 1/64); the 16 is taken out in fp32: the first product starts from -16 sum q,
-// the second is corrected by 16 (p d).  Queries are exact in the first product;
-// p d enters the second as two bf16 numbers.
+// 1/64); the 16 is taken out in fp32: the first product starts from -16 sum q.
+// Queries are exact in the first product; p d enters the second as two bf16
+// numbers, whose sum P is p d but for the last 7 of its 24 bits.  With 23.5 the
+// mean of 16 + c,
+//   sum p v = sum P (16 + c) - 23.5 sum P + sum p (m + 7.5 d):
+// what P leaves is multiplied by c - 7.5 rather than 16 + c, and the last sum's
+// terms are near the group's mean, so it loses nothing.  The matrix instructions
+// make the second sum too, from the same operands.  The first grows with the
+// slots and not with the result, hence it is kept for 8 blocks only, and its sum
+// for a group of channels brought back by the other two (kRebase below).
 //
 // The products are K q^T and V^T p^T: the queries that share a key/value head
 // are the 16 columns.  A lane of the first product's result then holds, for one
@@ -243,7 +250,7 @@ __device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
 template <int DIM, int GROUP, int NT>
 struct Sums {
   v4f o[NT][DIM / 16];
-  float shift[NT][DIM / GROUP];  // sum of p m - 16 p d over the lane's slots
+  float shift[NT][DIM / GROUP];  // a quarter of -23.5 sum P, plus the lane's slots' sum of p (m + 7.5 d)
   float mref[NT], sum[NT];       // reference of the exponents (log2 units), sum of p over the lane's slots
 };
 
@@ -255,6 +262,33 @@ __device__ __forceinline__ void clear(Sums<DIM, GROUP, NT>& a, int t) {
   for (int g = 0; g < DIM / GROUP; ++g) a.shift[t][g] = 0.0f;
 #pragma unroll
   for (int i = 0; i < DIM / 16; ++i) a.o[t][i] = v4f{0, 0, 0, 0};
+}
+
+// o as it is without the 16 of the codes: the four lanes' shifts are added to it.
+// Once in kRebase blocks (6 instructions a group and one a register of o): its
+// own rounding then stays that of a sum of 256 slots, not of all.  Nearly flat
+// attention of one wavefront over 65,536 slots is off by 2.6e-3 of the result
+// without this, by 1e-5 so, and by 3e-6 with every block's sum.
+constexpr int kRebase = 8;
+
+template <int DIM, int GROUP, int NT>
+__device__ __forceinline__ void rebase(Sums<DIM, GROUP, NT>& a) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int g = 0; g < DIM / GROUP; ++g) {
+      const float add = sum_over_rows(a.shift[t][g]);
+#pragma unroll
+      for (int i = g * (GROUP / 16); i < (g + 1) * (GROUP / 16); ++i) a.o[t][i] += add;
+      a.shift[t][g] = 0.0f;
+    }
+}
+
+// A quarter of -23.5 times the sum of a block's P, in every lane of a query.
+__device__ __forceinline__ float mean_shift(v4u hi, v4u lo) {
+  constexpr uint32_t kMean = 0xc0bcc0bcu;  // -5.875, exact in bf16
+  const v4u mean = {kMean, kMean, kMean, kMean};
+  return mfma<AS_BF16>(mean, lo, mfma<AS_BF16>(mean, hi, v4f{0, 0, 0, 0}))[0];
 }
 
 // The q.k of a lane's 8 slots of a block to p, the sums so far scaled where the
@@ -346,11 +380,12 @@ __device__ __forceinline__ void attend_block(const AttArgs& p, int blk, int lane
           if (RAGGED && slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) w = 0;
           pd[z] = fma_d(s[u][e], w, 0.0f);
           a.shift[u][g] = fma_m(s[u][e], w, a.shift[u][g]);
-          a.shift[u][g] = fmaf(-16.0f, pd[z], a.shift[u][g]);
+          a.shift[u][g] = fmaf(7.5f, pd[z], a.shift[u][g]);
         }
         const v2u two = split_bf16(pd[0], pd[1]);
         hi[u][j] = two[0], lo[u][j] = two[1];
       }
+      a.shift[u][g] += mean_shift(hi[u], lo[u]);
     }
 #pragma unroll
     for (int i = 0; i < GROUP / 16; ++i) {
@@ -561,7 +596,7 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
   }
   const Expand<TYPE> key_codes;
   const Expand<AS_BF16> value_codes;
-  int slot = 0;
+  int slot = 0, since = 0;
   // Blocks up to `to`, all of one kind.
   auto blocks = [&](int to, auto ragged) {
     for (; blk < to; blk += NW) {
@@ -582,6 +617,7 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
         if (p.c.n_pages > 0) S::bring(p, row, at, lane, here);
       }
       slot = slot + 1 == kStages ? 0 : slot + 1;
+      if (++since == kRebase) rebase(a), since = 0;
     }
   };
   blocks(min(end, least >> 5), std::false_type());  // all 32 slots seen by all queries
@@ -686,8 +722,8 @@ struct Operands {
   static constexpr int kV = 2 * kWords * 1024;                // K's operands: [2][kWords], then V's [2 kWords]
   static constexpr int kKeyPar = 2 * kV;                      // words [kNG][32]
   static constexpr int kValuePar = kKeyPar + kNG * 128;       // words [kNG][32]
-  static constexpr int kValueMin = kValuePar + kNG * 128;     // m - 16 d, fp32 [kNG][32]
-  static constexpr int kBytes = kValueMin + kNG * 128;
+  static constexpr int kValueMean = kValuePar + kNG * 128;    // m + 7.5 d, fp32 [kNG][32]
+  static constexpr int kBytes = kValueMean + kNG * 128;
 
   uint32_t words[kWords], par;  // this wavefront's quarter of a block
 
@@ -719,7 +755,7 @@ struct Operands {
     const int i = (wave & 1) * 16 * kNG + lane;
     if (lane < 16 * kNG) {
       *reinterpret_cast<uint32_t*>(lds + (wave < 2 ? kKeyPar : kValuePar) + i * 4) = par;
-      if (wave >= 2) *reinterpret_cast<float*>(lds + kValueMin + i * 4) = fma_m(1.0f, par, fma_d(-16.0f, par, 0.0f));
+      if (wave >= 2) *reinterpret_cast<float*>(lds + kValueMean + i * 4) = fma_m(1.0f, par, fma_d(7.5f, par, 0.0f));
     }
   }
 };
@@ -754,14 +790,14 @@ __device__ __forceinline__ void many_block(const AttArgs& p, int blk, int lane,
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
     v4u par[2], hi[2], lo[2];
-    v4f low[2];
+    v4f mean[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       par[t] = *reinterpret_cast<const v4u*>(lds + O::kValuePar + g * 128 + t * 64 + (lane >> 4) * 16);
-      low[t] = *reinterpret_cast<const v4f*>(lds + O::kValueMin + g * 128 + t * 64 + (lane >> 4) * 16);
+      mean[t] = *reinterpret_cast<const v4f*>(lds + O::kValueMean + g * 128 + t * 64 + (lane >> 4) * 16);
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float pd[2];
@@ -769,7 +805,7 @@ __device__ __forceinline__ void many_block(const AttArgs& p, int blk, int lane,
         for (int z = 0; z < 2; ++z) {
           const int e = 2 * j + z;
           uint32_t w = par[e >> 2][e & 3];
-          float m = low[e >> 2][e & 3];
+          float m = mean[e >> 2][e & 3];
           // a slot that is not seen may hold anything, infinities and NaN too
           if (RAGGED && slot0 + 16 * (e >> 2) + (e & 3) >= q[u].limit) w = 0, m = 0.0f;
           pd[z] = fma_d(s[u][e], w, 0.0f);
@@ -778,6 +814,8 @@ __device__ __forceinline__ void many_block(const AttArgs& p, int blk, int lane,
         const v2u two = split_bf16(pd[0], pd[1]);
         hi[u][j] = two[0], lo[u][j] = two[1];
       }
+      a.shift[u][g] += mean_shift(hi[u], lo[u]);
+    }
     // (the two products of one sum apart, so that neither waits for the other)
     constexpr int kRun = GROUP / 16 < 4 ? GROUP / 16 : 4;
 #pragma unroll
@@ -814,7 +852,7 @@ __device__ __forceinline__ void many_segment(const AttArgs& p, const Segment& s,
   const Expand<TYPE> key_codes;
   const Expand<AS_BF16> value_codes;
   O quarter;
-  int blk = s.blk, half = 0;
+  int blk = s.blk, half = 0, since = 0;
   bool valid[2];  // of this block and the next
   auto fetch = [&](int i, bool& ok) {
     int at;
@@ -841,6 +879,7 @@ __device__ __forceinline__ void many_segment(const AttArgs& p, const Segment& s,
       if (blk + 1 < end) quarter.store(lds + (half ^ 1) * O::kBytes, lane, wave, key_codes, value_codes);
       if (blk + 2 < end) fetch(blk + 2, valid[1]);
       if (here) many_block<TYPE, DIM, GROUP, decltype(ragged)::value>(p, blk, lane, q, lds + half * O::kBytes, a);
+      if (++since == kRebase) rebase(a), since = 0;
       lds_barrier();
     }
   };

@@ -358,6 +358,39 @@ def test_attention_over_extreme_logits():
     assert torch.isfinite(o).all()
 
 
+@pytest.mark.parametrize("dim,group,seqs,heads,n", [(64, 64, 1024, 1, 262144), (128, 32, 768, 2, 131072),
+                                                    (64, 64, 512, 128, 65536), (128, 64, 512, 128, 40000)])
+def test_attention_sums_over_long_runs(dim, group, seqs, heads, n):
+    """Nearly flat attention over many slots, one segment to a workgroup: what is
+    added up by one wavefront is far larger than the result.  All sequences
+    share one sequence's pages."""
+    say("long runs", dim, group, seqs, heads, n)
+    g = gen(n + dim)
+    c = make_cache(g, [n], 1, dim, group, 4096)
+    for x in (c.k_par, c.v_par):  # values of mean 0, of one size
+        x[..., 0] = 0.1370
+        x[..., 1] = -7.5 * 0.1370
+    shared = ops.Cache(c.k, c.v, c.k_par, c.v_par, c.pos, c.acc, c.page_table.expand(seqs, -1).contiguous())
+    q = (normal(g, seqs, 1, heads, dim) * 0.2).to(F16)
+    out = ops.attention_kv4(q, shared, torch.full((seqs,), n, dtype=torch.int32, device="cuda"))
+    h = host(c)
+    kc, vc, kp, vp = oo.read_cache(h["k"], h["v"], h["k_par"], h["v_par"], h["page_table"][0], 0, n, 4096, dim, group)
+    k, v = oo.values(kc, kp), oo.values(vc, vp)
+    pick = np.arange(0, seqs, seqs // 8)
+    rows = f64(q)[pick, 0, :2].reshape(-1, dim)
+    o, _ = oo.attend(rows, k, v, np.ones((len(rows), n), bool), dim ** -0.5)
+    off = f64(out)[pick, 0, :2].reshape(-1, dim) - o
+    # Rounding to fp16 is off by 2^-11 at most, 2^-11 / sqrt(3) in the mean of
+    # squares where all significands were 1.  Before it, sums of at most 8 blocks
+    # of 32 slots of p d (16 + c), c <= 15, are rounded twice a block, by 2^-25 of
+    # 8 * 32 * 31 p d at most, as if at random, against a result of
+    # sqrt(n) times the codes' spread, 4.6 p d: sqrt(2 n / 32) 2^-25 7936 /
+    # (4.6 sqrt(n)) = 1.3e-5 for any n.  2^-14 leaves four times that and p d's
+    # 17 bits.
+    assert np.linalg.norm(off) <= (2.0 ** -11 / 3 ** 0.5 + 2.0 ** -14) * np.linalg.norm(o), np.linalg.norm(
+        off) / np.linalg.norm(o)
+
+
 def test_attention_query_strides():
     g = gen(13)
     lengths = [50, 20, 77]
