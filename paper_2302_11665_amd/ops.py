@@ -94,6 +94,14 @@ def _workspace(n, device):
     return w, w.data_ptr()
 
 
+def _rows(x):
+    """x [rows, columns] as rows that lie apart, and their stride: a broadcast row or overlapping windows are copied."""
+    t, n = x.shape
+    if (n > 1 and x.stride(1) != 1) or (t > 1 and x.stride(0) < n):
+        x = x.contiguous()
+    return x, x.stride(0) if t > 1 else n
+
+
 _16 = (torch.bfloat16, torch.float16)
 _FLOATS = (torch.bfloat16, torch.float16, torch.float32)
 
@@ -118,12 +126,11 @@ class PackedWeight:
 def pack_weight(w) -> PackedWeight:
     """Quantise weights [n_out, n_in] (bf16, fp16 or fp32) per output, once."""
     _need(w, "weight", _FLOATS, 2, contiguous=False)
-    if w.stride(1) != 1:
-        w = w.contiguous()
+    w, stride = _rows(w)
     n, k = w.shape
     codes = torch.empty(lib().as_i8_bytes(n, k), dtype=torch.int8, device=w.device)
     scale = torch.empty(n, dtype=torch.float32, device=w.device)
-    _call(lib().as_quantize_i8, w.device, w.data_ptr(), _TYPES[w.dtype], n, k, max(k, w.stride(0)),
+    _call(lib().as_quantize_i8, w.device, w.data_ptr(), _TYPES[w.dtype], n, k, stride,
           codes.data_ptr(), scale.data_ptr())
     return PackedWeight(codes, scale, n, k)
 
@@ -131,15 +138,13 @@ def pack_weight(w) -> PackedWeight:
 def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
     """x [..., n_in] (bf16 or fp16) quantised per token, times the packed
     weights: [..., n_out] of `dtype` (default: x's; fp32 allowed).  `out`, if
-    given, is [tokens, n_out] with contiguous rows."""
+    given, is [tokens, n_out] with contiguous rows that do not overlap."""
     L = lib()
     _need(x, "x", _16, contiguous=False)
     dev = x.device
     if x.dim() < 1 or x.shape[-1] != w.n_in:
         _bad(f"linear_i8: x has {tuple(x.shape)}, the weights take {w.n_in} inputs")
-    x2 = x if x.dim() == 2 else x.reshape(-1, w.n_in)
-    if x2.stride(1) != 1 and w.n_in > 1:
-        x2 = x2.contiguous()
+    x2, x_stride = _rows(x if x.dim() == 2 else x.reshape(-1, w.n_in))
     t = x2.shape[0]
     codes, scale = w.codes, w.scale
     if not (codes.device == scale.device == dev and codes.dtype in (torch.int8, torch.uint8)
@@ -153,15 +158,16 @@ def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
         y = torch.empty((t, w.n_out), dtype=dtype or x.dtype, device=dev)
     else:
         y = _need(out, "out", _FLOATS, 2, dev, contiguous=False)
-        if tuple(y.shape) != (t, w.n_out) or (w.n_out > 1 and y.stride(1) != 1) or (dtype and y.dtype != dtype):
+        if tuple(y.shape) != (t, w.n_out) or (w.n_out > 1 and y.stride(1) != 1) or (
+                t > 1 and y.stride(0) < w.n_out) or (dtype and y.dtype != dtype):
             _bad(f"linear_i8: out has {tuple(y.shape)} with strides {y.stride()}, {y.dtype}")
     if y.dtype not in _TYPES:
         _bad(f"linear_i8: type {y.dtype}")
     n = L.as_linear_i8_workspace(t, w.n_in, w.n_out)
     _keep, ws = _workspace(n, dev)
-    _call(L.as_linear_i8, dev, x2.data_ptr(), _TYPES[x.dtype], t, w.n_in, max(w.n_in, x2.stride(0)),
+    _call(L.as_linear_i8, dev, x2.data_ptr(), _TYPES[x.dtype], t, w.n_in, x_stride,
           w.codes.data_ptr(), w.scale.data_ptr(), None if bias is None else bias.data_ptr(), w.n_out, y.data_ptr(),
-          _TYPES[y.dtype], max(w.n_out, y.stride(0)), ws, n)
+          _TYPES[y.dtype], y.stride(0) if t > 1 else w.n_out, ws, n)
     return y if out is not None or x.dim() == 2 else y.view(*x.shape[:-1], w.n_out)
 
 

@@ -144,6 +144,27 @@ def test_linear_strides_and_shapes(t):
     assert ops.linear_i8(x[:0], w).shape == (0, 50)
 
 
+@pytest.mark.parametrize("t", [2, 8, 40, 300, 2100])
+def test_linear_of_overlapping_rows(t):
+    """A row broadcast to all tokens, and windows of one line."""
+    g = gen(t + 1)
+    line = normal(g, 200 + 3 * t, dtype=BF16)
+    w = ops.pack_weight(normal(g, 40, 200))
+    codes = w.codes.cpu().numpy()[oo.tile_index(40, 200)]
+    one, windows = line[:200].expand(t, 200), line.unfold(0, 200, 3)[:t]
+    for x in (one, windows):
+        check_linear(x, codes, f64(w.scale), None, ops.linear_i8(x, w), BF16)
+        packed, apart = ops.pack_weight(x), ops.pack_weight(x.contiguous())
+        at = torch.from_numpy(oo.tile_index(t, 256)).cuda()  # (rows beyond the last hold anything)
+        assert torch.equal(packed.codes[at], apart.codes[at]) and torch.equal(packed.scale, apart.scale)
+    y = ops.linear_i8(line[:200].view(1, 1, 200).expand(t, 2, 200), w)
+    assert y.shape == (t, 2, 40) and torch.equal(y, ops.linear_i8(line[None, :200], w).expand(t, 2, 40))
+    for out in (torch.zeros(1, 40, dtype=BF16, device="cuda").expand(t, 40),
+                torch.zeros(40 + t, dtype=BF16, device="cuda").unfold(0, 40, 1)[:t]):
+        with pytest.raises(sim.SimError):
+            ops.linear_i8(one, w, out=out)
+
+
 @pytest.mark.parametrize("t", [3, 40, 2100])
 def test_linear_of_values_at_the_ends_of_the_range(t):
     """Rows of very large and very small values, subnormal ones too, and rows

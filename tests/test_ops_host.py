@@ -143,3 +143,67 @@ def test_profile_and_placement_problem():
     assert [len(x["group_cfg"]) for x in gp.partitions] == [4, 2, 1]
     assert gp.stage_lat.shape == (2, 3, 4) and gp.stage_lat[0, 0, 0] == 1.0
     assert set(gp.model.tolist()) <= {0, 1} and (gp.weight_mib == 25).all()
+
+
+@pytest.fixture
+def calls(L, monkeypatch):
+    """The operators' binding over tensors on the CPU, its calls recorded and not made."""
+    from paper_2302_11665_amd import ops
+    made = []
+
+    def need(x, name, dtypes, dim=None, device=None, contiguous=True):
+        return x
+
+    monkeypatch.setattr(ops, "_need", need)
+    monkeypatch.setattr(ops, "_call", lambda fn, device, *args: made.append((fn.__name__, args)))
+    return made
+
+
+def overlapping_rows():
+    import torch
+    line = torch.randn(400).to(torch.bfloat16)
+    yield line[:64].expand(8, 64)                       # one row for all tokens
+    yield line[:64].view(1, 1, 64).expand(2, 4, 64)     # the same, through a reshape
+    yield line.unfold(0, 64, 3)[:9]                     # windows that share most of their values
+    yield line[:1].expand(7, 1)                         # rows of one value
+
+
+def test_linear_does_not_read_overlapping_rows_as_if_they_lay_apart(calls):
+    import torch
+    from paper_2302_11665_amd import ops
+    for x in overlapping_rows():
+        k = x.shape[-1]
+        w = ops.PackedWeight(torch.zeros(ops.lib().as_i8_bytes(5, k), dtype=torch.int8), torch.zeros(5), 5, k)
+        ops.linear_i8(x, w)
+        ops.pack_weight(x.reshape(-1, k))
+        for name, args in calls:
+            rows, stride = args[2], args[4]
+            assert rows == x.numel() // k > 1 and args[3] == k
+            # the rows as they are passed: a copy, not x's memory with another stride
+            assert stride >= k and args[0] != x.data_ptr(), (name, tuple(x.shape), x.stride(), stride)
+        assert [name for name, _ in calls] == ["as_linear_i8", "as_quantize_i8"]
+        calls.clear()
+
+
+def test_linear_reads_rows_that_lie_apart_where_they_are(calls):
+    import torch
+    from paper_2302_11665_amd import ops
+    big = torch.randn(6, 100).to(torch.bfloat16)
+    w = ops.PackedWeight(torch.zeros(ops.lib().as_i8_bytes(5, 64), dtype=torch.int8), torch.zeros(5), 5, 64)
+    for x, stride in ((big[:, 3:67], 100), (big[:, :64][::2], 200), (big[:1, :64], None), (big[0, :64], None)):
+        ops.linear_i8(x, w)
+        assert calls[-1][1][0] == x.data_ptr()
+        assert calls[-1][1][4] == stride if stride else calls[-1][1][4] >= 64  # (of one row it does not matter)
+
+
+def test_linear_refuses_an_output_with_overlapping_rows(calls):
+    import torch
+    from paper_2302_11665_amd import ops
+    x = torch.randn(4, 64).to(torch.bfloat16)
+    w = ops.PackedWeight(torch.zeros(ops.lib().as_i8_bytes(5, 64), dtype=torch.int8), torch.zeros(5), 5, 64)
+    for out in (torch.zeros(1, 5).expand(4, 5), torch.zeros(40).unfold(0, 5, 2)[:4], torch.zeros(40).as_strided((4, 5), (4, 1))):
+        with pytest.raises(sim.SimError):
+            ops.linear_i8(x, w, out=out)
+    assert not calls
+    ops.linear_i8(x[:1], w, out=torch.zeros(9).as_strided((1, 5), (2, 1)))  # one row overlaps nothing
+    assert calls[-1][1][11] == 5
