@@ -173,13 +173,15 @@ def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
 
 # -------------------------------------------------------------------- cache
 
-@dataclasses.dataclass
+@dataclasses.dataclass(frozen=True, eq=False)
 class Cache:
     """A paged cache of 4 bits; the arrays are those of as_cache_t:
     k int32 [pages, heads, page, 4, dim/32], v int32 [pages, heads, page/32, 4,
     16, dim/16], k_par and v_par float16 [pages, heads, dim/group, page, 2], pos
     int32 and acc float32 [pages, heads, page] (either may be None where no
-    weights are kept), page_table int32 [seqs, max_pages]."""
+    weights are kept), page_table int32 [seqs, max_pages].  Calls use the
+    addresses that these had when the cache was made, so none can be replaced:
+    `dataclasses.replace(cache, page_table=..)` makes a cache with another one."""
     k: torch.Tensor
     v: torch.Tensor
     k_par: torch.Tensor
@@ -213,9 +215,10 @@ class Cache:
             what = [None if x is None else (tuple(x.shape), x.dtype, str(x.device)) if isinstance(x, torch.Tensor)
                     else type(x) for x in (k, v, kp, vp, pos, acc, table)]
             _bad(f"cache: contiguous CUDA arrays of one cache are needed, not {what}")
-        self._c = as_cache_t(pages, heads, dim, dim // groups, page, table.shape[0], table.shape[1], 0, k.data_ptr(),
-                             v.data_ptr(), kp.data_ptr(), vp.data_ptr(), None if pos is None else pos.data_ptr(),
-                             None if acc is None else acc.data_ptr(), table.data_ptr())
+        object.__setattr__(self, "_c", as_cache_t(
+            pages, heads, dim, dim // groups, page, table.shape[0], table.shape[1], 0, k.data_ptr(), v.data_ptr(),
+            kp.data_ptr(), vp.data_ptr(), None if pos is None else pos.data_ptr(),
+            None if acc is None else acc.data_ptr(), table.data_ptr()))
 
     @staticmethod
     def empty(n_pages, n_heads, dim, page_table, group=64, page=64, device="cuda") -> "Cache":

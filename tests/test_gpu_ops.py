@@ -1,6 +1,8 @@
 """The operators of a served model's step on the GPU against their 64-bit
 definitions.  Tolerances are first-order bounds of the roundings that the
 operators state, worked out beside each."""
+import dataclasses
+
 import numpy as np
 import pytest
 import torch
@@ -497,6 +499,24 @@ def test_append_beyond_the_table_writes_nothing_there():
     assert np.array_equal(before["acc"][~used], after["acc"][~used]) and (after["acc"][used] == 0).all()
     kept = ~used.any(axis=(1, 2))
     assert np.array_equal(before["k"][kept], after["k"][kept]) and np.array_equal(before["v"][kept], after["v"][kept])
+
+
+def test_a_longer_table_makes_another_cache():
+    g = gen(4)
+    c = make_cache(g, [40, 64], 2, 64, 64, 32, spare=3)
+    q = normal(g, 2, 1, 4, 64, dtype=BF16)
+    n = torch.tensor([40, 64], dtype=torch.int32, device="cuda")
+    want = ops.attention_kv4(q, c, n)
+    wide = torch.cat([c.page_table, torch.full((2, 9), -1, dtype=torch.int32, device="cuda")], 1)
+    with pytest.raises(AttributeError):
+        c.page_table = wide
+    d = dataclasses.replace(c, page_table=wide)
+    assert d.k is c.k and d.bytes_per_slot == c.bytes_per_slot and torch.equal(ops.attention_kv4(q, d, n), want)
+    free = torch.tensor(sorted(set(range(c.k.shape[0])) - set(c.page_table.flatten().tolist())))
+    d.page_table[0, 2] = int(free[0])
+    ops.cache_append(d, normal(g, 2, 1, 2, 64, dtype=BF16), normal(g, 2, 1, 2, 64, dtype=BF16),
+                     torch.tensor([64, 300], dtype=torch.int32, device="cuda"))
+    assert (c.acc[int(free[0]), :, 0] == 0).all() and torch.equal(ops.attention_kv4(q, d, n), want)
 
 
 # ----------------------------------------------------------------- eviction

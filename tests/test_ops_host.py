@@ -207,3 +207,12 @@ def test_linear_refuses_an_output_with_overlapping_rows(calls):
     assert not calls
     ops.linear_i8(x[:1], w, out=torch.zeros(9).as_strided((1, 5), (2, 1)))  # one row overlaps nothing
     assert calls[-1][1][11] == 5
+
+
+def test_a_cache_keeps_the_arrays_that_its_calls_use():
+    """A cache's calls take the addresses that it was made with: another array needs another cache."""
+    from paper_2302_11665_amd import ops
+    c = object.__new__(ops.Cache)
+    for name in ("k", "v", "k_par", "v_par", "pos", "acc", "page_table"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, None)
