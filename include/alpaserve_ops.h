@@ -174,7 +174,8 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
  *   length       [n_seqs] tokens in src
  *   total        [n_seqs] tokens that the sequence has had (next position)
  *   keep, recent 1 <= keep <= dst's max_pages * page, 0 <= recent <= keep
- *   out_length   [n_seqs] tokens in dst: min(length, keep)
+ *   out_length   [n_seqs] tokens in dst: min(length, keep); an array of its own,
+ *                length and total are read while it is written
  * src and dst agree in n_heads, dim, group and n_seqs; pos and acc are needed.
  */
 int64_t as_cache_evict_workspace(const as_cache_t* src, int32_t keep);

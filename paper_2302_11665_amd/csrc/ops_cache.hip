@@ -511,6 +511,10 @@ int as_cache_evict(const as_cache_t* src, const as_cache_t* dst, const int32_t* 
                 src->n_heads);
   if (src->n_seqs == 0) return as_host::ok();
   if (!length || !total || !out_length) return fail(AS_E_INVALID_ARG, "cache_evict: null pointer");
+  const uintptr_t out = (uintptr_t)out_length, n = (uintptr_t)src->n_seqs * 4;
+  for (const int32_t* read : {length, total})
+    if (out < (uintptr_t)read + n && (uintptr_t)read < out + n)
+      return fail(AS_E_INVALID_ARG, "cache_evict: out_length overlaps length or total");
   const int64_t need = as_cache_evict_workspace(src, keep);
   if (workspace_bytes < need || !workspace || !aligned(workspace, 256))
     return fail(AS_E_INVALID_ARG, "cache_evict: workspace of %lld bytes, %lld needed (aligned to 256)",

@@ -216,3 +216,10 @@ def test_a_cache_keeps_the_arrays_that_its_calls_use():
     for name in ("k", "v", "k_par", "v_par", "pos", "acc", "page_table"):
         with pytest.raises(AttributeError):
             setattr(c, name, None)
+
+
+def test_evict_refuses_new_lengths_over_the_old_ones(L):
+    """Workgroups of other heads still read the lengths and totals when the first one writes the new lengths."""
+    for out in (0x100, 0x104, 0xfc, 0x200, 0x204):
+        assert L.as_cache_evict(cache(), cache(), 0x100, 0x200, 8, 2, out, 0x400, 1 << 20, None) == sim.AS_E_INVALID_ARG
+        assert "out_length" in sim.as_last_error()
