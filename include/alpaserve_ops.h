@@ -97,6 +97,12 @@ int as_linear_i8(const void* x, int32_t x_type, int64_t n_tokens, int64_t n_in, 
  *   acc    [n_pages][n_heads][page] fp32 accumulated attention weight
  * The slots of a sequence are 0..length-1 for every head, in the order of their
  * tokens; heads may hold different tokens once a cache was evicted from.
+ * Sequences with a common beginning may name the same pages for it where a call
+ * only reads them: attention without acc_out, eviction's src.  What a call
+ * writes must be named once in the table: the pages that as_cache_append puts
+ * tokens on, those that hold slots below a length where attention gets acc_out
+ * (a slot has one accumulated weight, of one sequence), eviction's dst.  Of a
+ * slot that two sequences write, the contents are unspecified.
  */
 typedef struct {
   int32_t n_pages;   /* P, pages of the pool                                     */
@@ -149,7 +155,8 @@ int as_cache_append(const as_cache_t* cache, const void* k, const void* v, int32
  *   acc_in, acc_out  laid out as cache->acc: for every slot s below the
  *            length, acc_out = acc_in + sum of p_is over the queries and heads
  *            that read the key/value head (acc_in NULL: 0; the two may be the
- *            same array); other slots are not written.  acc_out NULL: no weights
+ *            same array); other slots are not written.  No two sequences may
+ *            share the pages of these slots.  acc_out NULL: no weights
  * At most 2^26 query rows, 65,535 sequences times heads, and 2^31 blocks of 32
  * slots over all sequences, heads and 16 rows (AS_E_LIMITS).
  * Products of codes and 16-bit numbers with fp32 sums; softmax in fp32; p times
@@ -169,8 +176,8 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
  * accumulated weight until there are `keep` (ties: the lowest slot; a NaN weight
  * comes last).  They go to slots 0.. of dst in their order, with codes, scales,
  * position and weight; codes behind the last one in its block of 32 slots of
- * dst->v become 0.  Out of place because pages may be shared by sequences with
- * a common beginning; src and dst must not share a page that dst's table names.
+ * dst->v become 0.  Out of place because sequences with a common beginning may
+ * share src's pages; src and dst must not share a page that dst's table names.
  *   length       [n_seqs] tokens in src
  *   total        [n_seqs] tokens that the sequence has had (next position)
  *   keep, recent 1 <= keep <= dst's max_pages * page, 0 <= recent <= keep

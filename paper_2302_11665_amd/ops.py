@@ -179,7 +179,9 @@ class Cache:
     k int32 [pages, heads, page, 4, dim/32], v int32 [pages, heads, page/32, 4,
     16, dim/16], k_par and v_par float16 [pages, heads, dim/group, page, 2], pos
     int32 and acc float32 [pages, heads, page] (either may be None where no
-    weights are kept), page_table int32 [seqs, max_pages].  Calls use the
+    weights are kept), page_table int32 [seqs, max_pages].  Sequences may share
+    pages that a call only reads; a page that it writes (tokens appended,
+    weights accumulated, an eviction's destination) is one sequence's.  Calls use the
     addresses that these had when the cache was made, so none can be replaced:
     `dataclasses.replace(cache, page_table=..)` makes a cache with another one."""
     k: torch.Tensor
@@ -282,7 +284,8 @@ def attention_kv4(q, cache: Cache, length, scale=None, acc_in=None, acc_out=None
     first length[b] slots of every sequence, the queries being the last of them:
     query i sees slots below length - queries + i + 1.  `scale` defaults to
     dim ** -0.5.  With acc_out (fp32, laid out as cache.acc), acc_out = acc_in +
-    the attention weight that every slot got from the queries of its head."""
+    the attention weight that every slot got from the queries of its head; the
+    sequences then may not share pages."""
     q = _tokens(q, "q", cache, 0)
     if q.data_ptr() % 16 or q.stride(0) % 8 or q.stride(1) % 8:
         q = q.contiguous()

@@ -501,6 +501,36 @@ def test_append_beyond_the_table_writes_nothing_there():
     assert np.array_equal(before["k"][kept], after["k"][kept]) and np.array_equal(before["v"][kept], after["v"][kept])
 
 
+def test_sequences_that_share_their_first_pages():
+    """Attention without weights, and a cut out of shared pages, as with pages of
+    their own; weights with pages of their own."""
+    g = gen(6)
+    lengths, shared = [150, 97, 64, 300], 2  # 64 slots in common
+    own = make_cache(g, lengths, 2, 64, 32, 32, spare=1)
+    table = own.page_table.clone()
+    table[1:, :shared] = table[0, :shared]
+    c = dataclasses.replace(own, page_table=table)
+    for name in ("k", "v", "k_par", "v_par", "pos", "acc"):
+        x = getattr(own, name)
+        x[own.page_table[1:, :shared].long()] = x[table[1:, :shared].long()]
+    q = normal(g, 4, 3, 6, 64, dtype=F16)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    o = ops.attention_kv4(q, c, n)
+    check_attention(c, q, lengths, o)
+    weights = torch.zeros_like(own.acc)
+    assert torch.equal(ops.attention_kv4(q, own, n, acc_out=weights), o)
+    check_attention(own, q, lengths, o, acc_out=weights.cpu().numpy())
+    at = torch.arange(own.pos.shape[0] * 32, device="cuda").view(-1, 1, 32).expand(-1, 2, 32).int()
+    own.pos.copy_(at)
+    own.pos[own.page_table[1:, :shared].long()] = own.pos[table[1:, :shared].long()]
+    kept = []
+    for src in (c, own):
+        dst = ops.Cache.empty(12, 2, 64, torch.arange(12, dtype=torch.int32, device="cuda").view(4, 3), group=32, page=32)
+        new = ops.cache_evict(src, dst, n, torch.full_like(n, 10 ** 6), keep=80, recent=0)
+        kept.append([new, dst.k, dst.v, dst.k_par, dst.v_par, dst.pos, dst.acc])
+    assert all(torch.equal(a, z) for a, z in zip(*kept)) and kept[0][0].tolist() == [80, 80, 64, 80]
+
+
 def test_a_longer_table_makes_another_cache():
     g = gen(4)
     c = make_cache(g, [40, 64], 2, 64, 64, 32, spare=3)
