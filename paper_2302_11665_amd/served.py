@@ -132,12 +132,13 @@ class Profile:
 
 def step_seconds(block: Block, batch: int, steps: int = 32) -> float:
     """Seconds of one step of the block at its budget's length, the cuts of the
-    cache included: `steps` steps in a row, a whole number of cuts apart."""
+    cache included: at least `steps` steps in a row, every `slack`-th of which
+    cuts, the first one among them."""
     import torch
     s = block.shape
     caches = Caches(s, batch, block.device)
     x = torch.randn(batch, s.hidden, device=block.device).to(torch.bfloat16)
-    for _ in range(s.budget):
+    for _ in range(s.budget + 2 * s.slack):  # full, and cut and full again
         block.step(x, caches)
     steps = -(-steps // s.slack) * s.slack
     start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)

@@ -68,6 +68,39 @@ def test_a_cut_changes_nothing_before_it():
     assert torch.equal(longer[:64], free) and torch.isfinite(longer).all()
 
 
+def test_a_step_is_timed_with_its_share_of_the_cuts(monkeypatch):
+    """Cuts made slower by a known amount show in the step's time, one in `slack` steps."""
+    import torch
+    from paper_2302_11665_amd import ops, served
+    block = served.Block(small(slack=32), seed=3)
+    a = torch.randn(6000, 6000, device="cuda")
+
+    def busy():
+        for _ in range(8):
+            torch.mm(a, a)
+
+    start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    for _ in range(2):
+        start.record()
+        busy()
+        stop.record()
+        torch.cuda.synchronize()
+    extra = start.elapsed_time(stop) * 1e-3
+    say("a slow cut:", extra, "s")
+    plain = served.step_seconds(block, 2)
+    evict = ops.cache_evict
+
+    def slow(*args, **kw):
+        busy()
+        return evict(*args, **kw)
+
+    monkeypatch.setattr(ops, "cache_evict", slow)
+    cuts = served.step_seconds(block, 2)
+    say("steps:", plain, cuts)
+    # a 32nd of it a step; half and twice that for the clock's changes between the two
+    assert extra / 32 / 2 < cuts - plain < extra / 32 * 2
+
+
 def test_profile_and_placement():
     from paper_2302_11665_amd import served
     shape = small()
