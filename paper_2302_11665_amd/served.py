@@ -35,10 +35,14 @@ class Shape:
     dim: int
     inner: int          # width of the feed-forward layer
     budget: int         # tokens that a request's cache keeps
-    slack: int = 64     # tokens that it may grow by before it is cut back
+    slack: int = 64     # tokens that it may grow by before it is cut back, at least 1
     recent: int = 64    # newest tokens that a cut always keeps
     group: int = 64
     page: int = 64
+
+    def __post_init__(self):
+        if self.budget < 1 or self.slack < 1 or self.recent < 0:
+            raise ValueError(f"a cache of {self.budget} tokens that grows by {self.slack}, the newest {self.recent} kept")
 
 
 class Block:

@@ -223,3 +223,13 @@ def test_evict_refuses_new_lengths_over_the_old_ones(L):
     for out in (0x100, 0x104, 0xfc, 0x200, 0x204):
         assert L.as_cache_evict(cache(), cache(), 0x100, 0x200, 8, 2, out, 0x400, 1 << 20, None) == sim.AS_E_INVALID_ARG
         assert "out_length" in sim.as_last_error()
+
+
+def test_a_cache_without_room_to_grow_is_refused():
+    """With no slack, a token behind a full table would be lost; with no budget, a cut keeps nothing."""
+    from paper_2302_11665_amd import served
+    f = dict(layers=1, hidden=64, heads=2, kv_heads=1, dim=64, inner=128, budget=64)
+    for kw in (dict(slack=0), dict(slack=-1), dict(budget=0), dict(recent=-1)):
+        with pytest.raises(ValueError):
+            served.Shape(**{**f, **kw})
+    served.Shape(**f, slack=1, recent=0)
