@@ -108,7 +108,8 @@ class Caches:
         self.held = 0  # length of all of them, on the host
 
     def bytes_per_sequence(self) -> int:
-        return self.now.bytes_per_slot * self.now.page_table.shape[1] * self.shape.page
+        """Of both sets of pages."""
+        return 2 * self.now.bytes_per_slot * self.now.page_table.shape[1] * self.shape.page
 
     def attend(self, q, k, v):
         """Append one token's keys and values, attend, and cut back if due."""

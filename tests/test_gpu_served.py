@@ -68,6 +68,15 @@ def test_a_cut_changes_nothing_before_it():
     assert torch.equal(longer[:64], free) and torch.isfinite(longer).all()
 
 
+def test_the_bytes_of_a_sequence_are_those_of_its_arrays():
+    from paper_2302_11665_amd import served
+    for shape in (small(), small(budget=100, dim=128, group=32, page=64)):
+        caches = served.Caches(shape, 3)
+        arrays = {x.data_ptr(): x.numel() * x.element_size() for c in (caches.now, caches.spare)
+                  for x in (c.k, c.v, c.k_par, c.v_par, c.pos, c.acc)}
+        assert len(arrays) == 12 and 3 * caches.bytes_per_sequence() == sum(arrays.values())
+
+
 def test_a_step_is_timed_with_its_share_of_the_cuts(monkeypatch):
     """Cuts made slower by a known amount show in the step's time, one in `slack` steps."""
     import torch
