@@ -116,13 +116,13 @@ class Caches:
         from . import ops
         s = self.shape
         if self.held == s.budget + s.slack:
-            self.length = ops.cache_evict(self.now, self.spare, self.length, self.total, keep=s.budget,
-                                          recent=min(s.recent, s.budget))
+            self.length.copy_(ops.cache_evict(self.now, self.spare, self.length, self.total, keep=s.budget,
+                                              recent=min(s.recent, s.budget)))
             self.now, self.spare = self.spare, self.now
             self.held = s.budget
         ops.cache_append(self.now, k, v, self.length, first_pos=self.total)
-        self.length = self.length + 1
-        self.total = self.total + 1
+        self.length.add_(1)  # in place: a captured step is replayed on the same numbers
+        self.total.add_(1)
         self.held += 1
         return ops.attention_kv4(q, self.now, self.length, acc_in=self.now.acc, acc_out=self.now.acc)
 
@@ -135,24 +135,39 @@ class Profile:
     weight_mib: int     # weights and the caches of `requests` requests
 
 
+def capture_cycle(block: Block, x, caches: Caches):
+    """A graph of 2 * slack steps on x from full caches on: a cut into the spare
+    pages, steps until they are full, a cut back and steps until the first ones
+    are full again.  Nothing is run; every replay takes the caches that far."""
+    import torch
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(2 * block.shape.slack):
+            block.step(x, caches)
+    return graph
+
+
 def step_seconds(block: Block, batch: int, steps: int = 32) -> float:
     """Seconds of one step of the block at its budget's length, the cuts of the
     cache included: at least `steps` steps in a row, every `slack`-th of which
-    cuts, the first one among them."""
+    cuts, the first one among them.  They are replayed from a graph: a step has
+    some twenty launches, which take the host longer than the device."""
     import torch
     s = block.shape
     caches = Caches(s, batch, block.device)
     x = torch.randn(batch, s.hidden, device=block.device).to(torch.bfloat16)
-    for _ in range(s.budget + 2 * s.slack):  # full, and cut and full again
+    for _ in range(s.budget + 3 * s.slack):  # full, and a cycle before the one that is captured
         block.step(x, caches)
-    steps = -(-steps // s.slack) * s.slack
+    graph = capture_cycle(block, x, caches)
+    graph.replay()
+    replays = -(-steps // (2 * s.slack))
     start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     start.record()
-    for _ in range(steps):
-        block.step(x, caches)
+    for _ in range(replays):
+        graph.replay()
     stop.record()
     torch.cuda.synchronize()
-    return start.elapsed_time(stop) * 1e-3 / steps
+    return start.elapsed_time(stop) * 1e-3 / (replays * 2 * s.slack)
 
 
 def measure(shape: Shape, tokens: int, requests: int = 8, batch: int = 8, device="cuda") -> Profile:

@@ -110,6 +110,52 @@ def test_a_step_is_timed_with_its_share_of_the_cuts(monkeypatch):
     assert extra / 32 / 2 < cuts - plain < extra / 32 * 2
 
 
+def test_a_step_is_timed_without_the_host(monkeypatch):
+    """What the host does between launches is no part of what a model costs on a device."""
+    import time
+    from paper_2302_11665_amd import served
+    block = served.Block(small(slack=4), seed=3)
+    step = block.step
+
+    def slow(x, caches):
+        time.sleep(3e-3)
+        return step(x, caches)
+
+    monkeypatch.setattr(block, "step", slow)
+    seconds = served.step_seconds(block, 2)
+    say("step:", seconds)
+    assert 0 < seconds < 1.5e-3
+
+
+@pytest.mark.parametrize("hidden,seqs", [(256, 3), (4096, 1), (1024, 8)])
+def test_replayed_steps_are_the_steps(hidden, seqs):
+    """A captured cycle of steps, replayed several times with other work between, leaves what as many steps leave."""
+    import torch
+    from paper_2302_11665_amd import served
+    shape = small(hidden=hidden, inner=2 * hidden, slack=5, budget=60)
+    block = served.Block(shape, seed=3)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    x = torch.randn(seqs, hidden, device="cuda", generator=g).to(torch.bfloat16)
+    eager, caches = served.Caches(shape, seqs), served.Caches(shape, seqs)
+    for c in (eager, caches):
+        for _ in range(shape.budget + shape.slack):
+            block.step(x, c)
+    graph = served.capture_cycle(block, x, caches)
+
+    def state(c):
+        return [c.length, c.total] + [t for s in (c.now, c.spare) for t in (s.k, s.v, s.k_par, s.v_par, s.pos, s.acc)]
+
+    for i in range(4):
+        graph.replay()
+        for _ in range(2 * shape.slack):
+            block.step(x, eager)
+        torch.cuda.synchronize()
+        assert caches.held == eager.held == shape.budget + shape.slack
+        for a, z in zip(state(caches), state(eager)):
+            assert torch.equal(a, z), i
+
+
 def test_profile_and_placement():
     from paper_2302_11665_amd import served
     shape = small()
