@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import ops_oracle as oo
-from gpu_common import say
+from gpu_common import kernels_run, say
 from paper_2302_11665_amd import ops, sim
 
 pytestmark = pytest.mark.gpu
@@ -128,6 +128,19 @@ def test_linear_tiles_to_outputs_at_odd_places(t, k, n, x_dtype, y_dtype, bias):
     assert (y[:, 0] == 7.0).all() and (y[:, n + 1:] == 7.0).all()
     codes = w.codes.cpu().numpy()[oo.tile_index(n, k)]
     check_linear(x, codes, f64(w.scale), f64(b) if bias else None, y[:, 1:n + 1], y_dtype)
+
+
+# Outputs of a vocabulary's size: two and four channel tiles to a workgroup, the
+# tokens quantised there or before, one to four tiles of them.
+MANY_OUTPUTS = [(1, 300, 16400), (7, 130, 17001), (16, 640, 20000), (20, 200, 16385), (40, 129, 30011), (64, 300, 17000),
+                (1, 700, 32801), (2, 64, 40000), (13, 200, 33333), (16, 128, 65536), (17, 130, 32800), (33, 250, 33001),
+                (64, 100, 34567), (65, 100, 34567)]
+
+
+@pytest.mark.parametrize("t,k,n", MANY_OUTPUTS)
+@pytest.mark.parametrize("x_dtype,y_dtype,bias", [(BF16, F32, False), (F16, F16, True)])
+def test_linear_to_very_many_outputs(t, k, n, x_dtype, y_dtype, bias):
+    test_linear(t, k, n, x_dtype, y_dtype, bias)
 
 
 @pytest.mark.parametrize("t", [1, 5, 40, 300])
@@ -338,6 +351,57 @@ SHORT = [([0, 1, 40, 226], 33, 10, 2, 64, 64, 64), ([0, 0], 120, 2, 2, 64, 64, 3
 @pytest.mark.parametrize("weights", [False, True])
 def test_attention_of_many_rows_over_short_tables(case, dtype, weights):
     test_attention(case, dtype, weights)
+
+
+# Few heads over long contexts, the parts of a row joined by sixteen wavefronts
+# (64 parts and more); prompts of more than eight groups of 128 rows.
+LONG = [([17001], 1, 1, 1, 64, 64, 64), ([9000, 8300], 1, 8, 2, 128, 64, 128), ([20011, 5], 2, 3, 1, 128, 32, 256),
+        ([12345], 1, 5, 1, 64, 32, 32), ([11000], 1, 16, 1, 128, 128, 4096), ([2600, 900], 700, 4, 1, 128, 64, 64),
+        ([1500], 1100, 2, 1, 64, 32, 32), ([1300], 1300, 1, 1, 128, 32, 64)]
+
+
+@pytest.mark.parametrize("case", LONG, ids=[str(i) for i in range(len(LONG))])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("weights", [False, True])
+def test_attention_of_long_contexts_and_prompts(case, dtype, weights):
+    test_attention(case, dtype, weights)
+
+
+@pytest.mark.parametrize("way", ["up", "down", "both"])
+@pytest.mark.parametrize("rows,n", [(1, 700), (1, 6000), (40, 3000), (130, 3000)])
+def test_attention_where_the_maximum_moves(way, rows, n):
+    """Logits that rise or fall by hundreds along the context, exact in fp32, so
+    that only the scaling of what was summed so far can be wrong."""
+    say("maximum", way, rows, n)
+    g = gen(n + rows)
+    dim = 64
+    c = make_cache(g, [n], 1, dim, 64, 64)
+    for x in (c.k_par, c.v_par):
+        x[..., 0] = 0.25
+        x[..., 1] = -2.0
+    # codes 15 where a channel counts, the more of them the further along
+    slot = torch.arange(n, device="cuda")
+    along = {"up": slot, "down": n - 1 - slot, "both": (2 * slot - n).abs()}[way] / (n - 1)
+    codes = torch.where(torch.rand(n, dim, device="cuda", generator=g) < along[:, None], 15, 0).cpu().numpy()
+    words = np.zeros((n, 4, 2), np.uint32)
+    for ch in range(dim):
+        words[:, ch // 8 % 4, ch // 32] |= codes[:, ch].astype(np.uint32) << np.uint32(oo.nibble(ch % 8))
+    table = c.page_table[0].long()
+    c.k[table[slot // 64], 0, slot % 64] = torch.from_numpy(words.view(np.int32)).cuda()
+    q = torch.randint(1, 4, (1, 1, rows, dim), device="cuda", generator=g).to(F16)
+    got = f64(ops.attention_kv4(q, c, torch.tensor([n], dtype=torch.int32, device="cuda"), scale=3.0))[0, 0]
+    h = host(c)
+    kc, vc, kp, vp = oo.read_cache(h["k"], h["v"], h["k_par"], h["v_par"], h["page_table"][0], 0, n, 64, dim, 64)
+    assert np.array_equal(kc, codes)
+    k, v, qd = oo.values(kc, kp), oo.values(vc, vp), f64(q)[0, 0]
+    o, p = oo.attend(qd, k, v, np.ones((rows, n), bool), 3.0)
+    # the logits are exact, scaled ones are rounded four times (the scale, its
+    # product with log2 e, theirs with the logit, the difference); p twice that
+    # much, p d as two bf16 numbers, sums of fp32
+    rel = 8 * 2.0 ** -24 * np.abs(3.0 * qd @ k.T).max(1) + 2.0 ** -17 + (n / 16 + 64) * 2.0 ** -24
+    slack = rel[:, None] * (p @ (31.0 * vp[..., 0] + np.abs(vp[..., 1])))
+    slack += HALF_ULP[F16] * (np.abs(o) + slack) + TINY[F16]
+    assert np.all(np.abs(got - o) <= slack), np.max(np.abs(got - o) / slack)
 
 
 def test_attention_ignores_what_it_does_not_see():
@@ -623,6 +687,40 @@ def test_evict(case, kind):
             assert not z[1][m:].any()  # values' codes behind the last one
     assert np.array_equal(there["acc"][~written], after["acc"][~written])
     assert np.array_equal(there["pos"][~written], after["pos"][~written])
+
+
+# Longer than 16,384 slots, and than the 65,536 that a workgroup's registers hold:
+# ties on both sides of the border, one slot behind it, all before it.
+LONG_EVICT = [([20000, 33], 2, 64, 64, 64, 128, 5000, 100), ([70001], 1, 64, 32, 4096, 64, 69000, 7),
+              ([66000, 300], 1, 128, 64, 256, 64, 500, 3), ([65537, 65536], 1, 64, 64, 128, 32, 65500, 65000),
+              ([140000], 1, 64, 64, 4096, 4096, 20000, 0)]
+
+
+@pytest.mark.parametrize("case", LONG_EVICT, ids=[str(i) for i in range(len(LONG_EVICT))])
+@pytest.mark.parametrize("kind", ["plain", "ties", "special"])
+def test_evict_of_long_caches(case, kind):
+    test_evict(case, kind)
+
+
+def test_the_long_cases_reach_their_kernels():
+    """Those that only many outputs, long tables or few long segments choose (on a device of 256 compute units)."""
+    if torch.cuda.get_device_properties(0).multi_processor_count != 256:
+        pytest.skip("the sizes are for 256 compute units")
+    g = gen(2)
+
+    def names(f):
+        return " ".join(kernels_run(f))
+
+    for t, n, want in ((3, 17001, "0, 2, 1, true>"), (3, 32801, "0, 4, 1, true>"), (40, 17001, "0, 2, 3, false>"),
+                       (40, 33001, "0, 4, 3, false>")):
+        x, w = normal(g, t, 130, dtype=BF16), ops.pack_weight(normal(g, n, 130))
+        assert f"product_few<0, {want}" in names(lambda: ops.linear_i8(x, w)), (t, n)
+    for n in (17001, 70001):
+        src, dst = make_cache(g, [n], 1, 64, 64, 4096), make_cache(g, [64], 1, 64, 64, 32)
+        lengths = torch.tensor([n], dtype=torch.int32, device="cuda")
+        assert "evict_select<16>" in names(lambda: ops.cache_evict(src, dst, lengths, lengths, keep=64, recent=3)), n
+        q = normal(g, 1, 1, 1, 64, dtype=BF16)
+        assert "join<0, 64, 1, 1024>" in names(lambda: ops.attention_kv4(q, src, lengths)), n
 
 
 # --------------------------------------------------------- streams and graphs
