@@ -48,7 +48,10 @@ extern "C" {
  * columns K..Kp-1 hold 0, rows beyond R anything.
  */
 
-/* Bytes of the codes of n_rows rows of n_cols columns (0 for sizes out of range). */
+/*
+ * Bytes of the codes of n_rows rows of n_cols columns (0 for sizes out of range:
+ * at most 2^24 - 1 rows and AS_I8_MAX_INPUTS columns).
+ */
 int64_t as_i8_bytes(int64_t n_rows, int64_t n_cols);
 
 /*
@@ -180,7 +183,8 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
  * share src's pages; src and dst must not share a page that dst's table names.
  *   length       [n_seqs] tokens in src
  *   total        [n_seqs] tokens that the sequence has had (next position)
- *   keep, recent 1 <= keep <= dst's max_pages * page, 0 <= recent <= keep
+ *   keep, recent 1 <= keep <= dst's max_pages * page, at most 2^29 - 32;
+ *                0 <= recent <= keep
  *   out_length   [n_seqs] tokens in dst: min(length, keep); an array of its own,
  *                length and total are read while it is written
  * src and dst agree in n_heads, dim, group and n_seqs; pos and acc are needed.

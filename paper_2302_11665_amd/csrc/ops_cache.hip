@@ -506,6 +506,8 @@ int as_cache_evict(const as_cache_t* src, const as_cache_t* dst, const int32_t* 
   if (keep < 1 || recent < 0 || recent > keep || keep > (int64_t)dst->max_pages * dst->page)
     return fail(AS_E_INVALID_ARG, "cache_evict: keep %d (the destination has room for %lld), recent %d", keep,
                 (long long)dst->max_pages * dst->page, recent);
+  // a workgroup of 256 for 32 of them, fewer than 2^32 threads a launch
+  if (keep > (1 << 29) - 32) return fail(AS_E_LIMITS, "cache_evict: keep %d (at most 2^29 - 32)", keep);
   if ((int64_t)src->n_seqs * src->n_heads > 65535)
     return fail(AS_E_LIMITS, "cache_evict: %d sequences of %d heads (at most 65535 in all)", src->n_seqs,
                 src->n_heads);

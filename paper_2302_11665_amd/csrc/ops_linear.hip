@@ -642,7 +642,7 @@ int launch_fused(const LinArgs& p, int y_type, hipStream_t s) {
   return few_by_channels<AS_F32, XTYPE, 1, true>(p, s);
 }
 
-constexpr int64_t kMaxRows = 1 << 24;
+constexpr int64_t kMaxRows = (1 << 24) - 1;  // a workgroup of 256 to a row, fewer than 2^32 threads a launch
 
 }  // namespace as_ops
 

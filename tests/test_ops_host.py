@@ -233,3 +233,12 @@ def test_a_cache_without_room_to_grow_is_refused():
         with pytest.raises(ValueError):
             served.Shape(**{**f, **kw})
     served.Shape(**f, slack=1, recent=0)
+
+
+def test_sizes_whose_launch_would_have_too_many_threads_are_refused(L):
+    """A launch has fewer than 2^32 threads a dimension: 256 a row of codes, 256 for 32 tokens that a cut keeps."""
+    assert L.as_quantize_i8(0x100, 0, 1 << 24, 64, 64, 0x1000, 0x2000, None) == sim.AS_E_LIMITS
+    assert L.as_i8_bytes(1 << 24, 64) == 0 and L.as_i8_bytes((1 << 24) - 1, 64) == (1 << 24) * 128
+    wide = cache(page=4096, max_pages=1 << 18)
+    for keep in ((1 << 29) - 31, 1 << 29, 1 << 30):
+        assert L.as_cache_evict(wide, wide, 0x100, 0x200, keep, 2, 0x300, 0x400, 1 << 62, None) == sim.AS_E_LIMITS
