@@ -74,14 +74,18 @@ def _need(x, name, dtypes, dim=None, device=None, contiguous=True):
     return x
 
 
-def _call(fn, device, *args):
-    """fn(*args, stream) on the current stream of the tensors' device, that device current meanwhile."""
+def _on(fn, device, *args):
+    """fn(*args) with the tensors' device current meanwhile."""
     index = device.index
     if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
-    else:
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+            return fn(*args)
+    return fn(*args)
+
+
+def _call(fn, device, *args):
+    """fn(*args, stream) on the current stream of the tensors' device, that device current meanwhile."""
+    rc = _on(fn, device, *args, torch._C._cuda_getCurrentRawStream(device.index))
     if rc != sim.AS_OK:
         sim._check(rc)
 
@@ -304,7 +308,8 @@ def attention_kv4(q, cache: Cache, length, scale=None, acc_in=None, acc_out=None
     out = torch.empty_like(q, memory_format=torch.contiguous_format)
     heads = q.shape[2]
     L = lib()
-    need = L.as_attention_kv4_workspace(c, q.shape[1], heads, 0 if acc_out is None else 1)
+    # (its size depends on the device's compute units)
+    need = _on(L.as_attention_kv4_workspace, q.device, c, q.shape[1], heads, 0 if acc_out is None else 1)
     _keep, ws = _workspace(need, q.device)
     _call(L.as_attention_kv4, q.device, c, q.data_ptr(), _TYPES[q.dtype], q.shape[1], heads, q.stride(0), q.stride(1),
           n, c.dim ** -0.5 if scale is None else scale, out.data_ptr(), None if acc_in is None else acc_in.data_ptr(),

@@ -242,3 +242,36 @@ def test_sizes_whose_launch_would_have_too_many_threads_are_refused(L):
     wide = cache(page=4096, max_pages=1 << 18)
     for keep in ((1 << 29) - 31, 1 << 29, 1 << 30):
         assert L.as_cache_evict(wide, wide, 0x100, 0x200, keep, 2, 0x300, 0x400, 1 << 62, None) == sim.AS_E_LIMITS
+
+
+def test_attention_asks_for_scratch_memory_with_the_tensors_device_current(monkeypatch):
+    """The size follows from the device's compute units: another device's would not do."""
+    import contextlib
+    import torch
+    from paper_2302_11665_amd import ops
+    current, seen = [5], []
+
+    @contextlib.contextmanager
+    def device(index):
+        current.append(index)
+        yield
+        current.pop()
+
+    class Lib:
+        def as_attention_kv4_workspace(self, *args):
+            seen.append(current[-1])
+            return 512
+
+        def as_attention_kv4(self, *args):
+            seen.append(current[-1])
+            return sim.AS_OK
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[-1], raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(ops, "lib", Lib)
+    c = object.__new__(ops.Cache)
+    object.__setattr__(c, "_c", cache())
+    object.__setattr__(c, "k", torch.zeros(1))
+    ops.attention_kv4(torch.zeros(2, 1, 4, 64, dtype=torch.float16), c, torch.zeros(2, dtype=torch.int32))
+    assert len(seen) == 2 and 5 not in seen
