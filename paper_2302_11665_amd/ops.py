@@ -291,10 +291,11 @@ def attention_kv4(q, cache: Cache, length, scale=None, acc_in=None, acc_out=None
     the attention weight that every slot got from the queries of its head; the
     sequences then may not share pages."""
     q = _tokens(q, "q", cache, 0)
-    if q.data_ptr() % 16 or q.stride(0) % 8 or q.stride(1) % 8:
-        q = q.contiguous()
-        if q.data_ptr() % 16:
-            q = q.clone(memory_format=torch.contiguous_format)
+    # (the stride of a dimension of one entry may be anything, and is not used)
+    q_seq, q_token = q.stride(0) if q.shape[0] > 1 else 0, q.stride(1) if q.shape[1] > 1 else 0
+    if q.data_ptr() % 16 or q_seq % 8 or q_token % 8:
+        q = q.clone(memory_format=torch.contiguous_format)
+        q_seq, q_token = q.stride(0), q.stride(1)
     n = _counts(length, "length", cache)
     c = cache._c
     if acc_out is not None:
@@ -311,8 +312,8 @@ def attention_kv4(q, cache: Cache, length, scale=None, acc_in=None, acc_out=None
     # (its size depends on the device's compute units)
     need = _on(L.as_attention_kv4_workspace, q.device, c, q.shape[1], heads, 0 if acc_out is None else 1)
     _keep, ws = _workspace(need, q.device)
-    _call(L.as_attention_kv4, q.device, c, q.data_ptr(), _TYPES[q.dtype], q.shape[1], heads, q.stride(0), q.stride(1),
-          n, c.dim ** -0.5 if scale is None else scale, out.data_ptr(), None if acc_in is None else acc_in.data_ptr(),
+    _call(L.as_attention_kv4, q.device, c, q.data_ptr(), _TYPES[q.dtype], q.shape[1], heads, q_seq, q_token, n,
+          c.dim ** -0.5 if scale is None else scale, out.data_ptr(), None if acc_in is None else acc_in.data_ptr(),
           None if acc_out is None else acc_out.data_ptr(), ws, need)
     return out
 

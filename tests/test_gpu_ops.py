@@ -492,6 +492,18 @@ def test_attention_query_strides():
     assert torch.equal(ops.attention_kv4(odd, c, n), want)
 
 
+def test_attention_of_one_token_at_any_stride():
+    g = gen(14)
+    c = make_cache(g, [50], 2, 64, 64, 32)
+    n = torch.tensor([50], dtype=torch.int32, device="cuda")
+    line = normal(g, 2048, dtype=F16)
+    want = ops.attention_kv4(line[:256].view(1, 1, 4, 64), c, n)
+    for strides in ((1003, 256, 64, 1), (1003, 77, 64, 1), (0, 0, 64, 1)):
+        assert torch.equal(ops.attention_kv4(line.as_strided((1, 1, 4, 64), strides), c, n), want)
+    two = line[256:].as_strided((1, 2, 4, 64), (5, 300, 64, 1))  # 300 is no multiple of 8
+    assert torch.equal(ops.attention_kv4(two, c, n), ops.attention_kv4(two.clone(memory_format=torch.contiguous_format), c, n))
+
+
 @pytest.mark.parametrize("dim,group,page", [(64, 32, 32), (64, 64, 64), (128, 32, 96), (128, 64, 32), (128, 128, 64)])
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("starts,t", [([0, 5, 31], 1), ([0, 32, 40], 33), ([7, 0, 90], 70)])

@@ -275,3 +275,32 @@ def test_attention_asks_for_scratch_memory_with_the_tensors_device_current(monke
     object.__setattr__(c, "k", torch.zeros(1))
     ops.attention_kv4(torch.zeros(2, 1, 4, 64, dtype=torch.float16), c, torch.zeros(2, dtype=torch.int32))
     assert len(seen) == 2 and 5 not in seen
+
+
+def test_queries_of_one_sequence_or_token_at_any_stride(monkeypatch):
+    """The stride of a dimension of one entry is never used, and torch leaves anything there."""
+    import torch
+    from paper_2302_11665_amd import ops
+    passed = []
+
+    class Lib:
+        def as_attention_kv4_workspace(self, *args):
+            return 0
+
+        def as_attention_kv4(self, *args):
+            pass
+
+    monkeypatch.setattr(ops, "lib", Lib)
+    monkeypatch.setattr(ops, "_on", lambda fn, device, *args: fn(*args), raising=False)
+    monkeypatch.setattr(ops, "_call", lambda fn, device, *args: passed.append(args))
+    line = torch.randn(4096).to(torch.bfloat16)
+    for seqs, strides in ((1, (1003, 256, 64, 1)), (1, (1003, 77, 64, 1)), (2, (512, 77, 64, 1)), (1, (0, 0, 64, 1)),
+                          (2, (0, 3, 64, 1))):
+        c = object.__new__(ops.Cache)
+        object.__setattr__(c, "_c", cache(n_seqs=seqs))
+        object.__setattr__(c, "k", torch.zeros(1))
+        q = line.as_strided((seqs, 1, 4, 64), strides)
+        ops.attention_kv4(q, c, torch.zeros(seqs, dtype=torch.int32))
+        _, at, _, queries, heads, q_seq, q_token = passed[-1][:7]
+        assert (queries, heads) == (1, 4) and q_seq % 8 == 0 and q_token % 8 == 0 and at % 16 == 0
+        assert at == q.data_ptr() and (seqs == 1 or q_seq == strides[0])  # where they are, not a copy
