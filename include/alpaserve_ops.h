@@ -152,7 +152,9 @@ int as_cache_append(const as_cache_t* cache, const void* k, const void* v, int32
  *            last two dimensions contiguous, q_seq and q_token strides in
  *            elements (multiples of 8), aligned to 16 bytes
  *   length   [n_seqs]
- *   scale    finite, > 0
+ *   scale    > 0, at most 2e38.  Logits (scale q.k) may reach 2^30 in magnitude;
+ *            beyond that, where fp32 numbers lie 64 and more apart, a query's
+ *            output and the weights that it gives are unspecified
  *   out      [n_seqs][n_queries][n_q_heads][dim] of `type`, contiguous, aligned
  *            to 8 bytes
  *   acc_in, acc_out  laid out as cache->acc: for every slot s below the

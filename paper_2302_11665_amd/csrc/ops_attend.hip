@@ -1499,7 +1499,8 @@ int as_attention_kv4(const as_cache_t* cache, const void* q, int32_t type, int32
   rc = check_queries(cache, n_queries, n_q_heads);
   if (rc != AS_OK) return rc;
   if (type != AS_BF16 && type != AS_F16) return fail(AS_E_INVALID_ARG, "attention_kv4: type %d", type);
-  if (!(scale > 0.0f) || scale > 3.0e38f) return fail(AS_E_INVALID_ARG, "attention_kv4: scale %g", (double)scale);
+  // (its product with log2 e has to be finite)
+  if (!(scale > 0.0f) || scale > 2.0e38f) return fail(AS_E_INVALID_ARG, "attention_kv4: scale %g", (double)scale);
   if (cache->n_seqs == 0 || n_queries == 0) return as_host::ok();
   if (!q || !length || !out) return fail(AS_E_INVALID_ARG, "attention_kv4: null pointer");
   if (!aligned(q, 16) || !aligned(out, 8) || q_seq % 8 || q_token % 8)

@@ -478,6 +478,39 @@ def test_attention_sums_over_long_runs(dim, group, seqs, heads, n):
         off) / np.linalg.norm(o)
 
 
+@pytest.mark.parametrize("rows,n", [(1, 100), (1, 3000), (40, 3000), (130, 1000)])
+def test_attention_over_the_largest_logits(rows, n):
+    """All logits far below zero, or above, up to 2^30: the largest one takes all, its value comes out as it is."""
+    say("largest logits", rows, n)
+    g = gen(n + rows)
+    c = make_cache(g, [n], 1, 64, 64, 64)
+    for x in (c.k_par, c.v_par):
+        x[..., 0] = 0.25
+        x[..., 1] = 0.5  # keys of 0.5 to 4.25: every logit has the sign of q
+    h = host(c)
+    kc, vc, kp, vp = oo.read_cache(h["k"], h["v"], h["k_par"], h["v_par"], h["page_table"][0], 0, n, 64, 64, 64)
+    k, v = oo.values(kc, kp), oo.values(vc, vp)
+    lengths = torch.tensor([n], dtype=torch.int32, device="cuda")
+    for size, scale in ((-2.0 ** 18, 1.0), (2.0 ** 18, 1.0), (-1.0, 2.0 ** 18), (-2.0 ** -90, 2.0 ** 108), (2.0 ** 21, 0.125), (-0.01, 3.0)):
+        q = (size * 2.0 ** torch.randint(0, 3, (1, 1, rows, 64), device="cuda", generator=g)).to(BF16)
+        out = f64(ops.attention_kv4(q, c, lengths, scale=scale))[0, 0]
+        weights = torch.zeros_like(c.acc)
+        assert np.array_equal(f64(ops.attention_kv4(q, c, lengths, scale=scale, acc_out=weights))[0, 0], out)
+        a = f64(q)[0, 0] @ k.T * scale
+        assert np.abs(a).max() < 2.0 ** 30
+        got = np.argsort(-a, axis=1)
+        first, second = (np.take_along_axis(a, got[:, i:i + 1], 1)[:, 0] for i in (0, 1))
+        # fp32 sums of 64 products tell them apart where they differ by 2^-16 of their size
+        clear = first - second > 2.0 ** -16 * np.abs(first) + 40.0  # (e^-40 of another value is nothing)
+        assert clear.any() or abs(size * scale) < 1.0
+        # all weight on one slot: the output's rounding, and p d as two bf16 numbers
+        want = v[got[:, 0]]
+        assert np.all(np.abs(out - want)[clear] <= 2.0 ** -8 * np.abs(want)[clear] + 2.0 ** -17 * (31 * 0.25 + 0.5)), (
+            size, scale)
+        pg = h["page_table"][0][np.arange(n) // 64]
+        assert weights.cpu().numpy()[pg, 0, np.arange(n) % 64].sum() == pytest.approx(rows, rel=1e-5)
+
+
 def test_attention_query_strides():
     g = gen(13)
     lengths = [50, 20, 77]

@@ -277,6 +277,14 @@ def test_attention_asks_for_scratch_memory_with_the_tensors_device_current(monke
     assert len(seen) == 2 and 5 not in seen
 
 
+def test_attention_refuses_scales_beyond_fp32_once_times_log2_e(L):
+    def call(scale):
+        return L.as_attention_kv4(cache(), 0x100, 0, 1, 4, 256, 256, 0x200, scale, 0x300, None, None, None, 0, None)
+
+    for scale in (2.4e38, 2.9e38, 3.4e38):
+        assert call(scale) == sim.AS_E_INVALID_ARG and "scale" in sim.as_last_error()
+
+
 def test_queries_of_one_sequence_or_token_at_any_stride(monkeypatch):
     """The stride of a dimension of one entry is never used, and torch leaves anything there."""
     import torch
