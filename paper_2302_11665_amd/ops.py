@@ -229,6 +229,9 @@ class Cache:
     @staticmethod
     def empty(n_pages, n_heads, dim, page_table, group=64, page=64, device="cuda") -> "Cache":
         """A cache of zeros."""
+        if dim < 1 or group < 1 or page < 1 or dim % 32 or dim % group or page % 32:
+            _bad(f"cache: heads of {dim} channels, {group} channels to a scale, pages of {page} slots (whole scales a "
+                 "head; multiples of 32)")
         z = lambda shape, dtype: torch.zeros(shape, dtype=dtype, device=device)  # noqa: E731
         par = (n_pages, n_heads, dim // group, page, 2)
         return Cache(k=z((n_pages, n_heads, page, 4, dim // 32), torch.int32),

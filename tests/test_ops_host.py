@@ -312,3 +312,14 @@ def test_queries_of_one_sequence_or_token_at_any_stride(monkeypatch):
         _, at, _, queries, heads, q_seq, q_token = passed[-1][:7]
         assert (queries, heads) == (1, 4) and q_seq % 8 == 0 and q_token % 8 == 0 and at % 16 == 0
         assert at == q.data_ptr() and (seqs == 1 or q_seq == strides[0])  # where they are, not a copy
+
+
+def test_an_empty_cache_has_the_sizes_that_were_asked_for(L):
+    """Sizes that the storage cannot hold are refused, not rounded to others."""
+    import torch
+    from paper_2302_11665_amd import ops
+    table = torch.zeros(1, 1, dtype=torch.int32)
+    for kw in (dict(dim=128, group=48), dict(dim=130), dict(dim=64, group=50), dict(dim=64, group=0), dict(dim=64, page=48),
+               dict(dim=64, group=128), dict(dim=65, group=33)):
+        with pytest.raises(sim.SimError, match="(?s)channels|slots"):
+            ops.Cache.empty(1, 1, page_table=table, device="cpu", **kw)
