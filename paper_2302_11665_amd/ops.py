@@ -329,6 +329,8 @@ def cache_evict(src: Cache, dst: Cache, length, total, keep, recent):
     n, t = _counts(length, "length", src), _counts(total, "total", src)
     if src.k.device != dst.k.device:
         _bad("cache_evict: caches on different devices")
+    if not 0 <= recent <= keep < 1 << 31:  # (ctypes passes the lowest 32 bits of others)
+        _bad(f"cache_evict: keep {keep}, recent {recent}")
     new = torch.empty(length.shape[0], dtype=torch.int32, device=length.device)
     L = lib()
     need = L.as_cache_evict_workspace(src._c, keep)

@@ -323,3 +323,19 @@ def test_an_empty_cache_has_the_sizes_that_were_asked_for(L):
                dict(dim=64, group=128), dict(dim=65, group=33)):
         with pytest.raises(sim.SimError, match="(?s)channels|slots"):
             ops.Cache.empty(1, 1, page_table=table, device="cpu", **kw)
+
+
+def test_counts_that_do_not_fit_32_bits_are_refused(calls):
+    """ctypes would pass their lowest bits."""
+    import torch
+    from paper_2302_11665_amd import ops
+    c = object.__new__(ops.Cache)
+    object.__setattr__(c, "_c", cache())
+    object.__setattr__(c, "k", torch.zeros(1))
+    n = torch.zeros(2, dtype=torch.int32)
+    for keep, recent in ((2 ** 32 + 8, 2), (8, 2 ** 32 + 2), (8, -2 ** 32 + 2), (2 ** 31, 0)):
+        with pytest.raises(sim.SimError):
+            ops.cache_evict(c, c, n, n, keep=keep, recent=recent)
+    assert not calls
+    ops.cache_evict(c, c, n, n, keep=8, recent=2)
+    assert calls[-1][1][4:6] == (8, 2)
