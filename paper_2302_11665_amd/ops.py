@@ -100,10 +100,10 @@ def _workspace(n, device):
 
 def _rows(x):
     """x [rows, columns] as rows that lie apart, and their stride: a broadcast row or overlapping windows are copied."""
-    t, n = x.shape
-    if (n > 1 and x.stride(1) != 1) or (t > 1 and x.stride(0) < n):
-        x = x.contiguous()
-    return x, x.stride(0) if t > 1 else n
+    (t, n), (stride, step) = x.shape, x.stride()
+    if (n > 1 and step != 1) or (t > 1 and stride < n):
+        x, stride = x.contiguous(), n
+    return x, stride if t > 1 else n
 
 
 _16 = (torch.bfloat16, torch.float16)
@@ -177,7 +177,7 @@ def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
 
 # -------------------------------------------------------------------- cache
 
-@dataclasses.dataclass(frozen=True, eq=False)
+@dataclasses.dataclass(frozen=True, eq=False, init=False)
 class Cache:
     """A paged cache of 4 bits; the arrays are those of as_cache_t:
     k int32 [pages, heads, page, 4, dim/32], v int32 [pages, heads, page/32, 4,
@@ -196,9 +196,9 @@ class Cache:
     acc: torch.Tensor
     page_table: torch.Tensor
 
-    def __post_init__(self):
+    def __init__(self, k, v, k_par, v_par, pos, acc, page_table):
         # one cheap look at everything first: a step may make its handles anew
-        k, v, kp, vp, pos, acc, table = self.k, self.v, self.k_par, self.v_par, self.pos, self.acc, self.page_table
+        kp, vp, table = k_par, v_par, page_table
         try:
             pages, heads, page, four, words = k.shape
             groups = kp.shape[2]
@@ -221,7 +221,7 @@ class Cache:
             what = [None if x is None else (tuple(x.shape), x.dtype, str(x.device)) if isinstance(x, torch.Tensor)
                     else type(x) for x in (k, v, kp, vp, pos, acc, table)]
             _bad(f"cache: contiguous CUDA arrays of one cache are needed, not {what}")
-        object.__setattr__(self, "_c", as_cache_t(
+        self.__dict__.update(k=k, v=v, k_par=kp, v_par=vp, pos=pos, acc=acc, page_table=table, _c=as_cache_t(
             pages, heads, dim, dim // groups, page, table.shape[0], table.shape[1], 0, k.data_ptr(), v.data_ptr(),
             kp.data_ptr(), vp.data_ptr(), None if pos is None else pos.data_ptr(),
             None if acc is None else acc.data_ptr(), table.data_ptr()))
@@ -295,10 +295,12 @@ def attention_kv4(q, cache: Cache, length, scale=None, acc_in=None, acc_out=None
     sequences then may not share pages."""
     q = _tokens(q, "q", cache, 0)
     # (the stride of a dimension of one entry may be anything, and is not used)
-    q_seq, q_token = q.stride(0) if q.shape[0] > 1 else 0, q.stride(1) if q.shape[1] > 1 else 0
+    seqs, queries, heads, _ = q.shape
+    q_seq, q_token, _, _ = q.stride()
+    q_seq, q_token = q_seq if seqs > 1 else 0, q_token if queries > 1 else 0
     if q.data_ptr() % 16 or q_seq % 8 or q_token % 8:
         q = q.clone(memory_format=torch.contiguous_format)
-        q_seq, q_token = q.stride(0), q.stride(1)
+        q_seq, q_token, _, _ = q.stride()
     n = _counts(length, "length", cache)
     c = cache._c
     if acc_out is not None:
@@ -310,12 +312,12 @@ def attention_kv4(q, cache: Cache, length, scale=None, acc_in=None, acc_out=None
     elif acc_in is not None:
         _bad("attention_kv4: acc_in without acc_out")
     out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    heads = q.shape[2]
     L = lib()
     # (its size depends on the device's compute units)
-    need = _on(L.as_attention_kv4_workspace, q.device, c, q.shape[1], heads, 0 if acc_out is None else 1)
-    _keep, ws = _workspace(need, q.device)
-    _call(L.as_attention_kv4, q.device, c, q.data_ptr(), _TYPES[q.dtype], q.shape[1], heads, q_seq, q_token, n,
+    dev = q.device
+    need = _on(L.as_attention_kv4_workspace, dev, c, queries, heads, 0 if acc_out is None else 1)
+    _keep, ws = _workspace(need, dev)
+    _call(L.as_attention_kv4, dev, c, q.data_ptr(), _TYPES[q.dtype], queries, heads, q_seq, q_token, n,
           c.dim ** -0.5 if scale is None else scale, out.data_ptr(), None if acc_in is None else acc_in.data_ptr(),
           None if acc_out is None else acc_out.data_ptr(), ws, need)
     return out
