@@ -75,6 +75,7 @@ int as_quantize_i8(const void* x, int32_t type, int64_t n_rows, int64_t n_cols, 
  *   w_scale   [n_out] fp32
  *   bias      [n_out] fp32, or NULL
  *   y         [n_tokens][n_out] of y_type (any of the three), rows y_stride apart
+ * At most 1,048,560 tokens, 2^24 - 1 outputs and AS_I8_MAX_INPUTS inputs.
  */
 int64_t as_linear_i8_workspace(int64_t n_tokens, int64_t n_in, int64_t n_out);
 int as_linear_i8(const void* x, int32_t x_type, int64_t n_tokens, int64_t n_in, int64_t x_stride,
@@ -87,7 +88,7 @@ int as_linear_i8(const void* x, int32_t x_type, int64_t n_tokens, int64_t n_in, 
  * s of sequence b lies on page page_table[b][s / page] at place s % page, for
  * every key/value head.  A group of `group` channels of one token has
  *   m = fp16(min), d = fp16((max - min) / 15), code = rint((x - m) / d) in
- *   [0, 15] (0 if d = 0), value = code * d + m,
+ *   [0, 15] (0 if d = 0; differences and quotients in fp32), value = code * d + m,
  * x clamped to +-65504 first; a NaN makes its group NaN.
  * Word layout: element e of a 32-bit word is at bits 4 * (e/2 + 4 * (e%2)).
  *   k      [n_pages][n_heads][page][4][dim/32] words: word [g][i] holds

@@ -948,8 +948,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(AttArgs p) {
 // joins ROWS rows of a segment, or 16.  Bound by latency: 3.6 us for 32 rows of 33
 // parts, 5.4 for 320 segments of 3 parts (7.6 with a workgroup to a row), 14 for
 // 1200 rows of 16 heads.
-constexpr int kMaxParts = 2048;
-
 template <int TYPE, int DIM, int ROWS, int THREADS>
 __global__ __launch_bounds__(THREADS) void join(AttArgs p) {
   constexpr int kSide = THREADS / (DIM / 4) / ROWS;
@@ -1380,8 +1378,7 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
     const int64_t most = segments * ((blocks + in_share - 1) / in_share);
     return (int)round_up(most > running ? running : most < 1 ? 1 : most, 8);
   };
-  int cus = as_host::compute_units();
-  if (cus > kMaxParts / 4) cus = kMaxParts / 4;
+  const int cus = as_host::compute_units();
   pl.workgroups = groups(heads * pl.row_groups, kWaves, (int64_t)cus * resident);
   pl.weigh_workgroups = groups(heads, 1 << pl.weigh_round, (int64_t)cus * (pl.rows > 16 ? 2 : 3));
   pl.parts = pl.workgroups / (heads * pl.row_groups);

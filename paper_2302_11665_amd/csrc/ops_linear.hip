@@ -692,7 +692,7 @@ int as_linear_i8(const void* x, int32_t x_type, int64_t n_tokens, int64_t n_in, 
   if (n_tokens < 0 || n_in < 1 || n_out < 1 || x_stride < n_in || y_stride < n_out)
     return fail(AS_E_INVALID_ARG, "linear_i8: %lld tokens, %lld -> %lld, strides %lld and %lld", (long long)n_tokens,
                 (long long)n_in, (long long)n_out, (long long)x_stride, (long long)y_stride);
-  // rows of 16 tokens are a grid's second dimension
+  // (tiles and their threads then fit a launch for every y that fits the memory)
   if (n_tokens > 65535 * 16 || n_out > kMaxRows || n_in > AS_I8_MAX_INPUTS)
     return fail(AS_E_LIMITS, "linear_i8: at most %d tokens, %lld outputs, %d inputs", 65535 * 16, (long long)kMaxRows,
                 AS_I8_MAX_INPUTS);
