@@ -367,6 +367,38 @@ def test_attention_of_long_contexts_and_prompts(case, dtype, weights):
     test_attention(case, dtype, weights)
 
 
+def with_room(c, slots):
+    """The cache with a table for so many slots; its entries behind those of the lengths are anything."""
+    g = gen(slots)
+    t = c.page_table
+    wide = torch.randint(-3, 10 ** 6, (t.shape[0], -(-slots // c._c.page)), dtype=torch.int32, device="cuda", generator=g)
+    wide[:, :t.shape[1]] = t
+    return dataclasses.replace(c, page_table=wide)
+
+
+# A server's tables: far wider than the present contexts.
+ROOM = [([300, 0, 1, 900], 1, 8, 2, 64, 64, 64, 32000), ([40, 33], 1, 16, 2, 128, 64, 32, 131072),
+        ([5, 700, 64], 4, 6, 2, 128, 32, 96, 2000), ([500, 3], 130, 2, 1, 64, 32, 64, 32000),
+        ([129, 250, 7], 96, 16, 4, 128, 128, 256, 2048), ([1, 1, 0], 20, 3, 3, 128, 64, 4096, 262144)]
+
+
+@pytest.mark.parametrize("case", ROOM, ids=[str(i) for i in range(len(ROOM))])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("weights", [False, True])
+def test_attention_over_tables_with_room_to_grow(case, dtype, weights):
+    lengths, t, hq, heads, dim, group, page, slots = case
+    say("room", case, dtype, weights)
+    g = gen(sum(lengths) + t)
+    c = with_room(make_cache(g, lengths, heads, dim, group, page, spare=1), slots)
+    q = (normal(g, len(lengths), t, hq, dim) * 0.7).to(dtype)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    if not weights:
+        return check_attention(c, q, lengths, ops.attention_kv4(q, c, n))
+    out = torch.full_like(c.acc, -5.0)
+    o = ops.attention_kv4(q, c, n, acc_in=c.acc, acc_out=out)
+    check_attention(c, q, lengths, o, acc_in=c.acc.cpu().numpy(), acc_out=out.cpu().numpy())
+
+
 @pytest.mark.parametrize("way", ["up", "down", "both"])
 @pytest.mark.parametrize("rows,n", [(1, 700), (1, 6000), (40, 3000), (130, 3000)])
 def test_attention_where_the_maximum_moves(way, rows, n):
@@ -592,6 +624,13 @@ def test_append(dim, group, page, dtype, starts, t):
         assert np.array_equal(before[x][same], after[x][same])
 
 
+@pytest.mark.parametrize("dim,group,page,starts,t", [(64, 32, 32, [0, 5, 64], 1000), (128, 64, 96, [31, 0, 7], 517),
+                                                     (128, 128, 4096, [100, 2, 33], 800), (64, 64, 64, [1, 0, 0], 1)])
+def test_append_of_prompts(dim, group, page, starts, t):
+    for dtype in (BF16, F16):
+        test_append(dim, group, page, dtype, starts, t)
+
+
 def test_append_beyond_the_table_writes_nothing_there():
     g = gen(3)
     c = make_cache(g, [40, 40], 1, 64, 64, 32, spare=1)
@@ -745,6 +784,23 @@ LONG_EVICT = [([20000, 33], 2, 64, 64, 64, 128, 5000, 100), ([70001], 1, 64, 32,
 @pytest.mark.parametrize("kind", ["plain", "ties", "special"])
 def test_evict_of_long_caches(case, kind):
     test_evict(case, kind)
+
+
+@pytest.mark.parametrize("slots", [3000, 20000, 140000])
+def test_evict_from_tables_with_room_to_grow(slots):
+    """As from a table of the present length."""
+    g = gen(slots)
+    lengths = [700, 5, 0, 1300]
+    src = make_cache(g, lengths, 2, 64, 32, 64, spare=1)
+    src.pos.copy_(torch.randperm(src.pos.numel(), device="cuda", generator=g).view_as(src.pos))
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    found = []
+    for c in (src, with_room(src, slots)):
+        table = torch.arange(4 * 13, dtype=torch.int32, device="cuda").view(4, 13)
+        dst = ops.Cache.empty(4 * 13, 2, 64, table, group=32, page=32)
+        new = ops.cache_evict(c, dst, n, torch.full_like(n, src.pos.numel()), keep=400, recent=100)
+        found.append([new, dst.k, dst.v, dst.k_par, dst.v_par, dst.pos, dst.acc])
+    assert all(torch.equal(a, z) for a, z in zip(*found)) and found[0][0].tolist() == [400, 5, 0, 400]
 
 
 def test_the_long_cases_reach_their_kernels():
