@@ -166,7 +166,8 @@ int as_cache_append(const as_cache_t* cache, const void* k, const void* v, int32
  * At most 2^26 query rows, 65,535 sequences times heads, and 2^31 blocks of 32
  * slots over all sequences, heads and 16 rows (AS_E_LIMITS).
  * Products of codes and 16-bit numbers with fp32 sums; softmax in fp32; p times
- * a value's scale enters its product as two bf16 numbers (17 bits).
+ * a value's scale enters its product as two bf16 numbers (17 bits), and what
+ * they leave of it is multiplied by code - 7.5.
  */
 int64_t as_attention_kv4_workspace(const as_cache_t* cache, int32_t n_queries, int32_t n_q_heads,
                                    int32_t weights);

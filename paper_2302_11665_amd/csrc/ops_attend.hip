@@ -675,8 +675,8 @@ __device__ __forceinline__ void attend_segment(const AttArgs& p, const Segment& 
 // One workgroup per share; its four wavefronts take a segment's blocks in turn,
 // each with a ring of its own in LDS so that none waits for another, and join
 // their results at the segment's end.  Bound by memory where rows are few (128
-// channels in groups of 64, 8 rows: 1.04 GB of long contexts in 204 us, 5.1 TB/s;
-// 403 MB of 40 ragged ones in 95 us, 4.2), by the vector instructions of codes and
+// channels in groups of 64, 8 rows: 1.04 GB of long contexts in 212 us, 4.9 TB/s;
+// 403 MB of 40 ragged ones in 96 us, 4.2), by the vector instructions of codes and
 // softmax above some 16 rows, and by a round's latency, 8 us, for one short
 // sequence.
 // (Segments of 32 rows, so that codes are expanded once for both halves, took as
@@ -709,11 +709,12 @@ __global__ __launch_bounds__(64 * kWaves, DIM == 4 * GROUP ? 3 : 4) void attend(
 // operands in LDS that all of them multiply with: 128 rows share the work at the
 // codes, which otherwise takes half of the vector instructions.  The words of the
 // next block are on their way, and the operands of the one after this are written
-// while this one is multiplied; one barrier a block.  Bound by the vector
-// instructions of the softmax and of splitting p d, with the matrix
-// instructions close behind: 1200 rows a head of two sequences of up to 12,000
-// slots take 184 us, 0.52 PFLOP/s as the formula counts, 0.78 with V's second
-// product.
+// while this one is multiplied; one barrier a block.  1200 rows a head of two
+// sequences of up to 12,000 slots take 201 us, 0.47 PFLOP/s as the formula counts,
+// 0.77 with V's second product and the means'.  Neither unit bounds it alone: the
+// vector instructions take 53 % of the cycles and the matrix instructions 32 %,
+// hardly ever at once, since K q^T, softmax and V p^T follow each other and a SIMD
+// has two wavefronts.
 constexpr int kManyRows = 128;
 
 template <int DIM, int GROUP>
@@ -1340,8 +1341,8 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   pl.per = n_q_heads / c->n_heads;
   pl.rows = pl.per * n_queries;
   // attend_many takes 4/5 as long for a row, empty ones of its 128 included (128
-  // channels in groups of 64, 9 sequences of up to 30,000 slots, 2 heads: 78 us
-  // against 86 for 100 rows, 140 against 106 for 130, 206 against 191 for 260), but
+  // channels in groups of 64, 9 sequences of up to 30,000 slots, 2 heads: 98 us
+  // against 109 for 100 rows, 156 against 122 for 130, 225 against 211 for 260), but
   // longer with groups of a fourth of the channels, whose sums leave room for one
   // wavefront a SIMD: 390 us against 261 for 260 rows.
   const bool wide = c->dim == 4 * c->group;
@@ -1362,9 +1363,10 @@ Plan make_plan(const as_cache_t* c, int n_queries, int n_q_heads, bool weights) 
   }
   if (!pl.many && !pl.whole) set_tiles(1);
   // Many rows of short tables: shares would only add parts to be joined, unless
-  // some segments are long and there are few.  226 new tokens of 15 sequences, 20
-  // heads of 64 channels: 16 us so, 57 in shares and joined; 300 tokens of 2 and of
-  // 15 sequences of up to 500 slots, 32 heads of 128: 34 us against 44, 75 against 152.
+  // some segments are long and there are few.  15 sequences of up to 500 slots,
+  // 226 new tokens, 20 heads of 64 channels: 36 us so, 54 in shares and joined; 300
+  // tokens of 2 and of 15 such sequences, 32 heads of 128: 32 us against 45, 79
+  // against 154.
   pl.alone = pl.many && (blocks <= kShortBlocks ||
                          (blocks <= kWholeBlocks && heads * pl.row_groups >= 2 * (int64_t)as_host::compute_units()));
   const int resident = pl.many ? 2 : wide ? 3 : 4;
