@@ -10,6 +10,14 @@
  *   as_attention_kv4   attention over that cache, with the attention weight
  *                      that every cached token got where asked for
  *   as_cache_evict     the cache cut to a budget by accumulated weight
+ * A request begins with its prompt; these take several requests' prompts in at
+ * once, packed one after the other:
+ *   as_norm_i8         a residual added, the root-mean-square norm, 8 bits, from
+ *                      which as_linear_i8_codes goes on
+ *   as_attention_prompt  causal attention of every token over its own prompt
+ *   as_pages_reserve   pages for new tokens, and where each of them goes
+ *   as_pages_release   pages of requests that ended, back to the pool
+ *   as_cache_append_packed  packed keys and values into the cache
  * They serve; none of them has a gradient.
  *
  * Conventions: those of alpaserve_sim.h (device pointers unless marked HOST,
@@ -83,6 +91,70 @@ int as_linear_i8(const void* x, int32_t x_type, int64_t n_tokens, int64_t n_in, 
                  int32_t y_type, int64_t y_stride, void* workspace, int64_t workspace_bytes,
                  void* stream);
 
+/*
+ * The same with activations that are codes already (as_norm_i8, as_quantize_i8):
+ *   codes, scale  n_tokens rows of n_in columns, codes aligned to 16 bytes
+ */
+int as_linear_i8_codes(const void* codes, const float* scale, int64_t n_tokens, int64_t n_in, const void* w,
+                       const float* w_scale, const float* bias, int64_t n_out, void* y, int32_t y_type,
+                       int64_t y_stride, void* stream);
+
+/*
+ * Rows of mean square 1, in 8 bits: with h = x, or x + residual rounded to their
+ * type, and t = h * gain (rounded to fp32; h without a gain),
+ *   a_r = max_k |t_rk|,  code = rint(127 t_rk / a_r),
+ *   scale_r = a_r / (127 sqrt(mean_k h_rk^2 + eps)),  value = code * scale_r.
+ * Codes are as_quantize_i8's of t; they do not depend on the root.  A row whose t
+ * holds an infinity or NaN gets codes 0 and the scale NaN, a row of zeros codes
+ * and scale 0.  Squares are summed in fp32, in fp64 where that could overflow or
+ * lose them; with a gain 127 t is rounded once before the division.
+ *   x         [n_tokens][n_cols] of `type` (AS_BF16 or AS_F16), rows x_stride apart
+ *   residual  likewise, residual_stride apart, or NULL
+ *   gain      [n_cols] fp32, or NULL
+ *   eps       >= 0
+ *   sum       h, sum_stride apart: where there is a residual, else NULL; may be x
+ *             or the residual itself (same address and stride), but share no
+ *             other memory with them
+ *   codes     [as_i8_bytes(n_tokens, n_cols)], aligned to 16 bytes
+ *   scale     [n_tokens] fp32
+ *   held      [n_tokens][n_cols] fp32: the values that codes and scale stand for,
+ *             or NULL
+ * At most 1,048,560 tokens and AS_I8_MAX_INPUTS columns.
+ */
+int as_norm_i8(const void* x, const void* residual, int32_t type, int64_t n_tokens, int64_t n_cols, int64_t x_stride,
+               int64_t residual_stride, const float* gain, float eps, void* sum, int64_t sum_stride, void* codes,
+               float* scale, float* held, void* stream);
+
+/* --------------------------------------------------------------- prompts --
+ * Packed sequences: token rows one after the other; sequence b has the rows
+ * offsets[b]..offsets[b+1]-1 of n_tokens (offsets [n_seqs + 1], rising from 0 on;
+ * rows from offsets[n_seqs] on are of no sequence).
+ *
+ * Causal attention within each sequence: token t attends to its sequence's
+ * tokens up to itself, head j of the queries to key/value head
+ * j / (n_q_heads / n_kv_heads):
+ *   o_t = sum_s p_ts v_s,  p_ts = exp(scale q_t.k_s) / sum_s' exp(scale q_t.k_s')
+ *   q        [n_tokens][n_q_heads][dim] of `type` (AS_BF16 or AS_F16), last two
+ *            dimensions contiguous, rows q_token elements apart (a multiple of
+ *            8), aligned to 16 bytes
+ *   k, v     [n_tokens][n_kv_heads][dim], likewise
+ *   dim      64 or 128
+ *   scale    > 0, at most 2e38; logits as for as_attention_kv4
+ *   out      [n_tokens][n_q_heads][dim] of `type`, contiguous, aligned to 8 bytes,
+ *            apart from the others; rows of no sequence are not written
+ * What a token may not see does not reach it, an infinity or NaN included.
+ * Invalid offsets give unspecified results, never an access outside the arrays.
+ * At most 2^26 tokens, 2^30 rows of queries, 2^20 sequences, 4096 query heads, and
+ * 2^24 blocks of 128 rows of a key/value head's queries (each sequence's last one
+ * may be a part).
+ * Products of 16-bit numbers with fp32 sums, softmax in fp32; p is rounded to the
+ * type for its product with v (half a unit in its last place each, as the output),
+ * not for its sum.
+ */
+int as_attention_prompt(const void* q, const void* k, const void* v, int32_t type, int64_t n_tokens, int32_t n_q_heads,
+                        int32_t n_kv_heads, int32_t dim, int64_t q_token, int64_t k_token, int64_t v_token,
+                        const int32_t* offsets, int32_t n_seqs, float scale, void* out, void* stream);
+
 /* ---------------------------------------------------------------- cache --
  * Keys and values of 4 bits in pages shared by all sequences of a batch.  Slot
  * s of sequence b lies on page page_table[b][s / page] at place s % page, for
@@ -142,6 +214,61 @@ int as_cache_append(const as_cache_t* cache, const void* k, const void* v, int32
                     int32_t n_tokens, int64_t k_seq, int64_t k_token, int64_t v_seq, int64_t v_token,
                     const int32_t* start, const int32_t* first_pos, float* held_k, float* held_v,
                     void* stream);
+
+/*
+ * Put packed tokens, of prompts and of single steps alike, where a slot map says:
+ * token t goes to slot[t] of sequence seq[t] (as_pages_reserve gives both).  Tokens
+ * whose sequence or slot does not exist (-1) are passed over.  The tokens that fall
+ * on one block of 32 slots have to be neighbours, in the order of their slots; of
+ * other blocks, and of a slot named twice, the contents are unspecified.
+ *   k, v        [n_tokens][n_heads][dim] of `type`, last two dimensions contiguous,
+ *               rows k_token and v_token elements apart
+ *   seq, slot   [n_tokens]
+ *   pos         [n_tokens] positions, or NULL: slot
+ *   held_k, held_v  [n_tokens][n_heads][dim] fp32: the values that the cache holds
+ *               now, or NULL; tokens passed over are not written
+ * cache->pos and cache->acc may be NULL (not kept).  Tokens times heads: below 2^29.
+ */
+int as_cache_append_packed(const as_cache_t* cache, const void* k, const void* v, int32_t type, int64_t n_tokens,
+                           int64_t k_token, int64_t v_token, const int32_t* seq, const int32_t* slot, const int32_t* pos,
+                           float* held_k, float* held_v, void* stream);
+
+/*
+ * Pages for the new tokens of every sequence, from a pool: a stack of free pages
+ * (stack[0..count), the next one taken is stack[count - 1]).  Sequence b holds
+ * length[b] tokens, on the first pages of its row of the table, and gets add[b]
+ * more: the rows behind those of the sequences before it, of n_tokens packed ones.
+ * It needs the pages that length[b] + add[b] slots take more than length[b] do.
+ * In their order, sequences get what they need as long as the pool has it for them
+ * and for all before them; one that does not get it, whose slots would not fit its
+ * row, or whose tokens are not all among the n_tokens, is refused: it keeps its
+ * length.  Sequences that need no page are never refused for others' sake.
+ *   count, new_count    [1]
+ *   length, new_length  [n_seqs]; new_length = length + add where granted
+ *   add        [n_seqs]; below 0 is 0
+ *   page_table [n_seqs][max_pages]: entries of new pages are written
+ *   offsets    [n_seqs + 1] first packed row of every sequence, granted or not, and
+ *              the number of all
+ *   seq, slot  [n_tokens] sequence and slot of every packed row; -1 for rows of
+ *              sequences that were refused, and of none
+ * new_count may be count, and new_length length.  At most 2^30 slots a sequence, 2^20
+ * sequences and 2^30 tokens.
+ */
+int64_t as_pages_reserve_workspace(int32_t n_seqs);
+int as_pages_reserve(const int32_t* stack, const int32_t* count, int32_t n_pages, int32_t* page_table, int32_t n_seqs,
+                     int32_t max_pages, int32_t page, const int32_t* length, const int32_t* add, int64_t n_tokens,
+                     int32_t* new_count, int32_t* new_length, int32_t* offsets, int32_t* seq, int32_t* slot,
+                     void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Give back the pages of the sequences that `which` [n_seqs] marks (not 0): in the
+ * order of sequences and of their pages they go onto the stack, which has room for
+ * n_pages; their new length is 0, others keep theirs.  The table is not written.
+ * new_count and new_length may be count and length.
+ */
+int as_pages_release(int32_t* stack, const int32_t* count, int32_t n_pages, const int32_t* page_table, int32_t n_seqs,
+                     int32_t max_pages, int32_t page, const int32_t* length, const uint8_t* which, int32_t* new_count,
+                     int32_t* new_length, void* stream);
 
 /*
  * Attention of n_queries new tokens of every sequence over its cache, which

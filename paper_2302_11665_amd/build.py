@@ -28,7 +28,7 @@ SIM_MULTI_SRC = os.path.join(CSRC, "sim_multi.hip")
 SIM_ALG2_SRC = os.path.join(CSRC, "sim_alg2.hip")
 SIM_BATCH_SRC = os.path.join(CSRC, "sim_batch.hip")
 SIM_SPEC_SRC = os.path.join(CSRC, "sim_spec.hip")
-OPS_SRCS = tuple(os.path.join(CSRC, f"ops_{n}.hip") for n in ("linear", "cache", "attend"))  # a served model's step
+OPS_SRCS = tuple(os.path.join(CSRC, f"ops_{n}.hip") for n in ("linear", "cache", "attend", "norm", "prompt", "pages"))
 LANE_WIDTHS = (1, 2, 4, 8, 16, 32, 64)  # one launcher translation unit per width
 SIM_LIB = os.path.join(BUILD, "libalpaserve_sim.so")
 PROBE_SRC = os.path.join(CSRC, "peak_probe.hip")

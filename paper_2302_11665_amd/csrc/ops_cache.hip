@@ -55,6 +55,87 @@ struct AppendArgs {
 // Bits of element e of a word.
 __device__ __forceinline__ int nibble(int e) { return 4 * ((e >> 1) + 4 * (e & 1)); }
 
+// What 8 channels of one token and head become, on one of the DIM/8 lanes that
+// hold it: their codes as a word of K and as a byte each, and the group's scale.
+struct Quantised {
+  uint32_t word, bytes[2];
+  _Float16 step, base;
+};
+
+template <int TYPE, int GROUP>
+__device__ __forceinline__ Quantised quantise8(const uint16_t* x, float* held) {
+  float f[8];
+  float low = kInf, high = -kInf;
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    f[e] = to_f32<TYPE>(x[e]);
+    bad |= f[e] != f[e];
+    f[e] = fminf(fmaxf(f[e], -65504.0f), 65504.0f);
+    low = fminf(low, f[e]);
+    high = fmaxf(high, f[e]);
+  }
+  int any = bad;
+#pragma unroll
+  for (int o = 1; o < GROUP / 8; o <<= 1) {
+    low = fminf(low, __shfl_xor(low, o));
+    high = fmaxf(high, __shfl_xor(high, o));
+    any |= __shfl_xor(any, o);
+  }
+  Quantised z{};
+  z.base = any ? (_Float16)__builtin_nanf("") : (_Float16)low;
+  z.step = any ? (_Float16)__builtin_nanf("") : (_Float16)((high - low) / 15.0f);
+  const float m = (float)z.base, d = (float)z.step;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    // x - m is exact for 16-bit x and m of like size, so the quotient rounds
+    // as in exact arithmetic
+    const float q = rintf((f[e] - m) / d);
+    const uint32_t code = d > 0.0f ? (uint32_t)fminf(fmaxf(q, 0.0f), 15.0f) : 0u;
+    z.word |= code << nibble(e);
+    z.bytes[e >> 2] |= code << (8 * (e & 3));
+    if (held) held[e] = (float)code * d + m;
+  }
+  return z;
+}
+
+// Puts one lane's 8 channels of a key or value at place `at` of a page and head
+// (row); V's codes go to v_codes, the token's row in LDS.
+template <int DIM, int GROUP>
+__device__ __forceinline__ void put8(const CacheArgs& c, int64_t row, int at, int lane, bool is_v, const Quantised& z,
+                                     v2u* v_codes) {
+  if (is_v)
+    v_codes[lane] = v2u{z.bytes[0], z.bytes[1]};
+  else
+    // channels 8 lane..: word [g = lane%4][i = lane/4] of the token
+    c.k[(row * c.page + at) * (DIM / 8) + (lane & 3) * (DIM / 32) + (lane >> 2)] = z.word;
+  if (lane % (GROUP / 8) == 0) {
+    uint32_t* par = is_v ? c.v_par : c.k_par;
+    par[(row * (DIM / GROUP) + lane / (GROUP / 8)) * c.page + at] =
+        (uint32_t)__builtin_bit_cast(uint16_t, z.step) | (uint32_t)__builtin_bit_cast(uint16_t, z.base) << 16;
+  }
+}
+
+// Word w of a block of 32 slots of V from the codes of its slots lo..hi-1, where
+// slot s has the DIM codes of row s + shift; the other slots' bits stay.
+template <int DIM>
+__device__ __forceinline__ void put_v_word(uint32_t* v, int w, const uint8_t* codes, int lo, int hi, int shift) {
+  const int i = w % (DIM / 16), c = w / (DIM / 16) % 16, g = w / DIM;
+  uint32_t mask = 0, word = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int s = 16 * (e >> 2) + 4 * g + (e & 3);
+    if (s >= lo && s < hi) {
+      word |= (uint32_t)codes[(s + shift) * DIM + 16 * i + c] << nibble(e);
+      mask |= 15u << nibble(e);
+    }
+  }
+  if (mask == 0xffffffffu)
+    v[w] = word;
+  else if (mask)
+    v[w] = (v[w] & ~mask) | word;
+}
+
 // One workgroup per (sequence, head, block of 32 slots).  DIM/8 lanes quantise
 // a token's key or value, 8 channels each: a word of K as it is; V's codes
 // change direction (a word holds 8 tokens of one channel), through LDS, and a
@@ -64,7 +145,6 @@ __device__ __forceinline__ int nibble(int e) { return 4 * ((e >> 1) + 4 * (e & 1
 template <int TYPE, int DIM, int GROUP>
 __global__ __launch_bounds__(256) void append(AppendArgs p) {
   constexpr int kLanes = DIM / 8;       // lanes of one token's key or value
-  constexpr int kShare = GROUP / 8;     // of them, those that share a scale
   constexpr int kWords = DIM / 8;
   __shared__ v2u v_codes[32][kLanes];   // a byte per channel
   const int b = blockIdx.y / p.c.n_heads, h = blockIdx.y % p.c.n_heads;
@@ -85,76 +165,19 @@ __global__ __launch_bounds__(256) void append(AppendArgs p) {
     const int64_t t = first + s - start;
     const uint16_t* x = (is_v ? p.v + b * p.v_seq + t * p.v_token : p.k + b * p.k_seq + t * p.k_token) +
                         (int64_t)h * DIM + lane * 8;
-    float f[8];
-    float low = kInf, high = -kInf;
-    bool bad = false;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      f[e] = to_f32<TYPE>(x[e]);
-      bad |= f[e] != f[e];
-      f[e] = fminf(fmaxf(f[e], -65504.0f), 65504.0f);
-      low = fminf(low, f[e]);
-      high = fmaxf(high, f[e]);
-    }
-    int any = bad;
-#pragma unroll
-    for (int o = 1; o < kShare; o <<= 1) {
-      low = fminf(low, __shfl_xor(low, o));
-      high = fmaxf(high, __shfl_xor(high, o));
-      any |= __shfl_xor(any, o);
-    }
-    const _Float16 base = any ? (_Float16)__builtin_nanf("") : (_Float16)low;
-    const _Float16 step = any ? (_Float16)__builtin_nanf("") : (_Float16)((high - low) / 15.0f);
-    const float m = (float)base, d = (float)step;
-    uint32_t word = 0, bytes[2] = {0, 0};
     float* held = is_v ? p.held_v : p.held_k;
     if (held) held += (((int64_t)b * p.n_tokens + t) * p.c.n_heads + h) * DIM + lane * 8;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      // x - m is exact for 16-bit x and m of like size, so the quotient rounds
-      // as in exact arithmetic
-      const float q = rintf((f[e] - m) / d);
-      const uint32_t code = d > 0.0f ? (uint32_t)fminf(fmaxf(q, 0.0f), 15.0f) : 0u;
-      word |= code << nibble(e);
-      bytes[e >> 2] |= code << (8 * (e & 3));
-      if (held) held[e] = (float)code * d + m;
-    }
     const int at = in_page + s;
-    if (is_v) {
-      v_codes[s][lane] = v2u{bytes[0], bytes[1]};
-    } else {
-      // channels 8 lane..: word [g = lane%4][i = lane/4] of the token
-      p.c.k[(row * p.c.page + at) * kWords + (lane & 3) * (DIM / 32) + (lane >> 2)] = word;
-    }
-    if (lane % kShare == 0) {
-      uint32_t* par = is_v ? p.c.v_par : p.c.k_par;
-      par[(row * (DIM / GROUP) + lane / kShare) * p.c.page + at] =
-          (uint32_t)__builtin_bit_cast(uint16_t, step) | (uint32_t)__builtin_bit_cast(uint16_t, base) << 16;
-    }
+    put8<DIM, GROUP>(p.c, row, at, lane, is_v, quantise8<TYPE, GROUP>(x, held), v_codes[s]);
     if (is_v && lane == 0) {
       if (p.c.pos) p.c.pos[row * p.c.page + at] = (int32_t)(p.first_pos ? p.first_pos[b] + t : first + s);
       if (p.c.acc) p.c.acc[row * p.c.page + at] = 0.0f;
     }
   }
   __syncthreads();
-  const uint8_t* codes = reinterpret_cast<const uint8_t*>(v_codes);
   uint32_t* v = p.c.v + (row * p.c.page + in_page) * kWords;
-  for (int w = threadIdx.x; w < 32 * kWords; w += 256) {
-    const int i = w % (DIM / 16), c = w / (DIM / 16) % 16, g = w / DIM;
-    uint32_t mask = 0, word = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int s = 16 * (e >> 2) + 4 * g + (e & 3);
-      if (s >= lo && s < hi) {
-        word |= (uint32_t)codes[s * DIM + 16 * i + c] << nibble(e);
-        mask |= 15u << nibble(e);
-      }
-    }
-    if (mask == 0xffffffffu)
-      v[w] = word;
-    else if (mask)
-      v[w] = (v[w] & ~mask) | word;
-  }
+  for (int w = threadIdx.x; w < 32 * kWords; w += 256)
+    put_v_word<DIM>(v, w, reinterpret_cast<const uint8_t*>(v_codes), lo, hi, 0);
 }
 
 template <int TYPE>
@@ -165,6 +188,81 @@ void launch_append(const AppendArgs& p, hipStream_t s) {
   if (p.c.dim == 128 && p.c.group == 32) hipLaunchKernelGGL((append<TYPE, 128, 32>), g, t, 0, s, p);
   if (p.c.dim == 128 && p.c.group == 64) hipLaunchKernelGGL((append<TYPE, 128, 64>), g, t, 0, s, p);
   if (p.c.dim == 128 && p.c.group == 128) hipLaunchKernelGGL((append<TYPE, 128, 128>), g, t, 0, s, p);
+}
+
+// ------------------------------------------------------------ packed append
+
+struct PackedArgs {
+  CacheArgs c;
+  const uint16_t *k, *v;
+  int64_t k_token, v_token;
+  const int32_t *seq, *slot, *pos;
+  float *held_k, *held_v;
+  int32_t n_tokens;
+};
+
+constexpr int kPackedTile = 32;  // tokens whose runs a workgroup takes
+
+// One workgroup per (tile of packed tokens, head).  Neighbouring tokens of one
+// sequence on neighbouring slots of one block of 32 are a run; a workgroup takes
+// the runs that begin in its tile, whole, so that no other one has their words
+// of V as long as no two tokens have the same slot and a block's new tokens are
+// neighbours.
+template <int TYPE, int DIM, int GROUP>
+__global__ __launch_bounds__(256) void append_packed(PackedArgs p) {
+  constexpr int kLanes = DIM / 8, kWords = DIM / 8;
+  __shared__ v2u v_codes[32][kLanes];
+  const int h = blockIdx.y, wide = threadIdx.x & 63;
+  const int64_t t0 = (int64_t)blockIdx.x * kPackedTile;
+  // every wavefront looks at the tile's tokens and as many behind them
+  const int64_t t = t0 + wide;
+  int seq = -1, slot = -1;
+  if (t < p.n_tokens) seq = p.seq[t], slot = p.slot[t];
+  const bool real = (unsigned)seq < (unsigned)p.c.n_seqs && slot >= 0;
+  bool follows = false;  // the token before, in its run
+  if (real && t > 0 && slot % 32 != 0) follows = p.seq[t - 1] == seq && p.slot[t - 1] == slot - 1;
+  const uint64_t in_run = __ballot(follows);
+  uint64_t begins = __ballot(real && !follows) & ((uint64_t(1) << kPackedTile) - 1);
+  const int lane = threadIdx.x % kLanes;
+  while (begins) {
+    const int at0 = __builtin_ctzll(begins);
+    begins &= begins - 1;
+    // tokens of the run: at most 32, so that the bits end before the 64 do
+    const int n = 1 + (int)__builtin_ctzll(~(in_run >> (at0 + 1)));
+    const int b = __builtin_amdgcn_readlane(seq, at0), first = __builtin_amdgcn_readlane(slot, at0);
+    const int64_t row = cache_row(p.c, b, h, first / p.c.page);
+    if (row < 0) continue;
+    const int in_page = first % p.c.page, lo = in_page % 32;
+    __syncthreads();  // the run before is written
+    for (int j = threadIdx.x / kLanes; j < 2 * n; j += 256 / kLanes) {
+      const bool is_v = j >= n;
+      const int i = is_v ? j - n : j;
+      const int64_t u = t0 + at0 + i;
+      const uint16_t* x = (is_v ? p.v + u * p.v_token : p.k + u * p.k_token) + (int64_t)h * DIM + lane * 8;
+      float* held = is_v ? p.held_v : p.held_k;
+      if (held) held += (u * p.c.n_heads + h) * DIM + lane * 8;
+      const int at = in_page + i;
+      put8<DIM, GROUP>(p.c, row, at, lane, is_v, quantise8<TYPE, GROUP>(x, held), v_codes[i]);
+      if (is_v && lane == 0) {
+        if (p.c.pos) p.c.pos[row * p.c.page + at] = p.pos ? p.pos[u] : first + i;
+        if (p.c.acc) p.c.acc[row * p.c.page + at] = 0.0f;
+      }
+    }
+    __syncthreads();
+    uint32_t* v = p.c.v + (row * p.c.page + in_page - lo) * kWords;
+    for (int w = threadIdx.x; w < 32 * kWords; w += 256)
+      put_v_word<DIM>(v, w, reinterpret_cast<const uint8_t*>(v_codes), lo, lo + n, -lo);
+  }
+}
+
+template <int TYPE>
+void launch_packed(const PackedArgs& p, hipStream_t s) {
+  const dim3 g((unsigned)((p.n_tokens + kPackedTile - 1) / kPackedTile), (unsigned)p.c.n_heads), t(256);
+  if (p.c.dim == 64 && p.c.group == 32) hipLaunchKernelGGL((append_packed<TYPE, 64, 32>), g, t, 0, s, p);
+  if (p.c.dim == 64 && p.c.group == 64) hipLaunchKernelGGL((append_packed<TYPE, 64, 64>), g, t, 0, s, p);
+  if (p.c.dim == 128 && p.c.group == 32) hipLaunchKernelGGL((append_packed<TYPE, 128, 32>), g, t, 0, s, p);
+  if (p.c.dim == 128 && p.c.group == 64) hipLaunchKernelGGL((append_packed<TYPE, 128, 64>), g, t, 0, s, p);
+  if (p.c.dim == 128 && p.c.group == 128) hipLaunchKernelGGL((append_packed<TYPE, 128, 128>), g, t, 0, s, p);
 }
 
 // ----------------------------------------------------------------- eviction
@@ -487,6 +585,29 @@ int as_cache_append(const as_cache_t* cache, const void* k, const void* v, int32
   else
     launch_append<AS_F16>(p, s);
   return launched("cache_append");
+}
+
+int as_cache_append_packed(const as_cache_t* cache, const void* k, const void* v, int32_t type, int64_t n_tokens,
+                           int64_t k_token, int64_t v_token, const int32_t* seq, const int32_t* slot, const int32_t* pos,
+                           float* held_k, float* held_v, void* stream) {
+  const int rc = check_cache(cache, "cache_append_packed", false, false);
+  if (rc != AS_OK) return rc;
+  if (type != AS_BF16 && type != AS_F16) return fail(AS_E_INVALID_ARG, "cache_append_packed: type %d", type);
+  if (n_tokens < 0) return fail(AS_E_INVALID_ARG, "cache_append_packed: %lld tokens", (long long)n_tokens);
+  // (a workgroup of 256 threads to 32 tokens and a head, fewer than 2^32 threads)
+  if (n_tokens > (1 << 28) || (n_tokens + 31) / 32 * cache->n_heads >= (1 << 24))
+    return fail(AS_E_LIMITS, "cache_append_packed: %lld tokens of %d heads (tokens times heads below 2^29)",
+                (long long)n_tokens, cache->n_heads);
+  if (n_tokens == 0 || cache->n_seqs == 0) return as_host::ok();
+  if (!k || !v || !seq || !slot) return fail(AS_E_INVALID_ARG, "cache_append_packed: null pointer");
+  const PackedArgs p{cache_args(cache), reinterpret_cast<const uint16_t*>(k), reinterpret_cast<const uint16_t*>(v),
+                     k_token, v_token, seq, slot, pos, held_k, held_v, (int32_t)n_tokens};
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (type == AS_BF16)
+    launch_packed<AS_BF16>(p, s);
+  else
+    launch_packed<AS_F16>(p, s);
+  return launched("cache_append_packed");
 }
 
 int64_t as_cache_evict_workspace(const as_cache_t* src, int32_t keep) {

@@ -5,7 +5,7 @@
 // takes them: a tile of 16 rows x 64 columns is 1 KiB in which lane l's 16
 // bytes (row l%16, columns 16 (l/16)..+15) lie at 16 l, so a wavefront's load of
 // an operand is one contiguous KiB.
-#include "ops_common.hpp"
+#include "ops_quant.hpp"
 
 using as_host::fail;
 
@@ -14,88 +14,6 @@ namespace as_ops {
 // ------------------------------------------------------------- quantisation
 
 constexpr int kQThreads = 256;
-
-template <int TYPE>
-__device__ __forceinline__ float load_one(const void* x, int64_t i) {
-  if (TYPE == AS_F32) return reinterpret_cast<const float*>(x)[i];
-  return to_f32<TYPE>(reinterpret_cast<const uint16_t*>(x)[i]);
-}
-
-// 16 values from column c of a row; columns beyond n_cols are 0.  Rows may start
-// anywhere: memory takes unaligned loads of 16 bytes.
-template <int TYPE>
-__device__ __forceinline__ void load16(const void* x, int64_t row, int64_t c, int64_t n_cols, float (&f)[16]) {
-  if (c + 16 <= n_cols) {
-    if (TYPE == AS_F32) {
-      const float* p = reinterpret_cast<const float*>(x) + row + c;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v4f v;
-        __builtin_memcpy(&v, p + 4 * i, 16);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) f[4 * i + j] = v[j];
-      }
-    } else {
-      const uint16_t* p = reinterpret_cast<const uint16_t*>(x) + row + c;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        v4u v;
-        __builtin_memcpy(&v, p + 8 * i, 16);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          f[8 * i + 2 * j] = to_f32<TYPE>(v[j] & 0xffffu);
-          f[8 * i + 2 * j + 1] = to_f32<TYPE>(v[j] >> 16);
-        }
-      }
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) f[i] = c + i < n_cols ? load_one<TYPE>(x, row + c + i) : 0.0f;
-}
-
-// Largest magnitude as ordered bits: infinities above every number, NaN above
-// them, so that one integer maximum finds both.
-__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-
-// How a row is quantised, from its largest magnitude.  A power of two takes
-// rows of very large or small numbers away from the ends of fp32's range.
-template <int TYPE>
-struct Quantiser {
-  float by, top, inv;  // 127 and the largest magnitude, scaled; 1 / top
-  bool none;           // all codes are 0
-  __device__ __forceinline__ Quantiser(float a, bool finite) {
-    none = !finite || a == 0.0f;
-    const float scale = a > 0x1p100f ? 0x1p-64f : a < 0x1p-64f ? 0x1p64f : 1.0f;
-    by = 127.0f * scale;
-    top = none ? 1.0f : a * scale;
-    inv = 1.0f / top;
-  }
-  // Codes of four values.  127 x is exact for 16-bit x.  Its quotient by top is
-  // taken with the reciprocal and corrected once by the exact remainder: off by
-  // 2^-46 of itself before the last rounding, so a quotient that ties between
-  // two codes comes out exactly, and no other one can reach a tie (the nearest
-  // is 2^-19 away).  The codes are therefore those of exact arithmetic.  fp32
-  // values are divided.  Adding 1.5 * 2^23 rounds to whole numbers, ties to
-  // even, and leaves the code in the low byte.
-  __device__ __forceinline__ uint32_t codes4(const float* f) const {
-    uint32_t u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = f[i] * by;
-      float q;
-      if (TYPE == AS_F32) {
-        q = x / top;
-      } else {
-        q = x * inv;
-        q = fmaf(fmaf(-q, top, x), inv, q);
-      }
-      u[i] = __float_as_uint(q + 12582912.0f);
-    }
-    const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(u[3], u[2], 0x04000c0cu);
-    return none ? 0u : lo | hi;
-  }
-};
 
 // One workgroup per row: its largest magnitude, then its codes; the second
 // reading comes from the caches.  Bound by latency for few rows, by the bytes
@@ -684,29 +602,23 @@ int64_t as_linear_i8_workspace(int64_t n_tokens, int64_t n_in, int64_t n_out) {
   return codes ? codes + round_up(n_tokens * 4, 256) : 0;
 }
 
-int as_linear_i8(const void* x, int32_t x_type, int64_t n_tokens, int64_t n_in, int64_t x_stride, const void* w,
-                 const float* w_scale, const float* bias, int64_t n_out, void* y, int32_t y_type, int64_t y_stride,
-                 void* workspace, int64_t workspace_bytes, void* stream) {
-  if (x_type != AS_BF16 && x_type != AS_F16) return fail(AS_E_INVALID_ARG, "linear_i8: x_type %d", x_type);
+// Checks of what both forms of the layer take.
+static int check_linear(const char* name, int64_t n_tokens, int64_t n_in, int64_t n_out, int32_t y_type,
+                        int64_t x_stride, int64_t y_stride) {
   if (y_type != AS_BF16 && y_type != AS_F16 && y_type != AS_F32)
-    return fail(AS_E_INVALID_ARG, "linear_i8: y_type %d", y_type);
+    return fail(AS_E_INVALID_ARG, "%s: y_type %d", name, y_type);
   if (n_tokens < 0 || n_in < 1 || n_out < 1 || x_stride < n_in || y_stride < n_out)
-    return fail(AS_E_INVALID_ARG, "linear_i8: %lld tokens, %lld -> %lld, strides %lld and %lld", (long long)n_tokens,
+    return fail(AS_E_INVALID_ARG, "%s: %lld tokens, %lld -> %lld, strides %lld and %lld", name, (long long)n_tokens,
                 (long long)n_in, (long long)n_out, (long long)x_stride, (long long)y_stride);
   // (tiles and their threads then fit a launch for every y that fits the memory)
   if (n_tokens > 65535 * 16 || n_out > kMaxRows || n_in > AS_I8_MAX_INPUTS)
-    return fail(AS_E_LIMITS, "linear_i8: at most %d tokens, %lld outputs, %d inputs", 65535 * 16, (long long)kMaxRows,
+    return fail(AS_E_LIMITS, "%s: at most %d tokens, %lld outputs, %d inputs", name, 65535 * 16, (long long)kMaxRows,
                 AS_I8_MAX_INPUTS);
-  if (n_tokens == 0) return as_host::ok();
-  if (!x || !w || !w_scale || !y) return fail(AS_E_INVALID_ARG, "linear_i8: null pointer");
-  if (!aligned(w, 16)) return fail(AS_E_INVALID_ARG, "linear_i8: weights not aligned to 16 bytes");
-  const int64_t need = as_linear_i8_workspace(n_tokens, n_in, n_out);
-  if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 256))))
-    return fail(AS_E_INVALID_ARG, "linear_i8: workspace of %lld bytes, %lld needed (aligned to 256)",
-                (long long)workspace_bytes, (long long)need);
-  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  uint8_t* codes = reinterpret_cast<uint8_t*>(workspace);
-  float* scale = reinterpret_cast<float*>(codes + as_i8_bytes(n_tokens, n_in));
+  return AS_OK;
+}
+
+static LinArgs linear_args(const uint8_t* codes, const float* scale, int64_t n_tokens, int64_t n_in, const void* w,
+                           const float* w_scale, const float* bias, int64_t n_out, void* y, int64_t y_stride) {
   LinArgs p{};
   p.a = codes;
   p.a_scale = scale;
@@ -718,17 +630,55 @@ int as_linear_i8(const void* x, int32_t x_type, int64_t n_tokens, int64_t n_in, 
   p.n_tokens = (int32_t)n_tokens;
   p.n_out = (int32_t)n_out;
   p.k_tiles = (int32_t)(round_up(n_in, 128) / 64);
+  p.n_in = (int32_t)n_in;
+  return p;
+}
+
+static int launch_codes(const LinArgs& p, int32_t y_type, hipStream_t s) {
+  if (y_type == AS_BF16) return launch_product<AS_BF16>(p, s);
+  if (y_type == AS_F16) return launch_product<AS_F16>(p, s);
+  return launch_product<AS_F32>(p, s);
+}
+
+int as_linear_i8(const void* x, int32_t x_type, int64_t n_tokens, int64_t n_in, int64_t x_stride, const void* w,
+                 const float* w_scale, const float* bias, int64_t n_out, void* y, int32_t y_type, int64_t y_stride,
+                 void* workspace, int64_t workspace_bytes, void* stream) {
+  if (x_type != AS_BF16 && x_type != AS_F16) return fail(AS_E_INVALID_ARG, "linear_i8: x_type %d", x_type);
+  const int rc = check_linear("linear_i8", n_tokens, n_in, n_out, y_type, x_stride, y_stride);
+  if (rc != AS_OK) return rc;
+  if (n_tokens == 0) return as_host::ok();
+  if (!x || !w || !w_scale || !y) return fail(AS_E_INVALID_ARG, "linear_i8: null pointer");
+  if (!aligned(w, 16)) return fail(AS_E_INVALID_ARG, "linear_i8: weights not aligned to 16 bytes");
+  const int64_t need = as_linear_i8_workspace(n_tokens, n_in, n_out);
+  if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 256))))
+    return fail(AS_E_INVALID_ARG, "linear_i8: workspace of %lld bytes, %lld needed (aligned to 256)",
+                (long long)workspace_bytes, (long long)need);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  uint8_t* codes = reinterpret_cast<uint8_t*>(workspace);
+  float* scale = reinterpret_cast<float*>(codes + as_i8_bytes(n_tokens, n_in));
+  LinArgs p = linear_args(codes, scale, n_tokens, n_in, w, w_scale, bias, n_out, y, y_stride);
   p.x = x;
   p.x_stride = x_stride;
-  p.n_in = (int32_t)n_in;
   if (fuses(n_tokens, n_in)) return x_type == AS_BF16 ? launch_fused<AS_BF16>(p, y_type, s) : launch_fused<AS_F16>(p, y_type, s);
   if (x_type == AS_BF16)
     launch_quantize<AS_BF16>(x, n_tokens, n_in, x_stride, codes, scale, s);
   else
     launch_quantize<AS_F16>(x, n_tokens, n_in, x_stride, codes, scale, s);
-  if (y_type == AS_BF16) return launch_product<AS_BF16>(p, s);
-  if (y_type == AS_F16) return launch_product<AS_F16>(p, s);
-  return launch_product<AS_F32>(p, s);
+  return launch_codes(p, y_type, s);
+}
+
+int as_linear_i8_codes(const void* codes, const float* scale, int64_t n_tokens, int64_t n_in, const void* w,
+                       const float* w_scale, const float* bias, int64_t n_out, void* y, int32_t y_type,
+                       int64_t y_stride, void* stream) {
+  const int rc = check_linear("linear_i8_codes", n_tokens, n_in, n_out, y_type, n_in, y_stride);
+  if (rc != AS_OK) return rc;
+  if (n_tokens == 0) return as_host::ok();
+  if (!codes || !scale || !w || !w_scale || !y) return fail(AS_E_INVALID_ARG, "linear_i8_codes: null pointer");
+  if (!aligned(w, 16) || !aligned(codes, 16))
+    return fail(AS_E_INVALID_ARG, "linear_i8_codes: codes or weights not aligned to 16 bytes");
+  return launch_codes(linear_args(reinterpret_cast<const uint8_t*>(codes), scale, n_tokens, n_in, w, w_scale, bias,
+                                  n_out, y, y_stride),
+                      y_type, reinterpret_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

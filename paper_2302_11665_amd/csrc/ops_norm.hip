@@ -1,0 +1,265 @@
+// Rows brought to mean square 1 and held in 8 bits (alpaserve_ops.h): a residual
+// added, the root-mean-square norm, a gain, codes and a scale per row.
+//
+// The code of an element is that of its share of the row's largest magnitude, so
+// the norm's root cancels from it: codes are those of t = h g, and only the scale,
+// max |t| / (127 sqrt(mean h^2 + eps)), needs the sum of squares.  Both reductions
+// therefore run side by side, over values that stay in registers.
+#include "ops_quant.hpp"
+
+using as_host::fail;
+
+namespace as_ops {
+
+struct NormArgs {
+  const uint16_t *x, *residual;  // residual may be null
+  const float* gain;             // [n_cols] or null
+  uint16_t* sum;                 // where there is a residual
+  uint8_t* codes;
+  float *scale, *held;           // held may be null
+  int64_t n_tokens, x_stride, residual_stride, sum_stride;
+  int32_t n_cols, k_tiles;
+  float eps;
+};
+
+// 16 values from column c of a row of 16-bit values, two to a word; columns
+// beyond n are 0.
+__device__ __forceinline__ void read16(const uint16_t* row, int c, int n, v4u (&w)[2]) {
+  w[0] = w[1] = v4u{0, 0, 0, 0};
+  if (c + 16 <= n) {
+    __builtin_memcpy(&w[0], row + c, 16);
+    __builtin_memcpy(&w[1], row + c + 8, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (c + e < n) w[e >> 3][(e >> 1) & 3] |= (uint32_t)row[c + e] << (16 * (e & 1));
+  }
+}
+
+__device__ __forceinline__ void write16(uint16_t* row, int c, int n, const v4u (&w)[2]) {
+  if (c + 16 <= n) {
+    __builtin_memcpy(row + c, &w[0], 16);
+    __builtin_memcpy(row + c + 8, &w[1], 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (c + e < n) row[c + e] = (uint16_t)(w[e >> 3][(e >> 1) & 3] >> (16 * (e & 1)));
+  }
+}
+
+template <int TYPE>
+__device__ __forceinline__ void unpack16(const v4u (&w)[2], float (&f)[16]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    f[2 * j] = to_f32<TYPE>(w[j >> 2][j & 3] & 0xffffu);
+    f[2 * j + 1] = to_f32<TYPE>(w[j >> 2][j & 3] >> 16);
+  }
+}
+
+// w += r, rounded to the type: the sum that is kept is the one that is normed.
+template <int TYPE>
+__device__ __forceinline__ void add16(v4u (&w)[2], const v4u (&r)[2]) {
+  float a[16], b[16];
+  unpack16<TYPE>(w, a);
+  unpack16<TYPE>(r, b);
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    w[j >> 2][j & 3] = (uint32_t)from_f32<TYPE>(a[2 * j] + b[2 * j]) |
+                       (uint32_t)from_f32<TYPE>(a[2 * j + 1] + b[2 * j + 1]) << 16;
+}
+
+// 16 gains from column c; 0 beyond n.
+__device__ __forceinline__ void gain16(const float* gain, int c, int n, float (&g)[16]) {
+  if (c + 16 <= n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) __builtin_memcpy(g + 4 * i, gain + c + 4 * i, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) g[e] = c + e < n ? gain[c + e] : 0.0f;
+  }
+}
+
+// A row's scale from its largest |t| and its sum of squares.  One lane's work: in
+// 64 bits, since nothing waits for it.
+__device__ __forceinline__ float norm_scale(float top, bool finite, double squares, int n_cols, float eps) {
+  if (!finite) return __builtin_nanf("");
+  if (top == 0.0f) return 0.0f;
+  return (float)((double)top / (127.0 * sqrt(squares / n_cols + (double)eps)));
+}
+
+// Sums of squares that fp32 holds without loss: beyond them a row is summed again
+// in 64 bits (16-bit values reach 3e38 in bf16, whose square does not).
+__device__ __forceinline__ bool fp32_holds(float squares) { return squares > 0x1p-60f && squares < 0x1p120f; }
+
+// One workgroup per row, 16 columns to a thread and chunk.  Latency bounds a few
+// rows.
+template <int TYPE, bool GAIN, int THREADS, int CHUNKS>
+__global__ __launch_bounds__(THREADS) void norm_rows(NormArgs p) {
+  constexpr int kWaves = THREADS / 64;
+  __shared__ uint32_t tops[kWaves];
+  __shared__ float sums[kWaves];
+  __shared__ double wide[kWaves];
+  __shared__ float row_scale;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t r = blockIdx.x;
+  const uint16_t* x = p.x + r * p.x_stride;
+  v4u w[CHUNKS][2];
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) read16(x, (i * THREADS + tid) * 16, p.n_cols, w[i]);
+  if (p.residual) {
+    const uint16_t* add = p.residual + r * p.residual_stride;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      v4u b[2];
+      read16(add, (i * THREADS + tid) * 16, p.n_cols, b);
+      add16<TYPE>(w[i], b);
+    }
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) write16(p.sum + r * p.sum_stride, (i * THREADS + tid) * 16, p.n_cols, w[i]);
+  }
+  uint32_t top = 0;
+  float squares = 0.0f;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    float f[16], g[16];
+    unpack16<TYPE>(w[i], f);
+    if (GAIN) gain16(p.gain, (i * THREADS + tid) * 16, p.n_cols, g);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      squares = fmaf(f[e], f[e], squares);
+      top = max(top, magnitude(GAIN ? f[e] * g[e] : f[e]));
+    }
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) {
+    top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    squares += __shfl_xor(squares, o);
+  }
+  if (lane == 0) tops[wave] = top, sums[wave] = squares;
+  __syncthreads();
+  squares = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    top = max(top, tops[i]);
+    squares += sums[i];
+  }
+  const bool finite = top < 0x7f800000u;
+  double total = squares;
+  if (finite && top != 0 && !fp32_holds(squares)) {
+    double d = 0.0;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      float f[16];
+      unpack16<TYPE>(w[i], f);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) d += (double)f[e] * f[e];
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) d += __shfl_xor(d, o);
+    if (lane == 0) wide[wave] = d;
+    __syncthreads();
+    total = 0.0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) total += wide[i];
+  }
+  if (tid == 0) {
+    row_scale = norm_scale(__uint_as_float(top), finite, total, p.n_cols, p.eps);
+    p.scale[r] = row_scale;
+  }
+  if (p.held) __syncthreads();
+  const Quantiser<GAIN ? AS_F32 : TYPE> quantiser(__uint_as_float(top), finite);
+  uint8_t* out = p.codes + (r >> 4) * p.k_tiles * 1024 + (r & 15) * 16;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int c = (i * THREADS + tid) * 16;
+    if (c >= p.k_tiles * 64) break;
+    float f[16], g[16];
+    unpack16<TYPE>(w[i], f);
+    if (GAIN) {
+      gain16(p.gain, c, p.n_cols, g);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) f[e] *= g[e];
+    }
+    const v4u q = {quantiser.codes4(f), quantiser.codes4(f + 4), quantiser.codes4(f + 8), quantiser.codes4(f + 12)};
+    *reinterpret_cast<v4u*>(out + (int64_t)(c >> 4) * 256) = q;
+    if (p.held) {
+      float* held = p.held + r * p.n_cols + c;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (c + e < p.n_cols) held[e] = (float)(int8_t)(q[e >> 2] >> (8 * (e & 3))) * row_scale;
+    }
+  }
+}
+
+template <int TYPE, bool GAIN>
+void launch_norm(const NormArgs& p, hipStream_t s) {
+  auto rows = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)p.n_tokens), dim3(threads), 0, s, p);
+  };
+  if (p.n_cols <= 4096)
+    rows(norm_rows<TYPE, GAIN, 256, 1>, 256);
+  else if (p.n_cols <= 16384)
+    rows(norm_rows<TYPE, GAIN, 1024, 1>, 1024);
+  else if (p.n_cols <= 32768)
+    rows(norm_rows<TYPE, GAIN, 1024, 2>, 1024);
+  else
+    rows(norm_rows<TYPE, GAIN, 1024, 8>, 1024);
+}
+
+// Whether rows of n elements of 16 bits from a share memory with those from b
+// without being them.
+bool clashes(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t rows, int64_t n) {
+  const int64_t u = (int64_t)((uintptr_t)a / 2), w = (int64_t)((uintptr_t)b / 2);
+  if (rows == 1) a_stride = b_stride = n;
+  if (u == w && a_stride == b_stride) return (uintptr_t)a != (uintptr_t)b;
+  if (u + (rows - 1) * a_stride + n <= w || w + (rows - 1) * b_stride + n <= u) return false;
+  if (a_stride != b_stride) return true;
+  const int64_t d = ((w - u) % a_stride + a_stride) % a_stride;  // columns of one buffer, side by side
+  return d < n || a_stride - d < n;
+}
+
+}  // namespace as_ops
+
+using namespace as_ops;
+
+extern "C" int as_norm_i8(const void* x, const void* residual, int32_t type, int64_t n_tokens, int64_t n_cols,
+                          int64_t x_stride, int64_t residual_stride, const float* gain, float eps, void* sum,
+                          int64_t sum_stride, void* codes, float* scale, float* held, void* stream) {
+  if (type != AS_BF16 && type != AS_F16) return fail(AS_E_INVALID_ARG, "norm_i8: type %d", type);
+  if (n_tokens < 0 || n_cols < 1 || x_stride < n_cols || (residual && (residual_stride < n_cols || sum_stride < n_cols)))
+    return fail(AS_E_INVALID_ARG, "norm_i8: %lld tokens of %lld columns, strides %lld, %lld and %lld",
+                (long long)n_tokens, (long long)n_cols, (long long)x_stride, (long long)residual_stride,
+                (long long)sum_stride);
+  if (!(eps >= 0.0f) || eps > 3.4e38f) return fail(AS_E_INVALID_ARG, "norm_i8: eps %g", (double)eps);
+  // (a workgroup of up to 1024 threads to a row, fewer than 2^32 threads a launch)
+  if (n_tokens > 65535 * 16 || n_cols > AS_I8_MAX_INPUTS)
+    return fail(AS_E_LIMITS, "norm_i8: at most %d tokens of %d columns", 65535 * 16, AS_I8_MAX_INPUTS);
+  if (n_tokens == 0) return as_host::ok();
+  if (!x || !codes || !scale || (residual != nullptr) != (sum != nullptr))
+    return fail(AS_E_INVALID_ARG, "norm_i8: null pointer, or one of residual and sum alone");
+  if (!aligned(codes, 16)) return fail(AS_E_INVALID_ARG, "norm_i8: codes not aligned to 16 bytes");
+  if (sum && (clashes(sum, sum_stride, x, x_stride, n_tokens, n_cols) ||
+              clashes(sum, sum_stride, residual, residual_stride, n_tokens, n_cols)))
+    return fail(AS_E_INVALID_ARG, "norm_i8: the sum shares memory with other rows of x or the residual");
+  NormArgs p{};
+  p.x = reinterpret_cast<const uint16_t*>(x);
+  p.residual = reinterpret_cast<const uint16_t*>(residual);
+  p.gain = gain;
+  p.sum = reinterpret_cast<uint16_t*>(sum);
+  p.codes = reinterpret_cast<uint8_t*>(codes);
+  p.scale = scale;
+  p.held = held;
+  p.n_tokens = n_tokens;
+  p.x_stride = x_stride;
+  p.residual_stride = residual_stride;
+  p.sum_stride = sum_stride;
+  p.n_cols = (int32_t)n_cols;
+  p.k_tiles = (int32_t)(round_up(n_cols, 128) / 64);
+  p.eps = eps;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (type == AS_BF16)
+    gain ? launch_norm<AS_BF16, true>(p, s) : launch_norm<AS_BF16, false>(p, s);
+  else
+    gain ? launch_norm<AS_F16, true>(p, s) : launch_norm<AS_F16, false>(p, s);
+  return launched("norm_i8");
+}

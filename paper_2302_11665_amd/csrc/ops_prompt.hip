@@ -1,0 +1,380 @@
+// Causal attention over packed prompts (alpaserve_ops.h): every token of a
+// sequence attends to the tokens of its sequence up to itself.
+//
+//   o_t = sum_s p_ts v_s,  p_ts = exp(scale q_t.k_s) / sum_s' exp(scale q_t.k_s')
+//
+// The products are made transposed, S^T = K Q^T and O^T = V^T P^T, in tiles of
+// 32x32x16: lane l then holds scores of one query (column l % 32) alone, so the
+// softmax's maximum and sum stay within a lane and its partner l ^ 32, a query's
+// rescaling is one factor per lane, and P^T is in the order in which the second
+// product takes it.  There a lane has keys 8 (r / 4) + 4 (l / 32) + r % 4 of 32;
+// V's operand takes the same order of keys, four of one channel at a time, from
+// rows in LDS by transposing reads.
+#include <algorithm>
+#include <type_traits>
+
+#include "ops_common.hpp"
+
+using as_host::fail;
+
+namespace as_ops {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef short v8s __attribute__((ext_vector_type(8)));
+
+struct PromptArgs {
+  const uint16_t *q, *k, *v;
+  uint16_t* out;
+  int64_t q_token, k_token, v_token;  // strides in elements
+  const int32_t* offsets;
+  int32_t n_tokens, n_seqs, n_heads, group;  // key/value heads; query heads to each
+  float factor;                              // scale log2 e
+};
+
+template <int TYPE>
+__device__ __forceinline__ v16f multiply(v8s a, v8s b, v16f c) {
+  if constexpr (TYPE == AS_BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float max_halves(float x) {
+  const v2u p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float sum_halves(float x) {
+  const v2u p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
+// A sequence's tokens, clipped to those that there are.
+__device__ __forceinline__ void sequence(const PromptArgs& p, int b, int& begin, int& length) {
+  begin = min(max(p.offsets[b], 0), p.n_tokens);
+  length = min(max(p.offsets[b + 1], begin), p.n_tokens) - begin;
+}
+
+// Blocks of ROWS rows (a row: one query of one head of the group).
+template <int ROWS>
+__device__ __forceinline__ int blocks_of(const PromptArgs& p, int b) {
+  int begin, length;
+  sequence(p, b, begin, length);
+  return (int)(((int64_t)length * p.group + ROWS - 1) / ROWS);
+}
+
+__device__ __forceinline__ uint32_t sum_lanes(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_readlane((int)scan_lanes(x), 63);
+}
+
+// The item-th block of all sequences, those with the most keys first: blocks
+// begin at their sequence's first token, so the j-th of every sequence has as
+// much work, and items are in order of falling j, then of sequences.  False
+// where there are fewer items.  A wavefront's work: lanes count for a sequence
+// each, and j is found by halving.
+template <int ROWS>
+__device__ __forceinline__ bool find_block(const PromptArgs& p, uint32_t item, int& seq, int& block) {
+  const int lane = threadIdx.x & 63;
+  auto beyond = [&](int j) {  // items of blocks j and later
+    uint32_t n = 0;
+    for (int b = lane; b < p.n_seqs; b += 64) n += (uint32_t)max(0, blocks_of<ROWS>(p, b) - j);
+    return sum_lanes(n);
+  };
+  if (beyond(0) <= item) return false;
+  int lo = 0, hi = (int)(((int64_t)p.n_tokens * p.group + ROWS - 1) / ROWS);  // beyond(lo) > item >= beyond(hi)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (beyond(mid) > item)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  block = lo;
+  uint32_t rank = item - beyond(lo + 1);  // among the sequences that have this block
+  for (int first = 0; first < p.n_seqs; first += 64) {
+    const int b = first + lane;
+    const uint64_t have = __ballot(b < p.n_seqs && blocks_of<ROWS>(p, min(b, p.n_seqs - 1)) > lo);
+    const uint32_t n = (uint32_t)__popcll(have);
+    if (rank < n) {
+      const uint64_t mine = __ballot((have >> lane & 1) && (uint32_t)__popcll(have & ((uint64_t(1) << lane) - 1)) == rank);
+      seq = first + __ffsll((unsigned long long)mine) - 1;
+      return true;
+    }
+    rank -= n;
+  }
+  return false;
+}
+
+constexpr int kKeys = 64;  // keys of a stage
+
+// Rows of a stage lie in LDS as in memory, in pieces of 16 bytes whose order is
+// swapped around by key: 16 keys at one piece (K's operand) and 4 keys at two
+// pieces side by side (V's) then fall on different banks.
+template <int DIM>
+__device__ __forceinline__ int swizzle(int key) {
+  return DIM == 128 ? (key & 3) << 2 | (key >> 2 & 3) : (key >> 1 & 1) << 2 | (key >> 2 & 3);
+}
+
+// Bits of a 16-bit value that is not finite.
+template <int TYPE>
+__device__ __forceinline__ bool not_finite(uint16_t u) {
+  return TYPE == AS_BF16 ? (u & 0x7f80u) == 0x7f80u : (u & 0x7c00u) == 0x7c00u;
+}
+template <int TYPE>
+constexpr uint16_t kOne = TYPE == AS_BF16 ? 0x3f80 : 0x3c00;
+template <int TYPE>
+constexpr uint16_t kInfinity = TYPE == AS_BF16 ? 0x7f80 : 0x7c00;
+
+// A workgroup takes 32 rows a wavefront of one key/value head (rows: queries and
+// the heads of their group, queries in order) over the keys that they see, 64 at
+// a time, which come into two stages of LDS straight from memory.
+//
+// Masked scores give p = 0, but 0 times an infinity or NaN in V is NaN.  A
+// workgroup whose results are all finite met none; otherwise it does its work
+// again, CAREFUL: at keys that some of its rows do not see, values that are not
+// finite are left out of the product and reach the rows that see them by products
+// of their marks with a mask.
+template <int TYPE, int DIM, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void prompt_attention(PromptArgs p) {
+  constexpr int kRows = 32 * WAVES, kRowBytes = DIM * 2, kTile = kKeys * kRowBytes;
+  constexpr int kLoads = kTile / 1024 / WAVES;  // of K and of V, by a wavefront, a stage
+  constexpr int kPieces = kRowBytes / 16, kPerLoad = 1024 / kRowBytes;  // keys of a load
+  constexpr int kSteps = DIM / 16, kDimTiles = DIM / 32;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][kTile];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int head = blockIdx.x % p.n_heads;
+  int seq, block;
+  if (!find_block<kRows>(p, blockIdx.x / p.n_heads, seq, block)) return;
+  int begin, length;
+  sequence(p, seq, begin, length);
+  const int rows = length * p.group, row0 = block * kRows + wave * 32;
+  // rows behind the last one do its work again
+  const int row = min(row0 + col, rows - 1), pos = row / p.group, member = row - pos * p.group;
+  const int first = min(row0, rows - 1) / p.group, last = min(row0 + 31, rows - 1) / p.group;  // queries
+  const bool busy = row0 < rows;
+  const int tiles = min(block * kRows + kRows - 1, rows - 1) / p.group / kKeys + 1;
+
+  v8s q[kSteps];
+  {
+    const uint16_t* at = p.q + (int64_t)(begin + pos) * p.q_token + (int64_t)(head * p.group + member) * DIM + half * 8;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) q[i] = *reinterpret_cast<const v8s*>(at + i * 16);
+  }
+
+  const uint8_t* k0 = reinterpret_cast<const uint8_t*>(p.k + (int64_t)begin * p.k_token + (int64_t)head * DIM);
+  const uint8_t* v0 = reinterpret_cast<const uint8_t*>(p.v + (int64_t)begin * p.v_token + (int64_t)head * DIM);
+  // a lane's key and piece in the wavefront's loads: keys (wave + j WAVES) kPerLoad + lane / kPieces
+  auto bring = [&](int slot, int tile) {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int in = (wave + j * WAVES) * kPerLoad + lane / kPieces;
+      const int piece = (lane % kPieces) ^ swizzle<DIM>(in);
+      const int64_t key = min(tile * kKeys + in, length - 1);
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)(k0 + key * p.k_token * 2 + piece * 16),
+          (__attribute__((address_space(3))) void*)(lds[slot][0] + (wave + j * WAVES) * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)(v0 + key * p.v_token * 2 + piece * 16),
+          (__attribute__((address_space(3))) void*)(lds[slot][1] + (wave + j * WAVES) * 1024), 16, 0, 0);
+    }
+  };
+
+  v16f o[kDimTiles];
+  float reference, total;  // of the exponents; sum of this lane's keys' p
+
+  auto work = [&](auto careful) {
+    constexpr bool kCareful = decltype(careful)::value;
+#pragma unroll
+    for (int i = 0; i < kDimTiles; ++i) o[i] = v16f{};
+    reference = -1e30f, total = 0.0f;
+    bring(0, 0);
+    for (int tile = 0; tile < tiles; ++tile) {
+      wait_loads<0>();
+      __syncthreads();  // this stage is there, and all are done with the other
+      if (tile + 1 < tiles) bring((tile + 1) & 1, tile + 1);
+      const int key0 = tile * kKeys;
+      if (!busy || key0 > last) continue;
+      const uint8_t* kt = lds[tile & 1][0];
+      const uint8_t* vt = lds[tile & 1][1];
+      v16f s[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s[h] = v16f{};
+        const int key = h * 32 + col;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          const int piece = (i * 2 + half) ^ swizzle<DIM>(key);
+          s[h] = multiply<TYPE>(*reinterpret_cast<const v8s*>(kt + key * kRowBytes + piece * 16), q[i], s[h]);
+        }
+      }
+      const bool masked = key0 + kKeys - 1 > first;
+      if (masked) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (key0 + h * 32 + 8 * (r >> 2) + 4 * half + (r & 3) > pos) s[h][r] = -kInf;
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[h][r]);
+      top = max_halves(top) * p.factor;
+      // a query's reference follows its maximum when it is passed by 2^8
+      if (__any(top > reference + 8.0f)) {
+        const float now = top > reference + 8.0f ? top : reference, by = __builtin_amdgcn_exp2f(reference - now);
+        reference = now;
+        total *= by;
+#pragma unroll
+        for (int i = 0; i < kDimTiles; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[i][r] *= by;
+      }
+      v8s weights[4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[h][r], p.factor, -reference));
+          total += e;
+          weights[h * 2 + (r >> 3)][r & 7] = (short)from_f32<TYPE>(e);
+        }
+#pragma unroll
+      for (int i = 0; i < kDimTiles; ++i) {
+        v16f nan = {}, plus = {}, minus = {};
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          v8s v;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int key = z * 16 + j * 8 + half * 4 + (lane & 15) / 4;
+            const int byte = i * 64 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+            const int at = key * kRowBytes + (((byte >> 4) ^ swizzle<DIM>(key)) << 4) + (byte & 8);
+            const v4s four = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(vt + at));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[j * 4 + e] = four[e];
+          }
+          if (kCareful && masked) {
+            v8s is_nan, is_plus, is_minus, seen;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const uint16_t u = (uint16_t)v[e];
+              const bool bad = not_finite<TYPE>(u);
+              is_plus[e] = (short)(u == kInfinity<TYPE> ? kOne<TYPE> : 0);
+              is_minus[e] = (short)(u == (kInfinity<TYPE> | 0x8000) ? kOne<TYPE> : 0);
+              is_nan[e] = (short)(bad && !is_plus[e] && !is_minus[e] ? kOne<TYPE> : 0);
+              v[e] = bad ? (short)0 : v[e];
+              const int key = key0 + z * 16 + 8 * (e >> 2) + 4 * half + (e & 3);
+              seen[e] = (short)(key <= pos ? kOne<TYPE> : 0);
+            }
+            nan = multiply<TYPE>(is_nan, seen, nan);
+            plus = multiply<TYPE>(is_plus, seen, plus);
+            minus = multiply<TYPE>(is_minus, seen, minus);
+          }
+          o[i] = multiply<TYPE>(v, weights[z], o[i]);
+        }
+        if (kCareful && masked) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            if (plus[r] > 0.0f) o[i][r] += kInf;
+            if (minus[r] > 0.0f) o[i][r] -= kInf;
+            if (nan[r] > 0.0f) o[i][r] = __builtin_nanf("");
+          }
+        }
+      }
+    }
+    total = sum_halves(total);
+  };
+
+  work(std::false_type{});
+  bool fine = true;
+  if (busy) {
+#pragma unroll
+    for (int i = 0; i < kDimTiles; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) fine &= fabsf(o[i][r]) < kInf;
+  }
+  if (__syncthreads_or(!fine)) work(std::true_type{});
+  if (row0 + col >= rows) return;
+  uint16_t* to = p.out + ((int64_t)(begin + pos) * p.n_heads * p.group + head * p.group + member) * DIM;
+  const float by = 1.0f / total;
+#pragma unroll
+  for (int i = 0; i < kDimTiles; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const uint32_t lo = from_f32<TYPE>(o[i][r] * by) | (uint32_t)from_f32<TYPE>(o[i][r + 1] * by) << 16;
+      const uint32_t hi = from_f32<TYPE>(o[i][r + 2] * by) | (uint32_t)from_f32<TYPE>(o[i][r + 3] * by) << 16;
+      *reinterpret_cast<v2u*>(to + i * 32 + 2 * r + 4 * half) = v2u{lo, hi};
+    }
+}
+
+constexpr int kPromptWaves = 4;
+
+// Workgroups that there can be at most: a part block for each sequence.
+int64_t prompt_groups(int64_t n_tokens, int64_t n_seqs, int64_t n_heads, int64_t group) {
+  return (n_tokens * group / (32 * kPromptWaves) + std::min(n_seqs, n_tokens * group)) * n_heads;
+}
+
+template <int TYPE>
+void launch_prompt(const PromptArgs& p, int dim, hipStream_t s) {
+  const dim3 g((unsigned)prompt_groups(p.n_tokens, p.n_seqs, p.n_heads, p.group)), t(64 * kPromptWaves);
+  if (dim == 64) hipLaunchKernelGGL((prompt_attention<TYPE, 64, kPromptWaves>), g, t, 0, s, p);
+  if (dim == 128) hipLaunchKernelGGL((prompt_attention<TYPE, 128, kPromptWaves>), g, t, 0, s, p);
+}
+
+}  // namespace as_ops
+
+using namespace as_ops;
+
+extern "C" int as_attention_prompt(const void* q, const void* k, const void* v, int32_t type, int64_t n_tokens,
+                                   int32_t n_q_heads, int32_t n_kv_heads, int32_t dim, int64_t q_token, int64_t k_token,
+                                   int64_t v_token, const int32_t* offsets, int32_t n_seqs, float scale, void* out,
+                                   void* stream) {
+  if (type != AS_BF16 && type != AS_F16) return fail(AS_E_INVALID_ARG, "attention_prompt: type %d", type);
+  if (dim != 64 && dim != 128) return fail(AS_E_LIMITS, "attention_prompt: heads of %d channels (64 or 128)", dim);
+  if (n_tokens < 0 || n_seqs < 0 || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads)
+    return fail(AS_E_INVALID_ARG, "attention_prompt: %lld tokens, %d sequences, %d query heads of %d key/value heads",
+                (long long)n_tokens, n_seqs, n_q_heads, n_kv_heads);
+  if (q_token < 0 || k_token < 0 || v_token < 0 || q_token % 8 || k_token % 8 || v_token % 8)
+    return fail(AS_E_INVALID_ARG, "attention_prompt: strides %lld, %lld and %lld (multiples of 8)", (long long)q_token,
+                (long long)k_token, (long long)v_token);
+  if (!(scale > 0.0f) || scale > 2e38f) return fail(AS_E_INVALID_ARG, "attention_prompt: scale %g", (double)scale);
+  const int group = n_q_heads / n_kv_heads;
+  // (a workgroup of 256 threads each, fewer than 2^32 in all)
+  if (n_tokens > (1 << 26) || n_seqs > (1 << 20) || n_q_heads > 4096 || n_tokens * n_q_heads > (1 << 30) ||
+      prompt_groups(n_tokens, n_seqs, n_kv_heads, group) >= (1 << 24))
+    return fail(AS_E_LIMITS, "attention_prompt: %lld tokens of %d heads in %d sequences", (long long)n_tokens, n_q_heads,
+                n_seqs);
+  if (n_tokens == 0 || n_seqs == 0) return as_host::ok();
+  if (!q || !k || !v || !offsets || !out) return fail(AS_E_INVALID_ARG, "attention_prompt: null pointer");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 8))
+    return fail(AS_E_INVALID_ARG, "attention_prompt: queries, keys and values aligned to 16 bytes, outputs to 8");
+  const uintptr_t out0 = (uintptr_t)out, out1 = out0 + (uintptr_t)(n_tokens * n_q_heads * dim * 2);
+  auto meets = [&](const void* x, int64_t token, int heads) {
+    return (uintptr_t)x < out1 && out0 < (uintptr_t)x + (uintptr_t)(((n_tokens - 1) * token + (int64_t)heads * dim) * 2);
+  };
+  if (meets(q, q_token, n_q_heads) || meets(k, k_token, n_kv_heads) || meets(v, v_token, n_kv_heads))
+    return fail(AS_E_INVALID_ARG, "attention_prompt: outputs share memory with queries, keys or values");
+  PromptArgs p{};
+  p.q = reinterpret_cast<const uint16_t*>(q);
+  p.k = reinterpret_cast<const uint16_t*>(k);
+  p.v = reinterpret_cast<const uint16_t*>(v);
+  p.out = reinterpret_cast<uint16_t*>(out);
+  p.q_token = q_token;
+  p.k_token = k_token;
+  p.v_token = v_token;
+  p.offsets = offsets;
+  p.n_tokens = (int32_t)n_tokens;
+  p.n_seqs = n_seqs;
+  p.n_heads = n_kv_heads;
+  p.group = group;
+  p.factor = scale * 1.44269504f;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (type == AS_BF16)
+    launch_prompt<AS_BF16>(p, dim, s);
+  else
+    launch_prompt<AS_F16>(p, dim, s);
+  return launched("attention_prompt");
+}

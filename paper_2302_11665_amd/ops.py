@@ -1,6 +1,8 @@
 """Thin ctypes binding of the operators of a served model's step (see
 include/alpaserve_ops.h): linear layers with 8-bit weights, a paged cache of 4
-bits with attention over it, and the cache's eviction by accumulated weight.
+bits with attention over it, and the cache's eviction by accumulated weight; and
+of those that take prompts in: norms in 8 bits, attention over packed prompts,
+pages from a pool, packed appends.
 
 Argument marshalling only, as in `sim`: arrays are torch CUDA tensors, outputs
 and scratch memory are torch allocations, calls run on torch's current stream of
@@ -48,6 +50,16 @@ def lib():
                 ("as_attention_kv4_workspace", _I64, [C, _I32, _I32, _I32]),
                 ("as_attention_kv4", ctypes.c_int, [C, _P, _I32, _I32, _I32, _I64, _I64, _P, ctypes.c_float, _P, _P,
                                                     _P, _P, _I64, _P]),
+                ("as_linear_i8_codes", ctypes.c_int, [_P, _P, _I64, _I64, _P, _P, _P, _I64, _P, _I32, _I64, _P]),
+                ("as_norm_i8", ctypes.c_int, [_P, _P, _I32, _I64, _I64, _I64, _I64, _P, ctypes.c_float, _P, _I64, _P,
+                                              _P, _P, _P]),
+                ("as_attention_prompt", ctypes.c_int, [_P, _P, _P, _I32, _I64, _I32, _I32, _I32, _I64, _I64, _I64, _P,
+                                                       _I32, ctypes.c_float, _P, _P]),
+                ("as_pages_reserve_workspace", _I64, [_I32]),
+                ("as_pages_reserve", ctypes.c_int, [_P, _P, _I32, _P, _I32, _I32, _I32, _P, _P, _I64, _P, _P, _P, _P,
+                                                    _P, _P, _I64, _P]),
+                ("as_pages_release", ctypes.c_int, [_P, _P, _I32, _P, _I32, _I32, _I32, _P, _P, _P, _P, _P]),
+                ("as_cache_append_packed", ctypes.c_int, [C, _P, _P, _I32, _I64, _I64, _I64, _P, _P, _P, _P, _P, _P]),
                 ("as_cache_evict_workspace", _I64, [C, _I32]),
                 ("as_cache_evict", ctypes.c_int, [C, C, _P, _P, _I32, _I32, _P, _P, _I64, _P])):
             f = getattr(L, name)
@@ -139,17 +151,80 @@ def pack_weight(w) -> PackedWeight:
     return PackedWeight(codes, scale, n, k)
 
 
-def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
-    """x [..., n_in] (bf16 or fp16) quantised per token, times the packed
-    weights: [..., n_out] of `dtype` (default: x's; fp32 allowed).  `out`, if
-    given, is [tokens, n_out] with contiguous rows that do not overlap."""
+@dataclasses.dataclass
+class Codes:
+    """Activations of 8 bits: the codes of n_rows rows of n_cols columns in the
+    tiles of as_quantize_i8 (int8), one fp32 scale per row, and the type of the
+    rows that they were made from."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+    n_rows: int
+    n_cols: int
+    dtype: torch.dtype
+
+
+def norm_i8(x, residual=None, gain=None, eps=1e-6, out=None, held=False):
+    """Rows of x [..., columns] (bf16 or fp16), or of x + residual rounded to
+    their type, brought to mean square 1, times gain [columns] (fp32), in 8 bits
+    for `linear_i8`: (Codes, the sum, which is x without a residual), with
+    `held` also the values that the codes stand for (fp32, x's shape).  `out`, if
+    given, gets the sum: [rows, columns] with contiguous rows that do not
+    overlap; it may be x or the residual."""
     L = lib()
     _need(x, "x", _16, contiguous=False)
     dev = x.device
-    if x.dim() < 1 or x.shape[-1] != w.n_in:
-        _bad(f"linear_i8: x has {tuple(x.shape)}, the weights take {w.n_in} inputs")
-    x2, x_stride = _rows(x if x.dim() == 2 else x.reshape(-1, w.n_in))
+    if x.dim() < 1 or x.shape[-1] < 1:
+        _bad(f"norm_i8: x has {tuple(x.shape)}")
+    cols = x.shape[-1]
+    x2, x_stride = _rows(x if x.dim() == 2 else x.reshape(-1, cols))
     t = x2.shape[0]
+    r2, r_stride, s, s_stride = None, 0, None, 0
+    if residual is not None:
+        _need(residual, "residual", (x.dtype,), device=dev, contiguous=False)
+        if residual.shape != x.shape:
+            _bad(f"norm_i8: x has {tuple(x.shape)}, the residual {tuple(residual.shape)}")
+        r2, r_stride = _rows(residual if x.dim() == 2 else residual.reshape(-1, cols))
+        s = torch.empty((t, cols), dtype=x.dtype, device=dev) if out is None else _need(
+            out, "out", (x.dtype,), 2, dev, contiguous=False)
+        s_stride = s.stride(0) if t > 1 else cols
+        if tuple(s.shape) != (t, cols) or (cols > 1 and s.stride(1) != 1) or s_stride < cols:
+            _bad(f"norm_i8: out has {tuple(s.shape)} with strides {s.stride()}")
+    elif out is not None:
+        _bad("norm_i8: out without a residual")
+    if gain is not None and _need(gain, "gain", (torch.float32,), 1, dev).numel() != cols:
+        _bad(f"norm_i8: {gain.numel()} gains for {cols} columns")
+    codes = torch.empty(L.as_i8_bytes(t, cols), dtype=torch.int8, device=dev)
+    scale = torch.empty(t, dtype=torch.float32, device=dev)
+    values = torch.empty(x.shape, dtype=torch.float32, device=dev) if held else None
+    _call(L.as_norm_i8, dev, x2.data_ptr(), None if r2 is None else r2.data_ptr(), _TYPES[x.dtype], t, cols, x_stride,
+          r_stride, None if gain is None else gain.data_ptr(), eps, None if s is None else s.data_ptr(), s_stride,
+          codes.data_ptr(), scale.data_ptr(), values.data_ptr() if held else None)
+    total = x if s is None else s if out is not None or x.dim() == 2 else s.view(x.shape)
+    c = Codes(codes, scale, t, cols, x.dtype)
+    return (c, total, values) if held else (c, total)
+
+
+def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
+    """x [..., n_in] (bf16 or fp16) quantised per token, times the packed
+    weights: [..., n_out] of `dtype` (default: x's; fp32 allowed).  x may be
+    `Codes`: [rows, n_out].  `out`, if given, is [tokens, n_out] with contiguous
+    rows that do not overlap."""
+    L = lib()
+    held = isinstance(x, Codes)
+    if held:
+        dev, t = x.codes.device, x.n_rows
+        if not (x.codes.is_cuda and x.codes.dtype is torch.int8 and x.scale.dtype is torch.float32
+                and x.scale.device == dev and x.codes.is_contiguous() and x.scale.is_contiguous()
+                and x.n_cols == w.n_in and x.codes.numel() == L.as_i8_bytes(t, w.n_in) and x.scale.numel() == t):
+            _bad(f"linear_i8: {x.codes.numel()} codes {x.codes.dtype} on {dev} and {x.scale.numel()} scales of "
+                 f"{t} x {x.n_cols}, the weights take {w.n_in} inputs")
+    else:
+        _need(x, "x", _16, contiguous=False)
+        dev = x.device
+        if x.dim() < 1 or x.shape[-1] != w.n_in:
+            _bad(f"linear_i8: x has {tuple(x.shape)}, the weights take {w.n_in} inputs")
+        x2, x_stride = _rows(x if x.dim() == 2 else x.reshape(-1, w.n_in))
+        t = x2.shape[0]
     codes, scale = w.codes, w.scale
     if not (codes.device == scale.device == dev and codes.dtype in (torch.int8, torch.uint8)
             and scale.dtype is torch.float32 and codes.is_contiguous() and scale.is_contiguous()
@@ -167,12 +242,148 @@ def linear_i8(x, w: PackedWeight, bias=None, dtype=None, out=None):
             _bad(f"linear_i8: out has {tuple(y.shape)} with strides {y.stride()}, {y.dtype}")
     if y.dtype not in _TYPES:
         _bad(f"linear_i8: type {y.dtype}")
+    y_stride = y.stride(0) if t > 1 else w.n_out
+    bias_at = None if bias is None else bias.data_ptr()
+    if held:
+        _call(L.as_linear_i8_codes, dev, x.codes.data_ptr(), x.scale.data_ptr(), t, w.n_in, codes.data_ptr(),
+              scale.data_ptr(), bias_at, w.n_out, y.data_ptr(), _TYPES[y.dtype], y_stride)
+        return y
     n = L.as_linear_i8_workspace(t, w.n_in, w.n_out)
     _keep, ws = _workspace(n, dev)
-    _call(L.as_linear_i8, dev, x2.data_ptr(), _TYPES[x.dtype], t, w.n_in, x_stride,
-          w.codes.data_ptr(), w.scale.data_ptr(), None if bias is None else bias.data_ptr(), w.n_out, y.data_ptr(),
-          _TYPES[y.dtype], y.stride(0) if t > 1 else w.n_out, ws, n)
+    _call(L.as_linear_i8, dev, x2.data_ptr(), _TYPES[x.dtype], t, w.n_in, x_stride, codes.data_ptr(),
+          scale.data_ptr(), bias_at, w.n_out, y.data_ptr(), _TYPES[y.dtype], y_stride, ws, n)
     return y if out is not None or x.dim() == 2 else y.view(*x.shape[:-1], w.n_out)
+
+
+# ------------------------------------------------------------------ prompts
+
+def _packed(x, name, dtype=None, device=None, dim=None):
+    """x [tokens, heads, dim] with its last two dimensions contiguous, and its
+    row stride (0 for one row, where it is not used)."""
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 3 and x.dtype in _16 and x.shape[1] >= 1
+            and (dtype is None or (x.dtype == dtype and x.device == device and x.shape[2] == dim))):
+        what = f"{tuple(x.shape)} {x.dtype} on {x.device}" if isinstance(x, torch.Tensor) else type(x)
+        _bad(f"{name}: {what}, not [tokens, heads, channels] in 16 bits on one device")
+    token, head, step = x.stride()
+    if step != 1 or (x.shape[1] > 1 and head != x.shape[2]):
+        x = x.contiguous()
+        token = x.stride(0)
+    return x, token if x.shape[0] > 1 else 0
+
+
+def _aligned_rows(x, stride):
+    """Rows at addresses that are multiples of 16 bytes."""
+    if x.data_ptr() % 16 or stride % 8:
+        x = x.clone(memory_format=torch.contiguous_format)
+        stride = x.stride(0) if x.shape[0] > 1 else 0
+    return x, stride
+
+
+def attention_prompt(q, k, v, offsets, scale=None, out=None):
+    """Causal attention of packed sequences: q [tokens, q_heads, dim], k and v
+    [tokens, kv_heads, dim] (bf16 or fp16; parts of one projection's output are
+    fine), rows offsets[b]..offsets[b + 1] - 1 being sequence b's (int32 [seqs +
+    1], rising from 0).  Every token attends to its sequence's tokens up to
+    itself, head j to key/value head j / (q_heads / kv_heads).  `scale` defaults
+    to dim ** -0.5.  Rows of no sequence are not written: give `out` (contiguous,
+    q's shape) where what they hold matters."""
+    q, q_token = _packed(q, "q")
+    dev, (t, heads, dim) = q.device, q.shape
+    k, k_token = _packed(k, "k", q.dtype, dev, dim)
+    v, v_token = _packed(v, "v", q.dtype, dev, dim)
+    if k.shape != v.shape or k.shape[0] != t:
+        _bad(f"attention_prompt: q has {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
+    if not (isinstance(offsets, torch.Tensor) and offsets.dtype is torch.int32 and offsets.dim() == 1
+            and offsets.shape[0] >= 1 and offsets.device == dev and offsets.is_contiguous()):
+        _bad("attention_prompt: offsets are int32 [sequences + 1] on the device of q")
+    q, q_token = _aligned_rows(q, q_token)
+    k, k_token = _aligned_rows(k, k_token)
+    v, v_token = _aligned_rows(v, v_token)
+    if out is None:
+        out = torch.empty((t, heads, dim), dtype=q.dtype, device=dev)
+    elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.shape == q.shape and out.device == dev
+              and out.is_contiguous()):
+        _bad("attention_prompt: out is contiguous and of q's shape, type and device")
+    _call(lib().as_attention_prompt, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), _TYPES[q.dtype], t, heads,
+          k.shape[1], dim, q_token, k_token, v_token, offsets.data_ptr(), offsets.shape[0] - 1,
+          dim ** -0.5 if scale is None else scale, out.data_ptr())
+    return out
+
+
+@dataclasses.dataclass
+class PagePool:
+    """Free pages: a stack of page numbers, int32 [pages], of which the first
+    count[0] (int32 [1]) are free; the last one is taken first."""
+    stack: torch.Tensor
+    count: torch.Tensor
+
+    @staticmethod
+    def full(n_pages, device="cuda") -> "PagePool":
+        """All of n_pages pages, page 0 taken first."""
+        return PagePool(torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device),
+                        torch.full((1,), n_pages, dtype=torch.int32, device=device))
+
+
+@dataclasses.dataclass
+class Places:
+    """Where packed tokens go: offsets int32 [seqs + 1] (first row of every
+    sequence, and the number of rows), sequence and slot of every row (int32
+    [tokens]; -1 where a sequence was refused)."""
+    offsets: torch.Tensor
+    seq: torch.Tensor
+    slot: torch.Tensor
+
+
+def _pool_args(name, pool, page_table, length, other, other_types, new_length, new_count):
+    """Checks of what a pool's calls take: addresses of the stack, its
+    count, the table, the lengths, the other array and the new lengths and count."""
+    i32 = (torch.int32,)
+    dev = _need(page_table, "page_table", i32, 2).device
+    seqs = page_table.shape[0]
+    for what, x, types, n in (("stack", pool.stack, i32, pool.stack.numel()), ("count", pool.count, i32, 1),
+                              ("length", length, i32, seqs), (name[1], other, other_types, seqs),
+                              ("new_length", new_length, i32, seqs), ("new_count", new_count, i32, 1)):
+        if _need(x, f"{name[0]}: {what}", types, 1, dev).numel() != n:
+            _bad(f"{name[0]}: {what} has {x.numel()} numbers, not {n}")
+    return [x.data_ptr() for x in (pool.stack, pool.count, page_table, length, other, new_length, new_count)]
+
+
+def pages_reserve(pool: PagePool, page_table, page, length, add, n_tokens, new_length=None, new_count=None) -> Places:
+    """Pages for add[b] more tokens of every sequence b, which holds length[b]
+    (int32 [seqs]), and where the n_tokens packed rows go.  In order, sequences get
+    their pages as long as the pool has them for all up to them; a refused one
+    keeps its length.  `length` and the pool's count are brought up to date in
+    place, or left alone and written to `new_length` and `new_count` where given."""
+    new_length = length if new_length is None else new_length
+    new_count = pool.count if new_count is None else new_count
+    stack, count, table, held, more, after, left = _pool_args(("pages_reserve", "add"), pool, page_table, length, add,
+                                                              (torch.int32,), new_length, new_count)
+    dev, (seqs, max_pages) = page_table.device, page_table.shape
+    if not 0 <= n_tokens <= 1 << 30 or not 0 < page <= 4096:  # (ctypes passes the lowest 32 bits of others)
+        _bad(f"pages_reserve: {n_tokens} tokens, pages of {page} slots")
+    ints = torch.empty(seqs + 1 + 2 * n_tokens, dtype=torch.int32, device=dev)
+    offsets, seq, slot = ints[:seqs + 1], ints[seqs + 1:seqs + 1 + n_tokens], ints[seqs + 1 + n_tokens:]
+    L = lib()
+    need = L.as_pages_reserve_workspace(seqs)
+    _keep, ws = _workspace(need, dev)
+    _call(L.as_pages_reserve, dev, stack, count, pool.stack.numel(), table, seqs, max_pages, page, held, more,
+          n_tokens, left, after, offsets.data_ptr(), seq.data_ptr(), slot.data_ptr(), ws, need)
+    return Places(offsets, seq, slot)
+
+
+def pages_release(pool: PagePool, page_table, page, length, which, new_length=None, new_count=None):
+    """Give back the pages of the sequences that `which` marks (bool [seqs]);
+    their lengths become 0.  In place, or into `new_length` and `new_count`, as
+    for `pages_reserve`; the stack of free pages is written in either case."""
+    new_length = length if new_length is None else new_length
+    new_count = pool.count if new_count is None else new_count
+    stack, count, table, held, marks, after, left = _pool_args(("pages_release", "which"), pool, page_table, length,
+                                                               which, (torch.bool, torch.uint8), new_length, new_count)
+    if not 0 < page <= 4096:
+        _bad(f"pages_release: pages of {page} slots")
+    seqs, max_pages = page_table.shape
+    _call(lib().as_pages_release, page_table.device, stack, count, pool.stack.numel(), table, seqs, max_pages, page,
+          held, marks, left, after)
 
 
 # -------------------------------------------------------------------- cache
@@ -282,6 +493,33 @@ def cache_append(cache: Cache, k, v, start, first_pos=None, held=False):
         hv = torch.empty_like(hk)
     _call(lib().as_cache_append, k.device, cache._c, k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], k.shape[1],
           k.stride(0), k.stride(1), v.stride(0), v.stride(1), at, pos, hk.data_ptr() if held else None,
+          hv.data_ptr() if held else None)
+    return (hk, hv) if held else None
+
+
+def cache_append_packed(cache: Cache, k, v, seq, slot, pos=None, held=False):
+    """Put packed k, v [tokens, heads, dim] into slot slot[t] of sequence seq[t]
+    (int32 [tokens]; -1: passed over), as `pages_reserve` gives them: the tokens on
+    one block of 32 slots are neighbours, in order.  Positions are pos[t] (default:
+    slot).  With `held`, returns the values that the cache holds for them now (two
+    fp32 tensors of k's shape, not written for tokens passed over)."""
+    c = cache._c
+    dev = cache.k.device
+    if not (isinstance(k, torch.Tensor) and k.dtype in _16):
+        _bad("cache_append_packed: k in 16 bits is needed")
+    k, k_token = _packed(k, "k", k.dtype, dev, c.dim)
+    v, v_token = _packed(v, "v", k.dtype, dev, c.dim)
+    t = k.shape[0]
+    if k.shape != v.shape or k.shape[1] != c.n_heads:
+        _bad(f"cache_append_packed: k has {tuple(k.shape)}, v {tuple(v.shape)}, the cache {c.n_heads} heads")
+    for name, x in (("seq", seq), ("slot", slot), ("pos", pos)):
+        if x is not None and _need(x, name, (torch.int32,), 1, dev).numel() != t:
+            _bad(f"{name}: {x.numel()} numbers for {t} tokens")
+    hk = hv = None
+    if held:
+        hk, hv = (torch.empty(k.shape, dtype=torch.float32, device=dev) for _ in range(2))
+    _call(lib().as_cache_append_packed, dev, c, k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], t, k_token, v_token,
+          seq.data_ptr(), slot.data_ptr(), None if pos is None else pos.data_ptr(), hk.data_ptr() if held else None,
           hv.data_ptr() if held else None)
     return (hk, hv) if held else None
 
