@@ -217,10 +217,9 @@ int as_cache_append(const as_cache_t* cache, const void* k, const void* v, int32
 
 /*
  * Put packed tokens, of prompts and of single steps alike, where a slot map says:
- * token t goes to slot[t] of sequence seq[t] (as_pages_reserve gives both).  Tokens
- * whose sequence or slot does not exist (-1) are passed over.  The tokens that fall
- * on one block of 32 slots have to be neighbours, in the order of their slots; of
- * other blocks, and of a slot named twice, the contents are unspecified.
+ * token t goes to slot[t] of sequence seq[t] (as_pages_reserve gives both), in any
+ * order.  Tokens whose sequence or slot does not exist (-1) are passed over.  Of a
+ * slot that is named twice the contents are unspecified.
  *   k, v        [n_tokens][n_heads][dim] of `type`, last two dimensions contiguous,
  *               rows k_token and v_token elements apart
  *   seq, slot   [n_tokens]

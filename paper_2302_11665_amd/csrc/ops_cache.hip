@@ -62,14 +62,22 @@ struct Quantised {
   _Float16 step, base;
 };
 
+// Codes are those of (x - m) / d rounded to fp32: the quotient is taken with the
+// reciprocal and corrected once by its remainder, which leaves it 2^-46 of itself
+// off before the last rounding.  d has 11 bits, so no quotient is that near to the
+// middle between two fp32 numbers without being there, and the result is the
+// division's.  x - m is exact for 16-bit x and m of like size.  Adding 1.5 * 2^23
+// rounds to whole numbers, ties to even.
 template <int TYPE, int GROUP>
 __device__ __forceinline__ Quantised quantise8(const uint16_t* x, float* held) {
+  v4u raw;
+  __builtin_memcpy(&raw, x, 16);
   float f[8];
   float low = kInf, high = -kInf;
   bool bad = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    f[e] = to_f32<TYPE>(x[e]);
+    f[e] = to_f32<TYPE>(e & 1 ? raw[e >> 1] >> 16 : raw[e >> 1] & 0xffffu);
     bad |= f[e] != f[e];
     f[e] = fminf(fmaxf(f[e], -65504.0f), 65504.0f);
     low = fminf(low, f[e]);
@@ -86,15 +94,23 @@ __device__ __forceinline__ Quantised quantise8(const uint16_t* x, float* held) {
   z.base = any ? (_Float16)__builtin_nanf("") : (_Float16)low;
   z.step = any ? (_Float16)__builtin_nanf("") : (_Float16)((high - low) / 15.0f);
   const float m = (float)z.base, d = (float)z.step;
+  const bool some = d > 0.0f;  // (not NaN)
+  const float by = some ? 1.0f / d : 0.0f, from = some ? m : 0.0f, step = some ? d : 0.0f;
+  float out[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    // x - m is exact for 16-bit x and m of like size, so the quotient rounds
-    // as in exact arithmetic
-    const float q = rintf((f[e] - m) / d);
-    const uint32_t code = d > 0.0f ? (uint32_t)fminf(fmaxf(q, 0.0f), 15.0f) : 0u;
+    const float y = f[e] - from;
+    float q = y * by;
+    q = fmaf(fmaf(-q, step, y), by, q);
+    const float r = __builtin_amdgcn_fmed3f(q, 0.0f, 15.0f) + 12582912.0f;
+    const uint32_t code = __float_as_uint(r) & 15u;
     z.word |= code << nibble(e);
     z.bytes[e >> 2] |= code << (8 * (e & 3));
-    if (held) held[e] = (float)code * d + m;
+    out[e] = (r - 12582912.0f) * d + m;
+  }
+  if (held) {
+    __builtin_memcpy(held, out, 16);
+    __builtin_memcpy(held + 4, out + 4, 16);
   }
   return z;
 }
@@ -117,8 +133,11 @@ __device__ __forceinline__ void put8(const CacheArgs& c, int64_t row, int at, in
 }
 
 // Word w of a block of 32 slots of V from the codes of its slots lo..hi-1, where
-// slot s has the DIM codes of row s + shift; the other slots' bits stay.
-template <int DIM>
+// slot s has the DIM codes of row s + shift; the other slots' bits stay.  SHARED:
+// others may write those meanwhile.  The slots' own bits are nobody else's, so what
+// has to change in them is known from any state of the word, and is changed by one
+// atomic exclusive or, in whatever order.
+template <int DIM, bool SHARED>
 __device__ __forceinline__ void put_v_word(uint32_t* v, int w, const uint8_t* codes, int lo, int hi, int shift) {
   const int i = w % (DIM / 16), c = w / (DIM / 16) % 16, g = w / DIM;
   uint32_t mask = 0, word = 0;
@@ -132,6 +151,8 @@ __device__ __forceinline__ void put_v_word(uint32_t* v, int w, const uint8_t* co
   }
   if (mask == 0xffffffffu)
     v[w] = word;
+  else if (mask && SHARED)
+    atomicXor(&v[w], (v[w] ^ word) & mask);
   else if (mask)
     v[w] = (v[w] & ~mask) | word;
 }
@@ -177,7 +198,7 @@ __global__ __launch_bounds__(256) void append(AppendArgs p) {
   __syncthreads();
   uint32_t* v = p.c.v + (row * p.c.page + in_page) * kWords;
   for (int w = threadIdx.x; w < 32 * kWords; w += 256)
-    put_v_word<DIM>(v, w, reinterpret_cast<const uint8_t*>(v_codes), lo, hi, 0);
+    put_v_word<DIM, false>(v, w, reinterpret_cast<const uint8_t*>(v_codes), lo, hi, 0);
 }
 
 template <int TYPE>
@@ -198,66 +219,78 @@ struct PackedArgs {
   int64_t k_token, v_token;
   const int32_t *seq, *slot, *pos;
   float *held_k, *held_v;
-  int32_t n_tokens;
+  int32_t n_tokens, tile;  // tile: tokens whose runs a workgroup takes, at most 32
 };
-
-constexpr int kPackedTile = 32;  // tokens whose runs a workgroup takes
 
 // One workgroup per (tile of packed tokens, head).  Neighbouring tokens of one
 // sequence on neighbouring slots of one block of 32 are a run; a workgroup takes
-// the runs that begin in its tile, whole, so that no other one has their words
-// of V as long as no two tokens have the same slot and a block's new tokens are
-// neighbours.
+// the runs that begin in its tile, whole, so that most words of V are written
+// without being read.  First all of its tokens are quantised side by side, then V's words
+// are written, a quarter of a run's block (the words of 8 of its slots) to a
+// wavefront at a time.
 template <int TYPE, int DIM, int GROUP>
 __global__ __launch_bounds__(256) void append_packed(PackedArgs p) {
-  constexpr int kLanes = DIM / 8, kWords = DIM / 8;
-  __shared__ v2u v_codes[32][kLanes];
-  const int h = blockIdx.y, wide = threadIdx.x & 63;
-  const int64_t t0 = (int64_t)blockIdx.x * kPackedTile;
-  // every wavefront looks at the tile's tokens and as many behind them
+  constexpr int kLanes = DIM / 8, kWords = DIM / 8, kAtOnce = 256 / kLanes;
+  __shared__ v2u v_codes[64][kLanes];  // of the tile's tokens and as many behind them
+  __shared__ int64_t rows[64];         // page and head of each, -1: none
+  __shared__ int32_t places[64];       // in the page
+  const int h = blockIdx.y, wide = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t t0 = (int64_t)blockIdx.x * p.tile;
+  // every wavefront looks at the tile's tokens and those behind them
   const int64_t t = t0 + wide;
   int seq = -1, slot = -1;
   if (t < p.n_tokens) seq = p.seq[t], slot = p.slot[t];
+  int before = __shfl_up(seq, 1), slot_before = __shfl_up(slot, 1);
+  if (wide == 0 && t > 0 && t < p.n_tokens) before = p.seq[t - 1], slot_before = p.slot[t - 1];
   const bool real = (unsigned)seq < (unsigned)p.c.n_seqs && slot >= 0;
-  bool follows = false;  // the token before, in its run
-  if (real && t > 0 && slot % 32 != 0) follows = p.seq[t - 1] == seq && p.slot[t - 1] == slot - 1;
-  const uint64_t in_run = __ballot(follows);
-  uint64_t begins = __ballot(real && !follows) & ((uint64_t(1) << kPackedTile) - 1);
-  const int lane = threadIdx.x % kLanes;
-  while (begins) {
-    const int at0 = __builtin_ctzll(begins);
-    begins &= begins - 1;
-    // tokens of the run: at most 32, so that the bits end before the 64 do
-    const int n = 1 + (int)__builtin_ctzll(~(in_run >> (at0 + 1)));
-    const int b = __builtin_amdgcn_readlane(seq, at0), first = __builtin_amdgcn_readlane(slot, at0);
-    const int64_t row = cache_row(p.c, b, h, first / p.c.page);
+  const bool follows = real && t > 0 && slot % 32 != 0 && before == seq && slot_before == slot - 1;
+  const uint64_t in_run = __ballot(follows), tile = (uint64_t(1) << p.tile) - 1;
+  uint64_t begins = __ballot(real && !follows) & tile;
+  if (!begins) return;
+  // from its first beginning on, the tile's tokens are its own, and behind the
+  // tile those that go on with its last run (at most 31)
+  const uint64_t own_from = ~uint64_t(0) << __builtin_ctzll(begins);
+  uint64_t own = __ballot(real) & tile & own_from;
+  if (own >> (p.tile - 1) & 1) own |= ((uint64_t(1) << __builtin_ctzll(~(in_run >> p.tile))) - 1) << p.tile;
+  if (wave == 0) {
+    const bool mine = own >> wide & 1;
+    rows[wide] = mine ? cache_row(p.c, seq, h, slot / p.c.page) : -1;
+    places[wide] = slot % p.c.page;
+  }
+  __syncthreads();
+  const int lane = threadIdx.x % kLanes, last = 63 - __builtin_clzll(own);
+  for (int i = __builtin_ctzll(own) + threadIdx.x / kLanes; i <= last; i += kAtOnce) {
+    const int64_t row = rows[i], u = t0 + i;
     if (row < 0) continue;
-    const int in_page = first % p.c.page, lo = in_page % 32;
-    __syncthreads();  // the run before is written
-    for (int j = threadIdx.x / kLanes; j < 2 * n; j += 256 / kLanes) {
-      const bool is_v = j >= n;
-      const int i = is_v ? j - n : j;
-      const int64_t u = t0 + at0 + i;
-      const uint16_t* x = (is_v ? p.v + u * p.v_token : p.k + u * p.k_token) + (int64_t)h * DIM + lane * 8;
-      float* held = is_v ? p.held_v : p.held_k;
-      if (held) held += (u * p.c.n_heads + h) * DIM + lane * 8;
-      const int at = in_page + i;
-      put8<DIM, GROUP>(p.c, row, at, lane, is_v, quantise8<TYPE, GROUP>(x, held), v_codes[i]);
-      if (is_v && lane == 0) {
-        if (p.c.pos) p.c.pos[row * p.c.page + at] = p.pos ? p.pos[u] : first + i;
-        if (p.c.acc) p.c.acc[row * p.c.page + at] = 0.0f;
-      }
+    const int at = places[i];
+    const int64_t from = (int64_t)h * DIM + lane * 8, held = (u * p.c.n_heads + h) * DIM + lane * 8;
+    const Quantised k = quantise8<TYPE, GROUP>(p.k + u * p.k_token + from, p.held_k ? p.held_k + held : nullptr);
+    const Quantised v = quantise8<TYPE, GROUP>(p.v + u * p.v_token + from, p.held_v ? p.held_v + held : nullptr);
+    put8<DIM, GROUP>(p.c, row, at, lane, false, k, nullptr);
+    put8<DIM, GROUP>(p.c, row, at, lane, true, v, v_codes[i]);
+    if (lane == 0) {
+      if (p.c.pos) p.c.pos[row * p.c.page + at] = p.pos ? p.pos[u] : p.slot[u];
+      if (p.c.acc) p.c.acc[row * p.c.page + at] = 0.0f;
     }
-    __syncthreads();
-    uint32_t* v = p.c.v + (row * p.c.page + in_page - lo) * kWords;
-    for (int w = threadIdx.x; w < 32 * kWords; w += 256)
-      put_v_word<DIM>(v, w, reinterpret_cast<const uint8_t*>(v_codes), lo, lo + n, -lo);
+  }
+  __syncthreads();
+  const uint8_t* codes = reinterpret_cast<const uint8_t*>(v_codes);
+  for (; begins; begins &= begins - 1) {
+    const int i = __builtin_ctzll(begins);
+    const int n = 1 + (i < 63 ? (int)__builtin_ctzll(~(in_run >> (i + 1))) : 0);  // at most 32
+    const int64_t row = rows[i];
+    const int at = places[i], lo = at % 32;
+    const uint32_t slots = (n < 32 ? (1u << n) - 1 : ~0u) << lo;
+    if (row < 0 || !(slots & 0x000f000fu << (4 * wave))) continue;  // slots 4 wave.. and 16 + 4 wave..
+    uint32_t* v = p.c.v + (row * p.c.page + at - lo) * kWords;
+#pragma unroll
+    for (int w = 0; w < DIM; w += 64) put_v_word<DIM, true>(v, wave * DIM + w + wide, codes, lo, lo + n, i - lo);
   }
 }
 
 template <int TYPE>
 void launch_packed(const PackedArgs& p, hipStream_t s) {
-  const dim3 g((unsigned)((p.n_tokens + kPackedTile - 1) / kPackedTile), (unsigned)p.c.n_heads), t(256);
+  const dim3 g((unsigned)((p.n_tokens + p.tile - 1) / p.tile), (unsigned)p.c.n_heads), t(256);
   if (p.c.dim == 64 && p.c.group == 32) hipLaunchKernelGGL((append_packed<TYPE, 64, 32>), g, t, 0, s, p);
   if (p.c.dim == 64 && p.c.group == 64) hipLaunchKernelGGL((append_packed<TYPE, 64, 64>), g, t, 0, s, p);
   if (p.c.dim == 128 && p.c.group == 32) hipLaunchKernelGGL((append_packed<TYPE, 128, 32>), g, t, 0, s, p);
@@ -600,8 +633,12 @@ int as_cache_append_packed(const as_cache_t* cache, const void* k, const void* v
                 (long long)n_tokens, cache->n_heads);
   if (n_tokens == 0 || cache->n_seqs == 0) return as_host::ok();
   if (!k || !v || !seq || !slot) return fail(AS_E_INVALID_ARG, "cache_append_packed: null pointer");
-  const PackedArgs p{cache_args(cache), reinterpret_cast<const uint16_t*>(k), reinterpret_cast<const uint16_t*>(v),
-                     k_token, v_token, seq, slot, pos, held_k, held_v, (int32_t)n_tokens};
+  PackedArgs p{cache_args(cache), reinterpret_cast<const uint16_t*>(k), reinterpret_cast<const uint16_t*>(v),
+               k_token, v_token, seq, slot, pos, held_k, held_v, (int32_t)n_tokens, 4};
+  // single tokens are a run each: few of them to a workgroup as long as all of
+  // them run at once (8 to a compute unit)
+  while (p.tile < 32 && (n_tokens + p.tile - 1) / p.tile * cache->n_heads > 8 * (int64_t)as_host::compute_units())
+    p.tile *= 2;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (type == AS_BF16)
     launch_packed<AS_BF16>(p, s);

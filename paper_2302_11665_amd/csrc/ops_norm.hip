@@ -29,10 +29,13 @@ __device__ __forceinline__ void read16(const uint16_t* row, int c, int n, v4u (&
   if (c + 16 <= n) {
     __builtin_memcpy(&w[0], row + c, 16);
     __builtin_memcpy(&w[1], row + c + 8, 16);
-  } else {
+  } else if (c < n) {  // all loads at once: one latency, not one after the other
+    uint16_t u[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) u[e] = row[min(c + e, n - 1)];
 #pragma unroll
     for (int e = 0; e < 16; ++e)
-      if (c + e < n) w[e >> 3][(e >> 1) & 3] |= (uint32_t)row[c + e] << (16 * (e & 1));
+      w[e >> 3][(e >> 1) & 3] |= (uint32_t)(c + e < n ? u[e] : 0) << (16 * (e & 1));
   }
 }
 
@@ -75,7 +78,9 @@ __device__ __forceinline__ void gain16(const float* gain, int c, int n, float (&
     for (int i = 0; i < 4; ++i) __builtin_memcpy(g + 4 * i, gain + c + 4 * i, 16);
   } else {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) g[e] = c + e < n ? gain[c + e] : 0.0f;
+    for (int e = 0; e < 16; ++e) g[e] = gain[min(c + e, n - 1)];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) g[e] = c + e < n ? g[e] : 0.0f;
   }
 }
 
@@ -91,44 +96,78 @@ __device__ __forceinline__ float norm_scale(float top, bool finite, double squar
 // in 64 bits (16-bit values reach 3e38 in bf16, whose square does not).
 __device__ __forceinline__ bool fp32_holds(float squares) { return squares > 0x1p-60f && squares < 0x1p120f; }
 
-// One workgroup per row, 16 columns to a thread and chunk.  Latency bounds a few
-// rows.
-template <int TYPE, bool GAIN, int THREADS, int CHUNKS>
-__global__ __launch_bounds__(THREADS) void norm_rows(NormArgs p) {
-  constexpr int kWaves = THREADS / 64;
-  __shared__ uint32_t tops[kWaves];
-  __shared__ float sums[kWaves];
-  __shared__ double wide[kWaves];
+// Largest magnitude and sum of squares of 16 columns' t and h.
+template <bool GAIN>
+__device__ __forceinline__ void measure16(const float (&f)[16], const float (&g)[16], uint32_t& top, float& squares) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    squares = fmaf(f[e], f[e], squares);
+    top = max(top, magnitude(GAIN ? f[e] * g[e] : f[e]));
+  }
+}
+
+// Codes of 16 columns from their h (two to a word); f: their t.
+template <int TYPE, bool GAIN>
+__device__ __forceinline__ v4u codes16(const NormArgs& p, const Quantiser<GAIN ? AS_F32 : TYPE>& quantiser,
+                                       const v4u (&w)[2], int c) {
+  float f[16], g[16];
+  unpack16<TYPE>(w, f);
+  if (GAIN) {
+    gain16(p.gain, c, p.n_cols, g);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) f[e] *= g[e];
+  }
+  return v4u{quantiser.codes4(f), quantiser.codes4(f + 4), quantiser.codes4(f + 8), quantiser.codes4(f + 12)};
+}
+
+// The values that 16 codes stand for.
+__device__ __forceinline__ void hold16(float* row, int c, int n, const v4u& q, float scale) {
+  float v[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] = (float)(int8_t)(q[e >> 2] >> (8 * (e & 3))) * scale;
+  if (c + 16 <= n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) __builtin_memcpy(row + c + 4 * i, v + 4 * i, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (c + e < n) row[c + e] = v[e];
+  }
+}
+
+// One workgroup per row, 16 columns to a thread (KEEP), which stay in registers;
+// rows of more than those are gone over twice, the second time from the caches.
+// Latency bounds a few rows.
+template <int TYPE, bool GAIN, bool KEEP>
+__global__ __launch_bounds__(1024) void norm_rows(NormArgs p) {
+  constexpr int kStep = KEEP ? 1 << 30 : 1024 * 16;
+  __shared__ uint32_t tops[16];
+  __shared__ float sums[16];
+  __shared__ double wide[16];
+  const int waves = blockDim.x >> 6;
   __shared__ float row_scale;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, padded = p.k_tiles * 64;
   const int64_t r = blockIdx.x;
   const uint16_t* x = p.x + r * p.x_stride;
-  v4u w[CHUNKS][2];
-#pragma unroll
-  for (int i = 0; i < CHUNKS; ++i) read16(x, (i * THREADS + tid) * 16, p.n_cols, w[i]);
-  if (p.residual) {
-    const uint16_t* add = p.residual + r * p.residual_stride;
-#pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
-      v4u b[2];
-      read16(add, (i * THREADS + tid) * 16, p.n_cols, b);
-      add16<TYPE>(w[i], b);
-    }
-#pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) write16(p.sum + r * p.sum_stride, (i * THREADS + tid) * 16, p.n_cols, w[i]);
-  }
+  const uint16_t* add = p.residual ? p.residual + r * p.residual_stride : nullptr;
+  uint16_t* sum = p.sum + r * p.sum_stride;
+  const uint16_t* h = add ? sum : x;  // what is read again
   uint32_t top = 0;
   float squares = 0.0f;
-#pragma unroll
-  for (int i = 0; i < CHUNKS; ++i) {
+  v4u kept[2];
+  for (int c = tid * 16; c < padded; c += kStep) {
+    v4u w[2], b[2];
     float f[16], g[16];
-    unpack16<TYPE>(w[i], f);
-    if (GAIN) gain16(p.gain, (i * THREADS + tid) * 16, p.n_cols, g);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      squares = fmaf(f[e], f[e], squares);
-      top = max(top, magnitude(GAIN ? f[e] * g[e] : f[e]));
+    read16(x, c, p.n_cols, w);
+    if (add) read16(add, c, p.n_cols, b);
+    if (GAIN) gain16(p.gain, c, p.n_cols, g);
+    if (add) {
+      add16<TYPE>(w, b);
+      write16(sum, c, p.n_cols, w);
     }
+    unpack16<TYPE>(w, f);
+    measure16<GAIN>(f, g, top, squares);
+    kept[0] = w[0], kept[1] = w[1];
   }
 #pragma unroll
   for (int o = 32; o; o >>= 1) {
@@ -138,8 +177,7 @@ __global__ __launch_bounds__(THREADS) void norm_rows(NormArgs p) {
   if (lane == 0) tops[wave] = top, sums[wave] = squares;
   __syncthreads();
   squares = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
+  for (int i = 0; i < waves; ++i) {
     top = max(top, tops[i]);
     squares += sums[i];
   }
@@ -147,10 +185,11 @@ __global__ __launch_bounds__(THREADS) void norm_rows(NormArgs p) {
   double total = squares;
   if (finite && top != 0 && !fp32_holds(squares)) {
     double d = 0.0;
-#pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
+    for (int c = tid * 16; c < padded; c += kStep) {
+      v4u w[2] = {kept[0], kept[1]};
       float f[16];
-      unpack16<TYPE>(w[i], f);
+      if (!KEEP) read16(h, c, p.n_cols, w);
+      unpack16<TYPE>(w, f);
 #pragma unroll
       for (int e = 0; e < 16; ++e) d += (double)f[e] * f[e];
     }
@@ -159,8 +198,7 @@ __global__ __launch_bounds__(THREADS) void norm_rows(NormArgs p) {
     if (lane == 0) wide[wave] = d;
     __syncthreads();
     total = 0.0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) total += wide[i];
+    for (int i = 0; i < waves; ++i) total += wide[i];
   }
   if (tid == 0) {
     row_scale = norm_scale(__uint_as_float(top), finite, total, p.n_cols, p.eps);
@@ -169,41 +207,128 @@ __global__ __launch_bounds__(THREADS) void norm_rows(NormArgs p) {
   if (p.held) __syncthreads();
   const Quantiser<GAIN ? AS_F32 : TYPE> quantiser(__uint_as_float(top), finite);
   uint8_t* out = p.codes + (r >> 4) * p.k_tiles * 1024 + (r & 15) * 16;
+  for (int c = tid * 16; c < padded; c += kStep) {
+    v4u w[2] = {kept[0], kept[1]};
+    if (!KEEP) read16(h, c, p.n_cols, w);
+    const v4u q = codes16<TYPE, GAIN>(p, quantiser, w, c);
+    *reinterpret_cast<v4u*>(out + (int64_t)(c >> 4) * 256) = q;
+    if (p.held) hold16(p.held + r * p.n_cols, c, p.n_cols, q, row_scale);
+  }
+}
+
+// Many rows: a workgroup of as many wavefronts as the columns need, up to 8, per
+// two rows, a lane of which has 16 columns of one row, TIMES over, in registers.
+// Rows are read once, and codes written 32 bytes side by side.
+constexpr int kNormRows = 2, kNormWaves = 8;
+
+template <int TYPE, bool GAIN, int TIMES>
+__global__ __launch_bounds__(64 * kNormWaves) void norm_pairs(NormArgs p) {
+  constexpr int kWide = 16 * 64 / kNormRows;  // columns of a wavefront
+  __shared__ uint32_t tops[kNormWaves][kNormRows];
+  __shared__ float sums[kNormWaves][kNormRows];
+  __shared__ double wide[kNormWaves][kNormRows];
+  __shared__ float scales[kNormRows];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in = lane % kNormRows, waves = blockDim.x >> 6;
+  const int64_t r = (int64_t)blockIdx.x * kNormRows + in;
+  const bool there = r < p.n_tokens;
+  const int64_t row = there ? r : p.n_tokens - 1;
+  const uint16_t* x = p.x + row * p.x_stride;
+  auto column = [&](int i) { return (i * waves + wave) * kWide + lane / kNormRows * 16; };
+  v4u w[TIMES][2];
 #pragma unroll
-  for (int i = 0; i < CHUNKS; ++i) {
-    const int c = (i * THREADS + tid) * 16;
-    if (c >= p.k_tiles * 64) break;
+  for (int i = 0; i < TIMES; ++i) read16(x, column(i), p.n_cols, w[i]);
+  if (p.residual) {
+    const uint16_t* add = p.residual + row * p.residual_stride;
+#pragma unroll
+    for (int i = 0; i < TIMES; ++i) {
+      v4u b[2];
+      read16(add, column(i), p.n_cols, b);
+      add16<TYPE>(w[i], b);
+    }
+    // (rows behind the last one do its work, which may be over before they read)
+    if (there) {
+#pragma unroll
+      for (int i = 0; i < TIMES; ++i) write16(p.sum + row * p.sum_stride, column(i), p.n_cols, w[i]);
+    }
+  }
+  uint32_t top = 0;
+  float squares = 0.0f;
+#pragma unroll
+  for (int i = 0; i < TIMES; ++i) {
     float f[16], g[16];
     unpack16<TYPE>(w[i], f);
-    if (GAIN) {
-      gain16(p.gain, c, p.n_cols, g);
+    if (GAIN) gain16(p.gain, column(i), p.n_cols, g);
+    measure16<GAIN>(f, g, top, squares);
+  }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) f[e] *= g[e];
+  for (int o = kNormRows; o < 64; o <<= 1) {
+    top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    squares += __shfl_xor(squares, o);
+  }
+  if (lane < kNormRows) tops[wave][in] = top, sums[wave][in] = squares;
+  __syncthreads();
+  squares = 0.0f;
+  for (int i = 0; i < waves; ++i) {
+    top = max(top, tops[i][in]);
+    squares += sums[i][in];
+  }
+  const bool finite = top < 0x7f800000u;
+  double total = squares;
+  const bool again = finite && top != 0 && !fp32_holds(squares);
+  if (__syncthreads_or(again)) {
+    double d = 0.0;
+#pragma unroll
+    for (int i = 0; i < TIMES; ++i) {
+      float f[16];
+      unpack16<TYPE>(w[i], f);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) d += (double)f[e] * f[e];
     }
-    const v4u q = {quantiser.codes4(f), quantiser.codes4(f + 4), quantiser.codes4(f + 8), quantiser.codes4(f + 12)};
+#pragma unroll
+    for (int o = kNormRows; o < 64; o <<= 1) d += __shfl_xor(d, o);
+    if (lane < kNormRows) wide[wave][in] = d;
+    __syncthreads();
+    if (again) {
+      total = 0.0;
+      for (int i = 0; i < waves; ++i) total += wide[i][in];
+    }
+  }
+  if (threadIdx.x < kNormRows) {
+    scales[in] = norm_scale(__uint_as_float(top), finite, total, p.n_cols, p.eps);
+    if (there) p.scale[r] = scales[in];
+  }
+  if (p.held) __syncthreads();
+  const Quantiser<GAIN ? AS_F32 : TYPE> quantiser(__uint_as_float(top), finite);
+  // (rows behind the last one are in its tile's storage)
+  uint8_t* out = p.codes + (r >> 4) * p.k_tiles * 1024 + (r & 15) * 16;
+#pragma unroll
+  for (int i = 0; i < TIMES; ++i) {
+    const int c = column(i);
+    if (c >= p.k_tiles * 64) break;
+    const v4u q = codes16<TYPE, GAIN>(p, quantiser, w[i], c);
     *reinterpret_cast<v4u*>(out + (int64_t)(c >> 4) * 256) = q;
-    if (p.held) {
-      float* held = p.held + r * p.n_cols + c;
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (c + e < p.n_cols) held[e] = (float)(int8_t)(q[e >> 2] >> (8 * (e & 3))) * row_scale;
-    }
+    if (p.held && there) hold16(p.held + r * p.n_cols, c, p.n_cols, q, scales[in]);
   }
 }
 
 template <int TYPE, bool GAIN>
 void launch_norm(const NormArgs& p, hipStream_t s) {
-  auto rows = [&](auto kernel, int threads) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)p.n_tokens), dim3(threads), 0, s, p);
+  auto launch = [&](auto kernel, int64_t groups, int threads) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), 0, s, p);
   };
-  if (p.n_cols <= 4096)
-    rows(norm_rows<TYPE, GAIN, 256, 1>, 256);
-  else if (p.n_cols <= 16384)
-    rows(norm_rows<TYPE, GAIN, 1024, 1>, 1024);
-  else if (p.n_cols <= 32768)
-    rows(norm_rows<TYPE, GAIN, 1024, 2>, 1024);
+  constexpr int kOnce = 16 * 64 / kNormRows;  // columns of a wavefront at a time
+  if (p.n_tokens >= 2 * as_host::compute_units() && p.n_cols <= 4 * kOnce * kNormWaves) {
+    const int times = p.n_cols <= kOnce * kNormWaves ? 1 : p.n_cols <= 2 * kOnce * kNormWaves ? 2 : 4;
+    const int threads = (p.n_cols + times * kOnce - 1) / (times * kOnce) * 64;
+    const int64_t groups = (p.n_tokens + kNormRows - 1) / kNormRows;
+    if (times == 1) return launch(norm_pairs<TYPE, GAIN, 1>, groups, threads);
+    if (times == 2) return launch(norm_pairs<TYPE, GAIN, 2>, groups, threads);
+    return launch(norm_pairs<TYPE, GAIN, 4>, groups, threads);
+  }
+  if (p.n_cols <= 16384)
+    launch(norm_rows<TYPE, GAIN, true>, p.n_tokens, (int)round_up((p.n_cols + 15) / 16, 64));
   else
-    rows(norm_rows<TYPE, GAIN, 1024, 8>, 1024);
+    launch(norm_rows<TYPE, GAIN, false>, p.n_tokens, 1024);
 }
 
 // Whether rows of n elements of 16 bits from a share memory with those from b

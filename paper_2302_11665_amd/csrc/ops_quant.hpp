@@ -67,20 +67,19 @@ struct Quantiser {
   // 2^-46 of itself before the last rounding, so a quotient that ties between
   // two codes comes out exactly, and no other one can reach a tie (the nearest
   // is 2^-19 away).  The codes are therefore those of exact arithmetic.  fp32
-  // values are divided.  Adding 1.5 * 2^23 rounds to whole numbers, ties to
-  // even, and leaves the code in the low byte.
+  // values are corrected twice: the first time leaves the quotient less than a unit
+  // in its last place off, and then a correction with a reciprocal that is rounded
+  // to nearest gives the quotient rounded to nearest (Markstein's theorem), in half
+  // the instructions of a division.  Adding 1.5 * 2^23 rounds to whole numbers,
+  // ties to even, and leaves the code in the low byte.
   __device__ __forceinline__ uint32_t codes4(const float* f) const {
     uint32_t u[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float x = f[i] * by;
-      float q;
-      if (TYPE == AS_F32) {
-        q = x / top;
-      } else {
-        q = x * inv;
-        q = fmaf(fmaf(-q, top, x), inv, q);
-      }
+      float q = x * inv;
+      q = fmaf(fmaf(-q, top, x), inv, q);
+      if (TYPE == AS_F32) q = fmaf(fmaf(-q, top, x), inv, q);
       u[i] = __float_as_uint(q + 12582912.0f);
     }
     const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(u[3], u[2], 0x04000c0cu);

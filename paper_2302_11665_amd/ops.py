@@ -499,9 +499,8 @@ def cache_append(cache: Cache, k, v, start, first_pos=None, held=False):
 
 def cache_append_packed(cache: Cache, k, v, seq, slot, pos=None, held=False):
     """Put packed k, v [tokens, heads, dim] into slot slot[t] of sequence seq[t]
-    (int32 [tokens]; -1: passed over), as `pages_reserve` gives them: the tokens on
-    one block of 32 slots are neighbours, in order.  Positions are pos[t] (default:
-    slot).  With `held`, returns the values that the cache holds for them now (two
+    (int32 [tokens]; -1: passed over), as `pages_reserve` gives them.  Positions are
+    pos[t] (default: slot).  With `held`, returns the values that the cache holds for them now (two
     fp32 tensors of k's shape, not written for tokens passed over)."""
     c = cache._c
     dev = cache.k.device

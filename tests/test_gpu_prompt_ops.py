@@ -558,6 +558,22 @@ def test_packed_append_passes_over():
     ops.cache_append_packed(c, k[:0], v[:0], ints([]), ints([]))
 
 
+@pytest.mark.parametrize("dim,t", [(64, 500), (128, 3000)])
+def test_packed_append_in_any_order(dim, t):
+    """Tokens of a few blocks dealt out over all workgroups."""
+    g = gen(t)
+    heads = 2
+    a = make_cache(g, [t, t], heads, dim, 64, 64)
+    k, v = normal(g, 2 * t, heads, dim, dtype=F16), normal(g, 2 * t, heads, dim, dtype=F16)
+    seq, slot = (ints(x) for x in packed_places([0, 0], [t, t]))
+    b = ops.Cache(*(x.clone() for x in (a.k, a.v, a.k_par, a.v_par, a.pos, a.acc, a.page_table)))
+    ops.cache_append_packed(a, k, v, seq, slot)
+    order = torch.randperm(2 * t, device="cuda", generator=g)
+    ops.cache_append_packed(b, k[order], v[order], seq[order], slot[order])
+    for x, z in zip((a.k, a.v, a.pos, a.acc, a.k_par, a.v_par), (b.k, b.v, b.pos, b.acc, b.k_par, b.v_par)):
+        assert torch.equal(x, z)
+
+
 @pytest.mark.parametrize("dim,group,page,starts,t", [(64, 32, 32, [0, 5, 64], 300), (128, 64, 96, [31, 0, 7], 90)])
 def test_packed_append_is_an_append(dim, group, page, starts, t):
     """Every sequence's tokens packed one after the other, and given side by side."""
