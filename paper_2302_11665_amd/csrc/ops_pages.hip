@@ -42,7 +42,7 @@ struct ReserveArgs {
 __device__ __forceinline__ int64_t pages_of(int64_t tokens, int page) { return (tokens + page - 1) / page; }
 
 // What every sequence needs and gets, in their order.  One workgroup.
-__device__ __forceinline__ void reserve_scan(const ReserveArgs& p) {
+__device__ __forceinline__ void reserve_scan(const ReserveArgs& p, int32_t* offsets, int32_t* base) {
   __shared__ int64_t waves[kPageWaves];
   __shared__ int32_t taken;
   const int tid = threadIdx.x;
@@ -63,40 +63,41 @@ __device__ __forceinline__ void reserve_scan(const ReserveArgs& p) {
     pages += total;
     const bool fits = (add == 0 || room) && (need == 0 || upto <= count);
     if (there) {
-      p.offsets[b] = (int32_t)min(at, (int64_t)p.n_tokens);
+      offsets[b] = (int32_t)min(at, (int64_t)p.n_tokens);
       p.new_length[b] = (int32_t)(fits ? length + add : length);
-      p.base[b] = fits ? (int32_t)(count - 1 - (upto - need)) : kRefused;
+      base[b] = fits ? (int32_t)(count - 1 - (upto - need)) : kRefused;
       if (fits && need) atomicMax(&taken, (int32_t)upto);
     }
   }
   __syncthreads();
   if (tid == 0) {
-    p.offsets[p.n_seqs] = (int32_t)min(tokens, (int64_t)p.n_tokens);
+    offsets[p.n_seqs] = (int32_t)min(tokens, (int64_t)p.n_tokens);
     p.new_count[0] = (int32_t)count - taken;
   }
 }
 
 // A packed token's sequence and slot; the token that begins a page writes it into
 // the table.
-__device__ __forceinline__ void reserve_fill(const ReserveArgs& p, int t) {
+__device__ __forceinline__ void reserve_fill(const ReserveArgs& p, const int32_t* offsets, const int32_t* base, int t) {
   int32_t seq = -1, slot = -1;
-  if (t < p.offsets[p.n_seqs]) {
+  if (t < offsets[p.n_seqs]) {
     int lo = 0, hi = p.n_seqs - 1;  // the first sequence that ends behind t
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (p.offsets[mid + 1] > t)
+      if (offsets[mid + 1] > t)
         hi = mid;
       else
         lo = mid + 1;
     }
-    if (p.base[lo] != kRefused) {
-      const int begin = p.offsets[lo], end = p.offsets[lo + 1];
+    const int from = base[lo];
+    if (from != kRefused) {
+      const int begin = offsets[lo], end = offsets[lo + 1];
       const int length = p.new_length[lo] - (end - begin);
       seq = lo;
       slot = length + (t - begin);
       if (slot % p.page == 0) {
         const int index = slot / p.page;
-        p.table[(int64_t)lo * p.max_pages + index] = p.stack[p.base[lo] - (index - (int)pages_of(length, p.page))];
+        p.table[(int64_t)lo * p.max_pages + index] = p.stack[from - (index - (int)pages_of(length, p.page))];
       }
     }
   }
@@ -104,11 +105,24 @@ __device__ __forceinline__ void reserve_fill(const ReserveArgs& p, int t) {
   p.slot[t] = slot;
 }
 
-__global__ __launch_bounds__(kPageThreads) void reserve_sequences(ReserveArgs p) { reserve_scan(p); }
+__global__ __launch_bounds__(kPageThreads) void reserve_sequences(ReserveArgs p) {
+  reserve_scan(p, p.offsets, p.base);
+}
 
 __global__ __launch_bounds__(256) void reserve_tokens(ReserveArgs p) {
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t < p.n_tokens) reserve_fill(p, (int)t);
+  if (t < p.n_tokens) reserve_fill(p, p.offsets, p.base, (int)t);
+}
+
+// Few sequences and tokens: both in one launch, what lies between in LDS.
+constexpr int kOnceSeqs = kPageThreads, kOnceTokens = 8 * kPageThreads;
+
+__global__ __launch_bounds__(kPageThreads) void reserve_once(ReserveArgs p) {
+  __shared__ int32_t offsets[kOnceSeqs + 1], base[kOnceSeqs];
+  reserve_scan(p, offsets, base);
+  __syncthreads();
+  for (int b = threadIdx.x; b <= p.n_seqs; b += kPageThreads) p.offsets[b] = offsets[b];
+  for (int t = threadIdx.x; t < p.n_tokens; t += kPageThreads) reserve_fill(p, offsets, base, t);
 }
 
 struct ReleaseArgs {
@@ -196,6 +210,10 @@ int as_pages_reserve(const int32_t* stack, const int32_t* count, int32_t n_pages
                       reinterpret_cast<int32_t*>(workspace),
                       n_pages, n_seqs, max_pages, page, (int32_t)n_tokens};
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (n_seqs <= kOnceSeqs && n_tokens <= kOnceTokens) {
+    hipLaunchKernelGGL(reserve_once, dim3(1), dim3(kPageThreads), 0, s, p);
+    return launched("pages_reserve");
+  }
   hipLaunchKernelGGL(reserve_sequences, dim3(1), dim3(kPageThreads), 0, s, p);
   if (n_tokens) hipLaunchKernelGGL(reserve_tokens, dim3((unsigned)((n_tokens + 255) / 256)), dim3(256), 0, s, p);
   return launched("pages_reserve");

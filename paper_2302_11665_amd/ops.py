@@ -184,7 +184,7 @@ def norm_i8(x, residual=None, gain=None, eps=1e-6, out=None, held=False):
         if residual.shape != x.shape:
             _bad(f"norm_i8: x has {tuple(x.shape)}, the residual {tuple(residual.shape)}")
         r2, r_stride = _rows(residual if x.dim() == 2 else residual.reshape(-1, cols))
-        s = torch.empty((t, cols), dtype=x.dtype, device=dev) if out is None else _need(
+        s = torch.empty_like(x2, memory_format=torch.contiguous_format) if out is None else _need(
             out, "out", (x.dtype,), 2, dev, contiguous=False)
         s_stride = s.stride(0) if t > 1 else cols
         if tuple(s.shape) != (t, cols) or (cols > 1 and s.stride(1) != 1) or s_stride < cols:
@@ -300,7 +300,7 @@ def attention_prompt(q, k, v, offsets, scale=None, out=None):
     k, k_token = _aligned_rows(k, k_token)
     v, v_token = _aligned_rows(v, v_token)
     if out is None:
-        out = torch.empty((t, heads, dim), dtype=q.dtype, device=dev)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.shape == q.shape and out.device == dev
               and out.is_contiguous()):
         _bad("attention_prompt: out is contiguous and of q's shape, type and device")
@@ -335,17 +335,26 @@ class Places:
 
 
 def _pool_args(name, pool, page_table, length, other, other_types, new_length, new_count):
-    """Checks of what a pool's calls take: addresses of the stack, its
-    count, the table, the lengths, the other array and the new lengths and count."""
-    i32 = (torch.int32,)
-    dev = _need(page_table, "page_table", i32, 2).device
-    seqs = page_table.shape[0]
-    for what, x, types, n in (("stack", pool.stack, i32, pool.stack.numel()), ("count", pool.count, i32, 1),
-                              ("length", length, i32, seqs), (name[1], other, other_types, seqs),
-                              ("new_length", new_length, i32, seqs), ("new_count", new_count, i32, 1)):
-        if _need(x, f"{name[0]}: {what}", types, 1, dev).numel() != n:
-            _bad(f"{name[0]}: {what} has {x.numel()} numbers, not {n}")
-    return [x.data_ptr() for x in (pool.stack, pool.count, page_table, length, other, new_length, new_count)]
+    """Checks of what a pool's calls take: addresses of the stack, its count, the
+    table, the lengths, the other array and the new lengths and count."""
+    stack, count, i32, one = pool.stack, pool.count, torch.int32, (1,)
+    try:
+        dev, row = page_table.device, page_table.shape[:1]
+        fine = (page_table.is_cuda and page_table.dim() == 2 and len(stack.shape) == 1
+                and page_table.dtype is stack.dtype is count.dtype is length.dtype is i32
+                and new_length.dtype is new_count.dtype is i32 and other.dtype in other_types
+                and count.shape == new_count.shape == one and length.shape == other.shape == new_length.shape == row
+                and stack.device == count.device == length.device == other.device == dev
+                and new_length.device == new_count.device == dev and page_table.is_contiguous()
+                and stack.is_contiguous() and length.is_contiguous() and other.is_contiguous()
+                and new_length.is_contiguous())
+    except AttributeError:
+        fine = False
+    if not fine:
+        what = [(tuple(x.shape), x.dtype, str(x.device)) if isinstance(x, torch.Tensor) else type(x)
+                for x in (stack, count, page_table, length, other, new_length, new_count)]
+        _bad(f"{name}: contiguous CUDA arrays of one pool and its sequences are needed, not {what}")
+    return [x.data_ptr() for x in (stack, count, page_table, length, other, new_length, new_count)]
 
 
 def pages_reserve(pool: PagePool, page_table, page, length, add, n_tokens, new_length=None, new_count=None) -> Places:
@@ -356,19 +365,21 @@ def pages_reserve(pool: PagePool, page_table, page, length, add, n_tokens, new_l
     place, or left alone and written to `new_length` and `new_count` where given."""
     new_length = length if new_length is None else new_length
     new_count = pool.count if new_count is None else new_count
-    stack, count, table, held, more, after, left = _pool_args(("pages_reserve", "add"), pool, page_table, length, add,
-                                                              (torch.int32,), new_length, new_count)
+    stack, count, table, held, more, after, left = _pool_args("pages_reserve", pool, page_table, length, add, (torch.int32,),
+                                                              new_length, new_count)
     dev, (seqs, max_pages) = page_table.device, page_table.shape
     if not 0 <= n_tokens <= 1 << 30 or not 0 < page <= 4096:  # (ctypes passes the lowest 32 bits of others)
         _bad(f"pages_reserve: {n_tokens} tokens, pages of {page} slots")
-    ints = torch.empty(seqs + 1 + 2 * n_tokens, dtype=torch.int32, device=dev)
-    offsets, seq, slot = ints[:seqs + 1], ints[seqs + 1:seqs + 1 + n_tokens], ints[seqs + 1 + n_tokens:]
     L = lib()
+    # one allocation: scratch memory, then the three results
     need = L.as_pages_reserve_workspace(seqs)
-    _keep, ws = _workspace(need, dev)
+    ints = torch.empty(need // 4 + seqs + 1 + 2 * n_tokens, dtype=torch.int32, device=dev)
+    at = ints.data_ptr()
+    first = at + need
+    seq = first + 4 * (seqs + 1)
     _call(L.as_pages_reserve, dev, stack, count, pool.stack.numel(), table, seqs, max_pages, page, held, more,
-          n_tokens, left, after, offsets.data_ptr(), seq.data_ptr(), slot.data_ptr(), ws, need)
-    return Places(offsets, seq, slot)
+          n_tokens, left, after, first, seq, seq + 4 * n_tokens, at, need)
+    return Places(*ints.split_with_sizes((need // 4, seqs + 1, n_tokens, n_tokens))[1:])
 
 
 def pages_release(pool: PagePool, page_table, page, length, which, new_length=None, new_count=None):
@@ -377,8 +388,8 @@ def pages_release(pool: PagePool, page_table, page, length, which, new_length=No
     for `pages_reserve`; the stack of free pages is written in either case."""
     new_length = length if new_length is None else new_length
     new_count = pool.count if new_count is None else new_count
-    stack, count, table, held, marks, after, left = _pool_args(("pages_release", "which"), pool, page_table, length,
-                                                               which, (torch.bool, torch.uint8), new_length, new_count)
+    stack, count, table, held, marks, after, left = _pool_args("pages_release", pool, page_table, length, which,
+                                                               (torch.bool, torch.uint8), new_length, new_count)
     if not 0 < page <= 4096:
         _bad(f"pages_release: pages of {page} slots")
     seqs, max_pages = page_table.shape
