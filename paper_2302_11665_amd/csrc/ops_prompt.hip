@@ -129,30 +129,27 @@ constexpr uint16_t kInfinity = TYPE == AS_BF16 ? 0x7f80 : 0x7c00;
 // the heads of their group, queries in order) over the keys that they see, 64 at
 // a time, which come into two stages of LDS straight from memory.
 //
-// Masked scores give p = 0, but 0 times an infinity or NaN in V is NaN.  A
-// workgroup whose results are all finite met none; otherwise it does its work
-// again, CAREFUL: at keys that some of its rows do not see, values that are not
-// finite are left out of the product and reach the rows that see them by products
-// of their marks with a mask.
-template <int TYPE, int DIM, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void prompt_attention(PromptArgs p) {
+// Masked scores give p = 0, but 0 times an infinity or NaN in V is NaN.  A block
+// whose results are all finite met none; otherwise (false is returned, and nothing
+// written) it is done again, CAREFUL: at keys that some of its rows do not see,
+// values that are not finite are left out of the product and reach the rows that see
+// them by products of their marks with a mask.
+template <int TYPE, int DIM, int WAVES, bool CAREFUL>
+__device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)[2][kKeys * DIM * 2], int head, int begin,
+                                             int length, int block) {
   constexpr int kRows = 32 * WAVES, kRowBytes = DIM * 2, kTile = kKeys * kRowBytes;
   constexpr int kLoads = kTile / 1024 / WAVES;  // of K and of V, by a wavefront, a stage
   constexpr int kPieces = kRowBytes / 16, kPerLoad = 1024 / kRowBytes;  // keys of a load
   constexpr int kSteps = DIM / 16, kDimTiles = DIM / 32;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][kTile];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
-  const int head = blockIdx.x % p.n_heads;
-  int seq, block;
-  if (!find_block<kRows>(p, blockIdx.x / p.n_heads, seq, block)) return;
-  int begin, length;
-  sequence(p, seq, begin, length);
   const int rows = length * p.group, row0 = block * kRows + wave * 32;
   // rows behind the last one do its work again
   const int row = min(row0 + col, rows - 1), pos = row / p.group, member = row - pos * p.group;
-  const int first = min(row0, rows - 1) / p.group, last = min(row0 + 31, rows - 1) / p.group;  // queries
-  const bool busy = row0 < rows;
+  // tiles that all rows of the block see whole, that this wavefront's rows see, and
+  // that any row does
+  const int open = (block * kRows / p.group + 1) / kKeys;
+  const int mine = min(row0 + 31, rows - 1) / p.group / kKeys + 1;
   const int tiles = min(block * kRows + kRows - 1, rows - 1) / p.group / kKeys + 1;
 
   v8s q[kSteps];
@@ -162,142 +159,204 @@ __global__ __launch_bounds__(64 * WAVES, 2) void prompt_attention(PromptArgs p) 
     for (int i = 0; i < kSteps; ++i) q[i] = *reinterpret_cast<const v8s*>(at + i * 16);
   }
 
+  // Stages come in by loads of 1 KiB, kPerLoad keys each, of which the wavefront
+  // brings every WAVES-th.  A lane has the same piece of all of its keys, so its
+  // place is one offset from an address that is the wavefront's.
+  const int in_load = wave * kPerLoad + lane / kPieces, piece = (lane % kPieces) ^ swizzle<DIM>(in_load);
+  const uint32_t k_lane = (uint32_t)(lane / kPieces * (int)p.k_token * 2 + piece * 16);
+  const uint32_t v_lane = (uint32_t)(lane / kPieces * (int)p.v_token * 2 + piece * 16);
   const uint8_t* k0 = reinterpret_cast<const uint8_t*>(p.k + (int64_t)begin * p.k_token + (int64_t)head * DIM);
   const uint8_t* v0 = reinterpret_cast<const uint8_t*>(p.v + (int64_t)begin * p.v_token + (int64_t)head * DIM);
-  // a lane's key and piece in the wavefront's loads: keys (wave + j WAVES) kPerLoad + lane / kPieces
-  auto bring = [&](int slot, int tile) {
+  auto bring = [&](uint8_t* to, const uint8_t* from, int64_t token, uint32_t offset, int tile) {
+    auto load = [&](int j, const uint8_t* at) {
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)at,
+                                       (__attribute__((address_space(3))) void*)(to + (wave + j * WAVES) * 1024), 16, 0,
+                                       0);
+    };
+    const int key = tile * kKeys + wave * kPerLoad;  // of the first lane and load
+    if ((tile + 1) * kKeys <= length) {
+      const uint8_t* at = from + (int64_t)key * token * 2;
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const int in = (wave + j * WAVES) * kPerLoad + lane / kPieces;
-      const int piece = (lane % kPieces) ^ swizzle<DIM>(in);
-      const int64_t key = min(tile * kKeys + in, length - 1);
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(k0 + key * p.k_token * 2 + piece * 16),
-          (__attribute__((address_space(3))) void*)(lds[slot][0] + (wave + j * WAVES) * 1024), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(v0 + key * p.v_token * 2 + piece * 16),
-          (__attribute__((address_space(3))) void*)(lds[slot][1] + (wave + j * WAVES) * 1024), 16, 0, 0);
+      for (int j = 0; j < kLoads; ++j) load(j, at + j * (int64_t)(WAVES * kPerLoad) * token * 2 + offset);
+    } else {  // keys behind the last one are it again: masked, and no other sequence's
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+        load(j, from + (int64_t)min(key + j * WAVES * kPerLoad + lane / kPieces, length - 1) * token * 2 + piece * 16);
     }
   };
+  auto bring_k = [&](int tile) { bring(lds[tile & 1][0], k0, p.k_token, k_lane, tile); };
+  auto bring_v = [&](int tile) { bring(lds[tile & 1][1], v0, p.v_token, v_lane, tile); };
 
   v16f o[kDimTiles];
   float reference, total;  // of the exponents; sum of this lane's keys' p
 
-  auto work = [&](auto careful) {
-    constexpr bool kCareful = decltype(careful)::value;
+  // Places of the operands: the pieces' order changes by exclusive ors of bits that
+  // nothing else in an address has, so a lane's places follow from one.
+  const uint32_t k_place = col * kRowBytes + ((half ^ swizzle<DIM>(col)) << 4);
+  const int v_key = half * 4 + (lane & 15) / 4;
+  const uint32_t v_place = v_key * kRowBytes + (((lane >> 4 & 1) * 2 + (lane >> 1 & 1) ^ swizzle<DIM>(v_key)) << 4) + (lane & 1) * 8;
+  auto scores = [&](int tile, v16f (&s)[2]) {
+    const uint32_t at = (uint32_t)(tile & 1) * (2 * kTile) + k_place;
 #pragma unroll
-    for (int i = 0; i < kDimTiles; ++i) o[i] = v16f{};
-    reference = -1e30f, total = 0.0f;
-    bring(0, 0);
-    for (int tile = 0; tile < tiles; ++tile) {
-      wait_loads<0>();
-      __syncthreads();  // this stage is there, and all are done with the other
-      if (tile + 1 < tiles) bring((tile + 1) & 1, tile + 1);
-      const int key0 = tile * kKeys;
-      if (!busy || key0 > last) continue;
-      const uint8_t* kt = lds[tile & 1][0];
-      const uint8_t* vt = lds[tile & 1][1];
-      v16f s[2];
+    for (int h = 0; h < 2; ++h) s[h] = v16f{};
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        s[h] = v16f{};
-        const int key = h * 32 + col;
+    for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-          const int piece = (i * 2 + half) ^ swizzle<DIM>(key);
-          s[h] = multiply<TYPE>(*reinterpret_cast<const v8s*>(kt + key * kRowBytes + piece * 16), q[i], s[h]);
-        }
+      for (int h = 0; h < 2; ++h)  // keys 32 h.., channels 16 i..
+        s[h] = multiply<TYPE>(*reinterpret_cast<const v8s*>(lds[0][0] + (at ^ 32 * i) + h * 32 * kRowBytes), q[i], s[h]);
+  };
+  // The reference of a query's exponents follows its maximum when it is passed by 2^8.
+  auto follow = [&](const v16f (&s)[2]) {
+    float top = s[0][0];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[h][r]);
+    top = max_halves(top) * p.factor;
+    if (__any(top > reference + 8.0f)) {
+      const float now = top > reference + 8.0f ? top : reference, by = __builtin_amdgcn_exp2f(reference - now);
+      reference = now;
+      total *= by;
+#pragma unroll
+      for (int i = 0; i < kDimTiles; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] *= by;
+    }
+  };
+  auto weigh = [&](const v16f (&s)[2], v8s (&weights)[4]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[h][r], p.factor, -reference));
+        total += e;
+        weights[h * 2 + (r >> 3)][r & 7] = (short)from_f32<TYPE>(e);
       }
-      const bool masked = key0 + kKeys - 1 > first;
-      if (masked) {
+  };
+  // V's operand: channels 32 i.. of keys 16 z..
+  auto values = [&](int tile, int i, int z) {
+    const uint32_t at = (uint32_t)(tile & 1) * (2 * kTile) + v_place;
+    v8s v;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+    for (int j = 0; j < 2; ++j) {
+      const v4s four = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) v4s*)(lds[0][1] + (at ^ (64 * i | 32 * j)) + (z * 16 + j * 8) * kRowBytes));
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (key0 + h * 32 + 8 * (r >> 2) + 4 * half + (r & 3) > pos) s[h][r] = -kInf;
+      for (int e = 0; e < 4; ++e) v[j * 4 + e] = four[e];
+    }
+    return v;
+  };
+  auto add = [&](int tile, const v8s (&weights)[4]) {
+#pragma unroll
+    for (int z = 0; z < 4; ++z)
+#pragma unroll
+      for (int i = 0; i < kDimTiles; ++i) o[i] = multiply<TYPE>(values(tile, i, z), weights[z], o[i]);
+  };
+  // The same where some rows do not see some keys and values may not be finite.
+  auto add_careful = [&](int tile, const v8s (&weights)[4]) {
+#pragma unroll
+    for (int i = 0; i < kDimTiles; ++i) {
+      v16f nan = {}, plus = {}, minus = {};
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        v8s v = values(tile, i, z), is_nan, is_plus, is_minus, seen;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint16_t u = (uint16_t)v[e];
+          const bool bad = not_finite<TYPE>(u);
+          is_plus[e] = (short)(u == kInfinity<TYPE> ? kOne<TYPE> : 0);
+          is_minus[e] = (short)(u == (kInfinity<TYPE> | 0x8000) ? kOne<TYPE> : 0);
+          is_nan[e] = (short)(bad && !is_plus[e] && !is_minus[e] ? kOne<TYPE> : 0);
+          v[e] = bad ? (short)0 : v[e];
+          const int key = tile * kKeys + z * 16 + 8 * (e >> 2) + 4 * half + (e & 3);
+          seen[e] = (short)(key <= pos ? kOne<TYPE> : 0);
+        }
+        nan = multiply<TYPE>(is_nan, seen, nan);
+        plus = multiply<TYPE>(is_plus, seen, plus);
+        minus = multiply<TYPE>(is_minus, seen, minus);
+        o[i] = multiply<TYPE>(v, weights[z], o[i]);
       }
-      float top = s[0][0];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[h][r]);
-      top = max_halves(top) * p.factor;
-      // a query's reference follows its maximum when it is passed by 2^8
-      if (__any(top > reference + 8.0f)) {
-        const float now = top > reference + 8.0f ? top : reference, by = __builtin_amdgcn_exp2f(reference - now);
-        reference = now;
-        total *= by;
-#pragma unroll
-        for (int i = 0; i < kDimTiles; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[i][r] *= by;
-      }
-      v8s weights[4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float e = __builtin_amdgcn_exp2f(fmaf(s[h][r], p.factor, -reference));
-          total += e;
-          weights[h * 2 + (r >> 3)][r & 7] = (short)from_f32<TYPE>(e);
-        }
-#pragma unroll
-      for (int i = 0; i < kDimTiles; ++i) {
-        v16f nan = {}, plus = {}, minus = {};
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          v8s v;
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int key = z * 16 + j * 8 + half * 4 + (lane & 15) / 4;
-            const int byte = i * 64 + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
-            const int at = key * kRowBytes + (((byte >> 4) ^ swizzle<DIM>(key)) << 4) + (byte & 8);
-            const v4s four = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(vt + at));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[j * 4 + e] = four[e];
-          }
-          if (kCareful && masked) {
-            v8s is_nan, is_plus, is_minus, seen;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const uint16_t u = (uint16_t)v[e];
-              const bool bad = not_finite<TYPE>(u);
-              is_plus[e] = (short)(u == kInfinity<TYPE> ? kOne<TYPE> : 0);
-              is_minus[e] = (short)(u == (kInfinity<TYPE> | 0x8000) ? kOne<TYPE> : 0);
-              is_nan[e] = (short)(bad && !is_plus[e] && !is_minus[e] ? kOne<TYPE> : 0);
-              v[e] = bad ? (short)0 : v[e];
-              const int key = key0 + z * 16 + 8 * (e >> 2) + 4 * half + (e & 3);
-              seen[e] = (short)(key <= pos ? kOne<TYPE> : 0);
-            }
-            nan = multiply<TYPE>(is_nan, seen, nan);
-            plus = multiply<TYPE>(is_plus, seen, plus);
-            minus = multiply<TYPE>(is_minus, seen, minus);
-          }
-          o[i] = multiply<TYPE>(v, weights[z], o[i]);
-        }
-        if (kCareful && masked) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            if (plus[r] > 0.0f) o[i][r] += kInf;
-            if (minus[r] > 0.0f) o[i][r] -= kInf;
-            if (nan[r] > 0.0f) o[i][r] = __builtin_nanf("");
-          }
-        }
+      for (int r = 0; r < 16; ++r) {
+        if (plus[r] > 0.0f) o[i][r] += kInf;
+        if (minus[r] > 0.0f) o[i][r] -= kInf;
+        if (nan[r] > 0.0f) o[i][r] = __builtin_nanf("");
       }
     }
-    total = sum_halves(total);
   };
 
-  work(std::false_type{});
-  bool fine = true;
-  if (busy) {
+#pragma unroll
+  for (int i = 0; i < kDimTiles; ++i) o[i] = v16f{};
+  reference = -1e30f, total = 0.0f;
+  bring_k(0);
+  bring_v(0);
+  if (tiles > 1) bring_k(1);
+  // V of a tile and K of the next are there, all are done with those before, and
+  // the ones behind are on their way
+  auto turn = [&](int tile) {
+    wait_loads<0>();
+    __syncthreads();
+    if (tile + 1 < tiles) bring_v(tile + 1);
+    if (tile + 2 < tiles) bring_k(tile + 2);
+  };
+  v16f s[2], next[2];
+  v8s weights[4];
+  int tile = 0;
+  if (tiles > 1)
+    wait_loads<2 * kLoads>();
+  else
+    wait_loads<kLoads>();
+  __syncthreads();  // K of the first tile is there
+  scores(0, s);
+  turn(0);
+  // A wavefront makes the scores of a tile while it turns the last one's into
+  // weights, so that its matrix and vector instructions overlap.
+  auto step = [&](v16f (&now)[2], v16f (&then)[2]) {
+    follow(now);
+    scores(tile + 1, then);  // (behind the last tile: of what lies in LDS, and not used)
+    weigh(now, weights);
+    add(tile, weights);
+    if (++tile < tiles) turn(tile);
+  };
+  if (!CAREFUL) {
+    while (tile + 1 < open) {
+      step(s, next);
+      step(next, s);
+    }
+    if (tile < open) {
+      step(s, next);
+      s[0] = next[0], s[1] = next[1];
+    }
+  }
+  // the tiles that some rows do not see whole, or not at all
+  while (tile < tiles) {
+    if (tile < mine) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (tile * kKeys + h * 32 + 8 * (r >> 2) + 4 * half + (r & 3) > pos) s[h][r] = -kInf;
+      follow(s);
+      weigh(s, weights);
+      if (CAREFUL && tile >= open)
+        add_careful(tile, weights);
+      else
+        add(tile, weights);
+      if (tile + 1 < mine) scores(tile + 1, s);
+    }
+    if (++tile < tiles) turn(tile);
+  }
+  total = sum_halves(total);
+
+  if (!CAREFUL) {
+    bool fine = true;
 #pragma unroll
     for (int i = 0; i < kDimTiles; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) fine &= fabsf(o[i][r]) < kInf;
+    if (__syncthreads_or(!fine)) return false;
   }
-  if (__syncthreads_or(!fine)) work(std::true_type{});
-  if (row0 + col >= rows) return;
+  if (row0 + col >= rows) return true;
   uint16_t* to = p.out + ((int64_t)(begin + pos) * p.n_heads * p.group + head * p.group + member) * DIM;
   const float by = 1.0f / total;
 #pragma unroll
@@ -308,6 +367,25 @@ __global__ __launch_bounds__(64 * WAVES, 2) void prompt_attention(PromptArgs p) 
       const uint32_t hi = from_f32<TYPE>(o[i][r + 2] * by) | (uint32_t)from_f32<TYPE>(o[i][r + 3] * by) << 16;
       *reinterpret_cast<v2u*>(to + i * 32 + 2 * r + 4 * half) = v2u{lo, hi};
     }
+  return true;
+}
+
+// (a function of its own: what it keeps in registers costs the ordinary case none)
+template <int TYPE, int DIM, int WAVES>
+__device__ __attribute__((noinline)) void attend_block_again(PromptArgs p, uint8_t (*lds)[2][kKeys * DIM * 2],
+                                                             int head, int begin, int length, int block) {
+  attend_block<TYPE, DIM, WAVES, true>(p, lds, head, begin, length, block);
+}
+
+template <int TYPE, int DIM, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void prompt_attention(PromptArgs p) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][kKeys * DIM * 2];  // of two tiles: K, V
+  const int head = blockIdx.x % p.n_heads;
+  int seq, block, begin, length;
+  if (!find_block<32 * WAVES>(p, blockIdx.x / p.n_heads, seq, block)) return;
+  sequence(p, seq, begin, length);
+  if (!attend_block<TYPE, DIM, WAVES, false>(p, lds, head, begin, length, block))
+    attend_block_again<TYPE, DIM, WAVES>(p, lds, head, begin, length, block);
 }
 
 constexpr int kPromptWaves = 4;
