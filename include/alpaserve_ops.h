@@ -144,16 +144,18 @@ int as_norm_i8(const void* x, const void* residual, int32_t type, int64_t n_toke
  *            apart from the others; rows of no sequence are not written
  * What a token may not see does not reach it, an infinity or NaN included.
  * Invalid offsets give unspecified results, never an access outside the arrays.
- * At most 2^26 tokens, 2^30 rows of queries, 2^20 sequences, 4096 query heads, and
- * 2^24 blocks of 128 rows of a key/value head's queries (each sequence's last one
- * may be a part).
+ * At most 2^26 tokens, 2^30 rows of queries, 2^20 sequences, 4096 query heads, keys
+ * and values 2^26 elements apart, and 2^24 blocks of 128 rows of a key/value head's
+ * queries (each sequence's last one may be a part).
  * Products of 16-bit numbers with fp32 sums, softmax in fp32; p is rounded to the
  * type for its product with v (half a unit in its last place each, as the output),
  * not for its sum.
  */
+int64_t as_attention_prompt_workspace(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_seqs);
 int as_attention_prompt(const void* q, const void* k, const void* v, int32_t type, int64_t n_tokens, int32_t n_q_heads,
                         int32_t n_kv_heads, int32_t dim, int64_t q_token, int64_t k_token, int64_t v_token,
-                        const int32_t* offsets, int32_t n_seqs, float scale, void* out, void* stream);
+                        const int32_t* offsets, int32_t n_seqs, float scale, void* out, void* workspace,
+                        int64_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------- cache --
  * Keys and values of 4 bits in pages shared by all sequences of a batch.  Slot

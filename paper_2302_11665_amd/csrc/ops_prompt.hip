@@ -49,39 +49,44 @@ __device__ __forceinline__ float sum_halves(float x) {
   return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
-// A sequence's tokens, clipped to those that there are.
-__device__ __forceinline__ void sequence(const PromptArgs& p, int b, int& begin, int& length) {
-  begin = min(max(p.offsets[b], 0), p.n_tokens);
-  length = min(max(p.offsets[b + 1], begin), p.n_tokens) - begin;
+// A sequence's tokens, clipped to those that there are, and its blocks of ROWS rows
+// (a row: one query of one head of the group).
+struct Sequence {
+  int begin, length;
+};
+__device__ __forceinline__ Sequence sequence(const PromptArgs& p, int b) {
+  const int begin = min(max(p.offsets[b], 0), p.n_tokens);
+  return {begin, min(max(p.offsets[b + 1], begin), p.n_tokens) - begin};
+}
+template <int ROWS>
+__device__ __forceinline__ int blocks_of(const PromptArgs& p, int length) {
+  return (int)((uint32_t)(length * p.group + ROWS - 1) / ROWS);
 }
 
-// Blocks of ROWS rows (a row: one query of one head of the group).
-template <int ROWS>
-__device__ __forceinline__ int blocks_of(const PromptArgs& p, int b) {
-  int begin, length;
-  sequence(p, b, begin, length);
-  return (int)(((int64_t)length * p.group + ROWS - 1) / ROWS);
-}
+// What a workgroup works on: a block of a sequence.
+struct Item {
+  int begin, length, block, none;
+};
 
 __device__ __forceinline__ uint32_t sum_lanes(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_readlane((int)scan_lanes(x), 63);
 }
 
-// The item-th block of all sequences, those with the most keys first: blocks
-// begin at their sequence's first token, so the j-th of every sequence has as
-// much work, and items are in order of falling j, then of sequences.  False
-// where there are fewer items.  A wavefront's work: lanes count for a sequence
-// each, and j is found by halving.
+// The item-th block of at most 64 sequences, those with the most keys first:
+// blocks begin at their sequence's first token, so the j-th of every sequence has
+// as much work, and items are in order of falling j, then of sequences.  False where
+// there are fewer items.  A wavefront's work: a lane to a sequence, and j is found
+// by halving.
 template <int ROWS>
-__device__ __forceinline__ bool find_block(const PromptArgs& p, uint32_t item, int& seq, int& block) {
+__device__ __forceinline__ bool find_block(const PromptArgs& p, uint32_t item, Item& found) {
   const int lane = threadIdx.x & 63;
-  auto beyond = [&](int j) {  // items of blocks j and later
-    uint32_t n = 0;
-    for (int b = lane; b < p.n_seqs; b += 64) n += (uint32_t)max(0, blocks_of<ROWS>(p, b) - j);
-    return sum_lanes(n);
-  };
+  Sequence s{0, 0};
+  if (lane < p.n_seqs) s = sequence(p, lane);
+  const int blocks = blocks_of<ROWS>(p, s.length);
+  auto beyond = [&](int j) { return sum_lanes((uint32_t)max(0, blocks - j)); };  // items of blocks j and later
   if (beyond(0) <= item) return false;
-  int lo = 0, hi = (int)(((int64_t)p.n_tokens * p.group + ROWS - 1) / ROWS);  // beyond(lo) > item >= beyond(hi)
+  int lo = 0, hi = 1;  // beyond(lo) > item >= beyond(hi)
+  while (beyond(hi) > item) lo = hi, hi *= 2;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (beyond(mid) > item)
@@ -89,20 +94,62 @@ __device__ __forceinline__ bool find_block(const PromptArgs& p, uint32_t item, i
     else
       hi = mid;
   }
-  block = lo;
-  uint32_t rank = item - beyond(lo + 1);  // among the sequences that have this block
-  for (int first = 0; first < p.n_seqs; first += 64) {
-    const int b = first + lane;
-    const uint64_t have = __ballot(b < p.n_seqs && blocks_of<ROWS>(p, min(b, p.n_seqs - 1)) > lo);
-    const uint32_t n = (uint32_t)__popcll(have);
-    if (rank < n) {
-      const uint64_t mine = __ballot((have >> lane & 1) && (uint32_t)__popcll(have & ((uint64_t(1) << lane) - 1)) == rank);
-      seq = first + __ffsll((unsigned long long)mine) - 1;
-      return true;
-    }
-    rank -= n;
+  const uint32_t rank = item - beyond(lo + 1);  // among the sequences that have this block
+  const uint64_t have = __ballot(blocks > lo);
+  const bool here = (have >> lane & 1) && (uint32_t)__popcll(have & ((uint64_t(1) << lane) - 1)) == rank;
+  const int at = __builtin_ctzll(__ballot(here));
+  found = Item{__builtin_amdgcn_readlane(s.begin, at), __builtin_amdgcn_readlane(s.length, at), lo, 0};
+  return true;
+}
+
+// The same for many sequences, once for all workgroups: the blocks of all
+// sequences, listed by classes of their numbers of blocks (four to a power of two),
+// the largest first, and within a sequence the last one first.  One workgroup: the
+// classes are counted, then every sequence takes its place in its class (in no
+// certain order, which changes nothing but when a block is worked on), then wavefronts write
+// the sequences' blocks.
+constexpr int kPlanThreads = 1024;
+
+template <int ROWS>
+__global__ __launch_bounds__(kPlanThreads) void prompt_plan(PromptArgs p, Item* items, int n_items) {
+  __shared__ uint32_t classes[128];
+  __shared__ Item part[kPlanThreads];  // block: how many; none: the first one's place
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto class_of = [](int blocks) { return 127 - min(127, (int)(__float_as_uint((float)blocks) >> 21) - (127 << 2)); };
+  if (tid < 128) classes[tid] = 0;
+  __syncthreads();
+  for (int b = tid; b < p.n_seqs; b += kPlanThreads) {
+    const int blocks = blocks_of<ROWS>(p, sequence(p, b).length);
+    if (blocks) atomicAdd(&classes[class_of(blocks)], (uint32_t)blocks);
   }
-  return false;
+  __syncthreads();
+  if (wave == 0) {  // where every class begins
+    const uint32_t a = classes[2 * lane], z = classes[2 * lane + 1], upto = scan_lanes(a + z);
+    classes[2 * lane] = upto - a - z;
+    classes[2 * lane + 1] = upto - z;
+    if (lane == 63) part[0].none = (int)upto;
+  }
+  __syncthreads();
+  for (int i = max(0, part[0].none) + tid; i < n_items; i += kPlanThreads) items[i] = Item{0, 0, 0, 1};
+  __syncthreads();
+  for (int first = 0; first < p.n_seqs; first += kPlanThreads) {
+    Item mine{0, 0, 0, 0};
+    if (first + tid < p.n_seqs) {
+      const Sequence s = sequence(p, first + tid);
+      const int blocks = blocks_of<ROWS>(p, s.length);
+      mine = Item{s.begin, s.length, blocks, blocks ? (int)atomicAdd(&classes[class_of(blocks)], (uint32_t)blocks) : 0};
+    }
+    part[tid] = mine;
+    __syncthreads();
+    for (int i = wave; i < min(kPlanThreads, p.n_seqs - first); i += kPlanThreads / 64) {
+      const Item s = part[i];
+      for (int j = lane; j < s.block; j += 64) {  // (offsets that make no sense may give more blocks than items)
+        const int64_t at = (int64_t)(uint32_t)s.none + j;
+        if (at < n_items) items[at] = Item{s.begin, s.length, s.block - 1 - j, 0};
+      }
+    }
+    __syncthreads();
+  }
 }
 
 constexpr int kKeys = 64;  // keys of a stage
@@ -377,39 +424,57 @@ __device__ __attribute__((noinline)) void attend_block_again(PromptArgs p, uint8
   attend_block<TYPE, DIM, WAVES, true>(p, lds, head, begin, length, block);
 }
 
-template <int TYPE, int DIM, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void prompt_attention(PromptArgs p) {
+template <int TYPE, int DIM, int WAVES, bool PLAN>
+__global__ __launch_bounds__(64 * WAVES, 2) void prompt_attention(PromptArgs p, const Item* items) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][kKeys * DIM * 2];  // of two tiles: K, V
-  const int head = blockIdx.x % p.n_heads;
-  int seq, block, begin, length;
-  if (!find_block<32 * WAVES>(p, blockIdx.x / p.n_heads, seq, block)) return;
-  sequence(p, seq, begin, length);
-  if (!attend_block<TYPE, DIM, WAVES, false>(p, lds, head, begin, length, block))
-    attend_block_again<TYPE, DIM, WAVES>(p, lds, head, begin, length, block);
+  const int head = blockIdx.x % p.n_heads, at = blockIdx.x / p.n_heads;
+  Item item;
+  if (PLAN) {
+    item = items[at];
+    if (item.none) return;
+  } else if (!find_block<32 * WAVES>(p, at, item)) {
+    return;
+  }
+  if (!attend_block<TYPE, DIM, WAVES, false>(p, lds, head, item.begin, item.length, item.block))
+    attend_block_again<TYPE, DIM, WAVES>(p, lds, head, item.begin, item.length, item.block);
 }
 
 constexpr int kPromptWaves = 4;
 
-// Workgroups that there can be at most: a part block for each sequence.
-int64_t prompt_groups(int64_t n_tokens, int64_t n_seqs, int64_t n_heads, int64_t group) {
-  return (n_tokens * group / (32 * kPromptWaves) + std::min(n_seqs, n_tokens * group)) * n_heads;
+// Blocks that there can be at most: a part of one for each sequence.
+int64_t prompt_items(int64_t n_tokens, int64_t n_seqs, int64_t group) {
+  return n_tokens * group / (32 * kPromptWaves) + std::min(n_seqs, n_tokens);
 }
 
-template <int TYPE>
-void launch_prompt(const PromptArgs& p, int dim, hipStream_t s) {
-  const dim3 g((unsigned)prompt_groups(p.n_tokens, p.n_seqs, p.n_heads, p.group)), t(64 * kPromptWaves);
-  if (dim == 64) hipLaunchKernelGGL((prompt_attention<TYPE, 64, kPromptWaves>), g, t, 0, s, p);
-  if (dim == 128) hipLaunchKernelGGL((prompt_attention<TYPE, 128, kPromptWaves>), g, t, 0, s, p);
+bool prompt_planned(int64_t n_seqs) { return n_seqs > 64; }
+
+template <int TYPE, int DIM>
+void launch_prompt(const PromptArgs& p, Item* items, hipStream_t s) {
+  const int n = (int)prompt_items(p.n_tokens, p.n_seqs, p.group);
+  const dim3 g((unsigned)(n * p.n_heads)), t(64 * kPromptWaves);
+  if (prompt_planned(p.n_seqs)) {
+    hipLaunchKernelGGL((prompt_plan<32 * kPromptWaves>), dim3(1), dim3(kPlanThreads), 0, s, p, items, n);
+    hipLaunchKernelGGL((prompt_attention<TYPE, DIM, kPromptWaves, true>), g, t, 0, s, p, items);
+  } else {
+    hipLaunchKernelGGL((prompt_attention<TYPE, DIM, kPromptWaves, false>), g, t, 0, s, p, nullptr);
+  }
 }
 
 }  // namespace as_ops
 
 using namespace as_ops;
 
-extern "C" int as_attention_prompt(const void* q, const void* k, const void* v, int32_t type, int64_t n_tokens,
-                                   int32_t n_q_heads, int32_t n_kv_heads, int32_t dim, int64_t q_token, int64_t k_token,
-                                   int64_t v_token, const int32_t* offsets, int32_t n_seqs, float scale, void* out,
-                                   void* stream) {
+extern "C" {
+
+int64_t as_attention_prompt_workspace(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_seqs) {
+  if (n_tokens < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || !prompt_planned(n_seqs)) return 0;
+  return round_up(prompt_items(n_tokens, n_seqs, n_q_heads / n_kv_heads) * (int64_t)sizeof(Item), 256);
+}
+
+int as_attention_prompt(const void* q, const void* k, const void* v, int32_t type, int64_t n_tokens,
+                        int32_t n_q_heads, int32_t n_kv_heads, int32_t dim, int64_t q_token, int64_t k_token,
+                        int64_t v_token, const int32_t* offsets, int32_t n_seqs, float scale, void* out, void* workspace,
+                        int64_t workspace_bytes, void* stream) {
   if (type != AS_BF16 && type != AS_F16) return fail(AS_E_INVALID_ARG, "attention_prompt: type %d", type);
   if (dim != 64 && dim != 128) return fail(AS_E_LIMITS, "attention_prompt: heads of %d channels (64 or 128)", dim);
   if (n_tokens < 0 || n_seqs < 0 || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads)
@@ -422,13 +487,18 @@ extern "C" int as_attention_prompt(const void* q, const void* k, const void* v, 
   const int group = n_q_heads / n_kv_heads;
   // (a workgroup of 256 threads each, fewer than 2^32 in all)
   if (n_tokens > (1 << 26) || n_seqs > (1 << 20) || n_q_heads > 4096 || n_tokens * n_q_heads > (1 << 30) ||
-      prompt_groups(n_tokens, n_seqs, n_kv_heads, group) >= (1 << 24))
-    return fail(AS_E_LIMITS, "attention_prompt: %lld tokens of %d heads in %d sequences", (long long)n_tokens, n_q_heads,
-                n_seqs);
+      prompt_items(n_tokens, n_seqs, group) * n_kv_heads >= (1 << 24) ||
+      k_token > (1 << 26) || v_token > (1 << 26))
+    return fail(AS_E_LIMITS, "attention_prompt: %lld tokens of %d heads in %d sequences, keys and values %lld and %lld apart",
+                (long long)n_tokens, n_q_heads, n_seqs, (long long)k_token, (long long)v_token);
   if (n_tokens == 0 || n_seqs == 0) return as_host::ok();
   if (!q || !k || !v || !offsets || !out) return fail(AS_E_INVALID_ARG, "attention_prompt: null pointer");
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 8))
     return fail(AS_E_INVALID_ARG, "attention_prompt: queries, keys and values aligned to 16 bytes, outputs to 8");
+  const int64_t need = as_attention_prompt_workspace(n_tokens, n_q_heads, n_kv_heads, n_seqs);
+  if (workspace_bytes < need || (need && (!workspace || !aligned(workspace, 256))))
+    return fail(AS_E_INVALID_ARG, "attention_prompt: workspace of %lld bytes, %lld needed (aligned to 256)",
+                (long long)workspace_bytes, (long long)need);
   const uintptr_t out0 = (uintptr_t)out, out1 = out0 + (uintptr_t)(n_tokens * n_q_heads * dim * 2);
   auto meets = [&](const void* x, int64_t token, int heads) {
     return (uintptr_t)x < out1 && out0 < (uintptr_t)x + (uintptr_t)(((n_tokens - 1) * token + (int64_t)heads * dim) * 2);
@@ -450,9 +520,12 @@ extern "C" int as_attention_prompt(const void* q, const void* k, const void* v, 
   p.group = group;
   p.factor = scale * 1.44269504f;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  Item* items = reinterpret_cast<Item*>(workspace);
   if (type == AS_BF16)
-    launch_prompt<AS_BF16>(p, dim, s);
+    dim == 64 ? launch_prompt<AS_BF16, 64>(p, items, s) : launch_prompt<AS_BF16, 128>(p, items, s);
   else
-    launch_prompt<AS_F16>(p, dim, s);
+    dim == 64 ? launch_prompt<AS_F16, 64>(p, items, s) : launch_prompt<AS_F16, 128>(p, items, s);
   return launched("attention_prompt");
 }
+
+}  // extern "C"

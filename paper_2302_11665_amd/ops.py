@@ -54,7 +54,8 @@ def lib():
                 ("as_norm_i8", ctypes.c_int, [_P, _P, _I32, _I64, _I64, _I64, _I64, _P, ctypes.c_float, _P, _I64, _P,
                                               _P, _P, _P]),
                 ("as_attention_prompt", ctypes.c_int, [_P, _P, _P, _I32, _I64, _I32, _I32, _I32, _I64, _I64, _I64, _P,
-                                                       _I32, ctypes.c_float, _P, _P]),
+                                                       _I32, ctypes.c_float, _P, _P, _I64, _P]),
+                ("as_attention_prompt_workspace", _I64, [_I64, _I32, _I32, _I32]),
                 ("as_pages_reserve_workspace", _I64, [_I32]),
                 ("as_pages_reserve", ctypes.c_int, [_P, _P, _I32, _P, _I32, _I32, _I32, _P, _P, _I64, _P, _P, _P, _P,
                                                     _P, _P, _I64, _P]),
@@ -304,9 +305,13 @@ def attention_prompt(q, k, v, offsets, scale=None, out=None):
     elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.shape == q.shape and out.device == dev
               and out.is_contiguous()):
         _bad("attention_prompt: out is contiguous and of q's shape, type and device")
-    _call(lib().as_attention_prompt, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), _TYPES[q.dtype], t, heads,
-          k.shape[1], dim, q_token, k_token, v_token, offsets.data_ptr(), offsets.shape[0] - 1,
-          dim ** -0.5 if scale is None else scale, out.data_ptr())
+    L = lib()
+    seqs, kv_heads = offsets.shape[0] - 1, k.shape[1]
+    need = L.as_attention_prompt_workspace(t, heads, kv_heads, seqs)
+    _keep, ws = _workspace(need, dev)
+    _call(L.as_attention_prompt, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), _TYPES[q.dtype], t, heads, kv_heads,
+          dim, q_token, k_token, v_token, offsets.data_ptr(), seqs, dim ** -0.5 if scale is None else scale,
+          out.data_ptr(), ws, need)
     return out
 
 

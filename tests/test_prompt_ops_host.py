@@ -48,8 +48,8 @@ def test_linear_codes_refusals(L):
 
 def test_prompt_refusals(L):
     def call(q=0x100000, k=0x200000, v=0x300000, t=0, n=10, hq=4, hk=2, dim=64, qs=256, ks=128, vs=128, off=0x400,
-             seqs=2, scale=0.1, out=0x400000):
-        return L.as_attention_prompt(q, k, v, t, n, hq, hk, dim, qs, ks, vs, off, seqs, scale, out, None)
+             seqs=2, scale=0.1, out=0x400000, ws=None, wb=0):
+        return L.as_attention_prompt(q, k, v, t, n, hq, hk, dim, qs, ks, vs, off, seqs, scale, out, ws, wb, None)
 
     for kw in (dict(q=None), dict(k=None), dict(v=None), dict(off=None), dict(out=None), dict(t=2), dict(n=-1),
                dict(seqs=-1), dict(hq=3), dict(hq=0), dict(hk=0), dict(hk=-2), dict(qs=-256), dict(qs=252), dict(ks=4),
@@ -61,6 +61,13 @@ def test_prompt_refusals(L):
     for kw in (dict(dim=96), dict(dim=0), dict(n=(1 << 26) + 1, hq=1, hk=1), dict(seqs=(1 << 20) + 1), dict(hq=8192),
                dict(n=1 << 22, hq=1024, hk=1), dict(n=1 << 18, seqs=1 << 18, hq=128, hk=128)):
         assert call(**kw) == sim.AS_E_LIMITS, kw
+    assert call(ks=(1 << 26) + 8) == sim.AS_E_LIMITS and call(vs=1 << 40) == sim.AS_E_LIMITS
+    # few sequences need no scratch memory; many need the list of their blocks
+    assert L.as_attention_prompt_workspace(10, 4, 2, 64) == 0
+    need = L.as_attention_prompt_workspace(1000, 4, 2, 65)
+    assert need >= (1000 * 2 // 128 + 65) * 16
+    for kw in (dict(wb=0), dict(wb=need - 1, ws=0x1000), dict(wb=need), dict(wb=need, ws=0x1010)):
+        assert call(n=1000, seqs=65, **kw) == sim.AS_E_INVALID_ARG, kw
     assert call(n=0, q=None) == sim.AS_OK and call(seqs=0, off=None) == sim.AS_OK
 
 
