@@ -40,6 +40,13 @@ __device__ __forceinline__ v16f multiply(v8s a, v8s b, v16f c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
 }
 
+// Two numbers rounded to the type, the first in the low half.
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack_two(float a, float b) {
+  if constexpr (TYPE == AS_BF16) return pack_bf16(a, b);
+  return __builtin_bit_cast(uint32_t, v2h{(_Float16)a, (_Float16)b});
+}
+
 __device__ __forceinline__ float max_halves(float x) {
   const v2u p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
@@ -299,35 +306,38 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
 #pragma unroll
       for (int i = 0; i < kDimTiles; ++i) o[i] = multiply<TYPE>(values(tile, i, z), weights[z], o[i]);
   };
-  // The same where some rows do not see some keys and values may not be finite.
+  // The same where some rows do not see some keys and values may not be finite:
+  // for each of NaN and the two infinities, the count of those that a row sees.
   auto add_careful = [&](int tile, const v8s (&weights)[4]) {
 #pragma unroll
     for (int i = 0; i < kDimTiles; ++i) {
-      v16f nan = {}, plus = {}, minus = {};
 #pragma unroll
       for (int z = 0; z < 4; ++z) {
-        v8s v = values(tile, i, z), is_nan, is_plus, is_minus, seen;
+        v8s v = values(tile, i, z);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint16_t u = (uint16_t)v[e];
-          const bool bad = not_finite<TYPE>(u);
-          is_plus[e] = (short)(u == kInfinity<TYPE> ? kOne<TYPE> : 0);
-          is_minus[e] = (short)(u == (kInfinity<TYPE> | 0x8000) ? kOne<TYPE> : 0);
-          is_nan[e] = (short)(bad && !is_plus[e] && !is_minus[e] ? kOne<TYPE> : 0);
-          v[e] = bad ? (short)0 : v[e];
-          const int key = tile * kKeys + z * 16 + 8 * (e >> 2) + 4 * half + (e & 3);
-          seen[e] = (short)(key <= pos ? kOne<TYPE> : 0);
-        }
-        nan = multiply<TYPE>(is_nan, seen, nan);
-        plus = multiply<TYPE>(is_plus, seen, plus);
-        minus = multiply<TYPE>(is_minus, seen, minus);
+        for (int e = 0; e < 8; ++e) v[e] = not_finite<TYPE>((uint16_t)v[e]) ? (short)0 : v[e];
         o[i] = multiply<TYPE>(v, weights[z], o[i]);
       }
+#pragma unroll 1
+      for (int kind = 0; kind < 3; ++kind) {
+        const uint16_t wanted = kind == 0 ? kInfinity<TYPE> : kInfinity<TYPE> | 0x8000;
+        v16f count = {};
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (plus[r] > 0.0f) o[i][r] += kInf;
-        if (minus[r] > 0.0f) o[i][r] -= kInf;
-        if (nan[r] > 0.0f) o[i][r] = __builtin_nanf("");
+        for (int z = 0; z < 4; ++z) {
+          v8s v = values(tile, i, z), seen;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint16_t u = (uint16_t)v[e];
+            const bool is = kind == 2 ? not_finite<TYPE>(u) && (u & 0x7fff) != kInfinity<TYPE> : u == wanted;
+            v[e] = (short)(is ? kOne<TYPE> : 0);
+            const int key = tile * kKeys + z * 16 + 8 * (e >> 2) + 4 * half + (e & 3);
+            seen[e] = (short)(key <= pos ? kOne<TYPE> : 0);
+          }
+          count = multiply<TYPE>(v, seen, count);
+        }
+        const float what = kind == 0 ? kInf : kind == 1 ? -kInf : __builtin_nanf("");
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] += count[r] > 0.0f ? what : 0.0f;
       }
     }
   };
@@ -410,9 +420,8 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
   for (int i = 0; i < kDimTiles; ++i)
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
-      const uint32_t lo = from_f32<TYPE>(o[i][r] * by) | (uint32_t)from_f32<TYPE>(o[i][r + 1] * by) << 16;
-      const uint32_t hi = from_f32<TYPE>(o[i][r + 2] * by) | (uint32_t)from_f32<TYPE>(o[i][r + 3] * by) << 16;
-      *reinterpret_cast<v2u*>(to + i * 32 + 2 * r + 4 * half) = v2u{lo, hi};
+      *reinterpret_cast<v2u*>(to + i * 32 + 2 * r + 4 * half) =
+          v2u{pack_two<TYPE>(o[i][r] * by, o[i][r + 1] * by), pack_two<TYPE>(o[i][r + 2] * by, o[i][r + 3] * by)};
     }
   return true;
 }
@@ -425,7 +434,7 @@ __device__ __attribute__((noinline)) void attend_block_again(PromptArgs p, uint8
 }
 
 template <int TYPE, int DIM, int WAVES, bool PLAN>
-__global__ __launch_bounds__(64 * WAVES, 2) void prompt_attention(PromptArgs p, const Item* items) {
+__global__ __launch_bounds__(64 * WAVES, DIM == 64 ? 3 : 2) void prompt_attention(PromptArgs p, const Item* items) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][kKeys * DIM * 2];  // of two tiles: K, V
   const int head = blockIdx.x % p.n_heads, at = blockIdx.x / p.n_heads;
   Item item;
