@@ -367,15 +367,17 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
   scores(0, s);
   turn(0);
   // A wavefront makes the scores of a tile while it turns the last one's into
-  // weights, so that its matrix and vector instructions overlap.
-  auto step = [&](v16f (&now)[2], v16f (&then)[2]) {
-    follow(now);
-    scores(tile + 1, then);  // (behind the last tile: of what lies in LDS, and not used)
-    weigh(now, weights);
-    add(tile, weights);
-    if (++tile < tiles) turn(tile);
-  };
-  if (!CAREFUL) {
+  // weights, so that its matrix and vector instructions overlap.  Heads of 64
+  // channels take less than it with the registers of three wavefronts a SIMD, which overlap
+  // without that.
+  if (!CAREFUL && DIM == 128) {
+    auto step = [&](v16f (&now)[2], v16f (&then)[2]) {
+      follow(now);
+      scores(tile + 1, then);  // (behind the last tile: of what lies in LDS, and not used)
+      weigh(now, weights);
+      add(tile, weights);
+      if (++tile < tiles) turn(tile);
+    };
     while (tile + 1 < open) {
       step(s, next);
       step(next, s);
@@ -383,6 +385,14 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
     if (tile < open) {
       step(s, next);
       s[0] = next[0], s[1] = next[1];
+    }
+  } else if (!CAREFUL) {
+    while (tile < open) {
+      follow(s);
+      weigh(s, weights);
+      add(tile, weights);
+      scores(tile + 1, s);
+      if (++tile < tiles) turn(tile);
     }
   }
   // the tiles that some rows do not see whole, or not at all
@@ -413,16 +423,33 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
       for (int r = 0; r < 16; ++r) fine &= fabsf(o[i][r]) < kInf;
     if (__syncthreads_or(!fine)) return false;
   }
-  if (row0 + col >= rows) return true;
-  uint16_t* to = p.out + ((int64_t)(begin + pos) * p.n_heads * p.group + head * p.group + member) * DIM;
+  // Rows go through LDS, where a row's lanes leave them 8 bytes each, and out as
+  // whole lines.  (All are done with the tiles: the barrier that the check makes, or
+  // the one here.)
+  if (CAREFUL) __syncthreads();
+  int late = lane;  // (what follows from it is computed here, not kept in registers all along)
+  asm volatile("" : "+v"(late));
+  const int row_in = late & 31, upper = late >> 5;
+  uint8_t* own = lds[0][0] + wave * 32 * kRowBytes;
   const float by = 1.0f / total;
 #pragma unroll
   for (int i = 0; i < kDimTiles; ++i)
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
-      *reinterpret_cast<v2u*>(to + i * 32 + 2 * r + 4 * half) =
-          v2u{pack_two<TYPE>(o[i][r] * by, o[i][r + 1] * by), pack_two<TYPE>(o[i][r + 2] * by, o[i][r + 3] * by)};
+      const v2u four = {pack_two<TYPE>(o[i][r] * by, o[i][r + 1] * by), pack_two<TYPE>(o[i][r + 2] * by, o[i][r + 3] * by)};
+      const int byte = i * 64 + r * 4 + upper * 8;
+      *reinterpret_cast<v2u*>(own + row_in * kRowBytes + (((byte >> 4) ^ swizzle<DIM>(row_in)) << 4) + (byte & 8)) = four;
     }
+#pragma unroll
+  for (int i = 0; i < 32 / kPerLoad; ++i) {
+    const int in = i * kPerLoad + late / kPieces, at = row0 + in;
+    const v4u eight = *reinterpret_cast<const v4u*>(own + in * kRowBytes + (((late % kPieces) ^ swizzle<DIM>(in)) << 4));
+    if (at >= rows) continue;
+    const int query = at / p.group;
+    uint16_t* to = p.out + ((int64_t)(begin + query) * p.n_heads * p.group + head * p.group + at - query * p.group) * DIM;
+    *reinterpret_cast<v2u*>(to + late % kPieces * 8) = v2u{eight[0], eight[1]};
+    *reinterpret_cast<v2u*>(to + late % kPieces * 8 + 4) = v2u{eight[2], eight[3]};
+  }
   return true;
 }
 
