@@ -346,15 +346,19 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
   for (int i = 0; i < kDimTiles; ++i) o[i] = v16f{};
   reference = -1e30f, total = 0.0f;
   bring_k(0);
-  bring_v(0);
   if (tiles > 1) bring_k(1);
-  // V of a tile and K of the next are there, all are done with those before, and
-  // the ones behind are on their way
-  auto turn = [&](int tile) {
+  bring_v(0);
+  // V of this tile and K of the one behind the next are there, and all are done with
+  // V of the last tile and K of the next.
+  auto turn = [&] {
     wait_loads<0>();
-    __syncthreads();
+    lds_barrier();
+  };
+  // In their places, when V of this tile has been read: reads that transpose are made
+  // to wait for all loads on their way.
+  auto bring_next = [&](int tile) {
     if (tile + 1 < tiles) bring_v(tile + 1);
-    if (tile + 2 < tiles) bring_k(tile + 2);
+    if (tile + 3 < tiles) bring_k(tile + 3);
   };
   v16f s[2], next[2];
   v8s weights[4];
@@ -363,21 +367,27 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
     wait_loads<2 * kLoads>();
   else
     wait_loads<kLoads>();
-  __syncthreads();  // K of the first tile is there
+  lds_barrier();  // K of the first tile is there
   scores(0, s);
-  turn(0);
+  wait_loads<kLoads>();
+  lds_barrier();  // and of the second, and all are done with the first
+  if (tiles > 2) bring_k(2);
   // A wavefront makes the scores of a tile while it turns the last one's into
   // weights, so that its matrix and vector instructions overlap.  Heads of 64
   // channels take less than it with the registers of three wavefronts a SIMD, which overlap
-  // without that.
+  // without that.  (Behind the last tile, scores are those of what lies in LDS, and
+  // not used.)
+  auto step = [&](v16f (&now)[2], v16f (&then)[2]) {
+    follow(now);
+    if (DIM == 128) scores(tile + 1, then);
+    weigh(now, weights);
+    if (DIM == 64) scores(tile + 1, then);
+    turn();
+    add(tile, weights);
+    bring_next(tile);
+    ++tile;
+  };
   if (!CAREFUL && DIM == 128) {
-    auto step = [&](v16f (&now)[2], v16f (&then)[2]) {
-      follow(now);
-      scores(tile + 1, then);  // (behind the last tile: of what lies in LDS, and not used)
-      weigh(now, weights);
-      add(tile, weights);
-      if (++tile < tiles) turn(tile);
-    };
     while (tile + 1 < open) {
       step(s, next);
       step(next, s);
@@ -387,16 +397,10 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
       s[0] = next[0], s[1] = next[1];
     }
   } else if (!CAREFUL) {
-    while (tile < open) {
-      follow(s);
-      weigh(s, weights);
-      add(tile, weights);
-      scores(tile + 1, s);
-      if (++tile < tiles) turn(tile);
-    }
+    while (tile < open) step(s, s);
   }
   // the tiles that some rows do not see whole, or not at all
-  while (tile < tiles) {
+  for (; tile < tiles; ++tile) {
     if (tile < mine) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -405,28 +409,37 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
           if (tile * kKeys + h * 32 + 8 * (r >> 2) + 4 * half + (r & 3) > pos) s[h][r] = -kInf;
       follow(s);
       weigh(s, weights);
+      if (tile + 1 < mine) scores(tile + 1, s);
+    }
+    turn();
+    if (tile < mine) {
       if (CAREFUL && tile >= open)
         add_careful(tile, weights);
       else
         add(tile, weights);
-      if (tile + 1 < mine) scores(tile + 1, s);
     }
-    if (++tile < tiles) turn(tile);
+    bring_next(tile);
   }
   total = sum_halves(total);
 
+  lds_barrier();  // all are done with the tiles
   if (!CAREFUL) {
     bool fine = true;
 #pragma unroll
     for (int i = 0; i < kDimTiles; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) fine &= fabsf(o[i][r]) < kInf;
-    if (__syncthreads_or(!fine)) return false;
+    uint32_t* found = reinterpret_cast<uint32_t*>(lds[1][0]);
+    const bool any = __any(!fine);
+    if (lane == 0) found[wave] = any;
+    lds_barrier();
+    uint32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) all |= found[i];
+    if (__builtin_amdgcn_readfirstlane(all)) return false;
   }
   // Rows go through LDS, where a row's lanes leave them 8 bytes each, and out as
-  // whole lines.  (All are done with the tiles: the barrier that the check makes, or
-  // the one here.)
-  if (CAREFUL) __syncthreads();
+  // whole lines.
   int late = lane;  // (what follows from it is computed here, not kept in registers all along)
   asm volatile("" : "+v"(late));
   const int row_in = late & 31, upper = late >> 5;
@@ -462,7 +475,11 @@ __device__ __attribute__((noinline)) void attend_block_again(PromptArgs p, uint8
 
 template <int TYPE, int DIM, int WAVES, bool PLAN>
 __global__ __launch_bounds__(64 * WAVES, DIM == 64 ? 3 : 2) void prompt_attention(PromptArgs p, const Item* items) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][kKeys * DIM * 2];  // of two tiles: K, V
+  // of two tiles: K, V.  (Memory of a size given at the launch: reads of an array of
+  // the kernel's own are made to wait for all loads on their way to it, those of the
+  // next tiles among them.)
+  extern __shared__ __attribute__((aligned(1024))) uint8_t stages[];
+  auto lds = reinterpret_cast<uint8_t (*)[2][kKeys * DIM * 2]>(stages);
   const int head = blockIdx.x % p.n_heads, at = blockIdx.x / p.n_heads;
   Item item;
   if (PLAN) {
@@ -488,11 +505,13 @@ template <int TYPE, int DIM>
 void launch_prompt(const PromptArgs& p, Item* items, hipStream_t s) {
   const int n = (int)prompt_items(p.n_tokens, p.n_seqs, p.group);
   const dim3 g((unsigned)(n * p.n_heads)), t(64 * kPromptWaves);
+  constexpr size_t kLds = 4 * kKeys * DIM * 2;
+  static_assert(kLds <= 64 * 1024, "more has to be allowed for a kernel");
   if (prompt_planned(p.n_seqs)) {
     hipLaunchKernelGGL((prompt_plan<32 * kPromptWaves>), dim3(1), dim3(kPlanThreads), 0, s, p, items, n);
-    hipLaunchKernelGGL((prompt_attention<TYPE, DIM, kPromptWaves, true>), g, t, 0, s, p, items);
+    hipLaunchKernelGGL((prompt_attention<TYPE, DIM, kPromptWaves, true>), g, t, kLds, s, p, items);
   } else {
-    hipLaunchKernelGGL((prompt_attention<TYPE, DIM, kPromptWaves, false>), g, t, 0, s, p, nullptr);
+    hipLaunchKernelGGL((prompt_attention<TYPE, DIM, kPromptWaves, false>), g, t, kLds, s, p, nullptr);
   }
 }
 
