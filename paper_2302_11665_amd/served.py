@@ -10,11 +10,17 @@ arrays give the bytes.  The budget makes both constants of the model: an
 unbounded cache has no fixed size, and its step no fixed time, which the
 admission rule of Sec. 4.3 needs.
 
+A request begins with its prompt.  `Requests` holds the caches of requests that
+come and go, on pages of one pool, and `Block.prompt` reads the prompts of
+several of them at once; the time of that can be counted in the latency.
+
 `python -m paper_2302_11665_amd.served` measures two small models and prints
-the placement that the partition search chooses for them.
+the placement that the partition search chooses for them; `--prompt N` counts
+prompts of N tokens.
 """
 from __future__ import annotations
 
+import argparse
 import dataclasses
 
 import numpy as np
@@ -80,6 +86,23 @@ class Block:
         h = torch.nn.functional.gelu(ops.linear_i8(_normed(x), self.up))
         return x + ops.linear_i8(h, self.down)
 
+    def prompt(self, x, requests: "Requests", add):
+        """The prompts of several requests, packed: x [tokens, hidden] (bf16),
+        add[b] rows (int32 [seqs]) of every request b, which has no tokens yet,
+        to the block's output.  Their keys and values are in the requests' caches
+        afterwards; a request that got no pages keeps its length of 0, and its rows
+        come out all the same.  Rows behind the last request's may be anything."""
+        import torch
+        from . import ops
+        s = self.shape
+        places = requests.admit(add, x.shape[0])
+        codes, _ = ops.norm_i8(x)
+        qkv = ops.linear_i8(codes, self.qkv).view(-1, s.heads + 2 * s.kv_heads, s.dim)
+        o = requests.prompt(qkv[:, :s.heads], qkv[:, s.heads:s.heads + s.kv_heads], qkv[:, s.heads + s.kv_heads:], places)
+        codes, x = ops.norm_i8(ops.linear_i8(o.view(-1, s.heads * s.dim), self.out), x)
+        h = torch.nn.functional.gelu(ops.linear_i8(codes, self.up))
+        return x + ops.linear_i8(h, self.down)
+
 
 def _normed(x):
     """Rows of mean square 1."""
@@ -127,6 +150,57 @@ class Caches:
         return ops.attention_kv4(q, self.now, self.length, acc_in=self.now.acc, acc_out=self.now.acc)
 
 
+class Requests:
+    """The caches of up to `n_seqs` requests that come and go in one block, each
+    of at most `tokens` tokens, on `n_pages` pages (default: enough for all).  All
+    of its state is on the device: calls can be captured and replayed."""
+
+    def __init__(self, shape: Shape, n_seqs: int, tokens: int, n_pages: int | None = None, device="cuda"):
+        import torch
+        from . import ops
+        self.shape = shape
+        per = -(-tokens // shape.page)
+        pages = n_seqs * per if n_pages is None else n_pages
+        table = torch.zeros(n_seqs, per, dtype=torch.int32, device=device)
+        self.cache = ops.Cache.empty(pages, shape.kv_heads, shape.dim, table, group=shape.group, page=shape.page,
+                                     device=device)
+        self.pool = ops.PagePool.full(pages, device)
+        self.length = torch.zeros(n_seqs, dtype=torch.int32, device=device)  # tokens of each request, 0: none
+        self._ids = torch.arange(n_seqs, dtype=torch.int32, device=device)
+        self._none = torch.full_like(self._ids, -1)
+
+    def admit(self, add, n_tokens):
+        """Pages for add[b] more tokens of every request, and their places
+        (`ops.pages_reserve`)."""
+        from . import ops
+        return ops.pages_reserve(self.pool, self.cache.page_table, self.shape.page, self.length, add, n_tokens)
+
+    def prompt(self, q, k, v, places):
+        """Attention of packed prompts over themselves; their keys and values go to
+        their places."""
+        from . import ops
+        ops.cache_append_packed(self.cache, k, v, places.seq, places.slot)
+        return ops.attention_prompt(q, k, v, places.offsets)
+
+    def attend(self, q, k, v):
+        """One token more of every request that has some: q, k, v [seqs, 1, heads,
+        dim].  A request without tokens gets zeros; one that got no page for its
+        token keeps its length, and attends without it."""
+        import torch
+        from . import ops
+        start = self.length.clone()
+        ops.pages_reserve(self.pool, self.cache.page_table, self.shape.page, start, start.clamp(max=1), len(start),
+                          new_length=self.length)
+        seq = torch.where(self.length > start, self._ids, self._none)
+        ops.cache_append_packed(self.cache, k[:, 0], v[:, 0], seq, start)
+        return ops.attention_kv4(q, self.cache, self.length)
+
+    def finish(self, which):
+        """The requests that `which` marks (bool [seqs]) end: their pages go back."""
+        from . import ops
+        ops.pages_release(self.pool, self.cache.page_table, self.shape.page, self.length, which)
+
+
 @dataclasses.dataclass(frozen=True)
 class Profile:
     """What the searches need to know of a model."""
@@ -170,21 +244,52 @@ def step_seconds(block: Block, batch: int, steps: int = 32) -> float:
     return start.elapsed_time(stop) * 1e-3 / (replays * 2 * s.slack)
 
 
-def measure(shape: Shape, tokens: int, requests: int = 8, batch: int = 8, device="cuda") -> Profile:
-    """Profile of a model whose requests generate `tokens` tokens, with room
-    for the caches of `requests` requests."""
+def prompt_seconds(block: Block, lengths, repeats: int = 8) -> float:
+    """Seconds in which the block reads prompts of these lengths at once, their
+    pages taken and given back: replayed from a graph, as steps are."""
+    import torch
+    requests = Requests(block.shape, len(lengths), max(max(lengths), 1), device=block.device)
+    add = torch.tensor(lengths, dtype=torch.int32, device=block.device)
+    x = torch.randn(sum(lengths), block.shape.hidden, device=block.device).to(torch.bfloat16)
+    ended = torch.ones(len(lengths), dtype=torch.bool, device=block.device)
+
+    def read():
+        block.prompt(x, requests, add)
+        requests.finish(ended)
+
+    for _ in range(2):
+        read()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        read()
+    graph.replay()
+    start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    for _ in range(repeats):
+        graph.replay()
+    stop.record()
+    torch.cuda.synchronize()
+    return start.elapsed_time(stop) * 1e-3 / repeats
+
+
+def measure(shape: Shape, tokens: int, requests: int = 8, batch: int = 8, device="cuda", prompt: int = 0) -> Profile:
+    """Profile of a model whose requests have prompts of `prompt` tokens (0: not
+    counted) and generate `tokens` tokens, with room for the caches of `requests`
+    requests."""
     block = Block(shape, device=device)
     one, many = step_seconds(block, 1), step_seconds(block, batch)
     cache = Caches(shape, 1, device).bytes_per_sequence()
-    return profile(shape, tokens, requests, block.nbytes, cache, one, many, batch)
+    before, all_before = (prompt_seconds(block, [prompt] * n) if prompt else 0.0 for n in (1, batch))
+    return profile(shape, tokens, requests, block.nbytes, cache, one, many, batch, before, all_before)
 
 
 def profile(shape: Shape, tokens: int, requests: int, block_bytes: int, cache_bytes: int, one: float, many: float,
-            batch: int) -> Profile:
+            batch: int, prompt_one: float = 0.0, prompt_many: float = 0.0) -> Profile:
     """A profile from a block's bytes, one request's cache bytes in it, and the
-    seconds of its step for one request and for `batch`."""
+    seconds of its step, and of its prompt, for one request and for `batch`."""
     total = shape.layers * (block_bytes + requests * cache_bytes)
-    return Profile(latency=tokens * shape.layers * one,
+    one, many = tokens * one + prompt_one, tokens * many + prompt_many
+    return Profile(latency=shape.layers * one,
                    slope=max(0.0, (many / one - 1.0) / (batch - 1)) if batch > 1 else 1.0,
                    weight_mib=-(-total // MIB))
 
@@ -216,14 +321,18 @@ def place(gp: problems.GreedyProblem, device="cuda") -> dict:
                                    gp.weight_mib, gp.partitions, gp.slo_scale)
 
 
-def main():
+def main(argv=None):
+    ap = argparse.ArgumentParser(prog="python -m paper_2302_11665_amd.served", description=__doc__.splitlines()[0])
+    ap.add_argument("--prompt", type=int, default=0, help="tokens of a request's prompt whose reading is counted")
+    prompt = ap.parse_args(argv).prompt
     shapes = [Shape(layers=24, hidden=2048, heads=16, kv_heads=4, dim=128, inner=8192, budget=1024),
               Shape(layers=32, hidden=4096, heads=32, kv_heads=8, dim=128, inner=16384, budget=2048)]
     found = []
     for s in shapes:
-        p = measure(s, tokens=128)
+        p = measure(s, tokens=128, prompt=prompt)
         found.append(p)
-        print(f"{s.layers} layers of {s.hidden}: {p.latency:.3f} s a request of 128 tokens, batching slope "
+        print(f"{s.layers} layers of {s.hidden}: {p.latency:.3f} s a request of 128 tokens"
+              f"{f' after {prompt}' if prompt else ''}, batching slope "
               f"{p.slope:.3f}, {p.weight_mib} MiB", flush=True)
     profiles = [found[i % len(found)] for i in range(8)]
     gp = placement_problem(profiles, n_devices=8, device_mem_gb=16, rate=0.5 / found[-1].latency)
