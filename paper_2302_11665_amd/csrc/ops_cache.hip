@@ -68,10 +68,13 @@ struct Quantised {
 // middle between two fp32 numbers without being there, and the result is the
 // division's.  x - m is exact for 16-bit x and m of like size.  Adding 1.5 * 2^23
 // rounds to whole numbers, ties to even.
-template <int TYPE, int GROUP>
-__device__ __forceinline__ Quantised quantise8(const uint16_t* x, float* held) {
+__device__ __forceinline__ v4u read8(const uint16_t* x) {
   v4u raw;
   __builtin_memcpy(&raw, x, 16);
+  return raw;
+}
+template <int TYPE, int GROUP>
+__device__ __forceinline__ Quantised quantise8(const v4u& raw, float* held) {
   float f[8];
   float low = kInf, high = -kInf;
   bool bad = false;
@@ -189,7 +192,7 @@ __global__ __launch_bounds__(256) void append(AppendArgs p) {
     float* held = is_v ? p.held_v : p.held_k;
     if (held) held += (((int64_t)b * p.n_tokens + t) * p.c.n_heads + h) * DIM + lane * 8;
     const int at = in_page + s;
-    put8<DIM, GROUP>(p.c, row, at, lane, is_v, quantise8<TYPE, GROUP>(x, held), v_codes[s]);
+    put8<DIM, GROUP>(p.c, row, at, lane, is_v, quantise8<TYPE, GROUP>(read8(x), held), v_codes[s]);
     if (is_v && lane == 0) {
       if (p.c.pos) p.c.pos[row * p.c.page + at] = (int32_t)(p.first_pos ? p.first_pos[b] + t : first + s);
       if (p.c.acc) p.c.acc[row * p.c.page + at] = 0.0f;
@@ -257,23 +260,36 @@ __global__ __launch_bounds__(256) void append_packed(PackedArgs p) {
     rows[wide] = mine ? cache_row(p.c, seq, h, slot / p.c.page) : -1;
     places[wide] = slot % p.c.page;
   }
-  __syncthreads();
+  lds_barrier();
   const int lane = threadIdx.x % kLanes, last = 63 - __builtin_clzll(own);
-  for (int i = __builtin_ctzll(own) + threadIdx.x / kLanes; i <= last; i += kAtOnce) {
-    const int64_t row = rows[i], u = t0 + i;
-    if (row < 0) continue;
-    const int at = places[i];
-    const int64_t from = (int64_t)h * DIM + lane * 8, held = (u * p.c.n_heads + h) * DIM + lane * 8;
-    const Quantised k = quantise8<TYPE, GROUP>(p.k + u * p.k_token + from, p.held_k ? p.held_k + held : nullptr);
-    const Quantised v = quantise8<TYPE, GROUP>(p.v + u * p.v_token + from, p.held_v ? p.held_v + held : nullptr);
-    put8<DIM, GROUP>(p.c, row, at, lane, false, k, nullptr);
-    put8<DIM, GROUP>(p.c, row, at, lane, true, v, v_codes[i]);
-    if (lane == 0) {
-      if (p.c.pos) p.c.pos[row * p.c.page + at] = p.pos ? p.pos[u] : p.slot[u];
-      if (p.c.acc) p.c.acc[row * p.c.page + at] = 0.0f;
+  for (int i0 = __builtin_ctzll(own) + threadIdx.x / kLanes; i0 <= last; i0 += 2 * kAtOnce) {
+    v4u raw[2][2];  // of two tokens, all on their way at once
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int i = i0 + j * kAtOnce;
+      if (i > last || rows[i] < 0) continue;
+      const int64_t u = t0 + i, from = (int64_t)h * DIM + lane * 8;
+      raw[j][0] = read8(p.k + u * p.k_token + from);
+      raw[j][1] = read8(p.v + u * p.v_token + from);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int i = i0 + j * kAtOnce;
+      if (i > last) continue;
+      const int64_t row = rows[i], u = t0 + i, held = (u * p.c.n_heads + h) * DIM + lane * 8;
+      if (row < 0) continue;
+      const int at = places[i];
+      const Quantised k = quantise8<TYPE, GROUP>(raw[j][0], p.held_k ? p.held_k + held : nullptr);
+      const Quantised v = quantise8<TYPE, GROUP>(raw[j][1], p.held_v ? p.held_v + held : nullptr);
+      put8<DIM, GROUP>(p.c, row, at, lane, false, k, nullptr);
+      put8<DIM, GROUP>(p.c, row, at, lane, true, v, v_codes[i]);
+      if (lane == 0) {
+        if (p.c.pos) p.c.pos[row * p.c.page + at] = p.pos ? p.pos[u] : p.slot[u];
+        if (p.c.acc) p.c.acc[row * p.c.page + at] = 0.0f;
+      }
     }
   }
-  __syncthreads();
+  lds_barrier();
   const uint8_t* codes = reinterpret_cast<const uint8_t*>(v_codes);
   for (; begins; begins &= begins - 1) {
     const int i = __builtin_ctzll(begins);

@@ -175,7 +175,7 @@ __global__ __launch_bounds__(1024) void norm_rows(NormArgs p) {
     squares += __shfl_xor(squares, o);
   }
   if (lane == 0) tops[wave] = top, sums[wave] = squares;
-  __syncthreads();
+  lds_barrier();
   squares = 0.0f;
   for (int i = 0; i < waves; ++i) {
     top = max(top, tops[i]);
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(1024) void norm_rows(NormArgs p) {
 #pragma unroll
     for (int o = 32; o; o >>= 1) d += __shfl_xor(d, o);
     if (lane == 0) wide[wave] = d;
-    __syncthreads();
+    lds_barrier();
     total = 0.0;
     for (int i = 0; i < waves; ++i) total += wide[i];
   }
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(1024) void norm_rows(NormArgs p) {
     row_scale = norm_scale(__uint_as_float(top), finite, total, p.n_cols, p.eps);
     p.scale[r] = row_scale;
   }
-  if (p.held) __syncthreads();
+  if (p.held) lds_barrier();
   const Quantiser<GAIN ? AS_F32 : TYPE> quantiser(__uint_as_float(top), finite);
   uint8_t* out = p.codes + (r >> 4) * p.k_tiles * 1024 + (r & 15) * 16;
   for (int c = tid * 16; c < padded; c += kStep) {
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(64 * kNormWaves) void norm_pairs(NormArgs p) {
     squares += __shfl_xor(squares, o);
   }
   if (lane < kNormRows) tops[wave][in] = top, sums[wave][in] = squares;
-  __syncthreads();
+  lds_barrier();
   squares = 0.0f;
   for (int i = 0; i < waves; ++i) {
     top = max(top, tops[i][in]);
@@ -274,8 +274,10 @@ __global__ __launch_bounds__(64 * kNormWaves) void norm_pairs(NormArgs p) {
   }
   const bool finite = top < 0x7f800000u;
   double total = squares;
+  // (a row's lanes agree, the rows of a workgroup need not: two barriers then)
   const bool again = finite && top != 0 && !fp32_holds(squares);
-  if (__syncthreads_or(again)) {
+  const bool rare = __any(again);  // every wavefront has lanes of all rows
+  if (rare) {
     double d = 0.0;
 #pragma unroll
     for (int i = 0; i < TIMES; ++i) {
@@ -287,7 +289,7 @@ __global__ __launch_bounds__(64 * kNormWaves) void norm_pairs(NormArgs p) {
 #pragma unroll
     for (int o = kNormRows; o < 64; o <<= 1) d += __shfl_xor(d, o);
     if (lane < kNormRows) wide[wave][in] = d;
-    __syncthreads();
+    lds_barrier();
     if (again) {
       total = 0.0;
       for (int i = 0; i < waves; ++i) total += wide[i][in];
@@ -297,7 +299,7 @@ __global__ __launch_bounds__(64 * kNormWaves) void norm_pairs(NormArgs p) {
     scales[in] = norm_scale(__uint_as_float(top), finite, total, p.n_cols, p.eps);
     if (there) p.scale[r] = scales[in];
   }
-  if (p.held) __syncthreads();
+  if (p.held) lds_barrier();
   const Quantiser<GAIN ? AS_F32 : TYPE> quantiser(__uint_as_float(top), finite);
   // (rows behind the last one are in its tile's storage)
   uint8_t* out = p.codes + (r >> 4) * p.k_tiles * 1024 + (r & 15) * 16;

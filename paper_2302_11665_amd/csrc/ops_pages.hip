@@ -19,9 +19,9 @@ __device__ __forceinline__ int64_t sum_before(int64_t x, int64_t* waves, int64_t
     const int64_t y = __shfl_up(upto, o);
     if (lane >= o) upto += y;
   }
-  __syncthreads();
+  lds_barrier();
   if (lane == 63) waves[wave] = upto;
-  __syncthreads();
+  lds_barrier();
   int64_t before = 0;
   total = 0;
 #pragma unroll
@@ -35,14 +35,14 @@ __device__ __forceinline__ int64_t sum_before(int64_t x, int64_t* waves, int64_t
 struct ReserveArgs {
   const int32_t *stack, *count, *length, *add;
   int32_t *new_count, *new_length, *table, *offsets, *seq, *slot;
-  int32_t* base;  // [n_seqs] place in the stack of a sequence's first new page
+  int32_t* base;  // [n_seqs] place in the stack of a sequence's first new page; [n_seqs] its length before
   int32_t n_pages, n_seqs, max_pages, page, n_tokens;
 };
 
 __device__ __forceinline__ int64_t pages_of(int64_t tokens, int page) { return (tokens + page - 1) / page; }
 
 // What every sequence needs and gets, in their order.  One workgroup.
-__device__ __forceinline__ void reserve_scan(const ReserveArgs& p, int32_t* offsets, int32_t* base) {
+__device__ __forceinline__ void reserve_scan(const ReserveArgs& p, int32_t* offsets, int32_t* base, int32_t* lengths) {
   __shared__ int64_t waves[kPageWaves];
   __shared__ int32_t taken;
   const int tid = threadIdx.x;
@@ -65,11 +65,12 @@ __device__ __forceinline__ void reserve_scan(const ReserveArgs& p, int32_t* offs
     if (there) {
       offsets[b] = (int32_t)min(at, (int64_t)p.n_tokens);
       p.new_length[b] = (int32_t)(fits ? length + add : length);
+      lengths[b] = (int32_t)length;
       base[b] = fits ? (int32_t)(count - 1 - (upto - need)) : kRefused;
       if (fits && need) atomicMax(&taken, (int32_t)upto);
     }
   }
-  __syncthreads();
+  lds_barrier();
   if (tid == 0) {
     offsets[p.n_seqs] = (int32_t)min(tokens, (int64_t)p.n_tokens);
     p.new_count[0] = (int32_t)count - taken;
@@ -78,7 +79,8 @@ __device__ __forceinline__ void reserve_scan(const ReserveArgs& p, int32_t* offs
 
 // A packed token's sequence and slot; the token that begins a page writes it into
 // the table.
-__device__ __forceinline__ void reserve_fill(const ReserveArgs& p, const int32_t* offsets, const int32_t* base, int t) {
+__device__ __forceinline__ void reserve_fill(const ReserveArgs& p, const int32_t* offsets, const int32_t* base,
+                                             const int32_t* lengths, int t) {
   int32_t seq = -1, slot = -1;
   if (t < offsets[p.n_seqs]) {
     int lo = 0, hi = p.n_seqs - 1;  // the first sequence that ends behind t
@@ -91,10 +93,9 @@ __device__ __forceinline__ void reserve_fill(const ReserveArgs& p, const int32_t
     }
     const int from = base[lo];
     if (from != kRefused) {
-      const int begin = offsets[lo], end = offsets[lo + 1];
-      const int length = p.new_length[lo] - (end - begin);
+      const int length = lengths[lo];
       seq = lo;
-      slot = length + (t - begin);
+      slot = length + (t - offsets[lo]);
       if (slot % p.page == 0) {
         const int index = slot / p.page;
         p.table[(int64_t)lo * p.max_pages + index] = p.stack[from - (index - (int)pages_of(length, p.page))];
@@ -106,23 +107,23 @@ __device__ __forceinline__ void reserve_fill(const ReserveArgs& p, const int32_t
 }
 
 __global__ __launch_bounds__(kPageThreads) void reserve_sequences(ReserveArgs p) {
-  reserve_scan(p, p.offsets, p.base);
+  reserve_scan(p, p.offsets, p.base, p.base + p.n_seqs);
 }
 
 __global__ __launch_bounds__(256) void reserve_tokens(ReserveArgs p) {
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t < p.n_tokens) reserve_fill(p, p.offsets, p.base, (int)t);
+  if (t < p.n_tokens) reserve_fill(p, p.offsets, p.base, p.base + p.n_seqs, (int)t);
 }
 
 // Few sequences and tokens: both in one launch, what lies between in LDS.
 constexpr int kOnceSeqs = kPageThreads, kOnceTokens = 8 * kPageThreads;
 
 __global__ __launch_bounds__(kPageThreads) void reserve_once(ReserveArgs p) {
-  __shared__ int32_t offsets[kOnceSeqs + 1], base[kOnceSeqs];
-  reserve_scan(p, offsets, base);
-  __syncthreads();
+  __shared__ int32_t offsets[kOnceSeqs + 1], base[kOnceSeqs], lengths[kOnceSeqs];
+  reserve_scan(p, offsets, base, lengths);
+  lds_barrier();
   for (int b = threadIdx.x; b <= p.n_seqs; b += kPageThreads) p.offsets[b] = offsets[b];
-  for (int t = threadIdx.x; t < p.n_tokens; t += kPageThreads) reserve_fill(p, offsets, base, t);
+  for (int t = threadIdx.x; t < p.n_tokens; t += kPageThreads) reserve_fill(p, offsets, base, lengths, t);
 }
 
 struct ReleaseArgs {
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(kPageThreads) void release_pages(ReleaseArgs p) {
     const int64_t room = max((int64_t)0, min(total, (int64_t)p.n_pages - at));
     begin[tid] = (int32_t)min(before, room);
     if (there) p.new_length[b] = ends ? 0 : (int32_t)length;
-    __syncthreads();
+    lds_barrier();
     for (int64_t i = tid; i < room; i += kPageThreads) {
       int lo = 0, hi = kPageThreads - 1;  // the last sequence that begins at or before i
       while (lo < hi) {
@@ -166,7 +167,7 @@ __global__ __launch_bounds__(kPageThreads) void release_pages(ReleaseArgs p) {
     }
     at += room;
   }
-  __syncthreads();
+  lds_barrier();
   if (tid == 0) p.new_count[0] = (int32_t)at;
 }
 
@@ -188,7 +189,7 @@ using namespace as_ops;
 
 extern "C" {
 
-int64_t as_pages_reserve_workspace(int32_t n_seqs) { return n_seqs > 0 ? round_up((int64_t)n_seqs * 4, 256) : 0; }
+int64_t as_pages_reserve_workspace(int32_t n_seqs) { return n_seqs > 0 ? round_up((int64_t)n_seqs * 8, 256) : 0; }
 
 int as_pages_reserve(const int32_t* stack, const int32_t* count, int32_t n_pages, int32_t* page_table, int32_t n_seqs,
                      int32_t max_pages, int32_t page, const int32_t* length, const int32_t* add, int64_t n_tokens,
