@@ -373,9 +373,9 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
   lds_barrier();  // and of the second, and all are done with the first
   if (tiles > 2) bring_k(2);
   // A wavefront makes the scores of a tile while it turns the last one's into
-  // weights, so that its matrix and vector instructions overlap.  Heads of 64
-  // channels take less than it with the registers of three wavefronts a SIMD, which overlap
-  // without that.  (Behind the last tile, scores are those of what lies in LDS, and
+  // weights, so that its matrix and vector instructions overlap.  Where heads have 64
+  // channels, three wavefronts a SIMD overlap instead, which have no registers for two
+  // tiles' scores.  (Behind the last tile, scores are those of what lies in LDS, and
   // not used.)
   auto step = [&](v16f (&now)[2], v16f (&then)[2]) {
     follow(now);
@@ -436,7 +436,10 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
     uint32_t all = 0;
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) all |= found[i];
-    if (__builtin_amdgcn_readfirstlane(all)) return false;
+    if (__builtin_amdgcn_readfirstlane(all)) {
+      lds_barrier();  // all have read it before the next pass writes there
+      return false;
+    }
   }
   // Rows go through LDS, where a row's lanes leave them 8 bytes each, and out as
   // whole lines.
