@@ -139,7 +139,7 @@ int as_norm_i8(const void* x, const void* residual, int32_t type, int64_t n_toke
  *            8), aligned to 16 bytes
  *   k, v     [n_tokens][n_kv_heads][dim], likewise
  *   dim      64 or 128
- *   scale    > 0, at most 2e38; logits as for as_attention_kv4
+ *   scale    > 0, at most 2e38; logits may reach 2^30 in magnitude, 2^24 in fp16
  *   out      [n_tokens][n_q_heads][dim] of `type`, contiguous, aligned to 8 bytes,
  *            apart from the others; rows of no sequence are not written
  * What a token may not see does not reach it, an infinity or NaN included.

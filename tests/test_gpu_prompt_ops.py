@@ -277,6 +277,31 @@ def test_prompt_where_the_maximum_moves(way, dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_prompt_of_the_largest_logits(dtype, dim, sign):
+    """Eight values of logits up to 2^30 (bf16) and 2^24 (fp16), far apart: the largest
+    that a row sees share its weight."""
+    g, n = gen(5), 300
+    q, k = torch.zeros(n, 1, dim, device="cuda"), torch.zeros(n, 1, dim, device="cuda")
+    v = normal(g, n, 1, dim).to(dtype)
+    q[..., 3] = 1.0 if dtype == BF16 else 2.0 ** 8
+    steps = torch.randint(0, 8, (n,), device="cuda", generator=g) * 30 + 45
+    k[:, 0, 3] = sign * steps * (2.0 ** 22 if dtype == BF16 else 2.0 ** 8)
+    out = ops.attention_prompt(q.to(dtype), k.to(dtype), v, ints([0, n]), scale=1.0)
+    with np.errstate(over="ignore"):  # of what is masked
+        o, p, a = po.attend_causal(f64(q)[:, 0], f64(k)[:, 0], f64(v)[:, 0], 1.0)
+    assert abs(a).max() > (2 ** 29.9 if dtype == BF16 else 2 ** 23.9) and ((p > 0).sum(1) > 5).any()
+    # logits are exact, so equal ones have equal weights 2^c, |c| half a unit in the last
+    # place of a logit log2 e; one rounding of it to the type, exp2 and the division
+    # 2^-22, fp32 sums of a term each 16 slots
+    u = HALF_ULP[dtype]
+    slack = (u + 2.0 ** -22 + (n / 8 + 16) * 2.0 ** -24) * (p @ np.abs(f64(v)[:, 0]))
+    slack += u * (np.abs(o) + slack) + TINY[dtype]
+    assert np.all(np.abs(f64(out)[:, 0] - o) <= slack)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("heads", [1, 3])
 def test_prompt_does_not_see_what_is_masked(dtype, dim, heads):
     """Infinities and NaN in later tokens, in other sequences and behind the last one change nothing before them."""
@@ -390,6 +415,18 @@ def test_reserve(seqs, page, add_hi, part, short):
     stack = r.permutation(free + 10)
     table = r.integers(-1, 99999, (seqs, max_pages))
     check_reserve(stack.tolist(), free, table.tolist(), page, length.tolist(), add.tolist(), int(add.sum()))
+
+
+@pytest.mark.parametrize("page", [4064, 4096, 2016, 1312])
+def test_reserve_far_along(page):
+    """Lengths up to 2^30 slots: quotients by the page stay whole."""
+    most = 2 ** 30 // page
+    r = np.random.default_rng(page)
+    ends = np.array([most, most, most - 1, most // 2 + 1, 3]) * page  # where pages begin, or the cache ends
+    length = ends - [70, 1, 1, 40, page]
+    add = [70, 1, 2, 90, page + 1]
+    table = r.integers(-1, 99, (5, most))
+    check_reserve(r.permutation(20).tolist(), 12, table, page, length.tolist(), add, int(sum(add)))
 
 
 def test_reserve_refuses_what_does_not_fit():
