@@ -4,8 +4,7 @@
 //
 // Sums over the sequences in their order, then work that does not depend on order.
 // What they move is nothing; a call is launches and the latency of a few loads and
-// barriers.  One workgroup makes the sums: 5 us for 48 sequences, 6 for a thousand, and
-// 3 for every further thousand.
+// barriers.  One workgroup makes the sums: 3.2 us for 48 sequences, 4.1 for a thousand.
 #include "ops_common.hpp"
 
 using as_host::fail;
@@ -15,26 +14,35 @@ namespace as_ops {
 constexpr int kPageThreads = 1024, kPageWaves = kPageThreads / 64;
 constexpr int32_t kRefused = INT32_MIN;
 
-// Sums over the workgroup's threads before this one; total: of all.
-__device__ __forceinline__ int64_t sum_before(int64_t x, int64_t* waves, int64_t& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t upto = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(upto, o);
-    if (lane >= o) upto += y;
+// Sums that stop at `most` (below 2^31): of as many lanes as rows of 16 or all.
+template <bool ROW>
+__device__ __forceinline__ uint32_t scan_capped(uint32_t x, uint32_t most) {
+#define AS_ADD_DPP(ctrl, rows) \
+  x = min(x + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false), most)
+  AS_ADD_DPP(0x111, 0xf);  // row_shr:1
+  AS_ADD_DPP(0x112, 0xf);
+  AS_ADD_DPP(0x114, 0xf);
+  AS_ADD_DPP(0x118, 0xf);
+  if (!ROW) {
+    AS_ADD_DPP(0x142, 0xa);  // row_bcast:15
+    AS_ADD_DPP(0x143, 0xc);  // row_bcast:31
   }
+#undef AS_ADD_DPP
+  return x;
+}
+
+// The sum over the workgroup's threads before this one, at most `most`, as x is;
+// total: of all, likewise.
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t most, uint32_t* waves, uint32_t& total) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t upto = scan_capped<false>(x, most);
+  const uint32_t own = __builtin_amdgcn_update_dpp(0, (int)upto, 0x138, 0xf, 0xf, false);  // of the lane before
   lds_barrier();
   if (lane == 63) waves[wave] = upto;
   lds_barrier();
-  int64_t before = 0;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < kPageWaves; ++w) {
-    if (w < wave) before += waves[w];
-    total += waves[w];
-  }
-  return before + upto - x;
+  const uint32_t all = scan_capped<true>(waves[lane & 15], most);
+  total = (uint32_t)__builtin_amdgcn_readlane((int)all, 15);
+  return min(own + (wave ? (uint32_t)__builtin_amdgcn_readlane((int)all, wave - 1) : 0u), most);
 }
 
 // Slots of a page, 32 m of them, and what quotients by m follow from: n / m is the
@@ -58,65 +66,69 @@ struct ReserveArgs {
   Page page;
 };
 
-// What every sequence needs and gets, in their order.  One workgroup.
+// What every sequence needs and gets, in their order.  One workgroup, a sequence to a
+// thread at a time (2, 4 and 8 were slower).  Sums of tokens stop behind n_tokens; those
+// of pages are below 2^30 / 32 and one for each sequence.
 __device__ __forceinline__ void reserve_scan(const ReserveArgs& p, int32_t* offsets, int32_t* base, int32_t* lengths) {
-  __shared__ int64_t waves[kPageWaves];
+  __shared__ uint32_t waves[kPageWaves];
   __shared__ int32_t taken;
   const int tid = threadIdx.x;
-  const int64_t count = min(max(p.count[0], 0), p.n_pages), cap = (int64_t)p.max_pages * p.page.slots;
+  const int count = min(max(p.count[0], 0), p.n_pages), cap = p.max_pages * p.page.slots;
+  const uint32_t beyond = (uint32_t)p.n_tokens + 1;
   if (tid == 0) taken = 0;
-  int64_t tokens = 0, pages = 0;  // of the sequences before this run of them
-  for (int first = 0; first < p.n_seqs; first += kPageThreads) {
-    const int b = first + tid;
+  uint32_t tokens = 0, pages = 0, total;  // of the sequences before this run of them
+  int most = 0;                           // pages up to the last sequence that gets any
+  for (int b = tid; b - tid < p.n_seqs; b += kPageThreads) {
     const bool there = b < p.n_seqs;
-    const int64_t length = there ? min((int64_t)max(p.length[b], 0), cap) : 0;
-    const int64_t add = there ? max(p.add[b], 0) : 0;
-    int64_t total;
-    const int64_t at = tokens + sum_before(add, waves, total);
-    tokens += total;
-    const bool room = length + add <= cap && at + add <= p.n_tokens;
-    const int64_t need = add && room ? pages_of(p.page, length + add) - pages_of(p.page, length) : 0;
-    const int64_t upto = pages + sum_before(need, waves, total) + need;
+    const int length = there ? min(max(p.length[b], 0), cap) : 0, add = there ? max(p.add[b], 0) : 0;
+    const uint32_t more = min((uint32_t)add, beyond), at = min(tokens + sum_before(more, beyond, waves, total), beyond);
+    tokens = min(tokens + total, beyond);
+    const bool room = (uint32_t)length + (uint32_t)add <= (uint32_t)cap && at + more < beyond;
+    const int need = add && room ? pages_of(p.page, length + add) - pages_of(p.page, length) : 0;
+    const int before = (int)(pages + sum_before((uint32_t)need, 0x7fffffffu, waves, total));
     pages += total;
-    const bool fits = (add == 0 || room) && (need == 0 || upto <= count);
+    const bool fits = (add == 0 || room) && (need == 0 || before + need <= count);
     if (there) {
-      offsets[b] = (int32_t)min(at, (int64_t)p.n_tokens);
-      p.new_length[b] = (int32_t)(fits ? length + add : length);
-      lengths[b] = (int32_t)length;
-      base[b] = fits ? (int32_t)(count - 1 - (upto - need)) : kRefused;
-      if (fits && need) atomicMax(&taken, (int32_t)upto);
+      offsets[b] = (int)min(at, (uint32_t)p.n_tokens);
+      p.new_length[b] = fits ? length + add : length;
+      lengths[b] = length;
+      base[b] = fits ? count - 1 - before : kRefused;
+      if (fits && need) most = before + need;
     }
   }
   lds_barrier();
+  if (most) atomicMax(&taken, most);
+  lds_barrier();
   if (tid == 0) {
-    offsets[p.n_seqs] = (int32_t)min(tokens, (int64_t)p.n_tokens);
-    p.new_count[0] = (int32_t)count - taken;
+    offsets[p.n_seqs] = (int)min(tokens, (uint32_t)p.n_tokens);
+    p.new_count[0] = count - taken;
   }
 }
 
-// A packed token's sequence and slot; the token that begins a page writes it into
-// the table.
-__device__ __forceinline__ void reserve_fill(const ReserveArgs& p, const int32_t* offsets, const int32_t* base,
-                                             const int32_t* lengths, int t) {
-  int32_t seq = -1, slot = -1;
-  if (t < offsets[p.n_seqs]) {
-    int lo = 0, hi = p.n_seqs - 1;  // the first sequence that ends behind t
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (offsets[mid + 1] > t)
-        hi = mid;
-      else
-        lo = mid + 1;
-    }
-    const int from = base[lo];
-    if (from != kRefused) {
-      const int length = lengths[lo];
-      seq = lo;
-      slot = length + (t - offsets[lo]);
-      const int index = page_at(p.page, slot);
-      if (index * p.page.slots == slot)
-        p.table[(int64_t)lo * p.max_pages + index] = p.stack[from - (index - pages_of(p.page, length))];
-    }
+// The first sequence from lo on that ends behind t: all of lo.. do before n.
+__device__ __forceinline__ int sequence_of(const int32_t* offsets, int lo, int n, int64_t t) {
+  int hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (offsets[mid + 1] > t)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return lo;
+}
+
+// A packed token's slot, from its sequence's first row, first new page's place in
+// the stack and length; the token that begins a page writes it into the table.
+__device__ __forceinline__ void reserve_token(const ReserveArgs& p, int t, int seq, int row, int from, int length) {
+  int slot = -1;
+  if (seq >= 0 && from != kRefused) {
+    slot = length + (t - row);
+    const int index = page_at(p.page, slot);
+    if (index * p.page.slots == slot)
+      p.table[(int64_t)seq * p.max_pages + index] = p.stack[from - (index - pages_of(p.page, length))];
+  } else {
+    seq = -1;
   }
   p.seq[t] = seq;
   p.slot[t] = slot;
@@ -126,23 +138,60 @@ __global__ __launch_bounds__(kPageThreads) void reserve_sequences(ReserveArgs p)
   reserve_scan(p, p.offsets, p.base, p.base + p.n_seqs);
 }
 
+// A wavefront takes kRun tokens.  It finds the first one's sequence, among 64 places at
+// once, and has that and the 63 behind it in registers: a token's own is found among
+// those, in memory only where it is none of them.  (A search in memory for every token
+// is 11 loads one after the other for 2000 sequences: 2000 of 350 tokens 22.4 us in
+// all, so 13.)
+constexpr int kRun = 256;
 __global__ __launch_bounds__(256) void reserve_tokens(ReserveArgs p) {
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t < p.n_tokens) reserve_fill(p, p.offsets, p.base, p.base + p.n_seqs, (int)t);
+  const int lane = threadIdx.x & 63;
+  const int64_t t0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * kRun;
+  if (t0 >= p.n_tokens) return;
+  const int64_t end = p.offsets[p.n_seqs];
+  int first = 0;
+  for (int n = p.n_seqs; n > 1;) {  // it is one of first..first + n - 1, if any
+    const int step = (n + 63) / 64, at = (lane + 1) * step;
+    const int before = __popcll(__ballot(at < n && p.offsets[first + min(at, n)] <= t0));
+    first += before * step;
+    n = min(step, n - before * step);
+  }
+  const bool any = p.n_seqs > 0;
+  const int mine = min(first + lane, p.n_seqs - 1);
+  const int row = any ? p.offsets[mine] : 0, stop = any ? p.offsets[mine + 1] : 0;
+  const int from = any ? p.base[mine] : kRefused, length = any ? p.base[p.n_seqs + mine] : 0;
+  const int last = __builtin_amdgcn_readlane(stop, 63);
+  for (int i = 0; i < kRun; i += 64) {  // (all lanes: they read from each other)
+    const int64_t t = t0 + i + lane;
+    int j = 0;  // sequences in registers that end at or before t
+#pragma unroll
+    for (int bit = 32; bit; bit >>= 1)
+      if (__shfl(stop, j + bit - 1) <= t) j += bit;
+    int u = first + j, r = __shfl(row, j), f = __shfl(from, j), l = __shfl(length, j);
+    if (t >= p.n_tokens) continue;
+    if (t >= last && t < end) {
+      u = sequence_of(p.offsets, min(first + 63, p.n_seqs - 1), p.n_seqs, t);
+      r = p.offsets[u], f = p.base[u], l = p.base[p.n_seqs + u];
+    }
+    reserve_token(p, (int)t, t < end ? u : -1, r, f, l);
+  }
 }
 
 // Few sequences and tokens: both in one launch, what lies between in LDS.  In one
 // launch and in two, on the device and for a call in a loop: 48 sequences of a token
-// 4.8 and 5.9 us, 9 and 12; 4800 tokens 9.0 and 8.5, 9 and 12; 8000 of 1000 sequences
-// 12.4 and 9.4, 12 and 12 (one workgroup's searches).
-constexpr int kOnceSeqs = kPageThreads, kOnceTokens = 4 * kPageThreads;
+// 3.3 and 5.3 us, 9 and 12; 8 of 1000 tokens 7.5 and 7.0, 9 and 12; 1000 of 8 11.1 and
+// 7.7 (one workgroup's searches), 11 and 12.
+constexpr int kOnceSeqs = kPageThreads, kOnceTokens = 8 * kPageThreads;
 
 __global__ __launch_bounds__(kPageThreads) void reserve_once(ReserveArgs p) {
   __shared__ int32_t offsets[kOnceSeqs + 1], base[kOnceSeqs], lengths[kOnceSeqs];
   reserve_scan(p, offsets, base, lengths);
   lds_barrier();
   for (int b = threadIdx.x; b <= p.n_seqs; b += kPageThreads) p.offsets[b] = offsets[b];
-  for (int t = threadIdx.x; t < p.n_tokens; t += kPageThreads) reserve_fill(p, offsets, base, lengths, t);
+  for (int t = threadIdx.x; t < p.n_tokens; t += kPageThreads) {
+    const int seq = t < offsets[p.n_seqs] ? sequence_of(offsets, 0, p.n_seqs, t) : -1, at = max(seq, 0);
+    reserve_token(p, t, seq, offsets[at], base[at], lengths[at]);
+  }
 }
 
 struct ReleaseArgs {
@@ -157,38 +206,35 @@ struct ReleaseArgs {
 // Pages of the sequences that end, in their order, behind the free ones.  One
 // workgroup.
 __global__ __launch_bounds__(kPageThreads) void release_pages(ReleaseArgs p) {
-  __shared__ int64_t waves[kPageWaves];
+  __shared__ uint32_t waves[kPageWaves];
   __shared__ int32_t begin[kPageThreads];
   const int tid = threadIdx.x;
-  const int64_t count = min(max(p.count[0], 0), p.n_pages), cap = (int64_t)p.max_pages * p.page.slots;
-  int64_t at = count;
+  const int cap = p.max_pages * p.page.slots;
+  int at = min(max(p.count[0], 0), p.n_pages);
   for (int first = 0; first < p.n_seqs; first += kPageThreads) {
     const int b = first + tid;
     const bool there = b < p.n_seqs, ends = there && p.which[b] != 0;
-    const int64_t length = there ? min((int64_t)max(p.length[b], 0), cap) : 0;
-    const int64_t pages = ends ? pages_of(p.page, length) : 0;
-    int64_t total;
-    const int64_t before = sum_before(pages, waves, total);
+    const int length = there ? min(max(p.length[b], 0), cap) : 0;
     // more pages than the pool has: lengths that no reservation gave
-    const int64_t room = max((int64_t)0, min(total, (int64_t)p.n_pages - at));
-    begin[tid] = (int32_t)min(before, room);
-    if (there) p.new_length[b] = ends ? 0 : (int32_t)length;
+    const uint32_t most = (uint32_t)(p.n_pages - at), pages = ends ? pages_of(p.page, length) : 0;
+    uint32_t room;
+    begin[tid] = (int)sum_before(min(pages, most), most, waves, room);
+    if (there) p.new_length[b] = ends ? 0 : length;
     lds_barrier();
-    for (int64_t i = tid; i < room; i += kPageThreads) {
+    for (uint32_t i = tid; i < room; i += kPageThreads) {
       int lo = 0, hi = kPageThreads - 1;  // the last sequence that begins at or before i
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (begin[mid] <= i)
+        if ((uint32_t)begin[mid] <= i)
           lo = mid;
         else
           hi = mid - 1;
       }
-      p.stack[at + i] = p.table[(int64_t)(first + lo) * p.max_pages + (i - begin[lo])];
+      p.stack[at + (int)i] = p.table[(int64_t)(first + lo) * p.max_pages + ((int)i - begin[lo])];
     }
-    at += room;
+    at += (int)room;
   }
-  lds_barrier();
-  if (tid == 0) p.new_count[0] = (int32_t)at;
+  if (tid == 0) p.new_count[0] = at;
 }
 
 Page page_args(int32_t page) {
@@ -241,7 +287,8 @@ int as_pages_reserve(const int32_t* stack, const int32_t* count, int32_t n_pages
     return launched("pages_reserve");
   }
   hipLaunchKernelGGL(reserve_sequences, dim3(1), dim3(kPageThreads), 0, s, p);
-  if (n_tokens) hipLaunchKernelGGL(reserve_tokens, dim3((unsigned)((n_tokens + 255) / 256)), dim3(256), 0, s, p);
+  if (n_tokens) hipLaunchKernelGGL(reserve_tokens, dim3((unsigned)((n_tokens + 4 * kRun - 1) / (4 * kRun))),
+                                   dim3(256), 0, s, p);
   return launched("pages_reserve");
 }
 

@@ -402,7 +402,8 @@ def check_reserve(stack, count, table, page, length, add, n_tokens):
 
 @pytest.mark.parametrize("seqs,page,add_hi,part", [(1, 32, 1, 1.0), (3, 32, 40, 0.7), (48, 64, 1, 0.9), (100, 96, 300, 0.3),
                                                    (1023, 32, 5, 0.5), (1024, 64, 90, 0.5), (1025, 32, 64, 0.8),
-                                                   (2500, 128, 200, 0.4), (5000, 32, 1, 0.9)])
+                                                   (2500, 128, 200, 0.4), (5000, 32, 1, 0.9), (9000, 32, 2, 0.02),
+                                                   (9000, 64, 700, 0.01), (7, 32, 5000, 0.9)])
 @pytest.mark.parametrize("short", [0, 3])
 def test_reserve(seqs, page, add_hi, part, short):
     say("reserve", seqs, page, add_hi, short)
@@ -440,11 +441,15 @@ def test_reserve_refuses_what_does_not_fit():
     check_reserve(stack, 0, table, 32, [31, 32, 0, 5, 0, 64], [1, 1, 0, 20, 1, 2], 25)
     check_reserve([], 0, table, 32, [0] * 6, [1] * 6, 6)
     check_reserve(stack, 20, table, 32, [2 ** 31 - 1, -2 ** 31, 3, 3, 3, 3], [2 ** 31 - 1] * 2 + [5] * 4, 20)
+    check_reserve(stack, 20, table * 800, 32, [40, 2 ** 31 - 1, -2 ** 31, 95, 0, 3] * 800, [1, 2 ** 31 - 1, 0, -9, 96, 2 ** 30] * 800, 7000)
+    check_reserve(stack, 20, table * 800, 32, [40, 32, 5, 1, 7, 0] * 800, ([1, 5, 0, 3, 0, 0] + [0] * 594) * 8, 5000)
     check_reserve(stack, 20, [[]] * 3, 32, [0, 0, 0], [1, 0, 2], 3)
     check_reserve(stack, 20, table, 32, [3] * 6, [0] * 6, 0)
     pool = ops.PagePool.full(4)
     none = ops.pages_reserve(pool, ints([[0]] * 2)[:0], 32, ints([]), ints([]), 3)
     assert none.offsets.tolist() == [0] and none.seq.tolist() == [-1] * 3 and pool.count.item() == 4
+    none = ops.pages_reserve(pool, ints([[0]] * 2)[:0], 32, ints([]), ints([]), 9000)
+    assert none.offsets.tolist() == [0] and (none.seq == -1).all() and (none.slot == -1).all()
     for count in (-5, 1000):  # a count that the stack does not have
         pool = ops.PagePool(ints(stack), ints([count]))
         n = ints([0, 0])
