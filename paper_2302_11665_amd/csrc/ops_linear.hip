@@ -540,10 +540,16 @@ int launch_product(const LinArgs& p, hipStream_t s) {
   const int64_t large = ((n_ct + 15) / 16) * ((n_tt + 15) / 16), middle = ((n_ct + 7) / 8) * ((n_tt + 7) / 8);
   const int64_t large_turns = (large + cus - 1) / cus, middle_turns = (middle + 2 * cus - 1) / (2 * cus);
   if (large >= cus && large_turns * 200 <= middle_turns * 115) return launch_many<YTYPE, 16, 16, 2, 4, 2, 2>(p, s);
-  if (middle >= cus) return launch_many<YTYPE, 8, 8, 2, 4, 2, 2>(p, s);
-  // Two workgroups of either of these run on a compute unit; the smaller tiles
-  // where all of them run at once (333 tokens 1500 -> 2777: 264 tiles of 64 x 64 took
-  // 12.6 us, 484 of 64 x 32 took 9.8).
+  // Two workgroups of each of the others run on a compute unit.  Where tiles of 64 x 64
+  // would take more than a turn, 128 x 64 if all of those run at once, else 128 x 128
+  // (64 x 64, 128 x 64, 128 x 128: 333 tokens 4096 -> 6144 24.1, 19.1 and 23.0 us; 777
+  // tokens 1500 -> 2777 12.7, 11.5 and 12.3; 777 tokens 4096 -> 6144, 624 tiles of 128 x
+  // 64: 36, 35 and 31); the smaller tiles where all of them run at once (333 tokens 1500
+  // -> 2777: 264 tiles of 64 x 64 7.8 us, 484 of 64 x 32 6.6).
+  if (((n_ct + 3) / 4) * ((n_tt + 3) / 4) > 2 * cus) {
+    if (((n_ct + 7) / 8) * ((n_tt + 3) / 4) <= 2 * cus) return launch_many<YTYPE, 8, 4, 2, 2, 2, 3>(p, s);
+    return launch_many<YTYPE, 8, 8, 2, 4, 2, 2>(p, s);
+  }
   if (((n_ct + 3) / 4) * ((n_tt + 1) / 2) > 2 * cus) return launch_many<YTYPE, 4, 4, 2, 2, 2, 4>(p, s);
   return launch_many<YTYPE, 4, 2, 4, 1, 2, 6>(p, s);
 }
