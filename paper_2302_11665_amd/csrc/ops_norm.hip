@@ -20,33 +20,52 @@ struct NormArgs {
   int64_t n_tokens, x_stride, residual_stride, sum_stride;
   int32_t n_cols, k_tiles;
   float eps;
+  bool past;  // write the sum past the caches
 };
 
-// 16 values from column c of a row of 16-bit values, two to a word; columns
-// beyond n are 0.
+// A wavefront takes 1024 / ROWS columns of ROWS rows at a time, lane `at` of a row's
+// 64 / ROWS two pieces of 8 columns: from column c + 8 at, and as many lanes further on.
+// A load or store then takes a row's columns side by side.
+template <int ROWS>
+__device__ __forceinline__ int piece_of(int z) {
+  return (z * (64 / ROWS) + (threadIdx.x & 63) / ROWS) * 8;
+}
+
+typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(2)));  // at any 16-bit value
+
+// A lane's pieces of a row of 16-bit values, two to a word; columns beyond n are 0.
+template <int ROWS>
 __device__ __forceinline__ void read16(const uint16_t* row, int c, int n, v4u (&w)[2]) {
-  w[0] = w[1] = v4u{0, 0, 0, 0};
-  if (c + 16 <= n) {
-    __builtin_memcpy(&w[0], row + c, 16);
-    __builtin_memcpy(&w[1], row + c + 8, 16);
-  } else if (c < n) {  // all loads at once: one latency, not one after the other
-    uint16_t u[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) u[e] = row[min(c + e, n - 1)];
+  for (int z = 0; z < 2; ++z) {
+    const int at = c + piece_of<ROWS>(z);
+    w[z] = v4u{0, 0, 0, 0};
+    if (at + 8 <= n) {
+      __builtin_memcpy(&w[z], row + at, 16);
+    } else if (at < n) {  // all loads at once: one latency, not one after the other
+      uint16_t u[8];
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-      w[e >> 3][(e >> 1) & 3] |= (uint32_t)(c + e < n ? u[e] : 0) << (16 * (e & 1));
+      for (int e = 0; e < 8; ++e) u[e] = row[min(at + e, n - 1)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[z][e >> 1] |= (uint32_t)(at + e < n ? u[e] : 0) << (16 * (e & 1));
+    }
   }
 }
 
-__device__ __forceinline__ void write16(uint16_t* row, int c, int n, const v4u (&w)[2]) {
-  if (c + 16 <= n) {
-    __builtin_memcpy(row + c, &w[0], 16);
-    __builtin_memcpy(row + c + 8, &w[1], 16);
-  } else {
+template <int ROWS>
+__device__ __forceinline__ void write16(uint16_t* row, int c, int n, const v4u (&w)[2], bool past) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (c + e < n) row[c + e] = (uint16_t)(w[e >> 3][(e >> 1) & 3] >> (16 * (e & 1)));
+  for (int z = 0; z < 2; ++z) {
+    const int at = c + piece_of<ROWS>(z);
+    if (at + 8 <= n && past) {
+      __builtin_nontemporal_store((v4u_any)w[z], reinterpret_cast<v4u_any*>(row + at));
+    } else if (at + 8 <= n) {
+      __builtin_memcpy(row + at, &w[z], 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (at + e < n) row[at + e] = (uint16_t)(w[z][e >> 1] >> (16 * (e & 1)));
+    }
   }
 }
 
@@ -71,16 +90,21 @@ __device__ __forceinline__ void add16(v4u (&w)[2], const v4u (&r)[2]) {
                        (uint32_t)from_f32<TYPE>(a[2 * j + 1] + b[2 * j + 1]) << 16;
 }
 
-// 16 gains from column c; 0 beyond n.
+// The gains of a lane's pieces; 0 beyond n.
+template <int ROWS>
 __device__ __forceinline__ void gain16(const float* gain, int c, int n, float (&g)[16]) {
-  if (c + 16 <= n) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) __builtin_memcpy(g + 4 * i, gain + c + 4 * i, 16);
-  } else {
+  for (int z = 0; z < 2; ++z) {
+    const int at = c + piece_of<ROWS>(z);
+    if (at + 8 <= n) {
+      __builtin_memcpy(g + 8 * z, gain + at, 16);
+      __builtin_memcpy(g + 8 * z + 4, gain + at + 4, 16);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) g[e] = gain[min(c + e, n - 1)];
+      for (int e = 0; e < 8; ++e) g[8 * z + e] = gain[min(at + e, n - 1)];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) g[e] = c + e < n ? g[e] : 0.0f;
+      for (int e = 0; e < 8; ++e) g[8 * z + e] = at + e < n ? g[8 * z + e] : 0.0f;
+    }
   }
 }
 
@@ -96,7 +120,7 @@ __device__ __forceinline__ float norm_scale(float top, bool finite, double squar
 // in 64 bits (16-bit values reach 3e38 in bf16, whose square does not).
 __device__ __forceinline__ bool fp32_holds(float squares) { return squares > 0x1p-60f && squares < 0x1p120f; }
 
-// Largest magnitude and sum of squares of 16 columns' t and h.
+// Largest magnitude and sum of squares of a lane's t and h.
 template <bool GAIN>
 __device__ __forceinline__ void measure16(const float (&f)[16], const float (&g)[16], uint32_t& top, float& squares) {
 #pragma unroll
@@ -106,33 +130,49 @@ __device__ __forceinline__ void measure16(const float (&f)[16], const float (&g)
   }
 }
 
-// Codes of 16 columns from their h (two to a word); f: their t.
-template <int TYPE, bool GAIN>
-__device__ __forceinline__ v4u codes16(const NormArgs& p, const Quantiser<GAIN ? AS_F32 : TYPE>& quantiser,
-                                       const v4u (&w)[2], int c) {
+// Codes of a lane's h (two to a word) go through LDS (`own`, of the wavefront alone) and
+// out, 16 columns to a lane as the tiles have them, and where held is not null the values
+// that they stand for, 4 columns to a lane at a time.
+template <int TYPE, bool GAIN, int ROWS>
+__device__ __forceinline__ void put_codes(const NormArgs& p, const Quantiser<GAIN ? AS_F32 : TYPE>& quantiser,
+                                          const v4u (&w)[2], int c, uint8_t* tile, float* held, float scale, bool there,
+                                          v4u* own) {
+  constexpr int kLanes = 64 / ROWS;
+  const int lane = threadIdx.x & 63, in = lane % ROWS, at = lane / ROWS;
   float f[16], g[16];
   unpack16<TYPE>(w, f);
   if (GAIN) {
-    gain16(p.gain, c, p.n_cols, g);
+    gain16<ROWS>(p.gain, c, p.n_cols, g);
 #pragma unroll
     for (int e = 0; e < 16; ++e) f[e] *= g[e];
   }
-  return v4u{quantiser.codes4(f), quantiser.codes4(f + 4), quantiser.codes4(f + 8), quantiser.codes4(f + 12)};
-}
-
-// The values that 16 codes stand for.
-__device__ __forceinline__ void hold16(float* row, int c, int n, const v4u& q, float scale) {
-  float v[16];
+  v4u* row = own + in * kLanes;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) v[e] = (float)(int8_t)(q[e >> 2] >> (8 * (e & 3))) * scale;
-  if (c + 16 <= n) {
+  for (int z = 0; z < 2; ++z)
+    reinterpret_cast<v2u*>(row)[z * kLanes + at] = v2u{quantiser.codes4(f + 8 * z), quantiser.codes4(f + 8 * z + 4)};
+  __builtin_amdgcn_wave_barrier();
+  // (rows behind the last one are in its tile's storage)
+  if (c + at * 16 < p.k_tiles * 64) *reinterpret_cast<v4u*>(tile + (int64_t)((c >> 4) + at) * 256) = row[at];
+  if (held) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) __builtin_memcpy(row + c + 4 * i, v + 4 * i, 16);
-  } else {
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t four = reinterpret_cast<const uint32_t*>(row)[i * kLanes + at];
+      const int from = c + (i * kLanes + at) * 4;
+      float v[4];
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (c + e < n) row[c + e] = v[e];
+      for (int e = 0; e < 4; ++e) v[e] = (float)(int8_t)(four >> (8 * e)) * scale;
+      if (!there) continue;
+      if (from + 4 <= p.n_cols) {
+        typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+        __builtin_nontemporal_store(v4f_any{v[0], v[1], v[2], v[3]}, reinterpret_cast<v4f_any*>(held + from));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (from + e < p.n_cols) held[from + e] = v[e];
+      }
+    }
   }
+  __builtin_amdgcn_wave_barrier();
 }
 
 // One workgroup per row, 16 columns to a thread (KEEP), which stay in registers;
@@ -141,12 +181,13 @@ __device__ __forceinline__ void hold16(float* row, int c, int n, const v4u& q, f
 // 3.9 us, 48 rows 4.1, 256 rows 5.0, with a residual and a gain).
 template <int TYPE, bool GAIN, bool KEEP>
 __global__ __launch_bounds__(1024) void norm_rows(NormArgs p) {
-  constexpr int kStep = KEEP ? 1 << 30 : 1024 * 16;
+  constexpr int kStep = KEEP ? 1 << 30 : 16 * 1024;
   __shared__ uint32_t tops[16];
   __shared__ float sums[16];
   __shared__ double wide[16];
   const int waves = blockDim.x >> 6;
   __shared__ float row_scale;
+  __shared__ v4u words[16][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, padded = p.k_tiles * 64;
   const int64_t r = blockIdx.x;
   const uint16_t* x = p.x + r * p.x_stride;
@@ -155,16 +196,16 @@ __global__ __launch_bounds__(1024) void norm_rows(NormArgs p) {
   const uint16_t* h = add ? sum : x;  // what is read again
   uint32_t top = 0;
   float squares = 0.0f;
-  v4u kept[2];
-  for (int c = tid * 16; c < padded; c += kStep) {
+  v4u kept[2] = {};
+  for (int c = wave * 1024; c < padded; c += kStep) {
     v4u w[2], b[2];
     float f[16], g[16];
-    read16(x, c, p.n_cols, w);
-    if (add) read16(add, c, p.n_cols, b);
-    if (GAIN) gain16(p.gain, c, p.n_cols, g);
+    read16<1>(x, c, p.n_cols, w);
+    if (add) read16<1>(add, c, p.n_cols, b);
+    if (GAIN) gain16<1>(p.gain, c, p.n_cols, g);
     if (add) {
       add16<TYPE>(w, b);
-      write16(sum, c, p.n_cols, w);
+      write16<1>(sum, c, p.n_cols, w, p.past);
     }
     unpack16<TYPE>(w, f);
     measure16<GAIN>(f, g, top, squares);
@@ -186,10 +227,10 @@ __global__ __launch_bounds__(1024) void norm_rows(NormArgs p) {
   double total = squares;
   if (finite && top != 0 && !fp32_holds(squares)) {
     double d = 0.0;
-    for (int c = tid * 16; c < padded; c += kStep) {
+    for (int c = wave * 1024; c < padded; c += kStep) {
       v4u w[2] = {kept[0], kept[1]};
       float f[16];
-      if (!KEEP) read16(h, c, p.n_cols, w);
+      if (!KEEP) read16<1>(h, c, p.n_cols, w);
       unpack16<TYPE>(w, f);
 #pragma unroll
       for (int e = 0; e < 16; ++e) d += (double)f[e] * f[e];
@@ -208,21 +249,20 @@ __global__ __launch_bounds__(1024) void norm_rows(NormArgs p) {
   if (p.held) lds_barrier();
   const Quantiser<GAIN ? AS_F32 : TYPE> quantiser(__uint_as_float(top), finite);
   uint8_t* out = p.codes + (r >> 4) * p.k_tiles * 1024 + (r & 15) * 16;
-  for (int c = tid * 16; c < padded; c += kStep) {
+  for (int c = wave * 1024; c < padded; c += kStep) {
     v4u w[2] = {kept[0], kept[1]};
-    if (!KEEP) read16(h, c, p.n_cols, w);
-    const v4u q = codes16<TYPE, GAIN>(p, quantiser, w, c);
-    *reinterpret_cast<v4u*>(out + (int64_t)(c >> 4) * 256) = q;
-    if (p.held) hold16(p.held + r * p.n_cols, c, p.n_cols, q, row_scale);
+    if (!KEEP) read16<1>(h, c, p.n_cols, w);
+    put_codes<TYPE, GAIN, 1>(p, quantiser, w, c, out, p.held ? p.held + r * p.n_cols : nullptr, row_scale, true, words[wave]);
   }
 }
 
 // Many rows: a workgroup of as many wavefronts as the columns need, up to 8, per
 // two rows, a lane of which has 16 columns of one row, TIMES over, in registers.
-// Rows are read once, and codes written 32 bytes side by side: 7 bytes a value in all,
-// which bound it (8192 rows of 8192 columns, residual and gain: 111 us, 4.2 TB/s, a row a
-// workgroup 140; of 4096 columns 41 and 52; a workgroup per 16 rows, whose codes are
-// whole tiles, 60: it waits for all of its loads at once).
+// Rows are read once, and codes written 32 bytes side by side: 7 bytes a value in all, 11
+// with the values held, which bound it (8192 rows of 8192 columns with a residual: 93 us, 5.0
+// TB/s, with the values held 129 us, 5.7 TB/s; when a lane had 16 columns side by side, and its
+// stores pieces of lines, 111 and 186).  Four rows a workgroup: 102 and 142 us; 16, whose codes
+// are whole tiles, half as fast again: they wait for all of their loads at once.
 constexpr int kNormRows = 2, kNormWaves = 8;
 
 template <int TYPE, bool GAIN, int TIMES>
@@ -232,27 +272,28 @@ __global__ __launch_bounds__(64 * kNormWaves) void norm_pairs(NormArgs p) {
   __shared__ float sums[kNormWaves][kNormRows];
   __shared__ double wide[kNormWaves][kNormRows];
   __shared__ float scales[kNormRows];
+  __shared__ v4u words[kNormWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in = lane % kNormRows, waves = blockDim.x >> 6;
   const int64_t r = (int64_t)blockIdx.x * kNormRows + in;
   const bool there = r < p.n_tokens;
   const int64_t row = there ? r : p.n_tokens - 1;
   const uint16_t* x = p.x + row * p.x_stride;
-  auto column = [&](int i) { return (i * waves + wave) * kWide + lane / kNormRows * 16; };
+  auto column = [&](int i) { return (i * waves + wave) * kWide; };
   v4u w[TIMES][2];
 #pragma unroll
-  for (int i = 0; i < TIMES; ++i) read16(x, column(i), p.n_cols, w[i]);
+  for (int i = 0; i < TIMES; ++i) read16<kNormRows>(x, column(i), p.n_cols, w[i]);
   if (p.residual) {
     const uint16_t* add = p.residual + row * p.residual_stride;
 #pragma unroll
     for (int i = 0; i < TIMES; ++i) {
       v4u b[2];
-      read16(add, column(i), p.n_cols, b);
+      read16<kNormRows>(add, column(i), p.n_cols, b);
       add16<TYPE>(w[i], b);
     }
     // (rows behind the last one do its work, which may be over before they read)
     if (there) {
 #pragma unroll
-      for (int i = 0; i < TIMES; ++i) write16(p.sum + row * p.sum_stride, column(i), p.n_cols, w[i]);
+      for (int i = 0; i < TIMES; ++i) write16<kNormRows>(p.sum + row * p.sum_stride, column(i), p.n_cols, w[i], p.past);
     }
   }
   uint32_t top = 0;
@@ -261,7 +302,7 @@ __global__ __launch_bounds__(64 * kNormWaves) void norm_pairs(NormArgs p) {
   for (int i = 0; i < TIMES; ++i) {
     float f[16], g[16];
     unpack16<TYPE>(w[i], f);
-    if (GAIN) gain16(p.gain, column(i), p.n_cols, g);
+    if (GAIN) gain16<kNormRows>(p.gain, column(i), p.n_cols, g);
     measure16<GAIN>(f, g, top, squares);
   }
 #pragma unroll
@@ -305,16 +346,11 @@ __global__ __launch_bounds__(64 * kNormWaves) void norm_pairs(NormArgs p) {
   }
   if (p.held) lds_barrier();
   const Quantiser<GAIN ? AS_F32 : TYPE> quantiser(__uint_as_float(top), finite);
-  // (rows behind the last one are in its tile's storage)
   uint8_t* out = p.codes + (r >> 4) * p.k_tiles * 1024 + (r & 15) * 16;
 #pragma unroll
-  for (int i = 0; i < TIMES; ++i) {
-    const int c = column(i);
-    if (c >= p.k_tiles * 64) break;
-    const v4u q = codes16<TYPE, GAIN>(p, quantiser, w[i], c);
-    *reinterpret_cast<v4u*>(out + (int64_t)(c >> 4) * 256) = q;
-    if (p.held && there) hold16(p.held + r * p.n_cols, c, p.n_cols, q, scales[in]);
-  }
+  for (int i = 0; i < TIMES; ++i)
+    put_codes<TYPE, GAIN, kNormRows>(p, quantiser, w[i], column(i), out, p.held ? p.held + r * p.n_cols : nullptr, scales[in],
+                                     there, words[wave]);
 }
 
 template <int TYPE, bool GAIN>
@@ -389,6 +425,12 @@ extern "C" int as_norm_i8(const void* x, const void* residual, int32_t type, int
   p.n_cols = (int32_t)n_cols;
   p.k_tiles = (int32_t)(round_up(n_cols, 128) / 64);
   p.eps = eps;
+  // What one call reads and writes beyond the last cache's 256 MiB is not found there by the
+  // next one, and writing it past the caches is faster (8192 rows of 5000 columns 85 us and
+  // 62, of 8192 111 and 93; of 4096, which it holds, 41 and 46).  Held values, which have
+  // the most bytes, always are (2048 rows of 8192 columns 32 us and 31, 8192 of 8192 186
+  // and 129).
+  p.past = n_tokens * n_cols * (held ? 11 : 7) > (int64_t(256) << 20);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (type == AS_BF16)
     gain ? launch_norm<AS_BF16, true>(p, s) : launch_norm<AS_BF16, false>(p, s);
