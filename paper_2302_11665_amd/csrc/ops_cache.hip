@@ -56,10 +56,12 @@ struct AppendArgs {
 __device__ __forceinline__ int nibble(int e) { return 4 * ((e >> 1) + 4 * (e & 1)); }
 
 // What 8 channels of one token and head become, on one of the DIM/8 lanes that
-// hold it: their codes as a word of K and as a byte each, and the group's scale.
+// hold it: their codes as a word of K and as a byte each, the group's scale, and
+// the values that they stand for.
 struct Quantised {
   uint32_t word, bytes[2];
   _Float16 step, base;
+  float value[8];
 };
 
 // Codes are those of (x - m) / d rounded to fp32: the quotient is taken with the
@@ -74,7 +76,7 @@ __device__ __forceinline__ v4u read8(const uint16_t* x) {
   return raw;
 }
 template <int TYPE, int GROUP>
-__device__ __forceinline__ Quantised quantise8(const v4u& raw, float* held) {
+__device__ __forceinline__ Quantised quantise8(const v4u& raw) {
   float f[8];
   float low = kInf, high = -kInf;
   bool bad = false;
@@ -99,7 +101,6 @@ __device__ __forceinline__ Quantised quantise8(const v4u& raw, float* held) {
   const float m = (float)z.base, d = (float)z.step;
   const bool some = d > 0.0f;  // (not NaN)
   const float by = some ? 1.0f / d : 0.0f, from = some ? m : 0.0f, step = some ? d : 0.0f;
-  float out[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float y = f[e] - from;
@@ -109,11 +110,7 @@ __device__ __forceinline__ Quantised quantise8(const v4u& raw, float* held) {
     const uint32_t code = __float_as_uint(r) & 15u;
     z.word |= code << nibble(e);
     z.bytes[e >> 2] |= code << (8 * (e & 3));
-    out[e] = (r - 12582912.0f) * d + m;
-  }
-  if (held) {
-    __builtin_memcpy(held, out, 16);
-    __builtin_memcpy(held + 4, out + 4, 16);
+    z.value[e] = (r - 12582912.0f) * d + m;
   }
   return z;
 }
@@ -192,7 +189,9 @@ __global__ __launch_bounds__(256) void append(AppendArgs p) {
     float* held = is_v ? p.held_v : p.held_k;
     if (held) held += (((int64_t)b * p.n_tokens + t) * p.c.n_heads + h) * DIM + lane * 8;
     const int at = in_page + s;
-    put8<DIM, GROUP>(p.c, row, at, lane, is_v, quantise8<TYPE, GROUP>(read8(x), held), v_codes[s]);
+    const Quantised z = quantise8<TYPE, GROUP>(read8(x));
+    put8<DIM, GROUP>(p.c, row, at, lane, is_v, z, v_codes[s]);
+    if (held) __builtin_memcpy(held, z.value, 32);
     if (is_v && lane == 0) {
       if (p.c.pos) p.c.pos[row * p.c.page + at] = (int32_t)(p.first_pos ? p.first_pos[b] + t : first + s);
       if (p.c.acc) p.c.acc[row * p.c.page + at] = 0.0f;
@@ -233,12 +232,27 @@ struct PackedArgs {
 // wavefront at a time.  Few tokens cost a launch and a chain of loads (places, page,
 // values): 39 of 8 heads of 128 channels 5.9 us.  Many are bound by what they read and
 // write: 58,000 with the values held 103 us, 87 at the rate of a copy.
+// Writes one token's values from its DIM/8 lanes, 8 channels each, past the caches, 4
+// channels side by side to a lane at a time (`own`: LDS of the token).
+template <int DIM>
+__device__ __forceinline__ void put_held(float* held, int lane, const float (&value)[8], v4f* own) {
+  own[2 * lane] = v4f{value[0], value[1], value[2], value[3]};
+  own[2 * lane + 1] = v4f{value[4], value[5], value[6], value[7]};
+  __builtin_amdgcn_wave_barrier();
+  typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    __builtin_nontemporal_store((v4f_any)own[i * (DIM / 8) + lane], reinterpret_cast<v4f_any*>(held) + i * (DIM / 8) + lane);
+  __builtin_amdgcn_wave_barrier();
+}
+
 template <int TYPE, int DIM, int GROUP>
 __global__ __launch_bounds__(256) void append_packed(PackedArgs p) {
   constexpr int kLanes = DIM / 8, kWords = DIM / 8, kAtOnce = 256 / kLanes;
   __shared__ v2u v_codes[64][kLanes];  // of the tile's tokens and as many behind them
   __shared__ int64_t rows[64];         // page and head of each, -1: none
   __shared__ int32_t places[64];       // in the page
+  __shared__ v4f values[kAtOnce][2 * kLanes];
   const int wide = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // Within a long run one tile in 32 / tile begins a block and has work, the others
   // none: such tiles of all heads are neighbours in the grid, which deals workgroups
@@ -283,11 +297,13 @@ __global__ __launch_bounds__(256) void append_packed(PackedArgs p) {
     for (int j = 0; j < 2; ++j) {
       const int i = i0 + j * kAtOnce;
       if (i > last) continue;
-      const int64_t row = rows[i], u = t0 + i, held = (u * p.c.n_heads + h) * DIM + lane * 8;
+      const int64_t row = rows[i], u = t0 + i, held = (u * p.c.n_heads + h) * DIM;
       if (row < 0) continue;
       const int at = places[i];
-      const Quantised k = quantise8<TYPE, GROUP>(raw[j][0], p.held_k ? p.held_k + held : nullptr);
-      const Quantised v = quantise8<TYPE, GROUP>(raw[j][1], p.held_v ? p.held_v + held : nullptr);
+      const Quantised k = quantise8<TYPE, GROUP>(raw[j][0]), v = quantise8<TYPE, GROUP>(raw[j][1]);
+      v4f* own = values[threadIdx.x / kLanes];
+      if (p.held_k) put_held<DIM>(p.held_k + held, lane, k.value, own);
+      if (p.held_v) put_held<DIM>(p.held_v + held, lane, v.value, own);
       put8<DIM, GROUP>(p.c, row, at, lane, false, k, nullptr);
       put8<DIM, GROUP>(p.c, row, at, lane, true, v, v_codes[i]);
       if (lane == 0) {
