@@ -75,6 +75,20 @@ __device__ __forceinline__ v4u read8(const uint16_t* x) {
   __builtin_memcpy(&raw, x, 16);
   return raw;
 }
+
+// The value of the lane at the other end of a pair, of four lanes, of 8 and of 16,
+// or in the other pair: exchanges within a row of 16.
+template <int CTRL>
+__device__ __forceinline__ int row_exchange(int x) {
+  return __builtin_amdgcn_update_dpp(x, x, CTRL, 0xf, 0xf, true);
+}
+template <int CTRL>
+__device__ __forceinline__ void group_step(float& low, float& high, int& any) {
+  low = fminf(low, __int_as_float(row_exchange<CTRL>(__float_as_int(low))));
+  high = fmaxf(high, __int_as_float(row_exchange<CTRL>(__float_as_int(high))));
+  any |= row_exchange<CTRL>(any);
+}
+
 template <int TYPE, int GROUP>
 __device__ __forceinline__ Quantised quantise8(const v4u& raw) {
   float f[8];
@@ -84,34 +98,39 @@ __device__ __forceinline__ Quantised quantise8(const v4u& raw) {
   for (int e = 0; e < 8; ++e) {
     f[e] = to_f32<TYPE>(e & 1 ? raw[e >> 1] >> 16 : raw[e >> 1] & 0xffffu);
     bad |= f[e] != f[e];
-    f[e] = fminf(fmaxf(f[e], -65504.0f), 65504.0f);
+    f[e] = __builtin_amdgcn_fmed3f(f[e], -65504.0f, 65504.0f);  // (finite, a NaN too)
     low = fminf(low, f[e]);
     high = fmaxf(high, f[e]);
   }
   int any = bad;
-#pragma unroll
-  for (int o = 1; o < GROUP / 8; o <<= 1) {
-    low = fminf(low, __shfl_xor(low, o));
-    high = fmaxf(high, __shfl_xor(high, o));
-    any |= __shfl_xor(any, o);
-  }
+  static_assert(GROUP == 32 || GROUP == 64 || GROUP == 128, "4, 8 or 16 lanes to a group");
+  group_step<0xb1>(low, high, any);   // lanes 1, 0, 3, 2 of four
+  group_step<0x4e>(low, high, any);   // 2, 3, 0, 1
+  if (GROUP >= 64) group_step<0x141>(low, high, any);   // 8 lanes mirrored: the other four's
+  if (GROUP >= 128) group_step<0x140>(low, high, any);  // 16: the other 8's
   Quantised z{};
   z.base = any ? (_Float16)__builtin_nanf("") : (_Float16)low;
   z.step = any ? (_Float16)__builtin_nanf("") : (_Float16)((high - low) / 15.0f);
   const float m = (float)z.base, d = (float)z.step;
   const bool some = d > 0.0f;  // (not NaN)
   const float by = some ? 1.0f / d : 0.0f, from = some ? m : 0.0f, step = some ? d : 0.0f;
+  uint32_t r[8];  // the code in the lowest byte
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float y = f[e] - from;
     float q = y * by;
     q = fmaf(fmaf(-q, step, y), by, q);
-    const float r = __builtin_amdgcn_fmed3f(q, 0.0f, 15.0f) + 12582912.0f;
-    const uint32_t code = __float_as_uint(r) & 15u;
-    z.word |= code << nibble(e);
-    z.bytes[e >> 2] |= code << (8 * (e & 3));
-    z.value[e] = (r - 12582912.0f) * d + m;
+    const float whole = __builtin_amdgcn_fmed3f(q, 0.0f, 15.0f) + 12582912.0f;
+    r[e] = __float_as_uint(whole);
+    z.value[e] = (whole - 12582912.0f) * d + m;
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)  // elements 2 i and 2 i + 1: nibbles i and 4 + i
+    z.word |= __builtin_amdgcn_perm(r[2 * i + 1], r[2 * i], 0x0c040c00) << (4 * i);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    z.bytes[i] = __builtin_amdgcn_perm(r[4 * i + 1], r[4 * i], 0x0c0c0400) |
+                 __builtin_amdgcn_perm(r[4 * i + 3], r[4 * i + 2], 0x04000c0c);
   return z;
 }
 
@@ -132,29 +151,51 @@ __device__ __forceinline__ void put8(const CacheArgs& c, int64_t row, int at, in
   }
 }
 
-// Word w of a block of 32 slots of V from the codes of its slots lo..hi-1, where
-// slot s has the DIM codes of row s + shift; the other slots' bits stay.  SHARED:
-// others may write those meanwhile.  The slots' own bits are nobody else's: one atomic
-// clears them and one sets them, neither of which is waited for (a read and an exclusive
-// or of what has to change: 64 single tokens 9.0 us, so 6.9).
-template <int DIM, bool SHARED>
-__device__ __forceinline__ void put_v_word(uint32_t* v, int w, const uint8_t* codes, int lo, int hi, int shift) {
+// Word w of a block of 32 slots of V from the codes of its slots lo..hi-1, a row of
+// DIM each; the other slots' bits stay.
+template <int DIM>
+__device__ __forceinline__ void put_v_word(uint32_t* v, int w, const uint8_t* codes, int lo, int hi) {
   const int i = w % (DIM / 16), c = w / (DIM / 16) % 16, g = w / DIM;
   uint32_t mask = 0, word = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int s = 16 * (e >> 2) + 4 * g + (e & 3);
     if (s >= lo && s < hi) {
-      word |= (uint32_t)codes[(s + shift) * DIM + 16 * i + c] << nibble(e);
+      word |= (uint32_t)codes[s * DIM + 16 * i + c] << nibble(e);
       mask |= 15u << nibble(e);
     }
   }
   if (mask == 0xffffffffu)
     v[w] = word;
-  else if (mask && SHARED)
-    atomicAnd(&v[w], ~mask), atomicOr(&v[w], word);
   else if (mask)
     v[w] = (v[w] & ~mask) | word;
+}
+
+// A wavefront's part of a block of 32 slots of V, the words of slots 4 g.. and 16 + 4 g..,
+// from rows of codes, row 0 being slot 0's; only `slots` are the call's.  Others
+// may write the other slots' bits of a word meanwhile.  The slots' own bits are nobody
+// else's: one atomic clears them and one sets them, neither of which is waited for (a
+// read and an exclusive or of what has to change: 64 single tokens 9.0 us, so 6.9).
+// Rows of other slots are read and left out, so that no read waits for another.
+template <int DIM>
+__device__ __forceinline__ void put_v_words(uint32_t* v, int g, uint32_t slots, const uint8_t* codes) {
+  const int lane = threadIdx.x & 63;
+  uint32_t mask = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) mask |= (slots >> (16 * (e >> 2) + 4 * g + (e & 3)) & 1u) * (15u << nibble(e));
+#pragma unroll
+  for (int w = lane; w < DIM; w += 64) {
+    const int i = w % (DIM / 16), c = w / (DIM / 16);
+    uint32_t word = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      word |= (uint32_t)(codes[(16 * (e >> 2) + 4 * g + (e & 3)) * DIM + 16 * i + c] & 15) << nibble(e);
+    uint32_t* to = v + g * DIM + w;
+    if (mask == 0xffffffffu)
+      *to = word;
+    else
+      atomicAnd(to, ~mask), atomicOr(to, word & mask);
+  }
 }
 
 // One workgroup per (sequence, head, block of 32 slots).  DIM/8 lanes quantise
@@ -200,7 +241,7 @@ __global__ __launch_bounds__(256) void append(AppendArgs p) {
   __syncthreads();
   uint32_t* v = p.c.v + (row * p.c.page + in_page) * kWords;
   for (int w = threadIdx.x; w < 32 * kWords; w += 256)
-    put_v_word<DIM, false>(v, w, reinterpret_cast<const uint8_t*>(v_codes), lo, hi, 0);
+    put_v_word<DIM>(v, w, reinterpret_cast<const uint8_t*>(v_codes), lo, hi);
 }
 
 template <int TYPE>
@@ -224,14 +265,6 @@ struct PackedArgs {
   int32_t n_tokens, n_blocks, tile;  // blocks of 32 tokens; tokens whose runs a workgroup takes, at most 32
 };
 
-// One workgroup per (tile of packed tokens, head).  Neighbouring tokens of one
-// sequence on neighbouring slots of one block of 32 are a run; a workgroup takes
-// the runs that begin in its tile, whole, so that most words of V are written
-// in one store.  First all of its tokens are quantised side by side, then V's words
-// are written, a quarter of a run's block (the words of 8 of its slots) to a
-// wavefront at a time.  Few tokens cost a launch and a chain of loads (places, page,
-// values): 39 of 8 heads of 128 channels 5.9 us.  Many are bound by what they read and
-// write: 58,000 with the values held 103 us, 87 at the rate of a copy.
 // Writes one token's values from its DIM/8 lanes, 8 channels each, past the caches, 4
 // channels side by side to a lane at a time (`own`: LDS of the token).
 template <int DIM>
@@ -246,14 +279,25 @@ __device__ __forceinline__ void put_held(float* held, int lane, const float (&va
   __builtin_amdgcn_wave_barrier();
 }
 
+// One workgroup per (tile of packed tokens, head).  Neighbouring tokens of one
+// sequence on neighbouring slots of one block of 32 are a run; a workgroup takes
+// the runs that begin in its tile, whole, so that most words of V are written
+// in one store.  First all of its tokens are quantised side by side, then V's words
+// are written, a quarter of a run's block (the words of 8 of its slots) to a
+// wavefront at a time.  Few tokens cost a launch and a chain of loads (places, page,
+// values): 39 of 8 heads of 128 channels 5.9 us.  Many are bound by what they read and
+// write: 58,000 with the values held 103 us, 87 at the rate of a copy.
 template <int TYPE, int DIM, int GROUP>
 __global__ __launch_bounds__(256) void append_packed(PackedArgs p) {
   constexpr int kLanes = DIM / 8, kWords = DIM / 8, kAtOnce = 256 / kLanes;
-  __shared__ v2u v_codes[64][kLanes];  // of the tile's tokens and as many behind them
+  // places for values; then V's codes of the tile's tokens and as many behind them
+  constexpr int kValues = kAtOnce * kLanes * 32;
+  static_assert(kValues >= 31 * DIM, "rows up to 31 before the first are read, and left out");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kValues + 64 * DIM];
+  auto v_codes = reinterpret_cast<v2u (*)[kLanes]>(lds + kValues);
   __shared__ int64_t rows[64];         // page and head of each, -1: none
   __shared__ int32_t places[64];       // in the page
-  __shared__ v4f values[kAtOnce][2 * kLanes];
-  const int wide = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wide = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Within a long run one tile in 32 / tile begins a block and has work, the others
   // none: such tiles of all heads are neighbours in the grid, which deals workgroups
   // to the XCDs in turn.  (With tiles in the order of their tokens, those that had work
@@ -301,7 +345,7 @@ __global__ __launch_bounds__(256) void append_packed(PackedArgs p) {
       if (row < 0) continue;
       const int at = places[i];
       const Quantised k = quantise8<TYPE, GROUP>(raw[j][0]), v = quantise8<TYPE, GROUP>(raw[j][1]);
-      v4f* own = values[threadIdx.x / kLanes];
+      v4f* own = reinterpret_cast<v4f*>(lds) + threadIdx.x / kLanes * 2 * kLanes;
       if (p.held_k) put_held<DIM>(p.held_k + held, lane, k.value, own);
       if (p.held_v) put_held<DIM>(p.held_v + held, lane, v.value, own);
       put8<DIM, GROUP>(p.c, row, at, lane, false, k, nullptr);
@@ -313,17 +357,14 @@ __global__ __launch_bounds__(256) void append_packed(PackedArgs p) {
     }
   }
   lds_barrier();
-  const uint8_t* codes = reinterpret_cast<const uint8_t*>(v_codes);
   for (; begins; begins &= begins - 1) {
     const int i = __builtin_ctzll(begins);
     const int n = 1 + (i < 63 ? (int)__builtin_ctzll(~(in_run >> (i + 1))) : 0);  // at most 32
     const int64_t row = rows[i];
-    const int at = places[i], lo = at % 32;
+    const int at = __builtin_amdgcn_readfirstlane(places[i]), lo = at % 32;
     const uint32_t slots = (n < 32 ? (1u << n) - 1 : ~0u) << lo;
     if (row < 0 || !(slots & 0x000f000fu << (4 * wave))) continue;  // slots 4 wave.. and 16 + 4 wave..
-    uint32_t* v = p.c.v + (row * p.c.page + at - lo) * kWords;
-#pragma unroll
-    for (int w = 0; w < DIM; w += 64) put_v_word<DIM, true>(v, wave * DIM + w + wide, codes, lo, lo + n, i - lo);
+    put_v_words<DIM>(p.c.v + (row * p.c.page + at - lo) * kWords, wave, slots, lds + kValues + (i - lo) * DIM);
   }
 }
 
