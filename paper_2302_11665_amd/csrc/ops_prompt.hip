@@ -38,6 +38,8 @@ struct PromptArgs {
   const int32_t* offsets;
   int32_t n_tokens, n_seqs, n_heads, group;  // key/value heads; query heads to each
   float factor;                              // scale log2 e
+  int32_t part_tiles, n_parts;               // of a split block (below), or 0
+  float* parts;
 };
 
 template <int TYPE>
@@ -76,6 +78,13 @@ __device__ __forceinline__ Sequence sequence(const PromptArgs& p, int b) {
 template <int ROWS>
 __device__ __forceinline__ int blocks_of(const PromptArgs& p, int length) {
   return (int)((uint32_t)(length * p.group + ROWS - 1) / ROWS);
+}
+
+// Tiles of 64 keys that a block's rows see.
+constexpr int kKeys = 64;
+template <int ROWS>
+__device__ __forceinline__ int tiles_of(const PromptArgs& p, int length, int block) {
+  return min(block * ROWS + ROWS - 1, length * p.group - 1) / p.group / kKeys + 1;
 }
 
 // What a workgroup works on: a block of a sequence.
@@ -168,8 +177,6 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan(PromptArgs p, Item* 
   }
 }
 
-constexpr int kKeys = 64;  // keys of a stage
-
 // Rows of a stage lie in LDS as in memory, in pieces of 16 bytes whose order is
 // swapped around by key: 16 keys at one piece (K's operand) and 4 keys at two
 // pieces side by side (V's) then fall on different banks.
@@ -200,9 +207,12 @@ constexpr uint16_t kInfinity = TYPE == AS_BF16 ? 0x7f80 : 0x7c00;
 // written) it is done again, CAREFUL: at keys that some of its rows do not see,
 // values that are not finite are left out of the product and reach the rows that see
 // them by products of their marks with a mask.
-template <int TYPE, int DIM, int WAVES, bool CAREFUL>
+//
+// SPLIT: its tiles of keys from first to end; sums, the reference of the weights and
+// their sums go to `part`.
+template <int TYPE, int DIM, int WAVES, bool CAREFUL, bool SPLIT>
 __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)[2][kKeys * DIM * 2], int head, int begin,
-                                             int length, int block) {
+                                             int length, int block, int first, int end, float* part) {
   constexpr int kRows = 32 * WAVES, kRowBytes = DIM * 2, kTile = kKeys * kRowBytes;
   constexpr int kLoads = kTile / 1024 / WAVES;  // of K and of V, by a wavefront, a stage
   constexpr int kPieces = kRowBytes / 16, kPerLoad = 1024 / kRowBytes;  // keys of a load
@@ -214,9 +224,10 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
   const int row = min(row0 + col, rows - 1), pos = row / p.group, member = row - pos * p.group;
   // tiles that all rows of the block see whole, that this wavefront's rows see, and
   // that any row does
-  const int open = (block * kRows / p.group + 1) / kKeys;
-  const int mine = min(row0 + 31, rows - 1) / p.group / kKeys + 1;
-  const int tiles = min(block * kRows + kRows - 1, rows - 1) / p.group / kKeys + 1;
+  if (!SPLIT) first = 0, end = INT32_MAX;
+  const int open = min((block * kRows / p.group + 1) / kKeys, end);
+  const int mine = min(min(row0 + 31, rows - 1) / p.group / kKeys + 1, end);
+  const int tiles = min(tiles_of<kRows>(p, length, block), end);
 
   v8s q[kSteps];
   {
@@ -357,9 +368,9 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
 #pragma unroll
   for (int i = 0; i < kDimTiles; ++i) o[i] = v16f{};
   reference = -1e30f, total = 0.0f;
-  bring_k(0);
-  if (tiles > 1) bring_k(1);
-  bring_v(0);
+  bring_k(first);
+  if (first + 1 < tiles) bring_k(first + 1);
+  bring_v(first);
   // V of this tile and K of the one behind the next are there, and all are done with
   // V of the last tile and K of the next.
   auto turn = [&] {
@@ -374,16 +385,16 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
   };
   v16f s[2], next[2];
   v8s weights[4];
-  int tile = 0;
-  if (tiles > 1)
+  int tile = first;
+  if (first + 1 < tiles)
     wait_loads<2 * kLoads>();
   else
     wait_loads<kLoads>();
   lds_barrier();  // K of the first tile is there
-  scores(0, s);
+  scores(first, s);
   wait_loads<kLoads>();
   lds_barrier();  // and of the second, and all are done with the first
-  if (tiles > 2) bring_k(2);
+  if (first + 2 < tiles) bring_k(first + 2);
   // A wavefront makes the scores of a tile while it turns the last one's into
   // weights, so that its matrix and vector instructions overlap.  Where heads have 64
   // channels, three wavefronts a SIMD overlap instead, which have no registers for two
@@ -453,6 +464,19 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
       return false;
     }
   }
+  if (SPLIT) {  // channels 4 c.. of row r at [c][r]
+#pragma unroll
+    for (int i = 0; i < kDimTiles; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        reinterpret_cast<v4f*>(part)[(i * 8 + r / 2 + half) * kRows + wave * 32 + col] =
+            v4f{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
+    if (half == 0) {
+      part[DIM * kRows + wave * 32 + col] = reference;
+      part[(DIM + 1) * kRows + wave * 32 + col] = total;
+    }
+    return true;
+  }
   // Rows go through LDS, where a row's lanes leave them 8 bytes each, and out as
   // whole lines.
   int late = lane;  // (what follows from it is computed here, not kept in registers all along)
@@ -482,32 +506,92 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
 }
 
 // (a function of its own: what it keeps in registers costs the ordinary case none)
-template <int TYPE, int DIM, int WAVES>
+template <int TYPE, int DIM, int WAVES, bool SPLIT>
 __device__ __attribute__((noinline)) void attend_block_again(PromptArgs p, uint8_t (*lds)[2][kKeys * DIM * 2],
-                                                             int head, int begin, int length, int block) {
-  attend_block<TYPE, DIM, WAVES, true>(p, lds, head, begin, length, block);
+                                                             int head, int begin, int length, int block, int first,
+                                                             int end, float* part) {
+  attend_block<TYPE, DIM, WAVES, true, SPLIT>(p, lds, head, begin, length, block, first, end, part);
 }
+
+// How a workgroup finds its block: in the list, or among few sequences; SPLIT: the
+// same, and a part of it.
+enum { kListed, kSearched, kSplit };
+
+// Floats of a part: its rows' sums, references and sums of weights.
+template <int DIM, int ROWS>
+constexpr int64_t kPart = (DIM + 2) * ROWS;
 
 // Two or three wavefronts a SIMD, heads of 64 channels: 29 ragged prompts 352 and 332 us,
 // 12,001 tokens 721 and 691, 33 tokens 8.5 and 6.7.  Those of 128 channels have registers
 // for two.
-template <int TYPE, int DIM, int WAVES, bool PLAN>
+template <int TYPE, int DIM, int WAVES, int HOW>
 __global__ __launch_bounds__(64 * WAVES, DIM == 64 ? 3 : 2) void prompt_attention(PromptArgs p, const Item* items) {
   // of two tiles: K, V.  (Memory of a size given at the launch: reads of an array of
   // the kernel's own are made to wait for all loads on their way to it, those of the
   // next tiles among them.)
   extern __shared__ __attribute__((aligned(1024))) uint8_t stages[];
   auto lds = reinterpret_cast<uint8_t (*)[2][kKeys * DIM * 2]>(stages);
+  constexpr int kRows = 32 * WAVES;
+  constexpr bool kParts = HOW == kSplit;
   const int head = blockIdx.x % p.n_heads, at = blockIdx.x / p.n_heads;
+  const int n_items = kParts ? gridDim.x / p.n_heads / p.n_parts : 0, which = kParts ? at / n_items : 0;
   Item item;
-  if (PLAN) {
+  if (HOW == kListed) {
     item = items[at];
     if (item.none) return;
-  } else if (!find_block<32 * WAVES>(p, at, item)) {
+  } else if (!find_block<kRows>(p, kParts ? at % n_items : at, item)) {
     return;
   }
-  if (!attend_block<TYPE, DIM, WAVES, false>(p, lds, head, item.begin, item.length, item.block))
-    attend_block_again<TYPE, DIM, WAVES>(p, lds, head, item.begin, item.length, item.block);
+  const int first = which * p.part_tiles;
+  const int end = which + 1 < p.n_parts ? first + p.part_tiles : INT32_MAX;  // (the last one takes the rest)
+  float* part = nullptr;
+  if (kParts) {
+    if (first >= tiles_of<kRows>(p, item.length, item.block)) return;
+    part = p.parts + ((int64_t)(at % n_items * p.n_heads + head) * p.n_parts + which) * kPart<DIM, kRows>;
+  }
+  if (!attend_block<TYPE, DIM, WAVES, false, kParts>(p, lds, head, item.begin, item.length, item.block, first, end, part))
+    attend_block_again<TYPE, DIM, WAVES, kParts>(p, lds, head, item.begin, item.length, item.block, first, end, part);
+}
+
+// Joins the parts of a block: sums and sums of weights, brought to the largest
+// reference.  A workgroup per 32 rows, 8 of them a wavefront, a row to 8 lanes, which
+// have 4 channels of 32 each.
+template <int TYPE, int DIM, int WAVES>
+__global__ __launch_bounds__(256) void prompt_join(PromptArgs p) {
+  constexpr int kRows = 32 * WAVES, kTimes = DIM / 32;
+  const int at = blockIdx.x / WAVES, head = at % p.n_heads, lane = threadIdx.x & 63;
+  const int in = blockIdx.x % WAVES * 32 + (threadIdx.x >> 6) * 8 + lane % 8;
+  Item item;
+  if (!find_block<kRows>(p, at / p.n_heads, item)) return;
+  const int row = item.block * kRows + in;
+  if (row >= item.length * p.group) return;
+  const int parts = min((tiles_of<kRows>(p, item.length, item.block) + p.part_tiles - 1) / p.part_tiles, p.n_parts);
+  const float* from = p.parts + (int64_t)at * p.n_parts * kPart<DIM, kRows> + in;
+  float top = from[DIM * kRows];
+#pragma unroll 4
+  for (int i = 1; i < parts; ++i) top = fmaxf(top, from[i * kPart<DIM, kRows> + DIM * kRows]);
+  v4f sum[kTimes] = {};
+  float total = 0.0f;
+#pragma unroll 2
+  for (int i = 0; i < parts; ++i) {
+    const float* x = from + i * kPart<DIM, kRows>;
+    const float by = __builtin_amdgcn_exp2f(x[DIM * kRows] - top);
+    total = fmaf(x[(DIM + 1) * kRows], by, total);
+#pragma unroll
+    for (int k = 0; k < kTimes; ++k) {
+      const v4f four = *reinterpret_cast<const v4f*>(x - in + ((int64_t)(k * 8 + lane / 8) * kRows + in) * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[k][e] = fmaf(four[e], by, sum[k][e]);
+    }
+  }
+  const float by = 1.0f / total;
+  const int query = row / p.group;
+  uint16_t* to =
+      p.out + ((int64_t)(item.begin + query) * p.n_heads * p.group + head * p.group + row - query * p.group) * DIM;
+#pragma unroll
+  for (int k = 0; k < kTimes; ++k)
+    *reinterpret_cast<v2u*>(to + (k * 8 + lane / 8) * 4) =
+        v2u{pack_two<TYPE>(sum[k][0] * by, sum[k][1] * by), pack_two<TYPE>(sum[k][2] * by, sum[k][3] * by)};
 }
 
 constexpr int kPromptWaves = 4;
@@ -522,17 +606,44 @@ int64_t prompt_items(int64_t n_tokens, int64_t n_seqs, int64_t group) {
 // 9.0 and 6.7 us, 8 of 200 20.1 and 16.3, 64 of 700 81 and 74, 29 ragged ones 324 and 332.
 bool prompt_planned(int64_t n_seqs) { return n_seqs > 64; }
 
+// Where there are few blocks, the longest of which take much longer than all of them
+// would together, they are split into parts of so many tiles of keys, and joined by
+// another launch.  Lengths are on the device: the host counts as if all tokens were one
+// prompt's, or the longest of several nearly twice as long as they are on average.  Not split,
+// a block takes 9 us and 1.1 for each of its tiles; split, all take 22 us and 2 for each of a
+// workgroup's share of all tiles.  Not split and split, heads of 128 channels: 12,000 tokens
+// of one head 208 and 63 us, of 6000 of 4 in a group 109 and 64, 1500 of 8 heads 36 and 28;
+// of 2048 tokens of 32 heads in groups of 4 52 and 59, which the rule leaves whole.
+struct Split {
+  int tiles, parts;  // 0: not split
+};
+Split prompt_split(int64_t n_tokens, int64_t n_seqs, int64_t n_heads, int64_t group) {
+  if (prompt_planned(n_seqs)) return {0, 0};
+  const int64_t room = 2 * as_host::compute_units(), blocks = (n_tokens * group + 127) / 128;
+  const int64_t longest = (2 * n_tokens / (n_seqs + 1) + kKeys - 1) / kKeys;
+  const int64_t share = (n_heads * blocks * (longest + 1) / 2 + room - 1) / room;
+  if (11 * longest <= 130 + 20 * share) return {0, 0};
+  const int64_t tiles = std::max<int64_t>(4, share + share / 3 + 2);
+  return {(int)tiles, (int)((longest + tiles - 1) / tiles)};
+}
+
 template <int TYPE, int DIM>
-void launch_prompt(const PromptArgs& p, Item* items, hipStream_t s) {
+void launch_prompt(PromptArgs p, void* workspace, hipStream_t s) {
   const int n = (int)prompt_items(p.n_tokens, p.n_seqs, p.group);
   const dim3 g((unsigned)(n * p.n_heads)), t(64 * kPromptWaves);
   constexpr size_t kLds = 4 * kKeys * DIM * 2;
   static_assert(kLds <= 64 * 1024, "more has to be allowed for a kernel");
+  const Split split = prompt_split(p.n_tokens, p.n_seqs, p.n_heads, p.group);
   if (prompt_planned(p.n_seqs)) {
+    Item* items = reinterpret_cast<Item*>(workspace);
     hipLaunchKernelGGL((prompt_plan<32 * kPromptWaves>), dim3(1), dim3(kPlanThreads), 0, s, p, items, n);
-    hipLaunchKernelGGL((prompt_attention<TYPE, DIM, kPromptWaves, true>), g, t, kLds, s, p, items);
+    hipLaunchKernelGGL((prompt_attention<TYPE, DIM, kPromptWaves, kListed>), g, t, kLds, s, p, items);
+  } else if (split.tiles) {
+    p.part_tiles = split.tiles, p.n_parts = split.parts, p.parts = reinterpret_cast<float*>(workspace);
+    hipLaunchKernelGGL((prompt_attention<TYPE, DIM, kPromptWaves, kSplit>), dim3(g.x * split.parts), t, kLds, s, p, nullptr);
+    hipLaunchKernelGGL((prompt_join<TYPE, DIM, kPromptWaves>), dim3(g.x * kPromptWaves), dim3(256), 0, s, p);
   } else {
-    hipLaunchKernelGGL((prompt_attention<TYPE, DIM, kPromptWaves, false>), g, t, kLds, s, p, nullptr);
+    hipLaunchKernelGGL((prompt_attention<TYPE, DIM, kPromptWaves, kSearched>), g, t, kLds, s, p, nullptr);
   }
 }
 
@@ -543,8 +654,11 @@ using namespace as_ops;
 extern "C" {
 
 int64_t as_attention_prompt_workspace(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_seqs) {
-  if (n_tokens < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || !prompt_planned(n_seqs)) return 0;
-  return round_up(prompt_items(n_tokens, n_seqs, n_q_heads / n_kv_heads) * (int64_t)sizeof(Item), 256);
+  if (n_tokens < 1 || n_kv_heads < 1 || n_q_heads < n_kv_heads || n_seqs < 1) return 0;
+  const int64_t group = n_q_heads / n_kv_heads, n = prompt_items(n_tokens, n_seqs, group);
+  if (prompt_planned(n_seqs)) return round_up(n * (int64_t)sizeof(Item), 256);
+  const Split split = prompt_split(n_tokens, n_seqs, n_kv_heads, group);
+  return round_up(n * n_kv_heads * split.parts * kPart<128, 32 * kPromptWaves> * (int64_t)sizeof(float), 256);
 }
 
 int as_attention_prompt(const void* q, const void* k, const void* v, int32_t type, int64_t n_tokens,
@@ -596,11 +710,10 @@ int as_attention_prompt(const void* q, const void* k, const void* v, int32_t typ
   p.group = group;
   p.factor = scale * 1.44269504f;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  Item* items = reinterpret_cast<Item*>(workspace);
   if (type == AS_BF16)
-    dim == 64 ? launch_prompt<AS_BF16, 64>(p, items, s) : launch_prompt<AS_BF16, 128>(p, items, s);
+    dim == 64 ? launch_prompt<AS_BF16, 64>(p, workspace, s) : launch_prompt<AS_BF16, 128>(p, workspace, s);
   else
-    dim == 64 ? launch_prompt<AS_F16, 64>(p, items, s) : launch_prompt<AS_F16, 128>(p, items, s);
+    dim == 64 ? launch_prompt<AS_F16, 64>(p, workspace, s) : launch_prompt<AS_F16, 128>(p, workspace, s);
   return launched("attention_prompt");
 }
 

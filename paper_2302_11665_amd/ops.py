@@ -307,7 +307,7 @@ def attention_prompt(q, k, v, offsets, scale=None, out=None):
         _bad("attention_prompt: out is contiguous and of q's shape, type and device")
     L = lib()
     seqs, kv_heads = offsets.shape[0] - 1, k.shape[1]
-    need = L.as_attention_prompt_workspace(t, heads, kv_heads, seqs)
+    need = _on(L.as_attention_prompt_workspace, dev, t, heads, kv_heads, seqs)
     _keep, ws = _workspace(need, dev)
     _call(L.as_attention_prompt, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), _TYPES[q.dtype], t, heads, kv_heads,
           dim, q_token, k_token, v_token, offsets.data_ptr(), seqs, dim ** -0.5 if scale is None else scale,

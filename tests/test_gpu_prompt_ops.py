@@ -338,6 +338,60 @@ def test_prompt_does_not_see_what_is_masked(dtype, dim, heads):
     assert torch.equal(out[:at[4]], want[:at[4]]) and (out[at[4]:] == 5).all()
 
 
+# Few heads and long prompts: blocks are split, and the last part takes what the host did not expect.
+SPLIT = [([1500], 1, 1, 128), ([4000, 30, 0, 700], 1, 1, 64), ([40, 0, 3300, 1], 6, 2, 128), ([900] * 7, 1, 1, 64),
+         ([64 * 30], 1, 1, 128), ([2049], 3, 1, 64)]
+
+
+@pytest.mark.parametrize("case", SPLIT, ids=[str(i) for i in range(len(SPLIT))])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_split_prompt(case, dtype):
+    lengths, heads, kv_heads, dim = case
+    say("split prompt", case, dtype)
+    assert ops.lib().as_attention_prompt_workspace(sum(lengths), heads, kv_heads, len(lengths)) > 0
+    q, k, v, offsets = prompt(gen(sum(lengths) + heads), lengths, heads, kv_heads, dim, dtype)
+    out = ops.attention_prompt(q, k, v, offsets)
+    check_prompt(q, k, v, lengths, out)
+    graph, held = torch.cuda.CUDAGraph(), torch.zeros_like(out)
+    with torch.cuda.graph(graph):
+        ops.attention_prompt(q, k, v, offsets, out=held)
+    for _ in range(3):
+        held.zero_()
+        graph.replay()
+        again = ops.attention_prompt(q, k, v, offsets)
+        torch.cuda.synchronize()
+        assert torch.equal(held, out) and torch.equal(again, out)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_split_prompt_does_not_see_what_is_masked(dtype, dim):
+    say("split, masked", dtype, dim)
+    g = gen(dim + 1)
+    lengths = [1700, 300]
+    q, k, v, offsets = prompt(g, lengths, 2, 1, dim, dtype, behind=40)
+    assert ops.lib().as_attention_prompt_workspace(2040, 2, 1, 2) > 0
+    want = ops.attention_prompt(q, k, v, offsets)
+    for value in (float("nan"), float("inf"), -float("inf")):
+        for bad, end in ((45, 1700), (255, 1700), (256, 1700), (1023, 1700), (1699, 1700), (1800, 2000), (2010, 2040)):
+            for which in ("k", "v"):
+                kk, vv = k.clone(), v.clone()
+                if which == "k":
+                    kk[bad] = value
+                else:
+                    vv[bad, 0, ::3] = value
+                out = ops.attention_prompt(q, kk, vv, offsets)
+                clean = [i for i in range(2000) if not bad <= i < end]
+                assert torch.equal(out[clean], want[clean]), (value, bad, which)
+                if which == "v" and end <= 2000:
+                    rest = torch.ones(dim, dtype=torch.bool)
+                    rest[::3] = False
+                    assert not torch.isfinite(out[bad:end][:, :, ::3]).any()
+                    assert torch.equal(out[bad:end][:, :, rest], want[bad:end][:, :, rest])
+                if which == "k" and end <= 2000 and value != value:
+                    assert torch.isnan(out[bad:end]).all()
+
+
 def test_prompt_of_opposite_infinities():
     """A row that sees both signs is NaN there, one that sees one of them has it."""
     g = gen(4)

@@ -71,6 +71,23 @@ def test_prompt_refusals(L):
     assert call(n=0, q=None) == sim.AS_OK and call(seqs=0, off=None) == sim.AS_OK
 
 
+def test_long_prompts_of_few_heads_need_scratch_memory(L):
+    need = L.as_attention_prompt_workspace(3000, 1, 1, 1)
+    assert need > 24 * 128 * 130 * 4  # a part for every block of 128 rows at least
+
+    def call(ws=None, wb=0):
+        return L.as_attention_prompt(0x1000000, 0x2000000, 0x3000000, 0, 3000, 1, 1, 64, 64, 64, 64, 0x400, 1, 0.1,
+                                     0x4000000, ws, wb, None)
+
+    for kw in (dict(), dict(wb=need - 1, ws=0x1000), dict(wb=need), dict(wb=need, ws=0x1010)):
+        assert call(**kw) == sim.AS_E_INVALID_ARG, kw
+    # and no more than 512 MiB, whatever the sizes
+    for tokens in (100, 1000, 5000, 20000, 100000, 1 << 20, 1 << 26):
+        for heads in (1, 2, 4, 8, 16, 64):
+            for seqs in (1, 2, 7, 64):
+                assert 0 <= L.as_attention_prompt_workspace(tokens, heads, heads, seqs) <= 512 << 20
+
+
 def test_pages_refusals(L):
     def reserve(stack=0x100, count=0x200, pages=8, table=0x300, seqs=2, mp=4, page=32, length=0x400, add=0x500, n=10,
                 nc=0x600, nl=0x700, off=0x800, seq=0x900, slot=0xa00, ws=0x1000, wb=1 << 20):
