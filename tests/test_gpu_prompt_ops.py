@@ -126,7 +126,8 @@ def test_norm_in_place_and_of_strided_rows(rows, cols):
 
 
 @pytest.mark.parametrize("t,k,n", [(1, 300, 77), (5, 4096, 130), (16, 512, 256), (17, 129, 4097), (40, 2048, 96),
-                                   (64, 1024, 1024), (100, 640, 300), (777, 1500, 2777), (2100, 900, 33)])
+                                   (64, 1024, 1024), (100, 640, 300), (777, 1500, 2777), (2100, 900, 33),
+                                   (333, 100, 8200), (385, 260, 5555)])
 @pytest.mark.parametrize("dtype,y_dtype,bias", [(BF16, BF16, False), (F16, F32, True), (BF16, F16, True)])
 def test_linear_of_codes(t, k, n, dtype, y_dtype, bias):
     say("linear of codes", t, k, n, dtype, y_dtype)
