@@ -284,6 +284,13 @@ def test_long_prompt(n, heads, kv_heads, dim, dtype):
     check_prompt(q[n:], k[n:], v[n:], [10], out[n:])
 
 
+@pytest.mark.parametrize("lengths,heads,kv_heads", [([1200], 32, 8), ([500, 3, 700, 0, 40], 32, 8), ([900, 333], 30, 10)])
+def test_prompt_of_as_many_blocks_as_run_at_once(lengths, heads, kv_heads):
+    say("two blocks a unit", lengths, heads)
+    q, k, v, offsets = prompt(gen(heads), lengths, heads, kv_heads, 128, BF16)
+    check_prompt(q, k, v, lengths, ops.attention_prompt(q, k, v, offsets))
+
+
 @pytest.mark.parametrize("way", ["up", "down", "flat"])
 @pytest.mark.parametrize("dtype", [BF16, F16])
 def test_prompt_where_the_maximum_moves(way, dtype):
