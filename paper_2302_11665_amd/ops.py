@@ -164,14 +164,8 @@ class Codes:
     dtype: torch.dtype
 
 
-def norm_i8(x, residual=None, gain=None, eps=1e-6, out=None, held=False):
-    """Rows of x [..., columns] (bf16 or fp16), or of x + residual rounded to
-    their type, brought to mean square 1, times gain [columns] (fp32), in 8 bits
-    for `linear_i8`: (Codes, the sum, which is x without a residual), with
-    `held` also the values that the codes stand for (fp32, x's shape).  `out`, if
-    given, gets the sum: [rows, columns] with contiguous rows that do not
-    overlap; it may be x or the residual."""
-    L = lib()
+def _norm_args(x, residual, gain, out):
+    """x and the residual as rows, their strides, and the sum: `norm_i8`'s checks."""
     _need(x, "x", _16, contiguous=False)
     dev = x.device
     if x.dim() < 1 or x.shape[-1] < 1:
@@ -194,6 +188,33 @@ def norm_i8(x, residual=None, gain=None, eps=1e-6, out=None, held=False):
         _bad("norm_i8: out without a residual")
     if gain is not None and _need(gain, "gain", (torch.float32,), 1, dev).numel() != cols:
         _bad(f"norm_i8: {gain.numel()} gains for {cols} columns")
+    return x2, x_stride, r2, r_stride, s, s_stride
+
+
+def norm_i8(x, residual=None, gain=None, eps=1e-6, out=None, held=False):
+    """Rows of x [..., columns] (bf16 or fp16), or of x + residual rounded to
+    their type, brought to mean square 1, times gain [columns] (fp32), in 8 bits
+    for `linear_i8`: (Codes, the sum, which is x without a residual), with
+    `held` also the values that the codes stand for (fp32, x's shape).  `out`, if
+    given, gets the sum: [rows, columns] with contiguous rows that do not
+    overlap; it may be x or the residual."""
+    L = lib()
+    try:  # one cheap look at everything first: most calls need no more
+        dev, dtype, (t, cols), x_stride = x.device, x.dtype, x.shape, x.stride(0)
+        plain = (x.is_cuda and dtype in _16 and t > 0 and cols > 1 and x.stride(1) == 1 and x_stride >= cols and out is None
+                 and (residual is None or (residual.dtype is dtype and residual.shape == x.shape and residual.device == dev
+                                           and residual.stride(1) == 1 and residual.stride(0) >= cols))
+                 and (gain is None or (gain.dtype is torch.float32 and gain.shape == (cols,) and gain.device == dev
+                                       and gain.is_contiguous())))
+    except (AttributeError, ValueError, TypeError, IndexError):
+        plain = False
+    if plain:
+        x2, r2, r_stride, s, s_stride = x, residual, 0, None, 0
+        if residual is not None:
+            r_stride, s, s_stride = residual.stride(0), torch.empty_like(x, memory_format=torch.contiguous_format), cols
+    else:
+        x2, x_stride, r2, r_stride, s, s_stride = _norm_args(x, residual, gain, out)
+        dev, (t, cols) = x.device, x2.shape
     codes = torch.empty(L.as_i8_bytes(t, cols), dtype=torch.int8, device=dev)
     scale = torch.empty(t, dtype=torch.float32, device=dev)
     values = torch.empty(x.shape, dtype=torch.float32, device=dev) if held else None
@@ -288,18 +309,30 @@ def attention_prompt(q, k, v, offsets, scale=None, out=None):
     itself, head j to key/value head j / (q_heads / kv_heads).  `scale` defaults
     to dim ** -0.5.  Rows of no sequence are not written: give `out` (contiguous,
     q's shape) where what they hold matters."""
-    q, q_token = _packed(q, "q")
-    dev, (t, heads, dim) = q.device, q.shape
-    k, k_token = _packed(k, "k", q.dtype, dev, dim)
-    v, v_token = _packed(v, "v", q.dtype, dev, dim)
-    if k.shape != v.shape or k.shape[0] != t:
-        _bad(f"attention_prompt: q has {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
+    try:  # one cheap look at everything first: most calls need no more
+        dev, dtype, (t, heads, dim) = q.device, q.dtype, q.shape
+        (q_token, q_head, q_step), (k_token, k_head, k_step), (v_token, v_head, v_step) = q.stride(), k.stride(), v.stride()
+        at = q.data_ptr(), k.data_ptr(), v.data_ptr()
+        plain = (q.is_cuda and dtype in _16 and k.dtype is dtype and v.dtype is dtype and k.device == v.device == dev
+                 and t > 1 and k.shape == v.shape == (t, k.shape[1], dim) and q_step == k_step == v_step == 1
+                 and q_head == k_head == v_head == dim and not (at[0] | at[1] | at[2]) & 15
+                 and not (q_token | k_token | v_token) & 7)
+    except (AttributeError, ValueError, TypeError, IndexError):
+        plain = False
+    if not plain:
+        q, q_token = _packed(q, "q")
+        dev, (t, heads, dim) = q.device, q.shape
+        k, k_token = _packed(k, "k", q.dtype, dev, dim)
+        v, v_token = _packed(v, "v", q.dtype, dev, dim)
+        if k.shape != v.shape or k.shape[0] != t:
+            _bad(f"attention_prompt: q has {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
+        q, q_token = _aligned_rows(q, q_token)
+        k, k_token = _aligned_rows(k, k_token)
+        v, v_token = _aligned_rows(v, v_token)
+        at = q.data_ptr(), k.data_ptr(), v.data_ptr()
     if not (isinstance(offsets, torch.Tensor) and offsets.dtype is torch.int32 and offsets.dim() == 1
             and offsets.shape[0] >= 1 and offsets.device == dev and offsets.is_contiguous()):
         _bad("attention_prompt: offsets are int32 [sequences + 1] on the device of q")
-    q, q_token = _aligned_rows(q, q_token)
-    k, k_token = _aligned_rows(k, k_token)
-    v, v_token = _aligned_rows(v, v_token)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif not (isinstance(out, torch.Tensor) and out.dtype == q.dtype and out.shape == q.shape and out.device == dev
@@ -309,8 +342,7 @@ def attention_prompt(q, k, v, offsets, scale=None, out=None):
     seqs, kv_heads = offsets.shape[0] - 1, k.shape[1]
     need = _on(L.as_attention_prompt_workspace, dev, t, heads, kv_heads, seqs)
     _keep, ws = _workspace(need, dev)
-    _call(L.as_attention_prompt, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), _TYPES[q.dtype], t, heads, kv_heads,
-          dim, q_token, k_token, v_token, offsets.data_ptr(), seqs, dim ** -0.5 if scale is None else scale,
+    _call(L.as_attention_prompt, dev, *at, _TYPES[q.dtype], t, heads, kv_heads, dim, q_token, k_token, v_token, offsets.data_ptr(), seqs, dim ** -0.5 if scale is None else scale,
           out.data_ptr(), ws, need)
     return out
 
@@ -520,19 +552,32 @@ def cache_append_packed(cache: Cache, k, v, seq, slot, pos=None, held=False):
     fp32 tensors of k's shape, not written for tokens passed over)."""
     c = cache._c
     dev = cache.k.device
-    if not (isinstance(k, torch.Tensor) and k.dtype in _16):
-        _bad("cache_append_packed: k in 16 bits is needed")
-    k, k_token = _packed(k, "k", k.dtype, dev, c.dim)
-    v, v_token = _packed(v, "v", k.dtype, dev, c.dim)
-    t = k.shape[0]
-    if k.shape != v.shape or k.shape[1] != c.n_heads:
-        _bad(f"cache_append_packed: k has {tuple(k.shape)}, v {tuple(v.shape)}, the cache {c.n_heads} heads")
-    for name, x in (("seq", seq), ("slot", slot), ("pos", pos)):
-        if x is not None and _need(x, name, (torch.int32,), 1, dev).numel() != t:
-            _bad(f"{name}: {x.numel()} numbers for {t} tokens")
+    try:  # one cheap look at everything first: most calls need no more
+        dtype, (t, heads, dim), (k_token, k_head, k_step), (v_token, v_head, v_step) = k.dtype, k.shape, k.stride(), v.stride()
+        i32, rows = torch.int32, (t,)
+        plain = (dtype in _16 and v.dtype is dtype and k.device == v.device == seq.device == slot.device == dev and t > 1
+                 and v.shape == k.shape and heads == c.n_heads and dim == c.dim and k_step == v_step == 1
+                 and k_head == v_head == dim and seq.dtype is slot.dtype is i32 and seq.shape == slot.shape == rows
+                 and seq.is_contiguous() and slot.is_contiguous()
+                 and (pos is None or (pos.dtype is i32 and pos.shape == rows and pos.device == dev
+                                      and pos.is_contiguous())))
+    except (AttributeError, ValueError, TypeError, IndexError):
+        plain = False
+    if not plain:
+        if not (isinstance(k, torch.Tensor) and k.dtype in _16):
+            _bad("cache_append_packed: k in 16 bits is needed")
+        k, k_token = _packed(k, "k", k.dtype, dev, c.dim)
+        v, v_token = _packed(v, "v", k.dtype, dev, c.dim)
+        t = k.shape[0]
+        if k.shape != v.shape or k.shape[1] != c.n_heads:
+            _bad(f"cache_append_packed: k has {tuple(k.shape)}, v {tuple(v.shape)}, the cache {c.n_heads} heads")
+        for name, x in (("seq", seq), ("slot", slot), ("pos", pos)):
+            if x is not None and _need(x, name, (torch.int32,), 1, dev).numel() != t:
+                _bad(f"{name}: {x.numel()} numbers for {t} tokens")
     hk = hv = None
     if held:
-        hk, hv = (torch.empty(k.shape, dtype=torch.float32, device=dev) for _ in range(2))
+        hk = torch.empty(k.shape, dtype=torch.float32, device=dev)
+        hv = torch.empty_like(hk)
     _call(lib().as_cache_append_packed, dev, c, k.data_ptr(), v.data_ptr(), _TYPES[k.dtype], t, k_token, v_token,
           seq.data_ptr(), slot.data_ptr(), None if pos is None else pos.data_ptr(), hk.data_ptr() if held else None,
           hv.data_ptr() if held else None)
