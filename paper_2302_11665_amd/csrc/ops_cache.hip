@@ -285,8 +285,9 @@ __device__ __forceinline__ void put_held(float* held, int lane, const float (&va
 // in one store.  First all of its tokens are quantised side by side, then V's words
 // are written, a quarter of a run's block (the words of 8 of its slots) to a
 // wavefront at a time.  Few tokens cost a launch and a chain of loads (places, page,
-// values): 39 of 8 heads of 128 channels 5.9 us.  Many are bound by what they read and
-// write: 58,000 with the values held 103 us, 87 at the rate of a copy.
+// values): 39 of 8 heads of 128 channels 4.9 us.  Many are bound by what they read and
+// write and by the quantisation's instructions, some ten a value, which take about as
+// long: 64,590 of 8 heads of 64 channels 54 us, with the values held 70.
 template <int TYPE, int DIM, int GROUP>
 __global__ __launch_bounds__(256) void append_packed(PackedArgs p) {
   constexpr int kLanes = DIM / 8, kWords = DIM / 8, kAtOnce = 256 / kLanes;
@@ -717,7 +718,7 @@ int as_cache_append_packed(const as_cache_t* cache, const void* k, const void* v
                k_token, v_token, seq, slot, pos, held_k, held_v, (int32_t)n_tokens, (int32_t)((n_tokens + 31) / 32), 4};
   // Single tokens are a run each: few of them to a workgroup as long as there are not
   // too many workgroups.  Tiles of 4 and of 32 tokens, 8 heads of 128 channels: 39 single
-  // tokens 5.9 and 18 us, 38 and a prompt of 1305 9.5 and 20, a prompt of 8000 24 and 20.
+  // tokens 4.9 and 10.6 us, 38 and a prompt of 1305 8.9 and 11.7, a prompt of 8000 23 and 18.
   while (p.tile < 32 && p.n_blocks * (32 / p.tile) * (int64_t)cache->n_heads > 16 * (int64_t)as_host::compute_units())
     p.tile *= 2;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
