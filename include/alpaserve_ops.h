@@ -148,8 +148,10 @@ int as_norm_i8(const void* x, const void* residual, int32_t type, int64_t n_toke
  * and values 2^26 elements apart, and 2^24 blocks of 128 rows of a key/value head's
  * queries (each sequence's last one may be a part).
  * Products of 16-bit numbers with fp32 sums, softmax in fp32; p is rounded to the
- * type for its product with v (half a unit in its last place each, as the output),
- * not for its sum.
+ * type for its product with v (half a unit in its last place each, as the output; in
+ * fp16, where weights below 2^-14 of the row's largest are subnormal, 2^-25 of that),
+ * not for its sum.  Values may have any magnitude: no sum leaves fp32's range where
+ * the result does not.
  */
 int64_t as_attention_prompt_workspace(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_seqs);
 int as_attention_prompt(const void* q, const void* k, const void* v, int32_t type, int64_t n_tokens, int32_t n_q_heads,

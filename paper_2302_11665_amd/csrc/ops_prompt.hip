@@ -209,11 +209,22 @@ constexpr uint16_t kInfinity = TYPE == AS_BF16 ? 0x7f80 : 0x7c00;
 // values that are not finite are left out of the product and reach the rows that see
 // them by products of their marks with a mask.
 //
+// Values of bf16 times weights that are not divided by their sum yet can also pass fp32's
+// range where the result does not (1e38).  Where the block's keys have finite values of
+// kLarge or more, CAREFUL takes the reference and the sum of weights that the first pass
+// found and divides each weight by that sum before it is rounded: what is added up then
+// stays below the largest value, but for roundings.  (fp16's sums cannot get there.)
+//
 // SPLIT: its tiles of keys from first to end; sums, the reference of the weights and
-// their sums go to `part`.
+// their sums go to `part`, the sum of weights with its sign turned where the sums are
+// divided by it.
+constexpr uint16_t kLarge = 0x4d80;  // 2^28, in bf16: 2^26 weights of 2^8, off by 2^64 for the largest logits
+struct Weights {
+  float reference, total;  // of a row's exponents; sum of its weights
+};
 template <int TYPE, int DIM, int WAVES, bool CAREFUL, bool SPLIT>
 __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)[2][kKeys * DIM * 2], int head, int begin,
-                                             int length, int block, int first, int end, float* part) {
+                                             int length, int block, int first, int end, float* part, Weights& found) {
   constexpr int kRows = 32 * WAVES, kRowBytes = DIM * 2, kTile = kKeys * kRowBytes;
   constexpr int kLoads = kTile / 1024 / WAVES;  // of K and of V, by a wavefront, a stage
   constexpr int kPieces = kRowBytes / 16, kPerLoad = 1024 / kRowBytes;  // keys of a load
@@ -267,6 +278,28 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
 
   v16f o[kDimTiles];
   float reference, total;  // of the exponents; sum of this lane's keys' p
+  bool divided = false;
+  if (CAREFUL && TYPE == AS_BF16) {
+    uint32_t top = 0;
+    const int from = first * kKeys, keys = min(tiles * kKeys, length) - from;
+    for (int64_t i = threadIdx.x; i < (int64_t)keys * kPieces; i += 64 * WAVES) {
+      const v4u eight = *reinterpret_cast<const v4u*>(v0 + ((from + i / kPieces) * p.v_token + i % kPieces * 8) * 2);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t u = (e & 1 ? eight[e >> 1] >> 16 : eight[e >> 1]) & 0x7fffu;
+        if (u < kInfinity<TYPE>) top = max(top, u);
+      }
+    }
+    uint32_t* marks = reinterpret_cast<uint32_t*>(lds[1][0]);
+    const bool any = __any(top >= kLarge);
+    if (lane == 0) marks[wave] = any;
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) divided |= marks[i] != 0;
+    lds_barrier();  // all have read it before tiles come in there
+    divided = divided && found.total > 0x1p-100f && found.total < 0x1p100f;
+  }
+  const float share = divided ? 1.0f / found.total : 1.0f;
 
   // Places of the operands: the pieces' order changes by exclusive ors of bits that
   // nothing else in an address has, so a lane's places follow from one.
@@ -301,12 +334,16 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
         for (int r = 0; r < 16; ++r) o[i][r] *= by;
     }
   };
+  // The matrix instructions take weights of the type: each is rounded to it, and their sum
+  // is of what they were before.  (Two numbers of the type to a weight would keep its bits
+  // for half as many products again.)
   auto weigh = [&](const v16f (&s)[2], v8s (&weights)[4]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(s[h][r], p.factor, -reference));
+        float e = __builtin_amdgcn_exp2f(fmaf(s[h][r], p.factor, -reference));
+        if (CAREFUL) e *= share;
         total += e;
         weights[h * 2 + (r >> 3)][r & 7] = (short)from_f32<TYPE>(e);
       }
@@ -368,7 +405,7 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
 
 #pragma unroll
   for (int i = 0; i < kDimTiles; ++i) o[i] = v16f{};
-  reference = -1e30f, total = 0.0f;
+  reference = divided ? found.reference : -1e30f, total = 0.0f;
   bring_k(first);
   if (first + 1 < tiles) bring_k(first + 1);
   bring_v(first);
@@ -453,15 +490,16 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
     for (int i = 0; i < kDimTiles; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) fine &= fabsf(o[i][r]) < kInf;
-    uint32_t* found = reinterpret_cast<uint32_t*>(lds[1][0]);
+    uint32_t* marks = reinterpret_cast<uint32_t*>(lds[1][0]);
     const bool any = __any(!fine);
-    if (lane == 0) found[wave] = any;
+    if (lane == 0) marks[wave] = any;
     lds_barrier();
     uint32_t all = 0;
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) all |= found[i];
+    for (int i = 0; i < WAVES; ++i) all |= marks[i];
     if (__builtin_amdgcn_readfirstlane(all)) {
       lds_barrier();  // all have read it before the next pass writes there
+      found = Weights{reference, total};
       return false;
     }
   }
@@ -474,7 +512,7 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
             v4f{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
     if (half == 0) {
       part[DIM * kRows + wave * 32 + col] = reference;
-      part[(DIM + 1) * kRows + wave * 32 + col] = total;
+      part[(DIM + 1) * kRows + wave * 32 + col] = divided ? -found.total : total;
     }
     return true;
   }
@@ -510,8 +548,8 @@ __device__ __forceinline__ bool attend_block(const PromptArgs& p, uint8_t (*lds)
 template <int TYPE, int DIM, int WAVES, bool SPLIT>
 __device__ __attribute__((noinline)) void attend_block_again(PromptArgs p, uint8_t (*lds)[2][kKeys * DIM * 2],
                                                              int head, int begin, int length, int block, int first,
-                                                             int end, float* part) {
-  attend_block<TYPE, DIM, WAVES, true, SPLIT>(p, lds, head, begin, length, block, first, end, part);
+                                                             int end, float* part, Weights found) {
+  attend_block<TYPE, DIM, WAVES, true, SPLIT>(p, lds, head, begin, length, block, first, end, part, found);
 }
 
 // How a workgroup finds its block: in the list, or among few sequences; SPLIT: the
@@ -552,8 +590,9 @@ __global__ __launch_bounds__(64 * WAVES, DIM == 64 ? 3 : 2) void prompt_attentio
     if (first >= tiles_of<kRows>(p, item.length, item.block)) return;
     part = p.parts + ((int64_t)(at % n_items * p.n_heads + head) * p.n_parts + which) * kPart<DIM, kRows>;
   }
-  if (!attend_block<TYPE, DIM, WAVES, false, kParts>(p, lds, head, item.begin, item.length, item.block, first, end, part))
-    attend_block_again<TYPE, DIM, WAVES, kParts>(p, lds, head, item.begin, item.length, item.block, first, end, part);
+  Weights found;
+  if (!attend_block<TYPE, DIM, WAVES, false, kParts>(p, lds, head, item.begin, item.length, item.block, first, end, part, found))
+    attend_block_again<TYPE, DIM, WAVES, kParts>(p, lds, head, item.begin, item.length, item.block, first, end, part, found);
 }
 
 // Joins the parts of a block: sums and sums of weights, brought to the largest
@@ -573,28 +612,56 @@ __global__ __launch_bounds__(256) void prompt_join(PromptArgs p) {
   float top = from[DIM * kRows];
 #pragma unroll 4
   for (int i = 1; i < parts; ++i) top = fmaxf(top, from[i * kPart<DIM, kRows> + DIM * kRows]);
-  v4f sum[kTimes] = {};
-  float total = 0.0f;
+  v4f sum[kTimes];
+  float total, share = 1.0f;
+  // What the parts' sums are multiplied by, and their sums of weights; share: of all.
+  auto add_up = [&] {
+#pragma unroll
+    for (int k = 0; k < kTimes; ++k) sum[k] = v4f{};
+    total = 0.0f;
 #pragma unroll 2
-  for (int i = 0; i < parts; ++i) {
-    const float* x = from + i * kPart<DIM, kRows>;
-    const float by = __builtin_amdgcn_exp2f(x[DIM * kRows] - top);
-    total = fmaf(x[(DIM + 1) * kRows], by, total);
+    for (int i = 0; i < parts; ++i) {
+      const float* x = from + i * kPart<DIM, kRows>;
+      const float weights = x[(DIM + 1) * kRows], by = __builtin_amdgcn_exp2f(x[DIM * kRows] - top);
+      total = fmaf(fabsf(weights), by, total);
+      const float times = (weights < 0.0f ? -weights * by : by) * share;
 #pragma unroll
-    for (int k = 0; k < kTimes; ++k) {
-      const v4f four = *reinterpret_cast<const v4f*>(x - in + ((int64_t)(k * 8 + lane / 8) * kRows + in) * 4);
+      for (int k = 0; k < kTimes; ++k) {
+        const v4f four = *reinterpret_cast<const v4f*>(x - in + ((int64_t)(k * 8 + lane / 8) * kRows + in) * 4);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[k][e] = fmaf(four[e], by, sum[k][e]);
+        for (int e = 0; e < 4; ++e) sum[k][e] = fmaf(four[e], times, sum[k][e]);
+      }
     }
-  }
+  };
+  add_up();
   const float by = 1.0f / total;
+  bool fine = true;
+#pragma unroll
+  for (int k = 0; k < kTimes; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      fine &= fabsf(sum[k][e]) < kInf;
+      sum[k][e] *= by;
+    }
+  if (TYPE == AS_BF16 && !fine) {  // as in a block's second pass: divided before they are added up
+    v4f before[kTimes];
+#pragma unroll
+    for (int k = 0; k < kTimes; ++k) before[k] = sum[k];
+    share = by;
+    add_up();
+#pragma unroll
+    for (int k = 0; k < kTimes; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (fabsf(before[k][e]) < kInf) sum[k][e] = before[k][e];
+  }
   const int query = row / p.group;
   uint16_t* to =
       p.out + ((int64_t)(item.begin + query) * p.n_heads * p.group + head * p.group + row - query * p.group) * DIM;
 #pragma unroll
   for (int k = 0; k < kTimes; ++k)
     *reinterpret_cast<v2u*>(to + (k * 8 + lane / 8) * 4) =
-        v2u{pack_two<TYPE>(sum[k][0] * by, sum[k][1] * by), pack_two<TYPE>(sum[k][2] * by, sum[k][3] * by)};
+        v2u{pack_two<TYPE>(sum[k][0], sum[k][1]), pack_two<TYPE>(sum[k][2], sum[k][3])};
 }
 
 constexpr int kPromptWaves = 4;
