@@ -275,7 +275,12 @@ def prompt_seconds(block: Block, lengths, repeats: int = 8) -> float:
 def measure(shape: Shape, tokens: int, requests: int = 8, batch: int = 8, device="cuda", prompt: int = 0) -> Profile:
     """Profile of a model whose requests have prompts of `prompt` tokens (0: not
     counted) and generate `tokens` tokens, with room for the caches of `requests`
-    requests."""
+    requests.  A request with a prompt has to fit its cache without a cut: a cut goes by
+    the attention weights of steps, and reading a prompt accumulates none.  Its prompt
+    and tokens then lie within the bytes that are counted for its cache."""
+    if prompt < 0 or prompt and prompt + tokens > shape.budget + shape.slack:
+        raise ValueError(f"a prompt of {prompt} tokens and {tokens} more in a cache that is cut at "
+                         f"{shape.budget} + {shape.slack}")
     block = Block(shape, device=device)
     one, many = step_seconds(block, 1), step_seconds(block, batch)
     cache = Caches(shape, 1, device).bytes_per_sequence()
@@ -324,14 +329,17 @@ def place(gp: problems.GreedyProblem, device="cuda") -> dict:
 def main(argv=None):
     ap = argparse.ArgumentParser(prog="python -m paper_2302_11665_amd.served", description=__doc__.splitlines()[0])
     ap.add_argument("--prompt", type=int, default=0, help="tokens of a request's prompt whose reading is counted")
-    prompt = ap.parse_args(argv).prompt
+    prompt, tokens = ap.parse_args(argv).prompt, 128
     shapes = [Shape(layers=24, hidden=2048, heads=16, kv_heads=4, dim=128, inner=8192, budget=1024),
               Shape(layers=32, hidden=4096, heads=32, kv_heads=8, dim=128, inner=16384, budget=2048)]
+    most = min(s.budget + s.slack for s in shapes) - tokens
+    if not 0 <= prompt <= most:
+        ap.error(f"prompts of {prompt} tokens (at most {most}, which fit the smallest cache before its first cut)")
     found = []
     for s in shapes:
-        p = measure(s, tokens=128, prompt=prompt)
+        p = measure(s, tokens=tokens, prompt=prompt)
         found.append(p)
-        print(f"{s.layers} layers of {s.hidden}: {p.latency:.3f} s a request of 128 tokens"
+        print(f"{s.layers} layers of {s.hidden}: {p.latency:.3f} s a request of {tokens} tokens"
               f"{f' after {prompt}' if prompt else ''}, batching slope "
               f"{p.slope:.3f}, {p.weight_mib} MiB", flush=True)
     profiles = [found[i % len(found)] for i in range(8)]
