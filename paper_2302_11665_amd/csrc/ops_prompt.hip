@@ -134,11 +134,13 @@ __device__ __forceinline__ bool find_block(const PromptArgs& p, uint32_t item, I
 // certain order, which changes nothing but when a block is worked on), then wavefronts write
 // the sequences' blocks.  (200 prompts of 700 tokens, heads of 64 channels: 461 us where
 // every workgroup went over the sequences to find its block, 281 with the list.)
+// Offsets that make no sense may give each of 2^20 sequences 2^23 blocks: blocks are
+// counted in 64 bits, and those behind the list's end neither written nor gone over.
 constexpr int kPlanThreads = 1024;
 
 template <int ROWS>
 __global__ __launch_bounds__(kPlanThreads) void prompt_plan(PromptArgs p, Item* items, int n_items) {
-  __shared__ uint32_t classes[128];
+  __shared__ unsigned long long classes[128];
   __shared__ Item part[kPlanThreads];  // block: how many; none: the first one's place
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   auto class_of = [](int blocks) { return 127 - min(127, (int)(__float_as_uint((float)blocks) >> 21) - (127 << 2)); };
@@ -146,33 +148,37 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan(PromptArgs p, Item* 
   __syncthreads();
   for (int b = tid; b < p.n_seqs; b += kPlanThreads) {
     const int blocks = blocks_of<ROWS>(p, sequence(p, b).length);
-    if (blocks) atomicAdd(&classes[class_of(blocks)], (uint32_t)blocks);
+    if (blocks) atomicAdd(&classes[class_of(blocks)], (unsigned long long)blocks);
   }
   __syncthreads();
-  if (wave == 0) {  // where every class begins
-    const uint32_t a = classes[2 * lane], z = classes[2 * lane + 1], upto = scan_lanes(a + z);
+  if (wave == 0) {  // where every class begins (n_items is below 2^24: the sum of 128 is below 2^31)
+    const unsigned long long most = n_items;
+    const uint32_t a = (uint32_t)min(classes[2 * lane], most), z = (uint32_t)min(classes[2 * lane + 1], most);
+    const uint32_t upto = scan_lanes(a + z);
     classes[2 * lane] = upto - a - z;
     classes[2 * lane + 1] = upto - z;
     if (lane == 63) part[0].none = (int)upto;
   }
   __syncthreads();
-  for (int i = max(0, part[0].none) + tid; i < n_items; i += kPlanThreads) items[i] = Item{0, 0, 0, 1};
+  for (int i = part[0].none + tid; i < n_items; i += kPlanThreads) items[i] = Item{0, 0, 0, 1};
   __syncthreads();
   for (int first = 0; first < p.n_seqs; first += kPlanThreads) {
     Item mine{0, 0, 0, 0};
     if (first + tid < p.n_seqs) {
       const Sequence s = sequence(p, first + tid);
       const int blocks = blocks_of<ROWS>(p, s.length);
-      mine = Item{s.begin, s.length, blocks, blocks ? (int)atomicAdd(&classes[class_of(blocks)], (uint32_t)blocks) : 0};
+      mine = Item{s.begin, s.length, blocks, 0};
+      if (blocks) {
+        const unsigned long long at = atomicAdd(&classes[class_of(blocks)], (unsigned long long)blocks);
+        mine.none = (int)min(at, (unsigned long long)n_items);
+      }
     }
     part[tid] = mine;
     __syncthreads();
     for (int i = wave; i < min(kPlanThreads, p.n_seqs - first); i += kPlanThreads / 64) {
       const Item s = part[i];
-      for (int j = lane; j < s.block; j += 64) {  // (offsets that make no sense may give more blocks than items)
-        const int64_t at = (int64_t)(uint32_t)s.none + j;
-        if (at < n_items) items[at] = Item{s.begin, s.length, s.block - 1 - j, 0};
-      }
+      for (int j = lane; j < min(s.block, n_items - s.none); j += 64)
+        items[s.none + j] = Item{s.begin, s.length, s.block - 1 - j, 0};
     }
     __syncthreads();
   }

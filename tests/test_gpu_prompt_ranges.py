@@ -93,3 +93,22 @@ def test_prompt_of_large_values_in_fp16():
     q.zero_()
     v = (65000.0 - 3000 * torch.rand(v.shape, device="cuda", generator=g)).to(F16)
     check_rows(q, k, v, lengths, ops.attention_prompt(q, k, v, offsets, scale=1.0), 1.0)
+
+
+def test_prompt_with_many_offsets_that_make_no_sense():
+    """Sequences that all have all tokens: 2^33 blocks of rows, of which those that can be are worked on, inside the
+    arrays."""
+    g = gen(4)
+    t, heads, seqs = 8192, 256, 1 << 20
+    q, k, v = normal(g, t, heads, 64, dtype=BF16), normal(g, t, 1, 64, dtype=BF16), normal(g, t, 1, 64, dtype=BF16)
+    offsets = torch.zeros(seqs + 1, dtype=torch.int32, device="cuda")
+    offsets[1::2] = t
+    out = torch.full((t + 64, heads, 64), 5.0, dtype=BF16, device="cuda")
+    say("offsets that make no sense", seqs)
+    ops.attention_prompt(q, k, v, offsets, out=out[32:-32])
+    torch.cuda.synchronize()
+    assert (out[:32] == 5).all() and (out[-32:] == 5).all()
+    offsets[:-1] = torch.randint(-t, 2 * t, (seqs,), device="cuda", generator=g)
+    ops.attention_prompt(q, k, v, offsets[-5000:].contiguous(), out=out[32:-32])
+    torch.cuda.synchronize()
+    assert (out[:32] == 5).all() and (out[-32:] == 5).all()
