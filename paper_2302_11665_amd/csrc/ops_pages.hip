@@ -180,7 +180,9 @@ __global__ __launch_bounds__(256) void reserve_tokens(ReserveArgs p) {
 // Few sequences and tokens: both in one launch, what lies between in LDS.  In one
 // launch and in two, on the device and for a call in a loop: 48 sequences of a token
 // 3.3 and 5.3 us, 9 and 12; 8 of 1000 tokens 7.5 and 7.0, 9 and 12; 1000 of 8 11.1 and
-// 7.7 (one workgroup's searches), 11 and 12.
+// 7.7 (one workgroup's searches), 11 and 12.  The rule goes by the call: in a replayed
+// graph, where the device's time counts, thousands of tokens of many sequences would be
+// faster in two.
 constexpr int kOnceSeqs = kPageThreads, kOnceTokens = 8 * kPageThreads;
 
 __global__ __launch_bounds__(kPageThreads) void reserve_once(ReserveArgs p) {

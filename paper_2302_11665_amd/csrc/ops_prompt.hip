@@ -14,10 +14,10 @@
 // What bounds it: 4 dim operations a head and pair of tokens, which the matrix units
 // would do in 0.96 ms for 12,001 tokens of 32 heads of 128 channels, and an exponential
 // for each pair, whose vector instructions take about half as long as the products.
-// The kernel takes 1.07 to 1.11 ms (830 to 860 TFLOP/s, of the pairs that count; the matrix units
-// busy for 52 % of the cycles, at 1.75 GHz under this load), 0.97 ms without the
-// softmax.  Heads of 64 channels have half the products for as many exponentials:
-// 32 of them 0.69 ms.
+// The kernel takes 1.07 to 1.11 ms (1063 to 1103 TFLOP/s, of the pairs that count; the matrix units
+// busy for 54 % of the cycles, at 1.75 GHz under this load), 0.97 ms without the
+// softmax.  Heads of 64 channels have half the products for as many exponentials, and matrix
+// and vector instructions follow one another (30 and 61 % of the cycles): 32 of them 0.67 to 0.69 ms.
 #include <algorithm>
 #include <type_traits>
 
